@@ -121,13 +121,14 @@ def draw(rng):
 def work(case):
     t, n, e = case["tokens"], case["n"], _BYTES[case["dtype"]]
     op = case["op"]
+    if op.startswith("ff"):
+        m, share = case["m"], case["keep"] or 1.0      # a pruned channel's products and inputs need not be touched
+        planes = 3 if case["saved"] else 1
     if op == "ff":
-        m = case["m"]
-        return {"bytes": e * (t * n + 2 * n * m + t * m * (3 if case["saved"] else 1)), "flops": 4 * t * n * m}
+        return {"bytes": e * (t * n + 2 * n * m * share + t * m * planes), "flops": 4 * t * n * m * share}
     if op == "ff_backward":
-        m = case["m"]
-        return {"bytes": e * (2 * t * n + 4 * n * m + t * m * (3 if case["saved"] else 1)),
-                "flops": (8 if case["saved"] else 12) * t * n * m}
+        return {"bytes": e * (2 * t * n + 2 * n * m * (1 + share) + t * m * planes * share),
+                "flops": (8 if case["saved"] else 12) * t * n * m * share}
     if op == "norm":
         rows = 5 if case["gate"] == "token" else 4
         return {"bytes": e * n * (rows * t + (2 if case["gate"] == "token" else 3)), "flops": 10 * t * n}
