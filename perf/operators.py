@@ -78,7 +78,7 @@ def listed():
     ]
 
 
-_MOST_FLOPS = 12 * 4096 * 4096 * 16384
+_MOST_FLOPS = 4 * 4096 * 4096 * 16384
 _MOST_NORM = 16384 * 4096
 
 
