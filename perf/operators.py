@@ -79,7 +79,7 @@ def listed():
 
 
 _MOST_FLOPS = 4 * 4096 * 4096 * 16384
-_MOST_NORM = 16384 * 4096
+_MOST_NORM = 6 * 16384 * 4096 * 2
 
 
 def _log_uniform(rng, lo, hi):
@@ -108,7 +108,7 @@ def draw(rng):
                 joined=rng.random() < 0.3, saved=rng.random() < 0.4)
     elif op.startswith("norm"):
         n = _size(rng, 64, 16384)
-        tokens = max(1, min(round(_log_uniform(rng, 1, 32768)), _MOST_NORM // n))
+        tokens = max(1, min(round(_log_uniform(rng, 1, 32768)), _MOST_NORM // (8 * _BYTES[dtype] * n) - 2))
         c = _norm("", tokens, n, dtype, op=op, gate=rng.choice(("channel", "token")))
     else:
         c = _w4("", op, round(_log_uniform(rng, 1, 64)), _size(rng, 64, 16384), _size(rng, 64, 16384), dtype,
