@@ -96,22 +96,27 @@ def _size(rng, lo, hi):
     return step * (2 * max(0, round((v / step - 1) / 2)) + 1)
 
 
+def _tokens(rng, hi, most):
+    """A power of two or an odd number."""
+    v = max(1, min(round(_log_uniform(rng, 1, hi)), most))
+    return v if v & (v - 1) == 0 else v - 1 + v % 2
+
+
 def draw(rng):
     op = rng.choice(("ff", "ff", "ff_backward", "ff_backward", "norm", "norm_backward", "w4", "w4_gated"))
     dtype = rng.choice(("bf16", "bf16", "f16", "f32"))
     act = rng.choice(("silu", "gelu", "relu"))
     if op.startswith("ff"):
         n, m = _size(rng, 64, 8192), _size(rng, 64, 16384)
-        tokens = round(_log_uniform(rng, 1, 8192))
-        tokens = max(1, min(tokens, _MOST_FLOPS // (12 * n * m)))
+        tokens = _tokens(rng, 8192, _MOST_FLOPS // (12 * n * m))
         c = _ff("", tokens, n, m, dtype, op=op, act=act, keep=rng.choice((0.0, 0.0, 0.1, 0.5)),
                 joined=rng.random() < 0.3, saved=rng.random() < 0.4)
     elif op.startswith("norm"):
         n = _size(rng, 64, 16384)
-        tokens = max(1, min(round(_log_uniform(rng, 1, 32768)), _MOST_NORM // (8 * _BYTES[dtype] * n) - 2))
+        tokens = _tokens(rng, 32768, _MOST_NORM // (8 * _BYTES[dtype] * n) - 2)
         c = _norm("", tokens, n, dtype, op=op, gate=rng.choice(("channel", "token")))
     else:
-        c = _w4("", op, round(_log_uniform(rng, 1, 64)), _size(rng, 64, 16384), _size(rng, 64, 16384), dtype,
+        c = _w4("", op, _tokens(rng, 64, 64), _size(rng, 64, 16384), _size(rng, 64, 16384), dtype,
                 rng.choice((32, 64, 128)))
         c["act"] = act
     del c["name"]
