@@ -52,9 +52,10 @@ typedef enum mlproj_status {
   MLPROJ_ERR_BAD_RADIUS = -4,     /* eta is negative, NaN or infinite                 */
   MLPROJ_ERR_WORKSPACE = -5,      /* workspace too small or misaligned                */
   MLPROJ_ERR_BAD_VARIANT = -6,    /* unknown variant / norm selector                  */
-  MLPROJ_ERR_ALIGNMENT = -7,      /* Y or X not aligned to the element size            */
+  MLPROJ_ERR_ALIGNMENT = -7,      /* an array is not aligned to its element size       */
   MLPROJ_ERR_LAUNCH = -8,         /* the HIP runtime refused a kernel launch of this call  */
-  MLPROJ_ERR_NO_ALLOC_LIMIT = -9  /* bilevel_proj_l1inf_no_alloc: the input needs more scratch than the built-in buffer */
+  MLPROJ_ERR_NO_ALLOC_LIMIT = -9, /* bilevel_proj_l1inf_no_alloc: the input needs more scratch than the built-in buffer */
+  MLPROJ_ERR_BAD_VALUE = -10      /* a scalar argument (eps, scale) is out of its range            */
 } mlproj_status;
 
 /* Which projection a workspace is sized for. */
@@ -410,6 +411,140 @@ int multilevel_proj_stored(int storage, int outer_norm, const void* Y /* device 
  * chain).  Host only, touches no GPU: here so that the rule can be checked without one.      */
 int mlproj_multilevel_one_pass(int storage, int fibre_norm, long long d0, long long d1, long long d2,
                                int compute_units);
+
+/* ---------------------------------------------------------------------------------------------
+ * THE PRUNED FEED-FORWARD BLOCK -- what a network runs around the matrices that the projection
+ * prunes (the use Sec. 6.3 makes of it): the gated products whose hidden channels are the columns
+ * (the groups) of the projection, the norms before and after the block, and the products of single
+ * tokens with the finished weights in 4 bits.
+ *
+ * Matrices are row-major with a stride: element (i, j) of A is A[i * lda + j], lda at least the
+ * length of a row (so the gate and up weights may be the halves of one n x 2m matrix).  Arrays are
+ * aligned to their element size and nothing more is asked; 16-byte aligned rows are fastest.
+ * `storage` is a mlproj_storage and applies to every matrix and vector of a call unless said
+ * otherwise; arithmetic and sums are fp32 throughout, and results are rounded to nearest-even
+ * once, on store.  `tokens` may be 0: then nothing is read, and sums over tokens are zeros.
+ * Calls enqueue on `stream`, keep no state and need no cleared workspace, as everywhere above.
+ * Outputs must not overlap inputs or one another except where said.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Activation of the gate: g/(1 + e^-g), g Phi(g) (the exact form, with erf), max(g, 0). */
+typedef enum mlproj_activation {
+  MLPROJ_ACT_SILU = 0,
+  MLPROJ_ACT_GELU = 1,
+  MLPROJ_ACT_RELU = 2
+} mlproj_activation;
+
+/* The inputs of a gated block.  mask: as bilevel_proj_stored returns it, one byte per hidden
+ * channel, 0 for a pruned one; a pruned channel's outputs and gradients are zeros whatever its
+ * weights are, and its products are left out where that saves time.                          */
+typedef struct mlproj_gated_block {
+  long long tokens, n, m;
+  const void* X;              /* device, tokens x n                                   */
+  long long ldx;
+  const void* Wg;             /* device, n x m: gate                                  */
+  const void* Wu;             /* device, n x m: up                                    */
+  long long ldw;              /* stride of both                                       */
+  const unsigned char* mask;  /* device, m; may be NULL: every channel is kept        */
+} mlproj_gated_block;
+
+/* Bytes of workspace that gated_ff_forward (backward = 0) or gated_ff_backward (1) needs: for calls without a mask
+ * (masked = 0), or for calls with and without one (1; the kept channels' weights and results are packed there).
+ * Host only.                                                                                 */
+int mlproj_gated_ff_workspace_bytes(int storage, long long tokens, long long n, long long m, int backward, int masked,
+                                    size_t* bytes_out /* host */);
+
+/* H = mask * act(X Wg) * (X Wu), tokens x m.  G, U (both or neither): also X Wg and X Wu, for a later
+ * backward pass (of pruned channels: zeros).                                                 */
+int gated_ff_forward(int storage, int activation, const mlproj_gated_block* block /* host */,
+                     void* H /* device, tokens x m */, long long ldh,
+                     void* G /* device, tokens x m; may be NULL */, void* U, long long ldg,
+                     void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* The gradients of gated_ff_forward for a given dH (tokens x m).  With U = X Wu, G = X Wg:
+ *   dG = mask * act'(G) * U * dH,  dU = mask * act(G) * dH      (rounded to the storage type: they are
+ *                                                        operands of the products that follow)
+ *   dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU
+ * G and U are the forward call's (both), or NULL (both): then they are computed again, unrounded.
+ * dX may be NULL; dWg and dWu may be NULL (both).  With fp16 storage scale dH so that dG and dU lie in
+ * its range.                                                                                */
+int gated_ff_backward(int storage, int activation, const mlproj_gated_block* block /* host */,
+                      const void* dH /* device, tokens x m */, long long ldh,
+                      const void* G /* device, tokens x m; may be NULL */, const void* U, long long ldg,
+                      void* dX /* device, tokens x n; may be NULL */, long long lddx,
+                      void* dWg /* device, n x m; may be NULL */, void* dWu, long long lddw,
+                      void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* The norms around a block, with its gate and residual scale:
+ *   r = x + scale * gate * w_post * b / rms(b)      b: the block's output, x: the residual stream
+ *   y = w_pre * r / rms(r)                          the next block's input
+ * rms(z) = sqrt(mean(z^2) + eps) over the n entries of a row, y from the r that is not yet rounded.
+ * gate_stride = 0: gate has one value per channel (n entries); otherwise one row per token.
+ * w_post = NULL: no block, r = x (not written; b, gate and r are not used).  w_pre = NULL: no y.
+ * r may be x (in place), and y may be b; eps >= 0 and scale finite (MLPROJ_ERR_BAD_VALUE otherwise).
+ * Rows are `ld*` elements apart.                                                             */
+typedef struct mlproj_norm_block {
+  long long tokens, n;
+  const void* b;              /* device, tokens x n                                   */
+  long long ldb;
+  const void* w_post;         /* device, n; may be NULL                               */
+  const void* gate;           /* device, n or tokens x n                              */
+  long long gate_stride;
+  const void* w_pre;          /* device, n; may be NULL                               */
+  float scale, eps;
+} mlproj_norm_block;
+
+int block_norm_forward(int storage, const mlproj_norm_block* block /* host */, const void* x /* device */, long long ldx,
+                       void* r /* device */, long long ldr, void* y /* device */, long long ldy, void* stream);
+
+int mlproj_block_norm_workspace_bytes(long long tokens, long long n, size_t* bytes_out /* host */);
+
+/* Its gradients.  r is the forward call's output (x where w_post is NULL); dr (may be NULL: zeros) and dy arrive at r
+ * and y (dy is not read where w_pre is NULL):
+ *   dx = dr + w_pre dy / rms(r) - r mean(r w_pre dy) / rms(r)^3
+ *   c  = scale * gate * dx
+ *   db = w_post c / rms(b) - b mean(b w_post c) / rms(b)^3
+ *   dw_post = sum over tokens of c b / rms(b),  dw_pre = sum of dy r / rms(r)        (fp32, n entries)
+ *   dgate = scale * dx * w_post * b / rms(b): per channel the sum over tokens (fp32, n entries), per token
+ *           a tokens x n matrix in the storage type, its rows dgate_stride apart
+ * dx may be dr, and db may be b or dy.  db, dw_post and dgate belong to w_post, dw_pre to w_pre; each may be NULL. */
+int block_norm_backward(int storage, const mlproj_norm_block* block /* host */, const void* r /* device */, long long ldr,
+                        const void* dr /* device; may be NULL */, long long lddr, const void* dy /* device */, long long lddy,
+                        void* dx /* device */, long long lddx, void* db /* device; may be NULL */, long long lddb,
+                        float* dw_post /* device, n; may be NULL */, void* dgate /* device; may be NULL */, long long dgate_stride,
+                        float* dw_pre /* device, n; may be NULL */,
+                        void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* A weight matrix in 4 bits.  Every entry is a code: sign bit, two exponent bits, one fraction bit (0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 and their negatives) times the bf16 scale of its group, `group` (32, 64 or 128) neighbouring rows of one
+ * column.  Column block c holds columns 16 c .. 16 c + 15 and row block k rows 128 k .. 128 k + 127; past the
+ * matrix codes and scales are zero.
+ *   codes   [column block][row block][64][16] bytes: entry l, byte 4 q + i holds column l % 16, rows
+ *           32 q + 8 (l / 16) + 2 i (low half) and the next one (high half): what lane l of a
+ *           wavefront feeds the matrix cores, so that 1 KiB loads are all a product does
+ *   scales  [column block][row block][16][128 / group] bf16                                     */
+typedef struct mlproj_w4 {
+  long long n, m;
+  int group;
+  const void* codes;          /* device, 16-byte aligned                              */
+  const void* scales;         /* device, 8-byte aligned                               */
+} mlproj_w4;
+
+int mlproj_w4_bytes(long long n, long long m, int group, size_t* codes_out /* host */, size_t* scales_out /* host */);
+
+/* Packs W (n x m): the scale of a group is its largest magnitude / 6, rounded to bf16, and a code is the entry
+ * over the scale, rounded to the nearest value, ties to the smaller magnitude.  A group of zeros (a pruned column) has scale 0.
+ * `packed`: codes and scales are written.                                                     */
+int w4_pack(int storage, const void* W /* device, n x m */, long long ldw, const mlproj_w4* packed /* host */, void* stream);
+
+/* y = x W (x: tokens x n, y: tokens x m), made for few tokens: every weight is read once per 64 tokens. */
+int w4_matvec(int storage, const mlproj_w4* W /* host */, const void* x /* device */, long long ldx, long long tokens,
+              void* y /* device */, long long ldy, void* stream);
+
+/* h = act(x Wg) * (x Wu): both products of a gated block in one pass; Wg and Wu of the same size and group. */
+int w4_gated_matvec(int storage, int activation, const mlproj_w4* Wg /* host */, const mlproj_w4* Wu /* host */,
+                    const void* x /* device */, long long ldx, long long tokens,
+                    void* h /* device */, long long ldh, void* stream);
 
 #ifdef __cplusplus
 }

@@ -12,7 +12,7 @@ import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmlproj.so")
-SRC_PATHS = [os.path.join(_HERE, "csrc", name) for name in ("mlproj.hip", "heldmulti.hip")]
+SRC_PATHS = [os.path.join(_HERE, "csrc", name) for name in ("mlproj.hip", "heldmulti.hip", "gatedff.hip", "blocknorm.hip", "w4.hip")]
 
 L1INF, L11, L12, L1INFINF = 0, 1, 2, 3
 _VARIANTS = {"l1inf": L1INF, "l11": L11, "l12": L12, "tri": L1INFINF}
@@ -128,6 +128,28 @@ def lib():
     L.trilevel_proj_stored.argtypes = [c_i, c_vp, c_vp, c_ll, c_ll, c_ll, c_f, c_vp, c_sz, c_vp, c_vp, c_vp, c_vp]
     L.trilevel_proj_l1infinf.restype = c_i
     L.trilevel_proj_l1infinf.argtypes = [c_vp, c_vp, c_ll, c_ll, c_ll, c_f, c_vp, c_sz, c_vp, c_vp, c_vp]
+    block, norm, w4 = ctypes.POINTER(GatedBlock), ctypes.POINTER(NormBlock), ctypes.POINTER(PackedW4)
+    L.mlproj_gated_ff_workspace_bytes.restype = c_i
+    L.mlproj_gated_ff_workspace_bytes.argtypes = [c_i, c_ll, c_ll, c_ll, c_i, c_i, ctypes.POINTER(c_sz)]
+    L.gated_ff_forward.restype = c_i
+    L.gated_ff_forward.argtypes = [c_i, c_i, block, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_sz, c_vp]
+    L.gated_ff_backward.restype = c_i
+    L.gated_ff_backward.argtypes = [c_i, c_i, block, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_sz, c_vp]
+    L.block_norm_forward.restype = c_i
+    L.block_norm_forward.argtypes = [c_i, norm, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp]
+    L.mlproj_block_norm_workspace_bytes.restype = c_i
+    L.mlproj_block_norm_workspace_bytes.argtypes = [c_ll, c_ll, ctypes.POINTER(c_sz)]
+    L.block_norm_backward.restype = c_i
+    L.block_norm_backward.argtypes = [c_i, norm, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_vp, c_ll,
+                                      c_vp, c_vp, c_sz, c_vp]
+    L.mlproj_w4_bytes.restype = c_i
+    L.mlproj_w4_bytes.argtypes = [c_ll, c_ll, c_i, ctypes.POINTER(c_sz), ctypes.POINTER(c_sz)]
+    L.w4_pack.restype = c_i
+    L.w4_pack.argtypes = [c_i, c_vp, c_ll, w4, c_vp]
+    L.w4_matvec.restype = c_i
+    L.w4_matvec.argtypes = [c_i, w4, c_vp, c_ll, c_ll, c_vp, c_ll, c_vp]
+    L.w4_gated_matvec.restype = c_i
+    L.w4_gated_matvec.argtypes = [c_i, c_i, w4, w4, c_vp, c_ll, c_ll, c_vp, c_ll, c_vp]
     _lib = L
     return L
 
@@ -139,6 +161,26 @@ class Problem(ctypes.Structure):
                 ("v_out", ctypes.c_void_p), ("u_out", ctypes.c_void_p), ("mask_out", ctypes.c_void_p)]
 
 
+class GatedBlock(ctypes.Structure):
+    """mlproj_gated_block of include/mlproj.h."""
+    _fields_ = [("tokens", ctypes.c_longlong), ("n", ctypes.c_longlong), ("m", ctypes.c_longlong),
+                ("X", ctypes.c_void_p), ("ldx", ctypes.c_longlong), ("Wg", ctypes.c_void_p), ("Wu", ctypes.c_void_p),
+                ("ldw", ctypes.c_longlong), ("mask", ctypes.c_void_p)]
+
+
+class NormBlock(ctypes.Structure):
+    """mlproj_norm_block of include/mlproj.h."""
+    _fields_ = [("tokens", ctypes.c_longlong), ("n", ctypes.c_longlong), ("b", ctypes.c_void_p), ("ldb", ctypes.c_longlong),
+                ("w_post", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_longlong),
+                ("w_pre", ctypes.c_void_p), ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class PackedW4(ctypes.Structure):
+    """mlproj_w4 of include/mlproj.h."""
+    _fields_ = [("n", ctypes.c_longlong), ("m", ctypes.c_longlong), ("group", ctypes.c_int), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p)]
+
+
 EXPORTS = (
     "mlproj_version", "mlproj_status_string", "mlproj_workspace_bytes", "mlproj_trace_begin", "mlproj_trace_end",
     "mlproj_norm_l1q", "bilevel_proj_l1inf", "bilevel_proj_l11", "bilevel_proj_l12",
@@ -147,6 +189,9 @@ EXPORTS = (
     "bilevel_proj_stored", "bilevel_proj_batch", "trilevel_proj_stored", "mlproj_set_l11_sweeps",
     "multilevel_proj_stored", "bilevel_proj_weighted", "multilevel_proj_weighted", "mlproj_set_search_spin_limit",
     "bilevel_proj_l1inf_no_alloc", "mlproj_stripe_of_workgroup", "mlproj_multilevel_one_pass",
+    "mlproj_gated_ff_workspace_bytes", "gated_ff_forward", "gated_ff_backward",
+    "block_norm_forward", "mlproj_block_norm_workspace_bytes", "block_norm_backward",
+    "mlproj_w4_bytes", "w4_pack", "w4_matvec", "w4_gated_matvec",
 )
 
 
@@ -528,6 +573,244 @@ def norm_l1q(Y, variant, workspace=None, v_out=None, stream=None):
                                _ptr(v_out), _stream(stream))
     _check(st, "mlproj_norm_l1q")
     return float(out.item())
+
+
+# ---------------------------------------------------------------- the pruned feed-forward block
+
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
+_ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU, "relu": ACT_RELU}
+_STORAGES = {}
+
+
+def _storage(dtype):
+    if not _STORAGES:
+        torch = _import_torch()
+        _STORAGES.update({torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float16: STORE_F16})
+    assert dtype in _STORAGES, "fp32, bf16 or fp16"
+    return _STORAGES[dtype]
+
+
+def _matrix(t, shape, like, what):
+    """A device matrix of `shape` and `like`'s dtype whose rows are contiguous; returns its row stride."""
+    assert t.is_cuda and t.dtype is like.dtype and t.shape == shape, what
+    rows, cols = shape
+    assert cols <= 1 or t.stride(1) == 1, what + ": the entries of a row must be neighbours"
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _result(t, shape, like, what):
+    if t is None:
+        t = _import_torch().empty(shape, dtype=like.dtype, device=like.device)
+    return t, _matrix(t, shape, like, what)
+
+
+def gated_ff_workspace_bytes(tokens, n, m, dtype, backward=False, masked=True):
+    """Bytes a call needs; masked=False: for calls without a mask only, which need far less."""
+    out = ctypes.c_size_t(0)
+    _check(lib().mlproj_gated_ff_workspace_bytes(_storage(dtype), tokens, n, m, int(backward), int(masked), ctypes.byref(out)),
+           "mlproj_gated_ff_workspace_bytes")
+    return out.value
+
+
+def _gated_block(X, Wg, Wu, mask):
+    assert X.dim() == 2 and Wg.dim() == 2
+    tokens, n = X.shape
+    m = Wg.shape[1]
+    ldx = _matrix(X, (tokens, n), X, "X")
+    ldw = _matrix(Wg, (n, m), X, "Wg")
+    assert _matrix(Wu, (n, m), X, "Wu") == ldw, "Wg and Wu: one row stride"
+    if mask is not None:
+        assert mask.is_cuda and mask.element_size() == 1 and mask.is_contiguous() and mask.numel() == m, "mask: one byte per column"
+    return GatedBlock(tokens, n, m, X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, _ptr(mask)), tokens, n, m
+
+
+def gated_ff(X, Wg, Wu, act="silu", mask=None, H=None, g_out=None, u_out=None, workspace=None, stream=None):
+    """H = mask * act(X Wg) * (X Wu): X is tokens x n, the weights n x m, all of one type (fp32, bf16, fp16), rows any
+    distance apart.  act: "silu", "gelu" (with erf) or "relu"; mask: the kept-column mask of a projection.
+    g_out, u_out: tensors that also receive X Wg and X Wu, for gated_ff_backward."""
+    block, tokens, n, m = _gated_block(X, Wg, Wu, mask)
+    H, ldh = _result(H, (tokens, m), X, "H")
+    ldg = 0
+    assert (g_out is None) == (u_out is None), "g_out and u_out: both or neither"
+    if g_out is not None:
+        ldg = _matrix(g_out, (tokens, m), X, "g_out")
+        assert _matrix(u_out, (tokens, m), X, "u_out") == ldg, "g_out and u_out: one row stride"
+    if workspace is None:
+        workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, False, mask is not None), device=X.device)
+    st = lib().gated_ff_forward(_storage(X.dtype), _ACTS[act], ctypes.byref(block), H.data_ptr(), ldh, _ptr(g_out), _ptr(u_out),
+                                ldg, workspace.buf.data_ptr(), workspace.nbytes, _stream(stream))
+    if st != 0:
+        _check(st, "gated_ff_forward")
+    return H
+
+
+def gated_ff_backward(dH, X, Wg, Wu, act="silu", mask=None, G=None, U=None, dX=None, dWg=None, dWu=None, workspace=None,
+                      stream=None, need_dx=True, need_dw=True):
+    """(dX, dWg, dWu) of gated_ff for the gradient dH of its result.  G, U: what the forward call wrote to g_out and
+    u_out; without them they are computed again.  need_dx, need_dw: leave out what is not needed (None comes back)."""
+    block, tokens, n, m = _gated_block(X, Wg, Wu, mask)
+    ldh = _matrix(dH, (tokens, m), X, "dH")
+    assert (G is None) == (U is None), "G and U: both or neither"
+    ldg = lddx = lddw = 0
+    if G is not None:
+        ldg = _matrix(G, (tokens, m), X, "G")
+        assert _matrix(U, (tokens, m), X, "U") == ldg, "G and U: one row stride"
+    if need_dx:
+        dX, lddx = _result(dX, (tokens, n), X, "dX")
+    if need_dw:
+        dWg, lddw = _result(dWg, (n, m), X, "dWg")
+        dWu, ld = _result(dWu, (n, m), X, "dWu")
+        assert ld == lddw, "dWg and dWu: one row stride"
+    if workspace is None:
+        workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, True, mask is not None), device=X.device)
+    st = lib().gated_ff_backward(_storage(X.dtype), _ACTS[act], ctypes.byref(block), dH.data_ptr(), ldh, _ptr(G), _ptr(U), ldg,
+                                 _ptr(dX) if need_dx else None, lddx, _ptr(dWg) if need_dw else None,
+                                 _ptr(dWu) if need_dw else None, lddw, workspace.buf.data_ptr(), workspace.nbytes,
+                                 _stream(stream))
+    if st != 0:
+        _check(st, "gated_ff_backward")
+    return (dX if need_dx else None, dWg if need_dw else None, dWu if need_dw else None)
+
+
+def _vector(t, n, like, what):
+    assert t.is_cuda and t.dtype is like.dtype and t.is_contiguous() and t.shape == (n,), what
+    return t.data_ptr()
+
+
+def _norm_block(z, b, w_post, gate, w_pre, scale, eps):
+    tokens, n = z.shape
+    block = NormBlock(tokens, n)
+    block.scale, block.eps = scale, eps
+    token_gate = False
+    if b is not None:
+        block.b, block.ldb = b.data_ptr(), _matrix(b, (tokens, n), z, "b")
+        block.w_post = _vector(w_post, n, z, "w_post: n entries")
+        token_gate = gate.dim() == 2
+        if token_gate:
+            block.gate, block.gate_stride = gate.data_ptr(), _matrix(gate, (tokens, n), z, "gate")
+        else:
+            block.gate = _vector(gate, n, z, "gate: n entries, or tokens x n")
+    if w_pre is not None:
+        block.w_pre = _vector(w_pre, n, z, "w_pre: n entries")
+    return block, tokens, n, token_gate
+
+
+def block_norm(x, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e-6, r=None, y=None, stream=None):
+    """(r, y) with r = x + scale * gate * w_post * b / rms(b) and y = w_pre * r / rms(r), rows of n entries.  gate is
+    a vector of n entries or a tokens x n matrix.  Without b, r is x itself; without w_pre there is no y.
+    r may be x and y may be b (in place)."""
+    assert x.dim() == 2
+    block, tokens, n, _ = _norm_block(x, b, w_post, gate, w_pre, scale, eps)
+    ldr = ldy = 0
+    if b is not None:
+        r, ldr = _result(r, (tokens, n), x, "r")
+    if w_pre is not None:
+        y, ldy = _result(y, (tokens, n), x, "y")
+    st = lib().block_norm_forward(_storage(x.dtype), ctypes.byref(block), x.data_ptr(), _matrix(x, (tokens, n), x, "x"),
+                                  None if b is None else r.data_ptr(), ldr, None if w_pre is None else y.data_ptr(), ldy,
+                                  _stream(stream))
+    if st != 0:
+        _check(st, "block_norm_forward")
+    return (x if b is None else r), (None if w_pre is None else y)
+
+
+def block_norm_workspace_bytes(tokens, n):
+    out = ctypes.c_size_t(0)
+    _check(lib().mlproj_block_norm_workspace_bytes(tokens, n, ctypes.byref(out)), "mlproj_block_norm_workspace_bytes")
+    return out.value
+
+
+def block_norm_backward(dr, dy, r, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e-6, dx=None, db=None,
+                        workspace=None, stream=None):
+    """(dx, db, dw_post, dgate, dw_pre) of block_norm for the gradients dr (None: zeros) and dy (None without w_pre) of
+    its results; r is what it returned.  The gradients of vectors are fp32 sums over the tokens, dgate of a
+    tokens x n gate is a matrix like it; what has no input is None.  dx may be dr, db may be b or dy."""
+    torch = _import_torch()
+    assert r.dim() == 2
+    block, tokens, n, token_gate = _norm_block(r, b, w_post, gate, w_pre, scale, eps)
+    lddr = lddy = lddb = ldg = 0
+    if dr is not None:
+        lddr = _matrix(dr, (tokens, n), r, "dr")
+    if w_pre is not None:
+        lddy = _matrix(dy, (tokens, n), r, "dy")
+    dx, lddx = _result(dx, (tokens, n), r, "dx")
+    dw_post = dgate = dw_pre = None
+    if b is not None:
+        db, lddb = _result(db, (tokens, n), r, "db")
+        if token_gate:
+            dgate, ldg = _result(None, (tokens, n), r, "dgate")
+            dw_post = torch.empty(n, dtype=torch.float32, device=r.device)
+        else:
+            dw_post, dgate = torch.empty(2, n, dtype=torch.float32, device=r.device)
+    else:
+        db = None
+    if w_pre is not None:
+        dw_pre = torch.empty(n, dtype=torch.float32, device=r.device)
+    if workspace is None:
+        workspace = Workspace(block_norm_workspace_bytes(tokens, n), device=r.device)
+    st = lib().block_norm_backward(_storage(r.dtype), ctypes.byref(block), r.data_ptr(), _matrix(r, (tokens, n), r, "r"),
+                                   _ptr(dr), lddr, None if w_pre is None else dy.data_ptr(), lddy, dx.data_ptr(), lddx,
+                                   _ptr(db), lddb, _ptr(dw_post), _ptr(dgate), ldg, _ptr(dw_pre), workspace.buf.data_ptr(),
+                                   workspace.nbytes, _stream(stream))
+    if st != 0:
+        _check(st, "block_norm_backward")
+    return dx, db, dw_post, dgate, dw_pre
+
+
+def w4_bytes(n, m, group):
+    codes, scales = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().mlproj_w4_bytes(n, m, group, ctypes.byref(codes), ctypes.byref(scales)), "mlproj_w4_bytes")
+    return codes.value, scales.value
+
+
+class W4:
+    """An n x m weight matrix in 4 bits with one bf16 scale per column and `group` rows (the layout is declared in
+    include/mlproj.h); `codes` is a uint8 tensor, `scales` a bf16 tensor, both contiguous."""
+
+    def __init__(self, n, m, group, codes, scales):
+        torch = _import_torch()
+        code_bytes, scale_bytes = w4_bytes(n, m, group)
+        assert codes.is_cuda and codes.dtype == torch.uint8 and codes.is_contiguous() and codes.numel() == code_bytes
+        assert scales.is_cuda and scales.dtype == torch.bfloat16 and scales.is_contiguous() and scales.numel() * 2 == scale_bytes
+        self.n, self.m, self.group, self.codes, self.scales = n, m, group, codes, scales
+        self._struct = PackedW4(n, m, group, codes.data_ptr(), scales.data_ptr())
+        self._ref = ctypes.byref(self._struct)
+
+
+def w4_pack(W, group=128, stream=None):
+    """Packs a device matrix (fp32, bf16, fp16) into a W4."""
+    torch = _import_torch()
+    assert W.dim() == 2
+    n, m = W.shape
+    ldw = _matrix(W, (n, m), W, "W")
+    code_bytes, scale_bytes = w4_bytes(n, m, group)
+    packed = W4(n, m, group, torch.empty(code_bytes, dtype=torch.uint8, device=W.device),
+                torch.empty(scale_bytes // 2, dtype=torch.bfloat16, device=W.device))
+    _check(lib().w4_pack(_storage(W.dtype), W.data_ptr(), ldw, packed._ref, _stream(stream)), "w4_pack")
+    return packed
+
+
+def w4_matvec(x, W, y=None, stream=None):
+    """y = x W for few tokens (x: tokens x n) and a packed W."""
+    tokens = x.shape[0]
+    ldx = _matrix(x, (tokens, W.n), x, "x")
+    y, ldy = _result(y, (tokens, W.m), x, "y")
+    st = lib().w4_matvec(_storage(x.dtype), W._ref, x.data_ptr(), ldx, tokens, y.data_ptr(), ldy, _stream(stream))
+    if st != 0:
+        _check(st, "w4_matvec")
+    return y
+
+
+def w4_gated_matvec(x, Wg, Wu, act="silu", h=None, stream=None):
+    """h = act(x Wg) * (x Wu) for few tokens and packed weights of one size and group."""
+    tokens = x.shape[0]
+    ldx = _matrix(x, (tokens, Wg.n), x, "x")
+    h, ldh = _result(h, (tokens, Wg.m), x, "h")
+    st = lib().w4_gated_matvec(_storage(x.dtype), _ACTS[act], Wg._ref, Wu._ref, x.data_ptr(), ldx, tokens, h.data_ptr(), ldh,
+                               _stream(stream))
+    if st != 0:
+        _check(st, "w4_gated_matvec")
+    return h
 
 
 class KernelTrace:

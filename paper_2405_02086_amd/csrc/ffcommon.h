@@ -1,0 +1,164 @@
+// mlproj: what the kernels of the gated feed-forward block share: the arguments of one product, element
+// access, the activation and the epilogues.
+#ifndef MLPROJ_FFCOMMON_H
+#define MLPROJ_FFCOMMON_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "../../include/mlproj.h"
+
+namespace mlproj {
+
+using bf16_t = __bf16;
+using f16_t = _Float16;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+
+// What a product leaves behind.
+//   STORE    C0 (and C1, where the tile holds two products side by side)
+//   FWD      C0 = keep * act(G) * U; G and U too where the caller wants them
+//   GRAD     C0 = keep * act'(G) * U * dH, C1 = keep * act(G) * dH
+//   PARTIAL  the sums over this workgroup's share of K, in fp32, for the join kernel
+enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3 };
+
+// One product C = A B (M x N, summed over K), or two that share A: C0 = A B0, C1 = A B1.
+// A: `a_kc` its rows run along K (row-major M x K); otherwise its rows are the K index (K x M).
+// B: `b_kc` row-major N x K; otherwise K x N.
+// With segs = 2 the sum runs over two pairs of operands: C = A0 B0 + A1 B1.
+struct FfProduct {
+  const void *A0, *A1, *B0, *B1;
+  long long lda, ldb;          // elements between rows
+  long long M, N, K;           // N: columns of each of the two products
+  int segs;
+  int act;
+  void *C0, *C1;
+  long long ldc;
+  void *G, *U;                 // FWD: optional outputs
+  const void* dH;              // GRAD
+  long long ldg, ldh;
+  const unsigned char* keep;   // one byte per column of the result, or null
+  const int* index;            // packed channels (ffcompact.h): the column of dH that a column of the product stands for, or null: its own number
+  const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
+  float* partial;              // PARTIAL: [splits][products][M][N]
+  int splits;
+};
+
+// ------------------------------------------------------------------ elements
+template <typename T> __device__ __forceinline__ T ff_round(float x) { return (T)x; }
+
+template <typename T> struct alignas(sizeof(T)) FfVec4 { T v[4]; };
+template <typename T> struct alignas(sizeof(T)) FfVec8 { T v[8]; };
+
+// Four neighbouring elements at any element-aligned address; the compiler makes one wide access of it.
+template <typename T>
+__device__ __forceinline__ f32x4 ff_load4(const T* p) {
+  FfVec4<T> t;
+  __builtin_memcpy(&t, p, sizeof(t));
+  f32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; i++) r[i] = (float)t.v[i];
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void ff_store4(T* p, f32x4 x) {
+  FfVec4<T> t;
+#pragma unroll
+  for (int i = 0; i < 4; i++) t.v[i] = ff_round<T>(x[i]);
+  __builtin_memcpy(p, &t, sizeof(t));
+}
+
+// ------------------------------------------------------------------ activation
+// act(g) and its slope in fp32.  silu: g s with s = 1/(1 + e^-g), slope s (1 + g (1 - s)).  gelu: g Phi(g),
+// slope Phi(g) + g phi(g).  relu: max(g, 0), slope 1 where g > 0 (NaN stays NaN in the product).
+__device__ __forceinline__ float ff_act(int act, float g) {
+  if (act == MLPROJ_ACT_SILU) return g / (1.0f + expf(-g));
+  if (act == MLPROJ_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678f));
+  return g > 0.0f ? g : (g == g ? 0.0f : g);
+}
+__device__ __forceinline__ float ff_slope(int act, float g) {
+  if (act == MLPROJ_ACT_SILU) {
+    const float s = 1.0f / (1.0f + expf(-g));
+    return s * (1.0f + g * (1.0f - s));
+  }
+  if (act == MLPROJ_ACT_GELU) return 0.5f * (1.0f + erff(g * 0.70710678f)) + g * 0.39894228f * expf(-0.5f * g * g);
+  return g > 0.0f ? 1.0f : (g == g ? 0.0f : g);
+}
+
+// ------------------------------------------------------------------ epilogue
+// Columns col .. col+3 of row `row`, of which those below N exist; v0, v1: their sums in the two products.
+// A pruned channel's outputs are zeros whatever its sums are, NaN included.
+template <int EPI, bool DUAL, typename T>
+__device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, long long col, long long N, f32x4 v0, f32x4 v1) {
+  const bool whole = col + 4 <= N;
+  const int count = whole ? 4 : (int)(N - col);
+  if constexpr (EPI == FF_PARTIAL) {
+    float* at = p.partial + ((long long)blockIdx.y * (DUAL ? 2 : 1) * p.M + row) * p.N + col;
+    if (whole) {
+      ff_store4(at, v0);
+      if constexpr (DUAL) ff_store4(at + p.M * p.N, v1);
+    } else {
+      for (int i = 0; i < count; i++) {
+        at[i] = v0[i];
+        if constexpr (DUAL) at[p.M * p.N + i] = v1[i];
+      }
+    }
+    return;
+  }
+  f32x4 o0 = v0, o1 = v1;
+  if constexpr (EPI == FF_FWD || EPI == FF_GRAD) {
+    f32x4 d = {};
+    if constexpr (EPI == FF_GRAD) {
+      const T* dh = static_cast<const T*>(p.dH) + row * p.ldh;
+      if (p.index) {
+        for (int i = 0; i < count; i++) d[i] = p.index[col + i] >= 0 ? (float)dh[p.index[col + i]] : 0.0f;
+      } else if (whole) {
+        d = ff_load4(dh + col);
+      } else {
+        for (int i = 0; i < count; i++) d[i] = (float)dh[col + i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float g = v0[i], u = v1[i];
+      if constexpr (EPI == FF_FWD) {
+        o0[i] = ff_act(p.act, g) * u;
+      } else {
+        o0[i] = d[i] * u * ff_slope(p.act, g);
+        o1[i] = d[i] * ff_act(p.act, g);
+      }
+      if (p.keep && i < count && !p.keep[col + i]) o0[i] = o1[i] = v0[i] = v1[i] = 0.0f;
+    }
+  }
+  T* c0 = static_cast<T*>(p.C0) + row * p.ldc + col;
+  T* c1 = (DUAL && EPI != FF_FWD) ? static_cast<T*>(p.C1) + row * p.ldc + col : nullptr;
+  if (whole) {
+    ff_store4(c0, o0);
+    if constexpr (DUAL && EPI != FF_FWD) ff_store4(c1, o1);
+  } else {
+    for (int i = 0; i < count; i++) {
+      c0[i] = ff_round<T>(o0[i]);
+      if constexpr (DUAL && EPI != FF_FWD) c1[i] = ff_round<T>(o1[i]);
+    }
+  }
+  if constexpr (EPI == FF_FWD) {
+    if (p.G) {
+      T* g = static_cast<T*>(p.G) + row * p.ldg + col;
+      T* u = static_cast<T*>(p.U) + row * p.ldg + col;
+      if (whole) {
+        ff_store4(g, v0);
+        ff_store4(u, v1);
+      } else {
+        for (int i = 0; i < count; i++) { g[i] = ff_round<T>(v0[i]); u[i] = ff_round<T>(v1[i]); }
+      }
+    }
+  }
+}
+
+}  // namespace mlproj
+#endif

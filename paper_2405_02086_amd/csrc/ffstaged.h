@@ -1,0 +1,235 @@
+// mlproj: matrix products of the gated feed-forward block on the matrix cores, operands staged through
+// registers: any size, stride and alignment, 16-bit elements and fp32.
+#ifndef MLPROJ_FFSTAGED_H
+#define MLPROJ_FFSTAGED_H
+
+#include "ffcommon.h"
+
+namespace mlproj {
+
+// ------------------------------------------------------------------ tiles staged through registers
+// A workgroup of four wavefronts computes 128 rows x 128 columns (two products: 128 x 64 of each, the same
+// columns of both), each wavefront 64 x 64 of them, in steps of 32 along K.  The next step's operands are
+// loaded into registers while the matrix cores work on the present one in LDS.  Loads take any address, and
+// what lies outside the matrix is filled with zeros element by element, so nothing is asked of sizes,
+// strides or alignment.
+//
+// fp32 goes through the bf16 matrix cores: an element is cut into three bf16 parts of 8 significant bits each
+// (x = p0 + p1 + p2 exactly, by truncation), and a product of two elements is summed from the six products of
+// parts that reach 2^-16 of it.  What is left out is 2^-24 of a product on average (2^-21 at most), and the sums are
+// fp32 throughout.  Six bf16 products cost 6/16 of what the chip's fp32 matrix instructions would.
+// (A part past the range of bf16's exponent, below 2^-126, is lost: an absolute error no sum can see.)
+constexpr int FS_M = 128, FS_N = 128, FS_K = 32, FS_THREADS = 256;
+
+template <typename T> struct FfParts { static constexpr int count = 1; using type = T; };
+template <> struct FfParts<float> { static constexpr int count = 3; using type = bf16_t; };
+
+__device__ __forceinline__ f32x4 ff_mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 ff_mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+template <typename E> struct FfFrag;
+template <> struct FfFrag<bf16_t> { using type = bf16x8; };
+template <> struct FfFrag<f16_t> { using type = f16x8; };
+
+// Eight neighbouring elements of which the first `valid` exist, the others zeros.
+template <typename T>
+__device__ __forceinline__ FfVec8<T> fs_load8(const T* p, long long valid) {
+  FfVec8<T> r;
+  if (valid >= 8) {
+    __builtin_memcpy(&r, p, sizeof(r));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i++) r.v[i] = i < valid ? p[i] : (T)0.0f;
+  }
+  return r;
+}
+
+// Eight elements as the 16 bytes of each of their parts.
+template <typename T>
+__device__ __forceinline__ void fs_parts(const FfVec8<T>& x, u32x4 (&out)[FfParts<T>::count]) {
+  if constexpr (FfParts<T>::count == 1) {
+    __builtin_memcpy(&out[0], &x, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      unsigned w[3][2];
+#pragma unroll
+      for (int j = 0; j < 2; j++) {
+        const float a = x.v[2 * i + j];
+        const unsigned a0 = __builtin_bit_cast(unsigned, a) & 0xffff0000u;
+        const bool finite = (a0 & 0x7f800000u) != 0x7f800000u;
+        // (a NaN whose upper half reads as an infinity stays a NaN)
+        w[0][j] = finite ? a0 : (a == a ? a0 : 0x7fc00000u);
+        const float r1 = finite ? a - __builtin_bit_cast(float, a0) : 0.0f;
+        w[1][j] = __builtin_bit_cast(unsigned, r1) & 0xffff0000u;
+        w[2][j] = __builtin_bit_cast(unsigned, r1 - __builtin_bit_cast(float, w[1][j]));
+      }
+#pragma unroll
+      for (int k = 0; k < 3; k++) out[k][i] = __builtin_amdgcn_perm(w[k][1], w[k][0], 0x07060302);
+    }
+  }
+}
+
+// A tile in LDS: 128 rows (columns) x 32 along K.  KC (K runs along the rows of memory): [128][32], so that a
+// lane's eight K values are 16 bytes; the 16-byte pieces of a row are permuted by the row's number, which
+// spreads eight rows over all banks.  Otherwise [32][128], read with the transposing LDS load: 16 lanes take
+// a 4 x 16 block and get its columns; the 32-byte pieces of a row are permuted for the same reason.
+__device__ __forceinline__ int fs_put(bool kc, int chunk) {
+  if (kc) {
+    const int row = chunk >> 2, c = chunk & 3;
+    return row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+  }
+  const int k = chunk >> 4, c = chunk & 15;
+  const int f = (k & 3) | (((k >> 3) & 1) << 2);
+  return k * 256 + (((c >> 1) ^ f) << 5) + ((c & 1) << 4);
+}
+template <bool KC, typename F>
+__device__ __forceinline__ F fs_frag(const unsigned char* tile, int idx, int lane) {
+  F r;
+  const int g = lane >> 4, c = lane & 15;
+  if constexpr (KC) {
+    const int row = idx * 16 + c;
+    r = *reinterpret_cast<const F*>(tile + row * 64 + ((g ^ ((row >> 1) & 3)) << 4));
+  } else {
+    const int f = (c >> 2) | ((g & 1) << 2);
+    const unsigned char* at = tile + (8 * g + (c >> 2)) * 256 + ((idx ^ f) << 5) + ((c & 3) << 3);
+    typedef __attribute__((address_space(3))) s16x4 lds_t;
+    s16x4 half[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)at), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(at + 4 * 256))};
+    __builtin_memcpy(&r, half, 16);
+  }
+  return r;
+}
+
+template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
+__global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
+  using E = typename FfParts<T>::type;
+  using F = typename FfFrag<E>::type;
+  constexpr int P = FfParts<T>::count;
+  constexpr int TILE = 128 * FS_K * 2;                     // bytes of a tile of one part
+  __shared__ __align__(16) unsigned char lds[2 * P * TILE];   // A's parts, then B's
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave >> 1, wn = wave & 1;
+  constexpr int COLS = DUAL ? 64 : 128;                    // columns of each product in a tile
+  const long long tiles_n = (p.N + COLS - 1) / COLS;
+  const long long N = p.kept && !(B_KC && A_KC) ? *p.kept : p.N;
+  const long long K = p.kept && (B_KC && A_KC) ? *p.kept : p.K;
+  const long long row0 = blockIdx.x / tiles_n * FS_M, col0 = blockIdx.x % tiles_n * COLS;
+  if (col0 >= N) return;
+  const long long ksteps = (K + FS_K - 1) / FS_K, all = ksteps * p.segs;
+  const long long first = all * blockIdx.y / p.splits, last = all * (blockIdx.y + 1) / p.splits;
+
+  FfVec8<T> ra[2], rb[2];
+  auto fetch = [&](long long step) {
+    const int seg = step >= ksteps;
+    const long long k0 = (step - (seg ? ksteps : 0)) * FS_K;
+    const T* A = static_cast<const T*>(seg ? p.A1 : p.A0);
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const int c = tid + i * FS_THREADS;
+      if constexpr (A_KC) {
+        const long long r = row0 + (c >> 2), k = k0 + (c & 3) * 8;
+        ra[i] = fs_load8(A + r * p.lda + k, r < p.M ? K - k : 0);
+      } else {
+        const long long k = k0 + (c >> 4), r = row0 + (c & 15) * 8;
+        ra[i] = fs_load8(A + k * p.lda + r, k < K ? p.M - r : 0);
+      }
+      if constexpr (B_KC) {
+        const int j = c >> 2;
+        const T* B = static_cast<const T*>(DUAL ? (j < 64 ? p.B0 : p.B1) : (seg ? p.B1 : p.B0));
+        const long long col = col0 + (DUAL ? j & 63 : j), k = k0 + (c & 3) * 8;
+        rb[i] = fs_load8(B + col * p.ldb + k, col < N ? K - k : 0);
+      } else {
+        const int j = (c & 15) * 8;
+        const T* B = static_cast<const T*>(DUAL ? (j < 64 ? p.B0 : p.B1) : (seg ? p.B1 : p.B0));
+        const long long col = col0 + (DUAL ? j & 63 : j), k = k0 + (c >> 4);
+        rb[i] = fs_load8(B + k * p.ldb + col, k < K ? N - col : 0);
+      }
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const int c = tid + i * FS_THREADS;
+      u32x4 parts[P];
+      fs_parts(ra[i], parts);
+#pragma unroll
+      for (int k = 0; k < P; k++) *reinterpret_cast<u32x4*>(lds + k * TILE + fs_put(A_KC, c)) = parts[k];
+      fs_parts(rb[i], parts);
+#pragma unroll
+      for (int k = 0; k < P; k++) *reinterpret_cast<u32x4*>(lds + (P + k) * TILE + fs_put(B_KC, c)) = parts[k];
+    }
+  };
+
+  // acc[i][j]: rows 16 i of the wavefront's 64; j = 0, 1: columns 32 wn + 16 j of the tile's left half, 2, 3 of
+  // the right one.  The operands are given in the order (B, A), so that a lane holds four neighbouring columns.
+  f32x4 acc[4][4] = {};
+  if (first < last) fetch(first);
+  for (long long step = first; step < last; step++) {
+    __syncthreads();
+    put();
+    __syncthreads();
+    if (step + 1 < last) fetch(step + 1);
+    F a[P][4], b[P][4];
+#pragma unroll
+    for (int k = 0; k < P; k++) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) a[k][i] = fs_frag<A_KC, F>(lds + k * TILE, wm * 4 + i, lane);
+#pragma unroll
+      for (int j = 0; j < 4; j++) b[k][j] = fs_frag<B_KC, F>(lds + (P + k) * TILE, (j >> 1) * 4 + wn * 2 + (j & 1), lane);
+    }
+    // the smallest parts first
+#pragma unroll
+    for (int sum = P - 1; sum >= 0; sum--)
+#pragma unroll
+      for (int ka = 0; ka <= sum; ka++)
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) acc[i][j] = ff_mfma(b[sum - ka][j], a[ka][i], acc[i][j]);
+  }
+
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const long long row = row0 + wm * 64 + i * 16 + (lane & 15);
+    if (row >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      const long long col = col0 + wn * 32 + j * 16 + (lane >> 4) * 4;
+      if constexpr (DUAL) {
+        if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][2 + j]);
+      } else {
+        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{});
+        if (col + 64 < N) ff_finish<EPI, false, T>(p, row, col + 64, N, acc[i][2 + j], f32x4{});
+      }
+    }
+  }
+}
+
+// Joins the shares of K: sums the partial products in their order and finishes them.
+template <typename T, bool DUAL, int EPI>
+__global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p) {
+  const long long quads = (p.N + 3) / 4, plane = p.M * p.N;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads * p.M) return;
+  const long long row = i / quads, col = i % quads * 4;
+  const long long N = p.kept && DUAL ? *p.kept : p.N;
+  if (col >= N) return;
+  const int count = col + 4 <= p.N ? 4 : (int)(p.N - col);
+  f32x4 v0 = {}, v1 = {};
+  const float* at = p.partial + row * p.N + col;
+  for (int s = 0; s < p.splits; s++, at += (DUAL ? 2 : 1) * plane) {
+    if (count == 4) {
+      v0 += ff_load4(at);
+      if constexpr (DUAL) v1 += ff_load4(at + plane);
+    } else {
+      for (int c = 0; c < count; c++) {
+        v0[c] += at[c];
+        if constexpr (DUAL) v1[c] += at[plane + c];
+      }
+    }
+  }
+  ff_finish<EPI, DUAL, T>(p, row, col, N, v0, v1);
+}
+
+}  // namespace mlproj
+#endif

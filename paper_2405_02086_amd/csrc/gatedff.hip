@@ -1,0 +1,316 @@
+// mlproj: the gated feed-forward block whose hidden channels the projection prunes, forward and backward:
+// argument checks, plans and the C ABI.  Kernels: ffcommon.h, ffstaged.h.
+#include "ffcommon.h"
+#include "ffcompact.h"
+#include "ffstaged.h"
+#include "host.h"
+
+namespace mlproj {
+namespace {
+
+constexpr long long FF_MAX_DIM = 1LL << 30;
+// A masked forward call of more tokens than this packs its kept channels first; fewer read every weight once
+// anyway, which is all that packing would do.
+constexpr long long FF_PACK_TOKENS = 64;
+
+static long long ff_cdiv(long long a, long long b) { return (a + b - 1) / b; }
+static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
+
+// ------------------------------------------------------------------ workspace
+struct FfLayout {
+  long long ldd;               // row length of packed and intermediate arrays: m in whole 16-byte pieces
+  size_t dG, dU;               // backward: gradients at the pre-activations, tokens x ldd
+  size_t index, position, kept, W[2], out[3];   // masked: the packed channels' maps, weights and results
+  size_t bytes;
+};
+FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
+  FfLayout L{};
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o += ff_up(bytes);
+    return at;
+  };
+  L.ldd = ff_cdiv(m, 8) * 8;
+  const size_t plane = (size_t)tokens * L.ldd * es, weights = (size_t)n * L.ldd * es;
+  if (backward) {
+    L.dG = take(plane);
+    L.dU = take(plane);
+  }
+  if (masked) {
+    L.index = take((size_t)L.ldd * 4);
+    L.position = take((size_t)L.ldd * 4);
+    L.kept = take(4);
+    for (size_t& w : L.W) w = take(weights);
+    for (int i = 0; i < (backward ? 2 : 3); i++) L.out[i] = take(backward ? weights : plane);
+  }
+  L.bytes = o + 256;
+  return L;
+}
+
+// ------------------------------------------------------------------ launches
+template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
+void ff_product(FfProduct p, hipStream_t stream) {
+  if (p.M == 0) return;
+  p.splits = 1;
+  const long long tiles = ff_cdiv(p.M, FS_M) * ff_cdiv(p.N, DUAL ? 64 : 128);
+  mark(stream);
+  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)tiles), dim3(FS_THREADS), stream, p);
+}
+
+// dG and dU from saved pre-activations; with packed channels G, U and dH are the caller's, read through the map.
+template <typename T>
+__global__ __launch_bounds__(256) void ff_slopes_kernel(FfProduct p) {
+  const long long quads = (p.N + 3) / 4, N = p.kept ? *p.kept : p.N;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= quads * p.M) return;
+  const long long row = i / quads, col = i % quads * 4;
+  if (col >= N) return;
+  f32x4 g = {}, u = {};
+  const T* pg = static_cast<const T*>(p.G) + row * p.ldg;
+  const T* pu = static_cast<const T*>(p.U) + row * p.ldg;
+  if (p.index) {
+    for (int c = 0; c < 4; c++) {
+      const int from = p.index[col + c];
+      if (from >= 0) { g[c] = (float)pg[from]; u[c] = (float)pu[from]; }
+    }
+  } else if (col + 4 <= N) {
+    g = ff_load4(pg + col);
+    u = ff_load4(pu + col);
+  } else {
+    for (int c = 0; c < N - col; c++) { g[c] = (float)pg[col + c]; u[c] = (float)pu[col + c]; }
+  }
+  ff_finish<FF_GRAD, true, T>(p, row, col, N, g, u);
+}
+// Zeros into what an empty batch leaves.
+template <typename T>
+__global__ __launch_bounds__(256) void ff_zero_kernel(T* a, T* b, long long rows, long long cols, long long ld) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i < rows * cols) a[i / cols * ld + i % cols] = b[i / cols * ld + i % cols] = (T)0.0f;
+}
+
+int ff_check(int storage, int act, const mlproj_gated_block* b) {
+  if (!b) return MLPROJ_ERR_NULL_POINTER;
+  if (storage < MLPROJ_STORE_F32 || storage > MLPROJ_STORE_F16 || act < MLPROJ_ACT_SILU || act > MLPROJ_ACT_RELU) return MLPROJ_ERR_BAD_VARIANT;
+  if (b->tokens < 0 || b->n <= 0 || b->m <= 0) return MLPROJ_ERR_BAD_DIMENSION;
+  if (b->tokens > FF_MAX_DIM || b->n > FF_MAX_DIM || b->m > FF_MAX_DIM) return MLPROJ_ERR_TOO_LARGE;
+  if (b->ldx < b->n || b->ldw < b->m) return MLPROJ_ERR_BAD_DIMENSION;
+  if (b->ldx > FF_MAX_DIM || b->ldw > FF_MAX_DIM) return MLPROJ_ERR_TOO_LARGE;
+  return MLPROJ_OK;
+}
+// An operand or result: present where it has entries, aligned to its elements, rows no longer than their stride.
+int ff_check_array(const void* p, bool needed, long long row, long long ld, int es) {
+  if (!p) return needed ? MLPROJ_ERR_NULL_POINTER : MLPROJ_OK;
+  if (ld < row) return MLPROJ_ERR_BAD_DIMENSION;
+  if (ld > FF_MAX_DIM) return MLPROJ_ERR_TOO_LARGE;
+  return aligned(p, es) ? MLPROJ_OK : MLPROJ_ERR_ALIGNMENT;
+}
+#define FF_TRY(x)                          \
+  do {                                     \
+    const int st_ = (x);                   \
+    if (st_ != MLPROJ_OK) return st_;      \
+  } while (0)
+
+int ff_check_workspace(const void* ws, size_t have, size_t need) {
+  if (!ws) return MLPROJ_ERR_NULL_POINTER;
+  return have >= need && aligned(ws, 256) ? MLPROJ_OK : MLPROJ_ERR_WORKSPACE;
+}
+
+// Enqueues the move of `count` matrices into packed form or out of it.
+template <typename T, bool GATHER>
+void ff_move(int count, const void* const* from, long long ld_from, void* const* to, long long ld_to, long long rows, long long cols,
+             const int* map, const int* kept, hipStream_t stream) {
+  FcArrays a{};
+  for (int i = 0; i < count; i++) {
+    a.from[i] = from[i];
+    a.to[i] = to[i];
+  }
+  a.ld_from = ld_from; a.ld_to = ld_to; a.rows = rows; a.cols = cols;
+  a.map = map; a.kept = kept;
+  const long long groups = ff_cdiv(rows, FC_ROWS);
+  mark(stream);
+  launch(ff_move_kernel<T, GATHER>, dim3((unsigned)ff_cdiv(cols, 256 * 8), (unsigned)(groups < 4096 ? groups : 4096), (unsigned)count), dim3(256), stream, a);
+}
+
+// A block's weights and the channels its products run over: the caller's, or the kept ones in packed form.
+struct FfChannels {
+  const void *Wg, *Wu;
+  long long ldw;
+  const int *index = nullptr, *position = nullptr, *kept = nullptr;
+};
+template <typename T>
+FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, hipStream_t stream) {
+  FfChannels c{b->Wg, b->Wu, b->ldw};
+  if (!pack) return c;
+  int *index = reinterpret_cast<int*>(ws + L.index), *position = reinterpret_cast<int*>(ws + L.position), *kept = reinterpret_cast<int*>(ws + L.kept);
+  mark(stream);
+  launch(ff_index_kernel, dim3(1), dim3(FC_THREADS), stream, b->mask, b->m, index, position, kept);
+  const void* from[2] = {b->Wg, b->Wu};
+  void* to[2] = {ws + L.W[0], ws + L.W[1]};
+  ff_move<T, true>(2, from, b->ldw, to, L.ldd, b->n, b->m, index, kept, stream);
+  c.Wg = to[0]; c.Wu = to[1]; c.ldw = L.ldd;
+  c.index = index; c.position = position; c.kept = kept;
+  return c;
+}
+
+template <typename T>
+int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, void* G, void* U, long long ldg,
+                void* workspace, hipStream_t stream) {
+  const bool pack = b->mask && b->tokens > FF_PACK_TOKENS;
+  const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, false, pack);
+  char* ws = static_cast<char*>(workspace);
+  const FfChannels ch = ff_channels<T>(b, L, ws, pack, stream);
+  FfProduct p{};
+  p.segs = 1; p.act = act;
+  p.A0 = b->X; p.lda = b->ldx;
+  p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
+  p.M = b->tokens; p.N = b->m; p.K = b->n;
+  p.C0 = H; p.ldc = ldh;
+  p.G = G; p.U = U; p.ldg = ldg;
+  void* packed[3] = {ws + L.out[0], ws + L.out[1], ws + L.out[2]};
+  if (pack) {
+    p.kept = ch.kept;
+    p.C0 = packed[0]; p.ldc = L.ldd;
+    if (G) { p.G = packed[1]; p.U = packed[2]; p.ldg = L.ldd; }
+  } else {
+    p.keep = b->mask;
+  }
+  ff_product<T, true, false, true, FF_FWD>(p, stream);
+  if (pack) {
+    void* to[2] = {G, U};
+    ff_move<T, false>(1, packed, L.ldd, &H, ldh, b->tokens, b->m, ch.position, ch.kept, stream);
+    if (G) ff_move<T, false>(2, packed + 1, L.ldd, to, ldg, b->tokens, b->m, ch.position, ch.kept, stream);
+  }
+  mark(stream);
+  return launch_status();
+}
+
+template <typename T>
+int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long ldh, const void* G, const void* U, long long ldg,
+                 void* dX, long long lddx, void* dWg, void* dWu, long long lddw, void* workspace, hipStream_t stream) {
+  if (b->tokens == 0) {
+    if (dWg) {
+      mark(stream);
+      launch(ff_zero_kernel<T>, dim3((unsigned)ff_cdiv(b->n * b->m, 256)), dim3(256), stream, static_cast<T*>(dWg), static_cast<T*>(dWu), b->n, b->m, lddw);
+    }
+    mark(stream);
+    return launch_status();
+  }
+  const bool pack = b->mask != nullptr;
+  const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, true, pack);
+  char* ws = static_cast<char*>(workspace);
+  const FfChannels ch = ff_channels<T>(b, L, ws, pack, stream);
+  T *dG = reinterpret_cast<T*>(ws + L.dG), *dU = reinterpret_cast<T*>(ws + L.dU);
+  {
+    FfProduct p{};
+    p.segs = 1; p.act = act;
+    p.M = b->tokens; p.N = b->m; p.K = b->n;
+    p.C0 = dG; p.C1 = dU; p.ldc = L.ldd;
+    p.dH = dH; p.ldh = ldh;
+    p.index = ch.index; p.kept = ch.kept;
+    if (G) {
+      p.G = const_cast<void*>(G); p.U = const_cast<void*>(U); p.ldg = ldg;
+      mark(stream);
+      launch(ff_slopes_kernel<T>, dim3((unsigned)ff_cdiv(ff_cdiv(b->m, 4) * b->tokens, 256)), dim3(256), stream, p);
+    } else {
+      p.A0 = b->X; p.lda = b->ldx;
+      p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
+      ff_product<T, true, false, true, FF_GRAD>(p, stream);
+    }
+  }
+  if (dX) {
+    FfProduct p{};
+    p.segs = 2;
+    p.A0 = dG; p.A1 = dU; p.lda = L.ldd;
+    p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
+    p.M = b->tokens; p.N = b->n; p.K = b->m;
+    p.C0 = dX; p.ldc = lddx;
+    p.kept = ch.kept;
+    ff_product<T, true, true, false, FF_STORE>(p, stream);
+  }
+  if (dWg) {
+    void* packed[2] = {ws + L.out[0], ws + L.out[1]};
+    FfProduct p{};
+    p.segs = 1;
+    p.A0 = b->X; p.lda = b->ldx;
+    p.B0 = dG; p.B1 = dU; p.ldb = L.ldd;
+    p.M = b->n; p.N = b->m; p.K = b->tokens;
+    p.C0 = pack ? packed[0] : dWg; p.C1 = pack ? packed[1] : dWu; p.ldc = pack ? L.ldd : lddw;
+    p.kept = ch.kept;
+    ff_product<T, false, false, true, FF_STORE>(p, stream);
+    if (pack) {
+      void* to[2] = {dWg, dWu};
+      ff_move<T, false>(2, packed, L.ldd, to, lddw, b->n, b->m, ch.position, ch.kept, stream);
+    }
+  }
+  mark(stream);
+  return launch_status();
+}
+
+int ff_workspace(int storage, long long tokens, long long n, long long m, int backward, int masked, size_t* out) {
+  if (!out) return MLPROJ_ERR_NULL_POINTER;
+  if (storage < MLPROJ_STORE_F32 || storage > MLPROJ_STORE_F16) return MLPROJ_ERR_BAD_VARIANT;
+  if (tokens < 0 || n <= 0 || m <= 0 || (backward | 1) != 1 || (masked | 1) != 1) return MLPROJ_ERR_BAD_DIMENSION;
+  if (tokens > FF_MAX_DIM || n > FF_MAX_DIM || m > FF_MAX_DIM || tokens * m > (1LL << 38) || tokens * n > (1LL << 38) || n * m > (1LL << 38)) return MLPROJ_ERR_TOO_LARGE;
+  *out = ff_layout(storage == MLPROJ_STORE_F32 ? 4 : 2, tokens, n, m, backward != 0, masked != 0).bytes;
+  return MLPROJ_OK;
+}
+
+}  // namespace
+}  // namespace mlproj
+
+using namespace mlproj;
+
+extern "C" {
+
+int mlproj_gated_ff_workspace_bytes(int storage, long long tokens, long long n, long long m, int backward, int masked,
+                                    size_t* bytes_out) {
+  return ff_workspace(storage, tokens, n, m, backward, masked, bytes_out);
+}
+
+int gated_ff_forward(int storage, int activation, const mlproj_gated_block* b, void* H, long long ldh, void* G, void* U,
+                     long long ldg, void* workspace, size_t workspace_bytes, void* stream) {
+  FF_TRY(ff_check(storage, activation, b));
+  const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
+  const bool some = b->tokens > 0;
+  size_t need;
+  FF_TRY(ff_workspace(storage, b->tokens, b->n, b->m, 0, b->mask != nullptr, &need));
+  FF_TRY(ff_check_array(b->X, some, b->n, b->ldx, es));
+  FF_TRY(ff_check_array(b->Wg, some, b->m, b->ldw, es));
+  FF_TRY(ff_check_array(b->Wu, some, b->m, b->ldw, es));
+  FF_TRY(ff_check_array(H, some, b->m, ldh, es));
+  FF_TRY(ff_check_array(G, U != nullptr, b->m, ldg, es));
+  FF_TRY(ff_check_array(U, G != nullptr, b->m, ldg, es));
+  FF_TRY(ff_check_workspace(workspace, workspace_bytes, need));
+  if (!some) return MLPROJ_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (storage == MLPROJ_STORE_F32) return run_forward<float>(activation, b, H, ldh, G, U, ldg, workspace, s);
+  if (storage == MLPROJ_STORE_BF16) return run_forward<bf16_t>(activation, b, H, ldh, G, U, ldg, workspace, s);
+  return run_forward<f16_t>(activation, b, H, ldh, G, U, ldg, workspace, s);
+}
+
+int gated_ff_backward(int storage, int activation, const mlproj_gated_block* b, const void* dH, long long ldh, const void* G,
+                      const void* U, long long ldg, void* dX, long long lddx, void* dWg, void* dWu, long long lddw,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  FF_TRY(ff_check(storage, activation, b));
+  const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
+  const bool some = b->tokens > 0;
+  size_t need;
+  FF_TRY(ff_workspace(storage, b->tokens, b->n, b->m, 1, b->mask != nullptr, &need));
+  FF_TRY(ff_check_array(b->X, some, b->n, b->ldx, es));
+  FF_TRY(ff_check_array(b->Wg, some, b->m, b->ldw, es));
+  FF_TRY(ff_check_array(b->Wu, some, b->m, b->ldw, es));
+  FF_TRY(ff_check_array(dH, some, b->m, ldh, es));
+  FF_TRY(ff_check_array(G, U != nullptr && some, b->m, ldg, es));
+  FF_TRY(ff_check_array(U, G != nullptr && some, b->m, ldg, es));
+  FF_TRY(ff_check_array(dX, false, b->n, lddx, es));
+  FF_TRY(ff_check_array(dWg, dWu != nullptr, b->m, lddw, es));
+  FF_TRY(ff_check_array(dWu, dWg != nullptr, b->m, lddw, es));
+  FF_TRY(ff_check_workspace(workspace, workspace_bytes, need));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (storage == MLPROJ_STORE_F32) return run_backward<float>(activation, b, dH, ldh, G, U, ldg, dX, lddx, dWg, dWu, lddw, workspace, s);
+  if (storage == MLPROJ_STORE_BF16) return run_backward<bf16_t>(activation, b, dH, ldh, G, U, ldg, dX, lddx, dWg, dWu, lddw, workspace, s);
+  return run_backward<f16_t>(activation, b, dH, ldh, G, U, ldg, dX, lddx, dWg, dWu, lddw, workspace, s);
+}
+
+}  // extern "C"

@@ -31,6 +31,7 @@
 #include <utility>
 
 #include "common.h"
+#include "host.h"
 #include "reduce.h"
 #include "aggregate.h"
 #include "search.h"
@@ -59,8 +60,6 @@ static int check_dims(long long a, long long b, long long c) {
   if (a > MAX_ELEMS / b || a * b > MAX_ELEMS / c) return MLPROJ_ERR_TOO_LARGE;
   return MLPROJ_OK;
 }
-
-static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // Elements per lane and access: 16 bytes when the rows allow it, one element otherwise.
 static int pick_vec(const void* Y, long long row_len, int elem_bytes = 4) {
@@ -110,60 +109,6 @@ static int workspace_bytes_impl(int variant, long long d0, long long d1, long lo
 static int check_radius(float eta) {
   if (!(eta >= 0.0f) || std::isinf(eta)) return MLPROJ_ERR_BAD_RADIUS;
   return MLPROJ_OK;
-}
-
-// Every kernel goes out through hipLaunchKernel, whose return value is the status of that launch
-// alone: the process-wide "last error" of the HIP runtime, which an unrelated earlier call of the
-// application may have set, is neither read nor cleared.  A refused launch is remembered for the
-// calling thread until the entry point returns (launch_status), which also stops what the call
-// had still to enqueue from going out behind it.
-static thread_local bool g_launch_refused = false;
-
-template <typename... KArgs, typename... Args>
-static inline void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_t stream, Args&&... args) {
-  static_assert(sizeof...(KArgs) == sizeof...(Args), "one argument per kernel parameter");
-  if (g_launch_refused) return;
-  std::tuple<std::decay_t<KArgs>...> held(static_cast<std::decay_t<KArgs>>(args)...);
-  const hipError_t e = std::apply(
-      [&](auto&... a) {
-        void* ptrs[] = {static_cast<void*>(&a)...};
-        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, 0, stream);
-      },
-      held);
-  if (e != hipSuccess) g_launch_refused = true;
-}
-
-static int launch_status() {
-  const bool refused = g_launch_refused;
-  g_launch_refused = false;
-  return refused ? MLPROJ_ERR_LAUNCH : MLPROJ_OK;
-}
-
-// Compute units of the current device (0 when there is none to ask).  A device's count never
-// changes, so it is asked for once per device and remembered.
-static int compute_units() {
-  constexpr int MAX_DEVICES = 64;
-  static std::atomic<int> known[MAX_DEVICES];   // 0: not asked yet
-  int dev = -1, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
-  if (dev < MAX_DEVICES && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) return 0;
-  if (dev < MAX_DEVICES) known[dev].store(cus, std::memory_order_relaxed);
-  return cus;
-}
-
-// Optional per-kernel timing: while a trace is open on the calling thread, an event is
-// recorded on the stream before every kernel of a call and after its last one.
-struct Trace {
-  hipEvent_t* events = nullptr;
-  int capacity = 0;
-  int count = 0;
-};
-static thread_local Trace g_trace;
-
-static inline void mark(hipStream_t stream) {
-  if (g_trace.events && g_trace.count < g_trace.capacity)
-    (void)hipEventRecord(g_trace.events[g_trace.count++], stream);
 }
 
 // Polls a lane of the grid-wide search may spend waiting for another workgroup's post before the
@@ -1142,7 +1087,7 @@ using namespace mlproj;
 
 extern "C" {
 
-int mlproj_version(void) { return 390; }
+int mlproj_version(void) { return 400; }
 
 const char* mlproj_status_string(int status) {
   switch (status) {
@@ -1153,9 +1098,10 @@ const char* mlproj_status_string(int status) {
     case MLPROJ_ERR_BAD_RADIUS: return "eta must be finite and >= 0";
     case MLPROJ_ERR_WORKSPACE: return "workspace too small or not 256-byte aligned";
     case MLPROJ_ERR_BAD_VARIANT: return "unknown variant";
-    case MLPROJ_ERR_ALIGNMENT: return "Y and X must be aligned to their element size";
+    case MLPROJ_ERR_ALIGNMENT: return "an array is not aligned to its element size";
     case MLPROJ_ERR_LAUNCH: return "HIP refused a kernel launch";
     case MLPROJ_ERR_NO_ALLOC_LIMIT: return "input needs more scratch memory than the built-in buffer of the no-allocation entry point holds";
+    case MLPROJ_ERR_BAD_VALUE: return "a scalar argument is out of its range";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,453 @@
+"""GPU parity of the pruned feed-forward block (gated products, norms, 4-bit products) against the 64-bit oracle.
+
+Tolerances are bounds, not fits.  With u = 2^-24 and e the unit roundoff of the storage type, a sum of K products
+in fp32 is off by at most (2 K + 64) u sum|a||b| (one rounding per addition, in whatever order and with a factor of two for
+matrix cores that align before they add; fp32 operands cut into bf16 parts lose another 2^-20), an elementary function by
+16 u of its value and its arguments' error times its slope, and a result by e of itself when it is stored."""
+import numpy as np
+import pytest
+
+from oracle import block_oracle as bo
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+ROUND = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8 * 1.001, "f16": 2.0 ** -11 * 1.001}
+TINY = {"f32": 1e-37, "bf16": 1e-37, "f16": 2.0 ** -24}      # what a stored result may lose below the normal range
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def mp():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2405_02086_amd import binding
+    binding.lib()
+    return binding
+
+
+def matrix(rng, rows, cols, dtype, scale=1.0, gap=0):
+    """A device matrix whose rows are `gap` elements further apart than they are long, and its values in 64 bits."""
+    host = torch.from_numpy(rng.standard_normal((rows, cols + gap)).astype(np.float32) * scale).to(TYPES[dtype])
+    return host.to("cuda")[:, :cols], host[:, :cols].double().numpy()
+
+
+def values(t):
+    return t.detach().double().cpu().numpy()
+
+
+def close(got, want, bound, what):
+    got = values(got)
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), "%s: %d of %d entries off, the first at %s: %r, not %r (+- %r)" % (
+        what, bad.sum(), bad.size, np.argwhere(bad)[0], got[bad][0], want[bad][0], np.broadcast_to(bound, want.shape)[bad][0])
+
+
+def sum_bound(K, dtype):
+    return (2 * K + 64) * U32 + (2.0 ** -20 if dtype == "f32" else 0.0)
+
+
+def stored(want, dtype):
+    return ROUND[dtype] * np.abs(want) + TINY[dtype]
+
+
+# |act'| <= 1.13 for both smooth activations, and |act''| <= 0.8
+SLOPE, CURVE = 1.13, 0.8
+
+SIZES = [(1, 1, 1), (2, 3, 5), (16, 256, 128), (1, 40, 300), (5, 129, 1000), (17, 33, 65), (31, 520, 72), (64, 64, 64), (65, 127, 129),
+         (128, 128, 128), (129, 200, 257), (200, 1001, 130), (257, 72, 520), (300, 264, 1032), (520, 512, 640)]
+
+
+def ff_case(mp, rng, tokens, n, m, dtype, mask_share, joined, gap=0):
+    X, x = matrix(rng, tokens, n, dtype, gap=gap)
+    if joined:
+        W, w = matrix(rng, n, 2 * m, dtype, scale=n ** -0.5, gap=gap)
+        Wg, Wu, wg, wu = W[:, :m], W[:, m:], w[:, :m], w[:, m:]
+    else:
+        (Wg, wg), (Wu, wu) = matrix(rng, n, m, dtype, n ** -0.5, gap), matrix(rng, n, m, dtype, n ** -0.5, gap)
+    mask = None
+    if mask_share is not None:
+        mask = (rng.random(m) < mask_share).astype(np.uint8)
+    return X, x, Wg, wg, Wu, wu, mask, None if mask is None else torch.from_numpy(mask).cuda()
+
+
+def check_forward(mp, rng, tokens, n, m, dtype, act, mask_share=None, joined=False, saved=False, gap=0):
+    X, x, Wg, wg, Wu, wu, mask, dmask = ff_case(mp, rng, tokens, n, m, dtype, mask_share, joined, gap)
+    H, G, U = bo.gated_ff(x, wg, wu, act, mask)
+    c = sum_bound(n, dtype)
+    eg, eu = c * (np.abs(x) @ np.abs(wg)), c * (np.abs(x) @ np.abs(wu))
+    if mask is not None:
+        eg[:, mask == 0] = eu[:, mask == 0] = 0
+    a = np.abs(bo.activation(act, G))
+    eh = (SLOPE * eg + 16 * U32 * (a + np.abs(G))) * (np.abs(U) + eu) + a * eu
+    pad = torch.full((tokens + 1, m + gap + 3), 7.0, dtype=TYPES[dtype], device="cuda")
+    out = pad[:tokens, :m]
+    g = u = None
+    if saved:
+        g, u = torch.full((2, tokens, m), 7.0, dtype=TYPES[dtype], device="cuda")
+    ws = mp.Workspace(mp.gated_ff_workspace_bytes(tokens, n, m, TYPES[dtype]))
+    ws.buf.fill_(255)
+    got = mp.gated_ff(X, Wg, Wu, act=act, mask=dmask, H=out, g_out=g, u_out=u, workspace=ws)
+    torch.cuda.synchronize()
+    assert got.data_ptr() == out.data_ptr()
+    close(out, H, eh + stored(H, dtype), "H")
+    assert (pad[tokens:] == 7).all() and (pad[:, m:] == 7).all(), "written outside of H"
+    if saved:
+        close(g, G, eg + stored(G, dtype), "G")
+        close(u, U, eu + stored(U, dtype), "U")
+
+
+def check_backward(mp, rng, tokens, n, m, dtype, act, mask_share=None, joined=False, saved=False, gap=0, need_dx=True, need_dw=True):
+    X, x, Wg, wg, Wu, wu, mask, dmask = ff_case(mp, rng, tokens, n, m, dtype, mask_share, joined, gap)
+    dH, dh = matrix(rng, tokens, m, dtype, gap=gap)
+    G = U = g = u = None
+    if saved:
+        (G, g), (U, u) = matrix(rng, tokens, m, dtype, gap=gap), matrix(rng, tokens, m, dtype, gap=gap)
+    dX, dWg, dWu, dG, dU = bo.gated_ff_backward(dh, x, wg, wu, act, mask, g, u)
+    # errors of dG and dU: of G and U where they are computed, of the functions, of one rounding to the storage type
+    c = sum_bound(n, dtype)
+    g0, u0 = (g, u) if saved else (x @ wg, x @ wu)
+    eg, eu = (0, 0) if saved else (c * (np.abs(x) @ np.abs(wg)), c * (np.abs(x) @ np.abs(wu)))
+    slope, a = np.abs(bo.activation_slope(act, g0)), np.abs(bo.activation(act, g0))
+    if act == "relu":       # the slope jumps where the sign of G is in doubt
+        jump = (np.abs(g0) <= eg).astype(float)
+        e_slope = jump
+    else:
+        e_slope = CURVE * eg + 32 * U32 * (1 + np.abs(g0))
+    e_dg = np.abs(dh) * (slope * eu + (np.abs(u0) + eu) * e_slope)
+    e_du = np.abs(dh) * (SLOPE * eg + 16 * U32 * (a + np.abs(g0)))
+    e_dg = e_dg + stored(dG, dtype) + ROUND[dtype] * e_dg
+    e_du = e_du + stored(dU, dtype) + ROUND[dtype] * e_du
+    if mask is not None:
+        e_dg[:, mask == 0] = e_du[:, mask == 0] = 0
+    kx, kw = sum_bound(2 * m, dtype), sum_bound(tokens, dtype)
+    wg_, wu_, x_ = np.abs(wg), np.abs(wu), np.abs(x)
+    ax = (np.abs(dG) + e_dg) @ wg_.T + (np.abs(dU) + e_du) @ wu_.T
+    bx = e_dg @ wg_.T + e_du @ wu_.T + kx * ax
+    bg = x_.T @ e_dg + kw * (x_.T @ (np.abs(dG) + e_dg))
+    bu = x_.T @ e_du + kw * (x_.T @ (np.abs(dU) + e_du))
+    ws = mp.Workspace(mp.gated_ff_workspace_bytes(tokens, n, m, TYPES[dtype], True))
+    ws.buf.fill_(255)
+    pads = [torch.full((r + 1, k + gap + 3), 7.0, dtype=TYPES[dtype], device="cuda") for r, k in ((tokens, n), (n, m), (n, m))]
+    outs = [p[:r, :k] for p, (r, k) in zip(pads, ((tokens, n), (n, m), (n, m)))]
+    got = mp.gated_ff_backward(dH, X, Wg, Wu, act=act, mask=dmask, G=G, U=U, dX=outs[0], dWg=outs[1], dWu=outs[2], workspace=ws,
+                               need_dx=need_dx, need_dw=need_dw)
+    torch.cuda.synchronize()
+    if need_dx:
+        close(got[0], dX, bx + stored(dX, dtype), "dX")
+    if need_dw:
+        close(got[1], dWg, bg + stored(dWg, dtype), "dWg")
+        close(got[2], dWu, bu + stored(dWu, dtype), "dWu")
+        if mask is not None:
+            assert (got[1][:, dmask == 0] == 0).all() and (got[2][:, dmask == 0] == 0).all()
+    assert (got[0] is None) == (not need_dx) and (got[1] is None) == (not need_dw)
+    for p, (r, k) in zip(pads, ((tokens, n), (n, m), (n, m))):
+        assert (p[r:] == 7).all() and (p[:, k:] == 7).all(), "written outside"
+
+
+ACTS = ["silu", "gelu", "relu"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("i", range(len(SIZES)))
+def test_gated_ff_forward(mp, i, dtype):
+    tokens, n, m = SIZES[i]
+    rng = np.random.default_rng(100 + i)
+    check_forward(mp, rng, tokens, n, m, dtype, ACTS[i % 3])
+    check_forward(mp, rng, tokens, n, m, dtype, ACTS[(i + 1) % 3], mask_share=0.4, joined=i % 2 == 0, saved=i % 4 == 1)
+    check_forward(mp, rng, tokens, n, m, dtype, ACTS[(i + 2) % 3], saved=True, gap=3 if i % 2 else 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("i", range(len(SIZES)))
+def test_gated_ff_backward(mp, i, dtype):
+    tokens, n, m = SIZES[i]
+    rng = np.random.default_rng(200 + i)
+    check_backward(mp, rng, tokens, n, m, dtype, ACTS[i % 3])
+    check_backward(mp, rng, tokens, n, m, dtype, ACTS[(i + 1) % 3], mask_share=0.4, joined=i % 2 == 0, saved=i % 4 == 1)
+    check_backward(mp, rng, tokens, n, m, dtype, ACTS[(i + 2) % 3], saved=True, gap=3 if i % 2 else 8, need_dx=i % 3 != 0, need_dw=i % 3 != 1)
+
+
+@pytest.mark.parametrize("share", [0.0, 0.02, 0.97, 1.0])
+@pytest.mark.parametrize("tokens", [1, 40, 150])
+def test_gated_ff_masks(mp, share, tokens):
+    """Nothing kept, nearly nothing, nearly everything, everything."""
+    rng = np.random.default_rng(7)
+    for dtype, n, m in (("bf16", 136, 520), ("f32", 40, 333), ("f16", 201, 77)):
+        check_forward(mp, rng, tokens, n, m, dtype, "silu", mask_share=share)
+        check_backward(mp, rng, tokens, n, m, dtype, "gelu", mask_share=share)
+        check_backward(mp, rng, tokens, n, m, dtype, "silu", mask_share=share, saved=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [3, 70, 200])
+def test_gated_ff_pruned_channels_ignore_what_they_hold(mp, dtype, tokens):
+    """NaN and infinities in the weights and gradients of pruned channels reach nothing."""
+    rng = np.random.default_rng(8)
+    n, m = 72, 264
+    X, x, Wg, wg, Wu, wu, mask, dmask = ff_case(mp, rng, tokens, n, m, dtype, 0.5, False)
+    dH, dh = matrix(rng, tokens, m, dtype)
+    G, U = torch.empty(2, tokens, m, dtype=TYPES[dtype], device="cuda")
+    clean = mp.gated_ff(X, Wg, Wu, mask=dmask, g_out=G, u_out=U)
+    grads = mp.gated_ff_backward(dH, X, Wg, Wu, mask=dmask)
+    pruned = dmask == 0
+    Wg, Wu, dH, G, U = Wg.clone(), Wu.clone(), dH.clone(), G.clone(), U.clone()
+    Wg[:, pruned] = float("nan")
+    Wu[:, pruned] = float("inf")
+    dH[:, pruned] = float("-inf")
+    G[:, pruned] = U[:, pruned] = float("nan")
+    dirty = mp.gated_ff(X, Wg, Wu, mask=dmask)
+    assert torch.equal(clean, dirty)
+    for a, b in zip(grads, mp.gated_ff_backward(dH, X, Wg, Wu, mask=dmask)):
+        assert torch.equal(a, b)
+    for a in mp.gated_ff_backward(dH, X, Wg, Wu, mask=dmask, G=G, U=U):
+        assert torch.isfinite(a).all()
+
+
+def test_gated_ff_non_finite_inputs_stay_in_their_rows(mp):
+    rng = np.random.default_rng(9)
+    for dtype in ("f32", "bf16"):
+        for tokens in (20, 150):
+            X, _ = matrix(rng, tokens, 96, dtype)
+            Wg, _ = matrix(rng, 96, 136, dtype, 0.1)
+            Wu, _ = matrix(rng, 96, 136, dtype, 0.1)
+            clean = mp.gated_ff(X, Wg, Wu)
+            X = X.clone()
+            X[3, 5] = float("nan")
+            X[7, 9] = float("inf")
+            dirty = mp.gated_ff(X, Wg, Wu)
+            assert torch.isnan(dirty[3]).all()
+            assert not torch.isfinite(dirty[7]).any()
+            rows = [t for t in range(tokens) if t not in (3, 7)]
+            assert torch.equal(clean[rows], dirty[rows])
+
+
+def test_gated_ff_without_tokens(mp):
+    for dtype in TYPES.values():
+        X = torch.empty(0, 24, dtype=dtype, device="cuda")
+        W = torch.ones(24, 40, dtype=dtype, device="cuda")
+        assert mp.gated_ff(X, W, W).shape == (0, 40)
+        dX, dWg, dWu = mp.gated_ff_backward(torch.empty(0, 40, dtype=dtype, device="cuda"), X, W, W)
+        assert dX.shape == (0, 24) and not dWg.any() and not dWu.any() and dWg.shape == (24, 40)
+
+
+@pytest.mark.parametrize("tokens,n,m", [(1, 4096, 2048), (40, 2048, 1024), (700, 1536, 1280), (2048, 1024, 1536)])
+def test_gated_ff_larger(mp, tokens, n, m):
+    rng = np.random.default_rng(10)
+    check_forward(mp, rng, tokens, n, m, "bf16", "silu", mask_share=0.5 if tokens > 1 else None, saved=True)
+    check_backward(mp, rng, tokens, n, m, "bf16", "gelu", mask_share=0.5)
+    check_backward(mp, rng, tokens, n, m, "f16", "silu", saved=True)
+
+
+def test_gated_ff_same_bits_every_time_and_on_another_stream(mp):
+    rng = np.random.default_rng(11)
+    for tokens, n, m in ((1, 2000, 520), (30, 2000, 520), (300, 1000, 700)):
+        X, x, Wg, wg, Wu, wu, mask, dmask = ff_case(mp, rng, tokens, n, m, "bf16", 0.5, False)
+        dH, _ = matrix(rng, tokens, m, "bf16")
+        torch.cuda.synchronize()
+        once = [mp.gated_ff(X, Wg, Wu), *mp.gated_ff_backward(dH, X, Wg, Wu, mask=dmask)]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = [mp.gated_ff(X, Wg, Wu), *mp.gated_ff_backward(dH, X, Wg, Wu, mask=dmask)]
+        side.synchronize()
+        for a, b in zip(once, again):
+            assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- norms
+
+NORM_SIZES = [(1, 1), (3, 5), (2, 63), (7, 64), (5, 512), (9, 513), (4, 1000), (3, 1025), (6, 2048), (5, 3001), (3, 4096), (2, 5001), (2, 8200),
+              (3, 16384), (2, 16390), (1300, 40), (700, 3003), (2100, 256)]
+
+
+def norm_case(rng, tokens, n, dtype, token_gate, gap):
+    x = matrix(rng, tokens, n, dtype, 2.0, gap)
+    b = matrix(rng, tokens, n, dtype, 0.7, gap)
+    w = [matrix(rng, 1, n, dtype) for _ in range(2)]
+    gate = matrix(rng, tokens, n, dtype, gap=gap) if token_gate else tuple(a[0] for a in matrix(rng, 1, n, dtype))
+    return x, b, (w[0][0][0], w[0][1][0]), gate, (w[1][0][0], w[1][1][0])
+
+
+def norm_forward_bounds(x, b, w_post, gate, w_pre, scale, eps, dtype):
+    """r, y and the bounds: a mean of squares is off by (n + 8) u of itself, its root by half of that."""
+    r, y = bo.block_norm(x, b, w_post, gate, w_pre, scale, eps)
+    n = x.shape[1]
+    k = (n + 32) * U32
+    er = np.zeros_like(r) if b is None else k * np.abs(r - x) + 4 * U32 * (np.abs(x) + np.abs(r))
+    ey = None
+    if y is not None:
+        # the root moves by the error of r's mean square, at most max|er| over rms
+        s = bo.rms(r, eps)
+        ey = np.abs(w_pre) * (er / s) + np.abs(y) * (k + np.sqrt((er * er).mean(1, keepdims=True)) / s)
+    return r, y, er, ey
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("i", range(len(NORM_SIZES)))
+def test_block_norm(mp, i, dtype):
+    tokens, n = NORM_SIZES[i]
+    rng = np.random.default_rng(300 + i)
+    for token_gate, gap in ((False, 0), (True, 5 if i % 2 else 0)):
+        (X, x), (B, b), (WP, wp), (G, g), (WQ, wq) = norm_case(rng, tokens, n, dtype, token_gate, gap)
+        for parts in ("both", "pre", "post"):
+            kw = dict(scale=0.6, eps=1e-5)
+            blk = {} if parts == "pre" else dict(b=B, w_post=WP, gate=G)
+            ref = {} if parts == "pre" else dict(b=b, w_post=wp, gate=g)
+            pre = None if parts == "post" else WQ
+            r, y, er, ey = norm_forward_bounds(x, ref.get("b"), ref.get("w_post"), ref.get("gate"), None if pre is None else wq, 0.6, 1e-5, dtype)
+            R, Y = mp.block_norm(X, w_pre=pre, **blk, **kw)
+            torch.cuda.synchronize()
+            if parts == "pre":
+                assert R is X
+            else:
+                close(R, r, er + stored(r, dtype), "r")
+            if pre is None:
+                assert Y is None
+            else:
+                close(Y, y, ey + stored(y, dtype), "y")
+    # in place: r over x, y over b
+    want_r, want_y = mp.block_norm(X, B, WP, G, WQ, scale=0.6)
+    Xc, Bc = X.clone(), B.clone()
+    mp.block_norm(Xc, Bc, WP, G, WQ, scale=0.6, r=Xc, y=Bc)
+    assert torch.equal(Xc, want_r) and torch.equal(Bc, want_y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("i", range(len(NORM_SIZES)))
+def test_block_norm_backward(mp, i, dtype):
+    tokens, n = NORM_SIZES[i]
+    rng = np.random.default_rng(400 + i)
+    eps, scale = 1e-5, 0.6
+    for token_gate, gap in ((False, 0), (True, 5 if i % 2 else 0)):
+        (R, r), (B, b), (WP, wp), (G, g), (WQ, wq) = norm_case(rng, tokens, n, dtype, token_gate, gap)
+        (DR, dr), (DY, dy) = matrix(rng, tokens, n, dtype, gap=gap), matrix(rng, tokens, n, dtype, gap=gap)
+        for parts in ("both", "pre", "post", "no dr"):
+            blk = {} if parts == "pre" else dict(b=B, w_post=WP, gate=G)
+            ref = {} if parts == "pre" else dict(b=b, w_post=wp, gate=g)
+            pre, wpre = (None, None) if parts == "post" else (WQ, wq)
+            DRp, drp = (None, None) if parts == "no dr" else (DR, dr)
+            dx, db, dwp, dg, dwq = bo.block_norm_backward(drp, dy, r, w_pre=wpre, scale=scale, eps=eps, **ref)
+            ws = mp.Workspace(mp.block_norm_workspace_bytes(tokens, n))
+            ws.buf.fill_(255)
+            got = mp.block_norm_backward(DRp, None if pre is None else DY, R, w_pre=pre, scale=scale, eps=eps, workspace=ws, **blk)
+            torch.cuda.synchronize()
+            # every sum over a row of n terms is off by (n + 32) u of the sum of its terms' magnitudes, every elementwise
+            # result by a few u of its terms
+            k = (n + 64) * U32
+            sr, sb = bo.rms(r, eps), bo.rms(b, eps)
+            e = np.zeros_like(r) if wpre is None else np.abs(wq * dy)
+            spread = np.abs(r) / sr * (np.abs(r) / sr * e).mean(1, keepdims=True) / sr
+            mag_x = np.abs(drp if drp is not None else 0) + e / sr + spread
+            ex = k * mag_x
+            close(got[0], dx, ex + stored(dx, dtype), "dx")
+            if pre is None:
+                assert got[4] is None
+            else:
+                t = np.abs(dy * (r / sr))
+                close(got[4], dwq, (k + (tokens + 16) * U32) * t.sum(0) + 1e-37, "dw_pre")
+            if parts == "pre":
+                assert got[1] is None and got[2] is None and got[3] is None
+                continue
+            f = np.abs(scale * g * wp)
+            bh = np.abs(b) / sb
+            fx = f * mag_x
+            close(got[1], db, 4 * k * (fx / sb + bh * (bh * fx).mean(1, keepdims=True) / sb) + stored(db, dtype), "db")
+            close(got[2], dwp, (4 * k + (tokens + 16) * U32) * (np.abs(scale * g) * mag_x * bh).sum(0) + 1e-37, "dw_post")
+            tg = np.abs(scale * wp) * mag_x * bh
+            if token_gate:
+                close(got[3], dg, 4 * k * tg + stored(dg, dtype), "dgate")
+            else:
+                close(got[3], dg, (4 * k + (tokens + 16) * U32) * tg.sum(0) + 1e-37, "dgate")
+
+
+def test_block_norm_in_place_gradients_and_zero_rows(mp):
+    rng = np.random.default_rng(12)
+    for n in (100, 1500, 17000):
+        (R, r), (B, b), (WP, wp), (G, g), (WQ, wq) = norm_case(rng, 6, n, "bf16", False, 0)
+        (DR, dr), (DY, dy) = matrix(rng, 6, n, "bf16"), matrix(rng, 6, n, "bf16")
+        R, B = R.clone(), B.clone()
+        R[2] = 0
+        B[3] = 0
+        want = mp.block_norm_backward(DR, DY, R, B, WP, G, WQ)
+        assert all(torch.isfinite(t).all() for t in want)
+        DRc, Bc = DR.clone(), B.clone()
+        got = mp.block_norm_backward(DRc, DY, R, Bc, WP, G, WQ, dx=DRc, db=Bc)
+        for a, c in zip(want, got):
+            assert torch.equal(a, c)
+        r2, y2 = mp.block_norm(torch.zeros(2, n, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, n, dtype=torch.bfloat16, device="cuda"), WP, G, WQ)
+        assert not r2.any() and not y2.any()
+
+
+def test_block_norm_without_tokens(mp):
+    e = torch.empty(0, 48, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(48, dtype=torch.bfloat16, device="cuda")
+    r, y = mp.block_norm(e, e, w, w, w)
+    assert r.shape == y.shape == (0, 48)
+    dx, db, dwp, dg, dwq = mp.block_norm_backward(e, e, e, e, w, w, w)
+    assert dx.shape == (0, 48) and not dwp.any() and not dg.any() and not dwq.any()
+
+
+# ---------------------------------------------------------------- 4-bit weights
+
+W4_SIZES = [(1, 1), (5, 3), (32, 16), (100, 33), (128, 16), (129, 17), (300, 200), (1000, 250), (2048, 64), (257, 1040)]
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_w4_pack(mp, dtype, group):
+    rng = np.random.default_rng(13)
+    for n, m in [(1, 1), (5, 3), (130, 33), (300, 17)]:
+        W, w = matrix(rng, n, m, dtype, 0.05, gap=3)
+        if m > 2:
+            W[:, 1] = 0           # a pruned column
+            w[:, 1] = 0
+        codes, scales = bo.w4_quantise(w, group)
+        want, want_scales = bo.w4_layout(codes, scales, group)
+        packed = mp.w4_pack(W, group)
+        torch.cuda.synchronize()
+        assert np.array_equal(packed.codes.cpu().numpy().reshape(want.shape), want)
+        assert np.array_equal(packed.scales.float().cpu().numpy().reshape(want_scales.shape), want_scales)
+
+
+def w4_matrix(mp, rng, n, m, group):
+    W, w = matrix(rng, n, m, "f32", n ** -0.5)
+    codes, scales = bo.w4_quantise(w, group)
+    return mp.w4_pack(W, group), bo.w4_values(codes, scales, group)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 16, 17, 32, 33, 64, 65, 150])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_w4_products(mp, dtype, tokens):
+    rng = np.random.default_rng(14 + tokens)
+    for i, (n, m) in enumerate(W4_SIZES):
+        group = (32, 64, 128)[(i + tokens) % 3]
+        act = ACTS[i % 3]
+        gap = (0, 3, 8)[i % 3]
+        X, x = matrix(rng, tokens, n, dtype, gap=gap)
+        Wg, wg = w4_matrix(mp, rng, n, m, group)
+        Wu, wu = w4_matrix(mp, rng, n, m, group)
+        c = sum_bound(n, dtype)
+        g, u = x @ wg, x @ wu
+        eg, eu = c * (np.abs(x) @ np.abs(wg)), c * (np.abs(x) @ np.abs(wu))
+        pad = torch.full((tokens + 1, m + 3), 7.0, dtype=TYPES[dtype], device="cuda")
+        mp.w4_matvec(X, Wg, y=pad[:tokens, :m])
+        torch.cuda.synchronize()
+        close(pad[:tokens, :m], g, eg + stored(g, dtype), "y")
+        assert (pad[tokens:] == 7).all() and (pad[:, m:] == 7).all()
+        a = np.abs(bo.activation(act, g))
+        h = bo.activation(act, g) * u
+        eh = (SLOPE * eg + 16 * U32 * (a + np.abs(g))) * (np.abs(u) + eu) + a * eu
+        close(mp.w4_gated_matvec(X, Wg, Wu, act=act), h, eh + stored(h, dtype), "h")
+
+
+def test_w4_larger_and_no_tokens(mp):
+    rng = np.random.default_rng(15)
+    for n, m, group, dtype, tokens in ((4096, 1024, 128, "bf16", 1), (8192, 256, 32, "f16", 16), (1000, 4100, 64, "bf16", 5)):
+        W, w = w4_matrix(mp, rng, n, m, group)
+        X, x = matrix(rng, tokens, n, dtype)
+        y = x @ w
+        close(mp.w4_matvec(X, W), y, sum_bound(n, dtype) * (np.abs(x) @ np.abs(w)) + stored(y, dtype), "y")
+        assert torch.equal(mp.w4_matvec(X, W), mp.w4_matvec(X, W))
+    assert mp.w4_matvec(torch.empty(0, 1000, device="cuda"), W).shape == (0, 4100)
