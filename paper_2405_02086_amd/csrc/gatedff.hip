@@ -2,6 +2,7 @@
 // argument checks, plans and the C ABI.  Kernels: ffcommon.h, ffstaged.h.
 #include "ffcommon.h"
 #include "ffcompact.h"
+#include "ffdirect.h"
 #include "ffstaged.h"
 #include "host.h"
 
@@ -49,12 +50,32 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
 }
 
 // ------------------------------------------------------------------ launches
+// Whether a product's operands can go straight into LDS: 16-bit elements, rows, starts and row lengths in whole
+// 16-byte pieces, and a tile's rows within a buffer resource's 2 GiB.
+// (A row's last piece may reach past N where B is the workspace's, whose rows are filled up.)
+template <bool A_KC, bool B_KC, typename T>
+bool ff_direct(const FfProduct& p) {
+  if (sizeof(T) != 2) return false;
+  const long long a_row = A_KC ? p.K : p.M, b_row = B_KC ? p.K : (p.filled ? 0 : p.N);
+  for (const void* q : {p.A0, p.A1, p.B0, p.B1})
+    if (!aligned(q, 16)) return false;
+  return a_row % 8 == 0 && b_row % 8 == 0 && p.lda % 8 == 0 && p.ldb % 8 == 0 && p.lda < (1 << 22) && p.ldb < (1 << 22) &&
+         p.K < (1LL << 31) - 64;
+}
+
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_product(FfProduct p, hipStream_t stream) {
   if (p.M == 0) return;
   p.splits = 1;
-  const long long tiles = ff_cdiv(p.M, FS_M) * ff_cdiv(p.N, DUAL ? 64 : 128);
   mark(stream);
+  if constexpr (sizeof(T) == 2) {
+    if (ff_direct<A_KC, B_KC, T>(p)) {
+      const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)tiles), dim3(512), stream, p);
+      return;
+    }
+  }
+  const long long tiles = ff_cdiv(p.M, FS_M) * ff_cdiv(p.N, DUAL ? 64 : 128);
   launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)tiles), dim3(FS_THREADS), stream, p);
 }
 
@@ -135,12 +156,12 @@ void ff_move(int count, const void* const* from, long long ld_from, void* const*
 // A block's weights and the channels its products run over: the caller's, or the kept ones in packed form.
 struct FfChannels {
   const void *Wg, *Wu;
-  long long ldw;
+  long long ldw, m;            // m: how many there can be
   const int *index = nullptr, *position = nullptr, *kept = nullptr;
 };
 template <typename T>
 FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, hipStream_t stream) {
-  FfChannels c{b->Wg, b->Wu, b->ldw};
+  FfChannels c{b->Wg, b->Wu, b->ldw, b->m};
   if (!pack) return c;
   int *index = reinterpret_cast<int*>(ws + L.index), *position = reinterpret_cast<int*>(ws + L.position), *kept = reinterpret_cast<int*>(ws + L.kept);
   mark(stream);
@@ -148,7 +169,7 @@ FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws,
   const void* from[2] = {b->Wg, b->Wu};
   void* to[2] = {ws + L.W[0], ws + L.W[1]};
   ff_move<T, true>(2, from, b->ldw, to, L.ldd, b->n, b->m, index, kept, stream);
-  c.Wg = to[0]; c.Wu = to[1]; c.ldw = L.ldd;
+  c.Wg = to[0]; c.Wu = to[1]; c.ldw = c.m = L.ldd;
   c.index = index; c.position = position; c.kept = kept;
   return c;
 }
@@ -164,7 +185,7 @@ int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, vo
   p.segs = 1; p.act = act;
   p.A0 = b->X; p.lda = b->ldx;
   p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
-  p.M = b->tokens; p.N = b->m; p.K = b->n;
+  p.M = b->tokens; p.N = ch.m; p.K = b->n;
   p.C0 = H; p.ldc = ldh;
   p.G = G; p.U = U; p.ldg = ldg;
   void* packed[3] = {ws + L.out[0], ws + L.out[1], ws + L.out[2]};
@@ -204,14 +225,14 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
   {
     FfProduct p{};
     p.segs = 1; p.act = act;
-    p.M = b->tokens; p.N = b->m; p.K = b->n;
+    p.M = b->tokens; p.N = ch.m; p.K = b->n;
     p.C0 = dG; p.C1 = dU; p.ldc = L.ldd;
     p.dH = dH; p.ldh = ldh;
     p.index = ch.index; p.kept = ch.kept;
     if (G) {
       p.G = const_cast<void*>(G); p.U = const_cast<void*>(U); p.ldg = ldg;
       mark(stream);
-      launch(ff_slopes_kernel<T>, dim3((unsigned)ff_cdiv(ff_cdiv(b->m, 4) * b->tokens, 256)), dim3(256), stream, p);
+      launch(ff_slopes_kernel<T>, dim3((unsigned)ff_cdiv(ff_cdiv(ch.m, 4) * b->tokens, 256)), dim3(256), stream, p);
     } else {
       p.A0 = b->X; p.lda = b->ldx;
       p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
@@ -223,7 +244,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.segs = 2;
     p.A0 = dG; p.A1 = dU; p.lda = L.ldd;
     p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
-    p.M = b->tokens; p.N = b->n; p.K = b->m;
+    p.M = b->tokens; p.N = b->n; p.K = ch.m;
     p.C0 = dX; p.ldc = lddx;
     p.kept = ch.kept;
     ff_product<T, true, true, false, FF_STORE>(p, stream);
@@ -235,6 +256,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.A0 = b->X; p.lda = b->ldx;
     p.B0 = dG; p.B1 = dU; p.ldb = L.ldd;
     p.M = b->n; p.N = b->m; p.K = b->tokens;
+    p.filled = true;
     p.C0 = pack ? packed[0] : dWg; p.C1 = pack ? packed[1] : dWu; p.ldc = pack ? L.ldd : lddw;
     p.kept = ch.kept;
     ff_product<T, false, false, true, FF_STORE>(p, stream);
