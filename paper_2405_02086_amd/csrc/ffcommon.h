@@ -44,7 +44,6 @@ struct FfProduct {
   const void* dH;              // GRAD
   long long ldg, ldh;
   const unsigned char* keep;   // one byte per column of the result, or null
-  const int* index;            // packed channels (ffcompact.h): the column of dH that a column of the product stands for, or null: its own number
   const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
   float* partial;              // PARTIAL: [splits][products][M][N]
   int splits;
@@ -72,6 +71,19 @@ __device__ __forceinline__ void ff_store4(T* p, f32x4 x) {
 #pragma unroll
   for (int i = 0; i < 4; i++) t.v[i] = ff_round<T>(x[i]);
   __builtin_memcpy(p, &t, sizeof(t));
+}
+
+// Eight neighbouring elements of which the first `valid` exist, the others zeros.
+template <typename T>
+__device__ __forceinline__ FfVec8<T> ff_load8(const T* p, long long valid) {
+  FfVec8<T> r;
+  if (valid >= 8) {
+    __builtin_memcpy(&r, p, sizeof(r));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i++) r.v[i] = i < valid ? p[i] : (T)0.0f;
+  }
+  return r;
 }
 
 // ------------------------------------------------------------------ activation
@@ -116,9 +128,7 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
     f32x4 d = {};
     if constexpr (EPI == FF_GRAD) {
       const T* dh = static_cast<const T*>(p.dH) + row * p.ldh;
-      if (p.index) {
-        for (int i = 0; i < count; i++) d[i] = p.index[col + i] >= 0 ? (float)dh[p.index[col + i]] : 0.0f;
-      } else if (whole) {
+      if (whole) {
         d = ff_load4(dh + col);
       } else {
         for (int i = 0; i < count; i++) d[i] = (float)dh[col + i];

@@ -7,76 +7,123 @@
 namespace mlproj {
 
 // ------------------------------------------------------------------ kept channels
-// What the projection leaves of a weight matrix is a set of whole columns, scattered over its rows.  Column j of
-// the packed matrices is column index[j] of the caller's; their number is known on the device only, so kernels are
-// launched for m columns and workgroups past the kept ones leave at once.  The number is filled up to a
-// multiple of 8 with columns of zeros (index -1), which keeps packed rows in whole 16-byte pieces.
-// position[c] is where the caller's column c went, or -1.
-constexpr int FC_THREADS = 1024;
-__global__ __launch_bounds__(FC_THREADS) void ff_index_kernel(const unsigned char* mask, long long m, int* index, int* position, int* kept) {
+// What the projection leaves of a weight matrix is a set of whole columns, scattered over its rows.  They are packed
+// side by side in their order; their number is known on the device only, so kernels are launched for m columns and
+// workgroups past the kept ones leave at once.  The number is filled up to a multiple of 8 with columns of zeros,
+// which keeps packed rows in whole 16-byte pieces.
+// position[c], c = 0 .. m: where the caller's column c went, p, or ~p if it was pruned, with p the number of
+// kept columns before it either way.
+constexpr int FC_THREADS = 1024, FC_OWN = 16;
+__global__ __launch_bounds__(FC_THREADS) void ff_index_kernel(const unsigned char* mask, long long m, int* position, int* kept) {
   __shared__ int wave_sum[FC_THREADS / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int base = 0;
-  for (long long at = 0; at < m; at += FC_THREADS) {
-    const long long c = at + threadIdx.x;
-    const bool there = c < m && mask[c];
-    const unsigned long long votes = __ballot(there);
-    if (lane == 0) wave_sum[wave] = __popcll(votes);
-    __syncthreads();
-    int before = base, all = 0;
-    for (int w = 0; w < FC_THREADS / 64; w++) {
-      if (w < wave) before += wave_sum[w];
-      all += wave_sum[w];
+  for (long long at = 0; at < m; at += FC_THREADS * FC_OWN) {
+    const long long c0 = at + (long long)threadIdx.x * FC_OWN;
+    unsigned char own[FC_OWN];
+    if (c0 + FC_OWN <= m) {
+      __builtin_memcpy(own, mask + c0, FC_OWN);
+    } else {
+#pragma unroll
+      for (int i = 0; i < FC_OWN; i++) own[i] = c0 + i < m ? mask[c0 + i] : 0;
     }
-    const int mine = before + __popcll(votes & ((1ull << lane) - 1));
-    if (c < m) position[c] = there ? mine : -1;
-    if (there) index[mine] = (int)c;
-    base += all;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < FC_OWN; i++) count += own[i] != 0;
+    int upto = count;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int below = __shfl_up(upto, s);
+      if (lane >= s) upto += below;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    int p = base + upto - count;
+    for (int w = 0; w < FC_THREADS / 64; w++) {
+      if (w < wave) p += wave_sum[w];
+      base += wave_sum[w];
+    }
+#pragma unroll
+    for (int i = 0; i < FC_OWN; i++) {
+      if (c0 + i < m) position[c0 + i] = own[i] ? p : ~p;
+      p += own[i] != 0;
+    }
     __syncthreads();
   }
-  const int whole = (base + 7) / 8 * 8;
-  if (threadIdx.x < whole - base) index[base + threadIdx.x] = -1;
-  if (threadIdx.x == 0) *kept = whole;
+  if (threadIdx.x == 0) {
+    position[m] = ~base;
+    *kept = (base + 7) / 8 * 8;
+  }
 }
 
 struct FcArrays {
-  const void* from[3];
-  void* to[3];
-  long long ld_from, ld_to, rows, cols;   // cols: of the caller's matrices
-  const int* map;                         // index or position
-  const int* kept;
+  const void* from[4];
+  void* to[4];
+  long long ld_from[4], ld_to[4], rows[4];
+  long long cols;                         // of the caller's matrices
+  const int *position, *kept;
+  int count, groups[4];                   // matrices; workgroups along each one's rows
 };
 
-// Eight columns x FC_ROWS rows per thread; the map's eight entries are read once for all of them.  GATHER: packed
-// columns from the caller's, else the caller's from packed ones, with zeros where a channel was pruned.
-constexpr int FC_ROWS = 8;
-template <typename T, bool GATHER>
+// A workgroup moves FC_COLS columns of the caller's matrix, FC_ROWS rows at a time, through LDS: packed ones out of the
+// caller's (PACK), or the caller's out of packed ones with zeros where a channel was pruned.  Both sides of memory see
+// whole 16-byte pieces of consecutive columns; the single elements are picked from LDS.  Bound by HBM: 4096 x 16384 bf16
+// at 40 % kept, two matrices, 375 MB.
+constexpr int FC_COLS = 2048, FC_ROWS = 4;
+template <typename T, bool PACK>
 __global__ __launch_bounds__(256) void ff_move_kernel(FcArrays a) {
-  const long long limit = GATHER ? *a.kept : a.cols;
-  const long long col = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (col >= limit) return;
-  const T* from = static_cast<const T*>(a.from[blockIdx.z]);
-  T* to = static_cast<T*>(a.to[blockIdx.z]);
-  const int count = limit - col < 8 ? (int)(limit - col) : 8;
-  int map[8];
+  __shared__ T held[FC_ROWS][FC_COLS + 8];
+  __shared__ short source[PACK ? FC_COLS : 1];
+  int which = 0, group = blockIdx.y;
+  while (which + 1 < a.count && group >= a.groups[which]) group -= a.groups[which++];
+  const T* from = static_cast<const T*>(a.from[which]);
+  T* to = static_cast<T*>(a.to[which]);
+  const long long ld_from = a.ld_from[which], ld_to = a.ld_to[which], rows = a.rows[which];
+  const long long c0 = (long long)blockIdx.x * FC_COLS, c1 = c0 + FC_COLS < a.cols ? c0 + FC_COLS : a.cols;
+  auto before = [&](long long c) { const int p = a.position[c]; return p < 0 ? ~p : p; };
+  const int p0 = before(c0), p1 = before(c1);
+  const int wide = (int)(c1 - c0), packed = p1 - p0;
+  const int t8 = threadIdx.x * 8;
+  int place[8];                                   // my eight columns in the packed segment, or -1
 #pragma unroll
-  for (int i = 0; i < 8; i++) map[i] = i < count ? a.map[col + i] : -1;
-  for (long long r0 = (long long)blockIdx.y * FC_ROWS; r0 < a.rows; r0 += (long long)gridDim.y * FC_ROWS) {
+  for (int i = 0; i < 8; i++) {
+    const int p = t8 + i < wide ? a.position[c0 + t8 + i] : -1;
+    place[i] = p < 0 ? -1 : p - p0;
+    if (PACK && p >= 0) source[p - p0] = (short)(t8 + i);
+  }
+  if (PACK) __syncthreads();
+  // the last segment also writes the columns of zeros that fill the packed rows up
+  const int filled = PACK ? (c1 == a.cols ? *a.kept - p0 : packed) : wide;
+  const int in = PACK ? wide : packed, out = filled;
+  from += PACK ? c0 : p0;
+  to += PACK ? p0 : c0;
+  int pick[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) pick[i] = PACK ? (t8 + i < packed ? source[t8 + i] : -1) : place[i];
+  for (long long r0 = (long long)group * FC_ROWS; r0 < rows; r0 += (long long)a.groups[which] * FC_ROWS) {
     FfVec8<T> v[FC_ROWS];
 #pragma unroll
-    for (int r = 0; r < FC_ROWS; r++)
+    for (int r = 0; r < FC_ROWS; r++) {
+      const long long left = r0 + r < rows ? in - t8 : 0;
+      v[r] = ff_load8(from + (r0 + r) * ld_from + t8, left);
+    }
+    __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 8; i++) v[r].v[i] = map[i] >= 0 && r0 + r < a.rows ? from[(r0 + r) * a.ld_from + map[i]] : (T)0.0f;
+    for (int r = 0; r < FC_ROWS; r++) *reinterpret_cast<FfVec8<T>*>(&held[r][t8]) = v[r];
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < FC_ROWS; r++) {
-      if (r0 + r >= a.rows) break;
-      T* at = to + (r0 + r) * a.ld_to + col;
-      if (count == 8) {
-        __builtin_memcpy(at, &v[r], sizeof(v[r]));
+      if (r0 + r >= rows || t8 >= out) continue;
+      T* at = to + (r0 + r) * ld_to + t8;
+      FfVec8<T> w;
+#pragma unroll
+      for (int i = 0; i < 8; i++) w.v[i] = pick[i] >= 0 ? held[r][pick[i]] : (T)0.0f;
+      if (t8 + 8 <= out) {
+        __builtin_memcpy(at, &w, sizeof(w));
       } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-          if (i < count) at[i] = v[r].v[i];
+          if (t8 + i < out) at[i] = w.v[i];
       }
     }
   }

@@ -31,19 +31,6 @@ template <typename E> struct FfFrag;
 template <> struct FfFrag<bf16_t> { using type = bf16x8; };
 template <> struct FfFrag<f16_t> { using type = f16x8; };
 
-// Eight neighbouring elements of which the first `valid` exist, the others zeros.
-template <typename T>
-__device__ __forceinline__ FfVec8<T> fs_load8(const T* p, long long valid) {
-  FfVec8<T> r;
-  if (valid >= 8) {
-    __builtin_memcpy(&r, p, sizeof(r));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) r.v[i] = i < valid ? p[i] : (T)0.0f;
-  }
-  return r;
-}
-
 // Eight elements as the 16 bytes of each of their parts.
 template <typename T>
 __device__ __forceinline__ void fs_parts(const FfVec8<T>& x, u32x4 (&out)[FfParts<T>::count]) {
@@ -128,21 +115,21 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
       const int c = tid + i * FS_THREADS;
       if constexpr (A_KC) {
         const long long r = row0 + (c >> 2), k = k0 + (c & 3) * 8;
-        ra[i] = fs_load8(A + r * p.lda + k, r < p.M ? K - k : 0);
+        ra[i] = ff_load8(A + r * p.lda + k, r < p.M ? K - k : 0);
       } else {
         const long long k = k0 + (c >> 4), r = row0 + (c & 15) * 8;
-        ra[i] = fs_load8(A + k * p.lda + r, k < K ? p.M - r : 0);
+        ra[i] = ff_load8(A + k * p.lda + r, k < K ? p.M - r : 0);
       }
       if constexpr (B_KC) {
         const int j = c >> 2;
         const T* B = static_cast<const T*>(DUAL ? (j < 64 ? p.B0 : p.B1) : (seg ? p.B1 : p.B0));
         const long long col = col0 + (DUAL ? j & 63 : j), k = k0 + (c & 3) * 8;
-        rb[i] = fs_load8(B + col * p.ldb + k, col < N ? K - k : 0);
+        rb[i] = ff_load8(B + col * p.ldb + k, col < N ? K - k : 0);
       } else {
         const int j = (c & 15) * 8;
         const T* B = static_cast<const T*>(DUAL ? (j < 64 ? p.B0 : p.B1) : (seg ? p.B1 : p.B0));
         const long long col = col0 + (DUAL ? j & 63 : j), k = k0 + (c >> 4);
-        rb[i] = fs_load8(B + k * p.ldb + col, k < K ? N - col : 0);
+        rb[i] = ff_load8(B + k * p.ldb + col, k < K ? N - col : 0);
       }
     }
   };

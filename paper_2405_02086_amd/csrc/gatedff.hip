@@ -21,7 +21,7 @@ static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
 struct FfLayout {
   long long ldd;               // row length of packed and intermediate arrays: m in whole 16-byte pieces
   size_t dG, dU;               // backward: gradients at the pre-activations, tokens x ldd
-  size_t index, position, kept, W[2], out[3];   // masked: the packed channels' maps, weights and results
+  size_t position, kept, W[2], in[3], out[3];   // masked: where the channels went; packed weights, inputs and results
   size_t bytes;
 };
 FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
@@ -39,10 +39,11 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
     L.dU = take(plane);
   }
   if (masked) {
-    L.index = take((size_t)L.ldd * 4);
-    L.position = take((size_t)L.ldd * 4);
+    L.position = take((size_t)(m + 1) * 4);
     L.kept = take(4);
     for (size_t& w : L.W) w = take(weights);
+    if (backward)
+      for (size_t& i : L.in) i = take(plane);
     for (int i = 0; i < (backward ? 2 : 3); i++) L.out[i] = take(backward ? weights : plane);
   }
   L.bytes = o + 256;
@@ -79,7 +80,7 @@ void ff_product(FfProduct p, hipStream_t stream) {
   launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)tiles), dim3(FS_THREADS), stream, p);
 }
 
-// dG and dU from saved pre-activations; with packed channels G, U and dH are the caller's, read through the map.
+// dG and dU from saved pre-activations.
 template <typename T>
 __global__ __launch_bounds__(256) void ff_slopes_kernel(FfProduct p) {
   const long long quads = (p.N + 3) / 4, N = p.kept ? *p.kept : p.N;
@@ -88,18 +89,13 @@ __global__ __launch_bounds__(256) void ff_slopes_kernel(FfProduct p) {
   const long long row = i / quads, col = i % quads * 4;
   if (col >= N) return;
   f32x4 g = {}, u = {};
-  const T* pg = static_cast<const T*>(p.G) + row * p.ldg;
-  const T* pu = static_cast<const T*>(p.U) + row * p.ldg;
-  if (p.index) {
-    for (int c = 0; c < 4; c++) {
-      const int from = p.index[col + c];
-      if (from >= 0) { g[c] = (float)pg[from]; u[c] = (float)pu[from]; }
-    }
-  } else if (col + 4 <= N) {
-    g = ff_load4(pg + col);
-    u = ff_load4(pu + col);
+  const T* pg = static_cast<const T*>(p.G) + row * p.ldg + col;
+  const T* pu = static_cast<const T*>(p.U) + row * p.ldg + col;
+  if (col + 4 <= N) {
+    g = ff_load4(pg);
+    u = ff_load4(pu);
   } else {
-    for (int c = 0; c < N - col; c++) { g[c] = (float)pg[col + c]; u[c] = (float)pu[col + c]; }
+    for (int c = 0; c < N - col; c++) { g[c] = (float)pg[c]; u[c] = (float)pu[c]; }
   }
   ff_finish<FF_GRAD, true, T>(p, row, col, N, g, u);
 }
@@ -137,40 +133,40 @@ int ff_check_workspace(const void* ws, size_t have, size_t need) {
   return have >= need && aligned(ws, 256) ? MLPROJ_OK : MLPROJ_ERR_WORKSPACE;
 }
 
-// Enqueues the move of `count` matrices into packed form or out of it.
-template <typename T, bool GATHER>
-void ff_move(int count, const void* const* from, long long ld_from, void* const* to, long long ld_to, long long rows, long long cols,
-             const int* map, const int* kept, hipStream_t stream) {
+// Matrices to be moved into packed form or out of it, all in one launch.
+template <typename T, bool PACK>
+struct FfMove {
   FcArrays a{};
-  for (int i = 0; i < count; i++) {
-    a.from[i] = from[i];
-    a.to[i] = to[i];
+  FfMove(long long cols, const int* position, const int* kept) { a.cols = cols; a.position = position; a.kept = kept; }
+  void add(const void* from, long long ld_from, void* to, long long ld_to, long long rows) {
+    const int i = a.count++;
+    a.from[i] = from; a.ld_from[i] = ld_from; a.to[i] = to; a.ld_to[i] = ld_to; a.rows[i] = rows;
+    const long long groups = ff_cdiv(rows, FC_ROWS);
+    a.groups[i] = (int)(groups < 4096 ? groups : 4096);
   }
-  a.ld_from = ld_from; a.ld_to = ld_to; a.rows = rows; a.cols = cols;
-  a.map = map; a.kept = kept;
-  const long long groups = ff_cdiv(rows, FC_ROWS);
-  mark(stream);
-  launch(ff_move_kernel<T, GATHER>, dim3((unsigned)ff_cdiv(cols, 256 * 8), (unsigned)(groups < 4096 ? groups : 4096), (unsigned)count), dim3(256), stream, a);
-}
+  void go(hipStream_t stream) {
+    int groups = 0;
+    for (int i = 0; i < a.count; i++) groups += a.groups[i];
+    mark(stream);
+    launch(ff_move_kernel<T, PACK>, dim3((unsigned)ff_cdiv(a.cols, FC_COLS), (unsigned)groups), dim3(256), stream, a);
+  }
+};
 
 // A block's weights and the channels its products run over: the caller's, or the kept ones in packed form.
 struct FfChannels {
   const void *Wg, *Wu;
   long long ldw, m;            // m: how many there can be
-  const int *index = nullptr, *position = nullptr, *kept = nullptr;
+  int *position = nullptr, *kept = nullptr;
 };
-template <typename T>
 FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, hipStream_t stream) {
   FfChannels c{b->Wg, b->Wu, b->ldw, b->m};
   if (!pack) return c;
-  int *index = reinterpret_cast<int*>(ws + L.index), *position = reinterpret_cast<int*>(ws + L.position), *kept = reinterpret_cast<int*>(ws + L.kept);
+  c.position = reinterpret_cast<int*>(ws + L.position);
+  c.kept = reinterpret_cast<int*>(ws + L.kept);
   mark(stream);
-  launch(ff_index_kernel, dim3(1), dim3(FC_THREADS), stream, b->mask, b->m, index, position, kept);
-  const void* from[2] = {b->Wg, b->Wu};
-  void* to[2] = {ws + L.W[0], ws + L.W[1]};
-  ff_move<T, true>(2, from, b->ldw, to, L.ldd, b->n, b->m, index, kept, stream);
-  c.Wg = to[0]; c.Wu = to[1]; c.ldw = c.m = L.ldd;
-  c.index = index; c.position = position; c.kept = kept;
+  launch(ff_index_kernel, dim3(1), dim3(FC_THREADS), stream, b->mask, b->m, c.position, c.kept);
+  c.Wg = ws + L.W[0]; c.Wu = ws + L.W[1];
+  c.ldw = c.m = L.ldd;
   return c;
 }
 
@@ -180,7 +176,13 @@ int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, vo
   const bool pack = b->mask && b->tokens > FF_PACK_TOKENS;
   const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, false, pack);
   char* ws = static_cast<char*>(workspace);
-  const FfChannels ch = ff_channels<T>(b, L, ws, pack, stream);
+  const FfChannels ch = ff_channels(b, L, ws, pack, stream);
+  if (pack) {
+    FfMove<T, true> in(b->m, ch.position, ch.kept);
+    in.add(b->Wg, b->ldw, ws + L.W[0], L.ldd, b->n);
+    in.add(b->Wu, b->ldw, ws + L.W[1], L.ldd, b->n);
+    in.go(stream);
+  }
   FfProduct p{};
   p.segs = 1; p.act = act;
   p.A0 = b->X; p.lda = b->ldx;
@@ -198,9 +200,13 @@ int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, vo
   }
   ff_product<T, true, false, true, FF_FWD>(p, stream);
   if (pack) {
-    void* to[2] = {G, U};
-    ff_move<T, false>(1, packed, L.ldd, &H, ldh, b->tokens, b->m, ch.position, ch.kept, stream);
-    if (G) ff_move<T, false>(2, packed + 1, L.ldd, to, ldg, b->tokens, b->m, ch.position, ch.kept, stream);
+    FfMove<T, false> out(b->m, ch.position, ch.kept);
+    out.add(packed[0], L.ldd, H, ldh, b->tokens);
+    if (G) {
+      out.add(packed[1], L.ldd, G, ldg, b->tokens);
+      out.add(packed[2], L.ldd, U, ldg, b->tokens);
+    }
+    out.go(stream);
   }
   mark(stream);
   return launch_status();
@@ -220,7 +226,25 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
   const bool pack = b->mask != nullptr;
   const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, true, pack);
   char* ws = static_cast<char*>(workspace);
-  const FfChannels ch = ff_channels<T>(b, L, ws, pack, stream);
+  const FfChannels ch = ff_channels(b, L, ws, pack, stream);
+  if (pack) {
+    // what runs over the channels: the weights where a product reads them, dH and the saved pre-activations
+    void *W[2] = {ws + L.W[0], ws + L.W[1]}, *in[3] = {ws + L.in[0], ws + L.in[1], ws + L.in[2]};
+    FfMove<T, true> weights(b->m, ch.position, ch.kept), planes(b->m, ch.position, ch.kept);
+    if (dX || !G) {
+      weights.add(b->Wg, b->ldw, W[0], L.ldd, b->n);
+      weights.add(b->Wu, b->ldw, W[1], L.ldd, b->n);
+      weights.go(stream);
+    }
+    planes.add(dH, ldh, in[0], L.ldd, b->tokens);
+    if (G) {
+      planes.add(G, ldg, in[1], L.ldd, b->tokens);
+      planes.add(U, ldg, in[2], L.ldd, b->tokens);
+      G = in[1]; U = in[2]; ldg = L.ldd;
+    }
+    planes.go(stream);
+    dH = in[0]; ldh = L.ldd;
+  }
   T *dG = reinterpret_cast<T*>(ws + L.dG), *dU = reinterpret_cast<T*>(ws + L.dU);
   {
     FfProduct p{};
@@ -228,7 +252,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.M = b->tokens; p.N = ch.m; p.K = b->n;
     p.C0 = dG; p.C1 = dU; p.ldc = L.ldd;
     p.dH = dH; p.ldh = ldh;
-    p.index = ch.index; p.kept = ch.kept;
+    p.kept = ch.kept;
     if (G) {
       p.G = const_cast<void*>(G); p.U = const_cast<void*>(U); p.ldg = ldg;
       mark(stream);
@@ -261,8 +285,10 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.kept = ch.kept;
     ff_product<T, false, false, true, FF_STORE>(p, stream);
     if (pack) {
-      void* to[2] = {dWg, dWu};
-      ff_move<T, false>(2, packed, L.ldd, to, lddw, b->n, b->m, ch.position, ch.kept, stream);
+      FfMove<T, false> out(b->m, ch.position, ch.kept);
+      out.add(packed[0], L.ldd, dWg, lddw, b->n);
+      out.add(packed[1], L.ldd, dWu, lddw, b->n);
+      out.go(stream);
     }
   }
   mark(stream);

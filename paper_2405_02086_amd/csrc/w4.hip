@@ -74,7 +74,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
         for (int q = 0; q < 4; q++) {
           const long long at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
           u32x4 parts[P];
-          fs_parts(fs_load8(x + t * a.ldx + at, t < a.tokens && there ? a.n - at : 0), parts);
+          fs_parts(ff_load8(x + t * a.ldx + at, t < a.tokens && there ? a.n - at : 0), parts);
 #pragma unroll
           for (int p = 0; p < P; p++) __builtin_memcpy(&xf[u][mt][p][q], &parts[p], 16);
         }
