@@ -9,33 +9,33 @@
 namespace mlproj {
 
 // ------------------------------------------------------------------ tiles straight into LDS
-// A tile is FD_K = 64 deep; two of them lie in LDS, one being computed while the loads of the next one, 16 bytes
-// per lane and straight into LDS, are under way.  One barrier per step: behind it the step's tile is complete
-// and everybody has left the other one.
+// A tile is 32 deep.  FD_STAGES of them lie in LDS as a ring: while the matrix cores work on the operands of one, which are in
+// registers, the next one's are read from LDS and the loads of the ones behind it, 16 bytes per lane and straight into
+// LDS, are under way.  One barrier per tile: behind it the next tile is complete and everybody has left the present one's
+// place, which the loads of the tile FD_STAGES further on then take.
 //
-// The tile is cut into parts of 64 or 128 rows (of A), columns (of B).  A part whose K runs along memory rows is [row][64]:
-// 128 bytes per row, the 16-byte pieces permuted by row % 8.  A part whose memory rows are the K index is
-// [64][columns], read with the transposing load, the 32-byte pieces permuted so that the eight rows a half
-// wavefront reads lie in different banks.  Lanes write LDS in order, so the permutation is applied to the
-// addresses they load from.
+// The tile is cut into parts of 64 or 128 rows (of A), columns (of B).  A part whose K runs along memory rows is [row][32]:
+// 64 bytes per row, its 16-byte pieces permuted by the row's number so that eight rows spread over all banks.  A part
+// whose memory rows are the K index is read with the transposing load, whose half wavefront reads 32 bytes (16 columns) of
+// eight rows k = 16 G + 8 g + 4 h + r (one G and h; g < 2, r < 4); so those eight rows x 64 columns are a block of 1 KiB,
+// [32 columns: 2][row 4 g + r][64 bytes], in which rows with g = 1 have their two halves exchanged: the half wavefront meets
+// every bank once, the four lanes that load a row's 64 bytes stay within one cache line, and operand after
+// operand lies at constant distances.  Lanes write LDS in order, so all permutations are applied to the addresses they load from.
 //
 // Requires (checked by ff_direct): 16-byte aligned operands, rows and K (or the row length) in whole 16-byte pieces.
 // Outside the matrix a lane's offset lies past the end of the buffer resource and the load returns zeros.
-constexpr int FD_K = 64;
+constexpr int FD_K = 32, FD_STAGES = 4;
 constexpr unsigned FD_OUT = 0xfffffff0u;         // past any buffer
 
 typedef __attribute__((address_space(3))) void fd_lds_t;
 
-// The swizzle of a part read with the transposing load: which 32-byte piece holds piece 0 of memory row k.
-template <int W>
-__device__ __forceinline__ int fd_turn(int k) {
-  return W == 128 ? (k & 3) | (((k >> 3) & 1) << 2) : ((k >> 1) & 1) | (((k >> 3) & 1) << 1);
-}
+// What the 16-byte pieces of a row [row][32] are permuted by.
+__device__ __forceinline__ int fd_row_turn(int row) { return (row >> 1) & 3; }
 
 // Loads of one part.  offset[i]: where lane's i-th piece lies from the part's first element of the step.
 template <bool KC, int W, int THREADS>
 struct FdPart {
-  static constexpr int LOADS = W * 8 / THREADS;
+  static constexpr int LOADS = W * FD_K / 8 / THREADS;
   unsigned offset[LOADS];
   unsigned k_of[LOADS];                          // KC: first K index of the piece within the step
 
@@ -45,13 +45,13 @@ struct FdPart {
     for (int i = 0; i < LOADS; i++) {
       const int p = tid + i * THREADS;
       if constexpr (KC) {
-        const int row = p >> 3, piece = (p & 7) ^ (row & 7);
+        const int row = p / (FD_K / 8), piece = (p % (FD_K / 8)) ^ fd_row_turn(row);
         offset[i] = row < there ? (unsigned)(row * ld * 2 + piece * 16) : FD_OUT;
         k_of[i] = piece * 8;
       } else {
-        constexpr int PIECES = W / 8;
-        const int k = p / PIECES, pos = p % PIECES;
-        const int col = (((pos >> 1) ^ fd_turn<W>(k)) * 2 + (pos & 1)) * 8;
+        const int block = p >> 6, in = p & 63, row = (in >> 2) & 7;
+        const int k = (block >> 1 & 1) * 16 + (row >> 2) * 8 + (block & 1) * 4 + (row & 3);
+        const int col = (block >> 2) * 64 + (in >> 5) * 32 + (((in >> 1) & 1) ^ (row >> 2)) * 16 + (in & 1) * 8;
         offset[i] = col < there ? (unsigned)(k * ld * 2 + col * 2) : FD_OUT;
       }
     }
@@ -69,22 +69,30 @@ struct FdPart {
   }
 };
 
-// Sixteen rows (columns) x 32 along K of the part at lds + part, as a lane's operand.  (Every address is one step
-// from the array it lies in: the compiler then still sees which of the two halves of the buffer it reads, and does not wait for
-// loads into the other one.)
-template <bool KC, int W, typename F>
-__device__ __forceinline__ F fd_frag(const unsigned char* lds, int part, int idx, int kk, int lane) {
-  F r;
+// Where a lane finds its operands in a part, from the part's sixteen rows (columns) number `first` on: the place of the
+// first one and of the second one.
+struct FdFrom { int at[2]; };
+template <bool KC>
+__device__ __forceinline__ FdFrom fd_from(int part, int first, int lane) {
   const int g = lane >> 4, c = lane & 15;
+  if (KC) {
+    const int at = part + (first * 16 + c) * (FD_K * 2) + ((g ^ fd_row_turn(c)) << 4);
+    return {{at, at + 16 * FD_K * 2}};
+  }
+  const int at = part + (first >> 2) * 4096 + ((first >> 1) & 1) * 512 + (g >> 1) * 2048 + ((g & 1) * 4 + (c >> 2)) * 64 + (c & 3) * 8;
+  return {{at + ((g & 1) << 5), at + ((~g & 1) << 5)}};
+}
+// Operand number idx from there on, `part` bytes further.  (Every address is one step from the array it lies in: the
+// compiler then still sees which stage it reads, and does not wait for loads into the others.)
+template <bool KC, typename F>
+__device__ __forceinline__ F fd_frag(const unsigned char* lds, const FdFrom& from, int part, int idx) {
+  F r;
   if constexpr (KC) {
-    const int at = part + (idx * 16 + c) * 128 + (((kk * 4 + g) ^ (c & 7)) << 4);
-    r = *reinterpret_cast<const F*>(lds + at);
+    r = *reinterpret_cast<const F*>(lds + (from.at[0] + (part + idx * 16 * FD_K * 2)));
   } else {
-    const int k = kk * 32 + 8 * g + (c >> 2);
-    const int at = part + k * (W * 2) + ((idx ^ fd_turn<W>(8 * g + (c >> 2))) << 5) + ((c & 3) << 3);
+    const int at = from.at[idx & 1] + (part + (idx >> 2) * 4096 + ((idx >> 1) & 1) * 512);
     typedef __attribute__((address_space(3))) s16x4 lds_t;
-    // (four rows further down the turn is the same: it does not look at bit 2)
-    s16x4 half[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(lds + at)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(lds + (at + 4 * W * 2)))};
+    s16x4 half[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(lds + at)), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(lds + (at + 1024)))};
     __builtin_memcpy(&r, half, 16);
   }
   return r;
@@ -106,28 +114,27 @@ __device__ __forceinline__ bool fd_tile(long long tiles_m, long long tiles_n, lo
   return true;
 }
 
-// The order of a step's instructions from group G on (see compute): the group's matrix instructions, then the reads
-// of the group two further on, and, in the last groups of the first half, one of B's operands of the second half.
-template <int G, int GROUPS, int PER, int READ_A, int READ_B, int LATE, int HALF>
+// The order of a step's instructions: its LDS reads spread evenly between its matrix instructions.
+template <int DONE, int MFMAS, int READS>
 __device__ __forceinline__ void fd_schedule() {
-  if constexpr (G < GROUPS) {
-    __builtin_amdgcn_sched_group_barrier(0x8, PER, 0);
-    constexpr int reads = (G + 2 < GROUPS ? READ_A : 0) + (G >= LATE && G < HALF ? READ_B * ((PER + HALF - LATE - 1) / (HALF - LATE)) : 0);
-    if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
-    fd_schedule<G + 1, GROUPS, PER, READ_A, READ_B, LATE, HALF>();
+  if constexpr (DONE < READS) {
+    constexpr int upto = (DONE + 1) * MFMAS / READS, from = DONE * MFMAS / READS;
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    if constexpr (upto > from) __builtin_amdgcn_sched_group_barrier(0x8, upto - from, 0);
+    fd_schedule<DONE + 1, MFMAS, READS>();
   }
 }
 
 // BM x BN of the result (two products: BM x BN/2 of each) per workgroup of WM x WN wavefronts.
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void ff_direct_kernel(FfProduct p) {
+__global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p) {
   using F = typename FfFrag<T>::type;
   constexpr int THREADS = WM * WN * 64;
   constexpr int AW = BM < 128 ? BM : 128, AP = BM / AW;        // A's parts: rows in one, how many
   constexpr int BW = BN / 2;                                   // B: two parts
   constexpr int RI = BM / WM / 16, CJ = BN / WN / 32;          // 16 x 16 tiles of a wavefront: down, across in each half
   constexpr int STAGE = (BM + BN) * FD_K * 2;
-  __shared__ __align__(16) unsigned char lds0[STAGE], lds1[STAGE];
+  __shared__ __align__(16) unsigned char lds0[STAGE], lds1[STAGE], lds2[STAGE], lds3[STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   constexpr bool SUMS_CHANNELS = A_KC && B_KC;                 // dX: K runs over the hidden channels
@@ -165,57 +172,66 @@ __global__ __launch_bounds__(WM * WN * 64) void ff_direct_kernel(FfProduct p) {
   };
 
   f32x4 acc[RI][2 * CJ] = {};
-  // A step: 2 RI groups of 2 CJ matrix instructions, one per 16 rows and half of K.  The operands of a group are
-  // read two groups ahead, and those of B's second half during the first one; left to itself the compiler reads everything
-  // at once and spills (KS operands: 102 to 164 registers).
-  auto compute = [&](const unsigned char* lds) {
-    constexpr int READ_A = A_KC ? 1 : 2, READ_B = B_KC ? 1 : 2;
-    F a[FD_K / 32][RI], b[FD_K / 32][2 * CJ];
+  struct Operands { F a[RI], b[2 * CJ]; };
+  const FdFrom from_a = fd_from<A_KC>((wm * RI / (AW / 16)) * AW * FD_K * 2, wm * RI % (AW / 16), lane);
+  const FdFrom from_b = fd_from<B_KC>(BM * FD_K * 2, wn * CJ, lane);
+  auto read = [&](const unsigned char* lds) {
+    Operands o;
+    // (B's operands, which live until the tile's last instruction, in the middle of A's, which free their registers in turn)
 #pragma unroll
-    for (int kk = 0; kk < FD_K / 32; kk++) {
+    for (int i = 0; i < RI / 2; i++) o.a[i] = fd_frag<A_KC, F>(lds, from_a, 0, i);
 #pragma unroll
-      for (int j = 0; j < 2 * CJ; j++)
-        b[kk][j] = fd_frag<B_KC, BW, F>(lds, (BM + (j / CJ) * BW) * FD_K * 2, wn * CJ + j % CJ, kk, lane);
+    for (int j = 0; j < 2 * CJ; j++) o.b[j] = fd_frag<B_KC, F>(lds, from_b, (j / CJ) * BW * FD_K * 2, j % CJ);
 #pragma unroll
-      for (int i = 0; i < RI; i++) {
-        const int r = wm * RI + i;
-        a[kk][i] = fd_frag<A_KC, AW, F>(lds, (r / (AW / 16)) * AW * FD_K * 2, r % (AW / 16), kk, lane);
-      }
-#pragma unroll
-      for (int i = 0; i < RI; i++)
-#pragma unroll
-        for (int j = 0; j < 2 * CJ; j++) acc[i][j] = ff_mfma(b[kk][j], a[kk][i], acc[i][j]);
-    }
-    constexpr int LATE = RI >= 2 * CJ ? RI - 2 * CJ : 0;
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * CJ * READ_B + 2 * READ_A, 0);
-    fd_schedule<0, 2 * RI, 2 * CJ, READ_A, READ_B, LATE, RI>();
+    for (int i = RI / 2; i < RI; i++) o.a[i] = fd_frag<A_KC, F>(lds, from_a, 0, i);
+    return o;
   };
-  // behind this: the loads of the step are in LDS, and nobody reads the other half any more
+  auto multiply = [&](const Operands& o) {
+#pragma unroll
+    for (int i = 0; i < RI; i++)
+#pragma unroll
+      for (int j = 0; j < 2 * CJ; j++) acc[i][j] = ff_mfma(o.b[j], o.a[i], acc[i][j]);
+  };
+  // Behind this all loads but those of the last `tiles` tiles are in LDS, and nobody reads what was read before.
+  constexpr int LOADS = (AW * AP + BN) * FD_K / 8 / THREADS;
   auto meet = [&]() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0) lgkmcnt(0)
+    // vmcnt((FD_STAGES - 2) LOADS) lgkmcnt(0)
+    constexpr int v = (FD_STAGES - 2) * LOADS;
+    __builtin_amdgcn_s_waitcnt(0x0070 | (v & 15) | ((v >> 4) << 14));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+  };
+  constexpr int READS = RI * (A_KC ? 1 : 2) + 2 * CJ * (B_KC ? 1 : 2);
+  Operands even, odd;
+  auto step_of = [&](int step, unsigned char* here, unsigned char* next, const Operands& now, Operands& then) {
+    meet();
+    load(step + FD_STAGES, here);
+    then = read(next);
+    multiply(now);
+    fd_schedule<0, RI * 2 * CJ, READS>();
   };
 
   // (a load past the last step asks for nothing and brings zeros)
   load(first, lds0);
+  load(first + 1, lds1);
+  load(first + 2, lds2);
+  meet();
+  even = read(lds0);
+  load(first + 3, lds3);
   int step = first;
-  for (; step + 1 < last; step += 2) {
-    meet();
-    load(step + 1, lds1);
-    compute(lds0);
-    meet();
-    load(step + 2, lds0);
-    compute(lds1);
+  for (; step + 3 < last; step += 4) {
+    step_of(step, lds0, lds1, even, odd);
+    step_of(step + 1, lds1, lds2, odd, even);
+    step_of(step + 2, lds2, lds3, even, odd);
+    step_of(step + 3, lds3, lds0, odd, even);
   }
-  if (step < last) {
-    meet();
-    compute(lds0);
-  }
+  if (step < last) step_of(step, lds0, lds1, even, odd);
+  if (step + 1 < last) step_of(step + 1, lds1, lds2, odd, even);
+  if (step + 2 < last) step_of(step + 2, lds2, lds3, even, odd);
   // no load may be under way when the workgroup's LDS is given to another
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);
+  __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0)
 
 #pragma unroll
   for (int i = 0; i < RI; i++) {

@@ -5,6 +5,7 @@
 #include "ffdirect.h"
 #include "ffstaged.h"
 #include "host.h"
+#include <cstdlib>
 
 namespace mlproj {
 namespace {
@@ -71,8 +72,14 @@ void ff_product(FfProduct p, hipStream_t stream) {
   mark(stream);
   if constexpr (sizeof(T) == 2) {
     if (ff_direct<A_KC, B_KC, T>(p)) {
+      static const int variant = getenv("FFV") ? atoi(getenv("FFV")) : 0;
+      if (variant == 0) {
       const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
       launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)tiles), dim3(512), stream, p);
+      } else if (variant == 1) {
+      const long long tiles = ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)tiles), dim3(256), stream, p);
+      }
       return;
     }
   }
