@@ -89,25 +89,67 @@ __device__ __forceinline__ FfVec8<T> ff_load8(const T* p, long long valid) {
 // ------------------------------------------------------------------ activation
 // act(g) and its slope in fp32.  silu: g s with s = 1/(1 + e^-g), slope s (1 + g (1 - s)).  gelu: g Phi(g),
 // slope Phi(g) + g phi(g).  relu: max(g, 0), slope 1 where g > 0 (NaN stays NaN in the product).
-__device__ __forceinline__ float ff_act(int act, float g) {
-  if (act == MLPROJ_ACT_SILU) return g / (1.0f + expf(-g));
-  if (act == MLPROJ_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678f));
-  return g > 0.0f ? g : (g == g ? 0.0f : g);
+//
+// EXACT (fp32 storage) takes the library's functions.  Results that are rounded to 16 bits take the hardware's exponential and
+// reciprocal (an ulp of fp32 each) and, for erf, Abramowitz and Stegun 7.1.26, off by 1.5e-7 at most: in the
+// epilogue of a 256 x 256 tile the library's forms cost a tenth of the whole tile's time.
+template <bool EXACT> __device__ __forceinline__ float ff_exp(float x) {
+  return EXACT ? expf(x) : __builtin_amdgcn_exp2f(x * 1.44269504f);
 }
-__device__ __forceinline__ float ff_slope(int act, float g) {
+template <bool EXACT> __device__ __forceinline__ float ff_reciprocal(float x) {
+  return EXACT ? 1.0f / x : __builtin_amdgcn_rcpf(x);
+}
+// erf(x) given e = exp(-x^2)
+template <bool EXACT> __device__ __forceinline__ float ff_erf(float x, float e) {
+  if (EXACT) return erff(x);
+  const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * fabsf(x));
+  const float y = 1.0f - ((((1.061405429f * t - 1.453152027f) * t + 1.421413741f) * t - 0.284496736f) * t + 0.254829592f) * t * e;
+  return copysignf(y, x);
+}
+template <bool EXACT> __device__ __forceinline__ void ff_gate4(int act, f32x4 g, f32x4& value, f32x4& slope) {
   if (act == MLPROJ_ACT_SILU) {
-    const float s = 1.0f / (1.0f + expf(-g));
-    return s * (1.0f + g * (1.0f - s));
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float s = ff_reciprocal<EXACT>(1.0f + ff_exp<EXACT>(-g[i]));
+      value[i] = g[i] * s;
+      slope[i] = s * (1.0f + g[i] * (1.0f - s));
+    }
+  } else if (act == MLPROJ_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float e = ff_exp<EXACT>(-0.5f * g[i] * g[i]);
+      const float phi = 0.5f * (1.0f + ff_erf<EXACT>(g[i] * 0.70710678f, e));
+      value[i] = g[i] * phi;
+      slope[i] = phi + g[i] * 0.39894228f * e;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      value[i] = g[i] > 0.0f ? g[i] : (g[i] == g[i] ? 0.0f : g[i]);
+      slope[i] = g[i] > 0.0f ? 1.0f : (g[i] == g[i] ? 0.0f : g[i]);
+    }
   }
-  if (act == MLPROJ_ACT_GELU) return 0.5f * (1.0f + erff(g * 0.70710678f)) + g * 0.39894228f * expf(-0.5f * g * g);
-  return g > 0.0f ? 1.0f : (g == g ? 0.0f : g);
 }
 
 // ------------------------------------------------------------------ epilogue
 // Columns col .. col+3 of row `row`, of which those below N exist; v0, v1: their sums in the two products.
 // A pruned channel's outputs are zeros whatever its sums are, NaN included.
+// ff_upstream: GRAD's four entries of dH; all of a thread's are fetched before its first store, which the compiler
+// could not move them across.
+template <typename T>
+__device__ __forceinline__ FfVec4<T> ff_upstream(const FfProduct& p, long long row, long long col, long long N) {
+  FfVec4<T> d;
+  const T* at = static_cast<const T*>(p.dH) + row * p.ldh + col;
+  if (col + 4 <= N) {
+    __builtin_memcpy(&d, at, sizeof(d));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) d.v[i] = col + i < N ? at[i] : (T)0.0f;
+  }
+  return d;
+}
 template <int EPI, bool DUAL, typename T>
-__device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, long long col, long long N, f32x4 v0, f32x4 v1) {
+__device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, long long col, long long N, f32x4 v0, f32x4 v1, FfVec4<T> d) {
   const bool whole = col + 4 <= N;
   const int count = whole ? 4 : (int)(N - col);
   if constexpr (EPI == FF_PARTIAL) {
@@ -125,25 +167,21 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
   }
   f32x4 o0 = v0, o1 = v1;
   if constexpr (EPI == FF_FWD || EPI == FF_GRAD) {
-    f32x4 d = {};
-    if constexpr (EPI == FF_GRAD) {
-      const T* dh = static_cast<const T*>(p.dH) + row * p.ldh;
-      if (whole) {
-        d = ff_load4(dh + col);
-      } else {
-        for (int i = 0; i < count; i++) d[i] = (float)dh[col + i];
+    f32x4 value, slope;
+    ff_gate4<sizeof(T) == 4>(p.act, v0, value, slope);
+    if constexpr (EPI == FF_FWD) {
+      o0 = value * v1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        o0[i] = (float)d.v[i] * v1[i] * slope[i];
+        o1[i] = (float)d.v[i] * value[i];
       }
     }
+    if (p.keep) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const float g = v0[i], u = v1[i];
-      if constexpr (EPI == FF_FWD) {
-        o0[i] = ff_act(p.act, g) * u;
-      } else {
-        o0[i] = d[i] * u * ff_slope(p.act, g);
-        o1[i] = d[i] * ff_act(p.act, g);
-      }
-      if (p.keep && i < count && !p.keep[col + i]) o0[i] = o1[i] = v0[i] = v1[i] = 0.0f;
+      for (int i = 0; i < 4; i++)
+        if (i < count && !p.keep[col + i]) o0[i] = o1[i] = v0[i] = v1[i] = 0.0f;
     }
   }
   T* c0 = static_cast<T*>(p.C0) + row * p.ldc + col;

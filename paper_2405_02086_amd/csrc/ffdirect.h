@@ -233,18 +233,27 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p)
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0)
 
+  const long long my_row = row0 + wm * RI * 16 + (lane & 15), my_col = col0 + wn * CJ * 16 + (lane >> 4) * 4;
+  FfVec4<T> d[RI][CJ] = {};
+  if constexpr (EPI == FF_GRAD) {
+#pragma unroll
+    for (int i = 0; i < RI; i++)
+#pragma unroll
+      for (int j = 0; j < CJ; j++)
+        if (my_row + i * 16 < p.M && my_col + j * 16 < N) d[i][j] = ff_upstream<T>(p, my_row + i * 16, my_col + j * 16, N);
+  }
 #pragma unroll
   for (int i = 0; i < RI; i++) {
-    const long long row = row0 + (wm * RI + i) * 16 + (lane & 15);
+    const long long row = my_row + i * 16;
     if (row >= p.M) continue;
 #pragma unroll
     for (int j = 0; j < CJ; j++) {
-      const long long col = col0 + (wn * CJ + j) * 16 + (lane >> 4) * 4;
+      const long long col = my_col + j * 16;
       if constexpr (DUAL) {
-        if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][CJ + j]);
+        if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][CJ + j], d[i][j]);
       } else {
-        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{});
-        if (col + BW < N) ff_finish<EPI, false, T>(p, row, col + BW, N, acc[i][CJ + j], f32x4{});
+        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, {});
+        if (col + BW < N) ff_finish<EPI, false, T>(p, row, col + BW, N, acc[i][CJ + j], f32x4{}, {});
       }
     }
   }

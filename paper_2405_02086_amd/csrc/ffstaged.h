@@ -175,6 +175,16 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
           for (int j = 0; j < 4; j++) acc[i][j] = ff_mfma(b[sum - ka][j], a[ka][i], acc[i][j]);
   }
 
+  FfVec4<T> d[4][2] = {};
+  if constexpr (EPI == FF_GRAD) {
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+      for (int j = 0; j < 2; j++) {
+        const long long row = row0 + wm * 64 + i * 16 + (lane & 15), col = col0 + wn * 32 + j * 16 + (lane >> 4) * 4;
+        if (row < p.M && col < N) d[i][j] = ff_upstream<T>(p, row, col, N);
+      }
+  }
 #pragma unroll
   for (int i = 0; i < 4; i++) {
     const long long row = row0 + wm * 64 + i * 16 + (lane & 15);
@@ -183,10 +193,10 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
     for (int j = 0; j < 2; j++) {
       const long long col = col0 + wn * 32 + j * 16 + (lane >> 4) * 4;
       if constexpr (DUAL) {
-        if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][2 + j]);
+        if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][2 + j], d[i][j]);
       } else {
-        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{});
-        if (col + 64 < N) ff_finish<EPI, false, T>(p, row, col + 64, N, acc[i][2 + j], f32x4{});
+        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, {});
+        if (col + 64 < N) ff_finish<EPI, false, T>(p, row, col + 64, N, acc[i][2 + j], f32x4{}, {});
       }
     }
   }
@@ -215,7 +225,9 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p) {
       }
     }
   }
-  ff_finish<EPI, DUAL, T>(p, row, col, N, v0, v1);
+  FfVec4<T> d = {};
+  if constexpr (EPI == FF_GRAD) d = ff_upstream<T>(p, row, col, N);
+  ff_finish<EPI, DUAL, T>(p, row, col, N, v0, v1, d);
 }
 
 }  // namespace mlproj

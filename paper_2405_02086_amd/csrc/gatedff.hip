@@ -5,7 +5,6 @@
 #include "ffdirect.h"
 #include "ffstaged.h"
 #include "host.h"
-#include <cstdlib>
 
 namespace mlproj {
 namespace {
@@ -18,12 +17,62 @@ constexpr long long FF_PACK_TOKENS = 64;
 static long long ff_cdiv(long long a, long long b) { return (a + b - 1) / b; }
 static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
 
+// ------------------------------------------------------------------ plan of a product
+// Which tiles a product takes and into how many shares its sum is cut.  Three kinds of tiles: direct 256 x 256 (one workgroup
+// per compute unit), direct 128 x 128 (two), staged 128 x 128 (three).  What a 32-deep step of a tile takes with every place
+// taken, the price of a workgroup beside its steps and the price of joining shares were measured (4096 x 4096 x 16384
+// and 1000 x 1000 x 20000, bf16 and fp32); the plan is the cheapest of them.
+struct FfPlan {
+  int kind;      // 0: direct 256, 1: direct 128, 2: staged
+  int splits;
+};
+struct FfKind {
+  int rows, cols, places;      // of the tile; workgroups per compute unit
+  double step_us, tile_us;
+};
+static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool direct, int es) {
+  static const FfKind kinds[3] = {{256, 256, 1, 0.86, 9.0}, {128, 128, 2, 0.53, 5.0}, {128, 128, 3, 1.3, 5.0}};
+  FfPlan best{2, 1};
+  double least = 1e30;
+  for (int kind = direct ? 0 : 2; kind <= (direct ? 1 : 2); kind++) {
+    const FfKind& k = kinds[kind];
+    const double step_us = k.step_us * (kind == 2 && es == 4 ? 4.0 : 1.0);
+    const long long tiles = ff_cdiv(M, k.rows) * ff_cdiv(N, dual ? k.cols / 2 : k.cols);
+    const double planes = 4.0 * M * N * (dual ? 2 : 1);
+    for (int splits = 1; splits <= 64; splits *= 2) {
+      if (splits > 1 && (steps / splits < 8 || planes * splits > 512e6)) break;
+      const double units = 256.0 * k.places, groups = (double)tiles * splits;
+      // workgroups in turn on the fullest place; a place shared with empty ones is faster, at best as fast as half of them
+      const double turns = ff_cdiv((long long)groups, (long long)units);
+      const double share = groups < units / 2 && k.places > 1 ? 0.65 : 1.0;
+      double us = turns * ((double)ff_cdiv(steps, splits) * step_us * share + k.tile_us);
+      if (splits > 1) us += 4.0 + planes * (splits + splits) / 4.0e6;
+      if (us < least) {
+        least = us;
+        best = {kind, splits};
+      }
+    }
+  }
+  return best;
+}
+static long long ff_steps(long long K, int segs) { return ff_cdiv(K, 32) * segs; }
+static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, int es) {
+  size_t most = 0;
+  for (int direct = 0; direct < 2; direct++) {
+    const FfPlan plan = ff_plan(M, N, ff_steps(K, segs), dual, direct, es);
+    const size_t bytes = plan.splits > 1 ? (size_t)plan.splits * (dual ? 2 : 1) * M * N * 4 : 0;
+    if (bytes > most) most = bytes;
+  }
+  return most;
+}
+
 // ------------------------------------------------------------------ workspace
 struct FfLayout {
   long long ldd;               // row length of packed and intermediate arrays: m in whole 16-byte pieces
+  size_t partial;              // shares of sums, of one product at a time
   size_t dG, dU;               // backward: gradients at the pre-activations, tokens x ldd
   size_t position, kept, W[2], in[3], out[3];   // masked: where the channels went; packed weights, inputs and results
-  size_t bytes;
+  size_t shares, bytes;
 };
 FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
   FfLayout L{};
@@ -34,6 +83,20 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
     return at;
   };
   L.ldd = ff_cdiv(m, 8) * 8;
+  // (the packed channels' products run over ldd of them)
+  const long long widest = masked ? L.ldd : m;
+  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, es);
+  if (backward) {
+    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, es), w = ff_partial_bytes(n, m, tokens, 1, true, es);
+    shares = shares > x ? shares : x;
+    shares = shares > w ? shares : w;
+  }
+  if (masked) {      // a workspace for masked calls serves the others too
+    const size_t plain = ff_layout(es, tokens, n, m, backward, false).shares;
+    shares = shares > plain ? shares : plain;
+  }
+  L.shares = shares;
+  L.partial = take(shares);
   const size_t plane = (size_t)tokens * L.ldd * es, weights = (size_t)n * L.ldd * es;
   if (backward) {
     L.dG = take(plane);
@@ -66,25 +129,36 @@ bool ff_direct(const FfProduct& p) {
 }
 
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
-void ff_product(FfProduct p, hipStream_t stream) {
-  if (p.M == 0) return;
-  p.splits = 1;
+void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
   mark(stream);
   if constexpr (sizeof(T) == 2) {
-    if (ff_direct<A_KC, B_KC, T>(p)) {
-      static const int variant = getenv("FFV") ? atoi(getenv("FFV")) : 0;
-      if (variant == 0) {
+    if (kind == 0) {
       const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)tiles), dim3(512), stream, p);
-      } else if (variant == 1) {
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)tiles, p.splits), dim3(512), stream, p);
+      return;
+    }
+    if (kind == 1) {
       const long long tiles = ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)tiles), dim3(256), stream, p);
-      }
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)tiles, p.splits), dim3(256), stream, p);
       return;
     }
   }
   const long long tiles = ff_cdiv(p.M, FS_M) * ff_cdiv(p.N, DUAL ? 64 : 128);
-  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)tiles), dim3(FS_THREADS), stream, p);
+  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)tiles, p.splits), dim3(FS_THREADS), stream, p);
+}
+template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
+void ff_product(FfProduct p, void* partial, hipStream_t stream) {
+  if (p.M == 0) return;
+  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
+  p.splits = plan.splits;
+  p.partial = static_cast<float*>(partial);
+  if (p.splits == 1) {
+    ff_launch<T, A_KC, B_KC, DUAL, EPI>(p, plan.kind, stream);
+    return;
+  }
+  ff_launch<T, A_KC, B_KC, DUAL, FF_PARTIAL>(p, plan.kind, stream);
+  mark(stream);
+  launch(ff_join_kernel<T, DUAL, EPI>, dim3((unsigned)ff_cdiv(ff_cdiv(p.N, 4) * p.M, 256)), dim3(256), stream, p);
 }
 
 // dG and dU from saved pre-activations.
@@ -104,7 +178,7 @@ __global__ __launch_bounds__(256) void ff_slopes_kernel(FfProduct p) {
   } else {
     for (int c = 0; c < N - col; c++) { g[c] = (float)pg[c]; u[c] = (float)pu[c]; }
   }
-  ff_finish<FF_GRAD, true, T>(p, row, col, N, g, u);
+  ff_finish<FF_GRAD, true, T>(p, row, col, N, g, u, ff_upstream<T>(p, row, col, N));
 }
 // Zeros into what an empty batch leaves.
 template <typename T>
@@ -205,7 +279,7 @@ int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, vo
   } else {
     p.keep = b->mask;
   }
-  ff_product<T, true, false, true, FF_FWD>(p, stream);
+  ff_product<T, true, false, true, FF_FWD>(p, ws + L.partial, stream);
   if (pack) {
     FfMove<T, false> out(b->m, ch.position, ch.kept);
     out.add(packed[0], L.ldd, H, ldh, b->tokens);
@@ -267,7 +341,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     } else {
       p.A0 = b->X; p.lda = b->ldx;
       p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
-      ff_product<T, true, false, true, FF_GRAD>(p, stream);
+      ff_product<T, true, false, true, FF_GRAD>(p, ws + L.partial, stream);
     }
   }
   if (dX) {
@@ -278,7 +352,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.M = b->tokens; p.N = b->n; p.K = ch.m;
     p.C0 = dX; p.ldc = lddx;
     p.kept = ch.kept;
-    ff_product<T, true, true, false, FF_STORE>(p, stream);
+    ff_product<T, true, true, false, FF_STORE>(p, ws + L.partial, stream);
   }
   if (dWg) {
     void* packed[2] = {ws + L.out[0], ws + L.out[1]};
@@ -290,7 +364,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.filled = true;
     p.C0 = pack ? packed[0] : dWg; p.C1 = pack ? packed[1] : dWu; p.ldc = pack ? L.ldd : lddw;
     p.kept = ch.kept;
-    ff_product<T, false, false, true, FF_STORE>(p, stream);
+    ff_product<T, false, false, true, FF_STORE>(p, ws + L.partial, stream);
     if (pack) {
       FfMove<T, false> out(b->m, ch.position, ch.kept);
       out.add(packed[0], L.ldd, dWg, lddw, b->n);

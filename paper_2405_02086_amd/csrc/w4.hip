@@ -119,7 +119,11 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
 #pragma unroll
       for (int k = 0; k < WAVES; k++) r[i] += sums[k][i][mt][src][v];
     float out = r[0];
-    if constexpr (GATED) out = ff_act(a.act, r[0]) * r[MATS - 1];
+    if constexpr (GATED) {
+      f32x4 value, slope;
+      ff_gate4<sizeof(T) == 4>(a.act, f32x4{r[0], 0.0f, 0.0f, 0.0f}, value, slope);
+      out = value[0] * r[MATS - 1];
+    }
     static_cast<T*>(a.y)[t * a.ldy + col] = ff_round<T>(out);
   }
 }
