@@ -18,7 +18,8 @@ namespace mlproj {
 // (x = p0 + p1 + p2 exactly, by truncation), and a product of two elements is summed from the six products of
 // parts that reach 2^-16 of it.  What is left out is 2^-24 of a product on average (2^-21 at most), and the sums are
 // fp32 throughout.  Six bf16 products cost 6/16 of what the chip's fp32 matrix instructions would.
-// (A part past the range of bf16's exponent, below 2^-126, is lost: an absolute error no sum can see.)
+// (A part past the range of bf16's exponent, below 2^-126, is lost: an absolute error no sum can see.  The remainder of an
+// infinity is a NaN, so an infinity makes the sums that it is part of NaN.)
 constexpr int FS_M = 128, FS_N = 128, FS_K = 32, FS_THREADS = 256;
 
 template <typename T> struct FfParts { static constexpr int count = 1; using type = T; };
@@ -44,12 +45,11 @@ __device__ __forceinline__ void fs_parts(const FfVec8<T>& x, u32x4 (&out)[FfPart
       for (int j = 0; j < 2; j++) {
         const float a = x.v[2 * i + j];
         const unsigned a0 = __builtin_bit_cast(unsigned, a) & 0xffff0000u;
-        const bool finite = (a0 & 0x7f800000u) != 0x7f800000u;
-        // (a NaN whose upper half reads as an infinity stays a NaN)
-        w[0][j] = finite ? a0 : (a == a ? a0 : 0x7fc00000u);
-        const float r1 = finite ? a - __builtin_bit_cast(float, a0) : 0.0f;
-        w[1][j] = __builtin_bit_cast(unsigned, r1) & 0xffff0000u;
-        w[2][j] = __builtin_bit_cast(unsigned, r1 - __builtin_bit_cast(float, w[1][j]));
+        const float r1 = a - __builtin_bit_cast(float, a0);
+        const unsigned a1 = __builtin_bit_cast(unsigned, r1) & 0xffff0000u;
+        w[0][j] = a0;
+        w[1][j] = a1;
+        w[2][j] = __builtin_bit_cast(unsigned, r1 - __builtin_bit_cast(float, a1));
       }
 #pragma unroll
       for (int k = 0; k < 3; k++) out[k][i] = __builtin_amdgcn_perm(w[k][1], w[k][0], 0x07060302);
@@ -211,19 +211,22 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p) {
   const long long row = i / quads, col = i % quads * 4;
   const long long N = p.kept && DUAL ? *p.kept : p.N;
   if (col >= N) return;
-  const int count = col + 4 <= p.N ? 4 : (int)(p.N - col);
   f32x4 v0 = {}, v1 = {};
   const float* at = p.partial + row * p.N + col;
-  for (int s = 0; s < p.splits; s++, at += (DUAL ? 2 : 1) * plane) {
-    if (count == 4) {
-      v0 += ff_load4(at);
-      if constexpr (DUAL) v1 += ff_load4(at + plane);
-    } else {
-      for (int c = 0; c < count; c++) {
-        v0[c] += at[c];
-        if constexpr (DUAL) v1[c] += at[plane + c];
-      }
+  constexpr int PLANES = DUAL ? 2 : 1;
+  if (col + 4 <= p.N) {
+#pragma unroll 8
+    for (int s = 0; s < p.splits; s++) {
+      v0 += ff_load4(at + s * PLANES * plane);
+      if constexpr (DUAL) v1 += ff_load4(at + (s * PLANES + 1) * plane);
     }
+  } else {
+    for (int c = 0; c < p.N - col; c++)
+#pragma unroll 8
+      for (int s = 0; s < p.splits; s++) {
+        v0[c] += at[s * PLANES * plane + c];
+        if constexpr (DUAL) v1[c] += at[(s * PLANES + 1) * plane + c];
+      }
   }
   FfVec4<T> d = {};
   if constexpr (EPI == FF_GRAD) d = ff_upstream<T>(p, row, col, N);

@@ -3,6 +3,7 @@
 #include "ffcommon.h"
 #include "ffcompact.h"
 #include "ffdirect.h"
+#include "ffskinny.h"
 #include "ffstaged.h"
 #include "host.h"
 
@@ -13,6 +14,8 @@ constexpr long long FF_MAX_DIM = 1LL << 30;
 // A masked forward call of more tokens than this packs its kept channels first; fewer read every weight once
 // anyway, which is all that packing would do.
 constexpr long long FF_PACK_TOKENS = 64;
+// fp32 forward products of at most this many tokens go without tiles (ffskinny.h).
+constexpr long long FK_TOKENS = 32;
 
 static long long ff_cdiv(long long a, long long b) { return (a + b - 1) / b; }
 static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -23,15 +26,23 @@ static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
 // taken, the price of a workgroup beside its steps and the price of joining shares were measured (4096 x 4096 x 16384
 // and 1000 x 1000 x 20000, bf16 and fp32); the plan is the cheapest of them.
 struct FfPlan {
-  int kind;      // 0: direct 256, 1: direct 128, 2: staged
+  int kind;      // 0: direct 256, 1: direct 128, 2: staged, 3: few tokens
   int splits;
 };
+// (forward: A's rows and B's columns run along memory, as in the forward product)
 struct FfKind {
   int rows, cols, places;      // of the tile; workgroups per compute unit
   double step_us, tile_us;
 };
-static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool direct, int es) {
+static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool forward, bool direct, int es) {
   static const FfKind kinds[3] = {{256, 256, 1, 0.86, 9.0}, {128, 128, 2, 0.53, 5.0}, {128, 128, 3, 1.3, 5.0}};
+  if (es == 4 && forward && M <= FK_TOKENS) {
+    // shares until there are two workgroups per compute unit or a wavefront has one step left
+    int splits = 1;
+    const long long groups = ff_cdiv(N, FK_COLS) * ff_cdiv(M, 16);
+    while (groups * splits < 512 && steps > FK_WAVES * splits && splits < 64) splits *= 2;
+    return {3, splits};
+  }
   FfPlan best{2, 1};
   double least = 1e30;
   for (int kind = direct ? 0 : 2; kind <= (direct ? 1 : 2); kind++) {
@@ -40,13 +51,13 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool
     const long long tiles = ff_cdiv(M, k.rows) * ff_cdiv(N, dual ? k.cols / 2 : k.cols);
     const double planes = 4.0 * M * N * (dual ? 2 : 1);
     for (int splits = 1; splits <= 64; splits *= 2) {
-      if (splits > 1 && (steps / splits < 8 || planes * splits > 512e6)) break;
+      if (splits > 1 && (steps / splits < 2 || planes * splits > 512e6)) break;
       const double units = 256.0 * k.places, groups = (double)tiles * splits;
       // workgroups in turn on the fullest place; a place shared with empty ones is faster, at best as fast as half of them
       const double turns = ff_cdiv((long long)groups, (long long)units);
       const double share = groups < units / 2 && k.places > 1 ? 0.65 : 1.0;
       double us = turns * ((double)ff_cdiv(steps, splits) * step_us * share + k.tile_us);
-      if (splits > 1) us += 4.0 + planes * (splits + splits) / 4.0e6;
+      if (splits > 1) us += 4.0 + 0.3 * splits + planes * (splits + splits) / 4.0e6;
       if (us < least) {
         least = us;
         best = {kind, splits};
@@ -56,10 +67,10 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool
   return best;
 }
 static long long ff_steps(long long K, int segs) { return ff_cdiv(K, 32) * segs; }
-static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, int es) {
+static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, bool forward, int es) {
   size_t most = 0;
   for (int direct = 0; direct < 2; direct++) {
-    const FfPlan plan = ff_plan(M, N, ff_steps(K, segs), dual, direct, es);
+    const FfPlan plan = ff_plan(M, N, ff_steps(K, segs), dual, forward, direct, es);
     const size_t bytes = plan.splits > 1 ? (size_t)plan.splits * (dual ? 2 : 1) * M * N * 4 : 0;
     if (bytes > most) most = bytes;
   }
@@ -85,9 +96,9 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
   L.ldd = ff_cdiv(m, 8) * 8;
   // (the packed channels' products run over ldd of them)
   const long long widest = masked ? L.ldd : m;
-  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, es);
+  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, true, es);
   if (backward) {
-    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, es), w = ff_partial_bytes(n, m, tokens, 1, true, es);
+    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, false, es), w = ff_partial_bytes(n, widest, tokens, 1, true, false, es);
     shares = shares > x ? shares : x;
     shares = shares > w ? shares : w;
   }
@@ -131,6 +142,13 @@ bool ff_direct(const FfProduct& p) {
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
   mark(stream);
+  if constexpr (sizeof(T) == 4 && A_KC && !B_KC) {
+    if (kind == 3) {
+      const dim3 grid((unsigned)(ff_cdiv(ff_cdiv(p.N, FK_COLS), 8) * 8 * ff_cdiv(p.M, 16)), p.splits);
+      launch(ff_skinny_kernel<EPI>, grid, dim3(FK_WAVES * 64), stream, p);
+      return;
+    }
+  }
   if constexpr (sizeof(T) == 2) {
     if (kind == 0) {
       const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
@@ -149,7 +167,7 @@ void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_product(FfProduct p, void* partial, hipStream_t stream) {
   if (p.M == 0) return;
-  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
+  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, A_KC && !B_KC, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
   p.splits = plan.splits;
   p.partial = static_cast<float*>(partial);
   if (p.splits == 1) {
@@ -360,7 +378,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.segs = 1;
     p.A0 = b->X; p.lda = b->ldx;
     p.B0 = dG; p.B1 = dU; p.ldb = L.ldd;
-    p.M = b->n; p.N = b->m; p.K = b->tokens;
+    p.M = b->n; p.N = ch.m; p.K = b->tokens;
     p.filled = true;
     p.C0 = pack ? packed[0] : dWg; p.C1 = pack ? packed[1] : dWu; p.ldc = pack ? L.ldd : lddw;
     p.kept = ch.kept;
