@@ -7,10 +7,11 @@ namespace {
 
 // ------------------------------------------------------------------ rows in registers
 // A row's entries are dealt in 16-byte pieces: piece i of a row belongs to thread i % THREADS of the row's
-// threads (a wavefront, or a workgroup of 256 or 1024), CH of them per thread, and stays in its registers from the one
-// load to the one store.  Loads take any address; the last piece of a row is filled up element by element.
+// threads (16, a wavefront, or a workgroup of 256 or 512), CH of them per thread, and stays in its registers from the
+// one load to the one store.  Loads take any address; the last piece of a row is filled up element by element.
 // Both directions are bound by HBM: forward reads x and b and writes r and y once, backward reads four
-// arrays and writes two.
+// arrays and writes two.  A row group takes many rows: the vectors (weights, a gate per channel) stay in registers
+// too, and the next row's loads go out before the present row is reduced, as far as there are registers for it.
 template <typename T> constexpr int BN_VEC = 16 / sizeof(T);
 
 struct BnArgs {
@@ -56,7 +57,7 @@ __device__ __forceinline__ void bn_store(T* p, long long valid, const float (&x)
 template <int THREADS, int N>
 __device__ __forceinline__ void bn_sum(float (&v)[N], float (*slot)[16], int lane, int wave) {
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1)
+  for (int s = 1; s < (THREADS < 64 ? THREADS : 64); s <<= 1)
 #pragma unroll
     for (int i = 0; i < N; i++) v[i] += __shfl_xor(v[i], s);
   if constexpr (THREADS > 64) {
@@ -75,17 +76,17 @@ __device__ __forceinline__ void bn_sum(float (&v)[N], float (*slot)[16], int lan
   }
 }
 
-// HELD: the row's pieces fit the registers (CH per thread); otherwise CH of them at a time, and every phase
-// reads them again (from L2, where a row still is).
-template <typename T, int THREADS, int CH, bool HELD>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_forward_kernel(BnArgs a) {
+constexpr int BN_LONG = 512;
+// Rows too long for registers: CH pieces per thread at a time, and every phase reads them again (from L2, where a row
+// still is).
+template <typename T>
+__global__ __launch_bounds__(BN_LONG) void bn_forward_long_kernel(BnArgs a) {
+  constexpr int THREADS = BN_LONG, CH = 2;
   constexpr int VEC = BN_VEC<T>;
-  constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
   __shared__ float slots[2][1][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t = THREADS < 256 ? lane : threadIdx.x;
-  const long long row = (long long)blockIdx.x * ROWS + (ROWS > 1 ? wave : 0);
-  if (row >= a.tokens) return;                 // (with THREADS > 64 the whole workgroup)
+  const int t = threadIdx.x;
+  const long long row = blockIdx.x;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   const T* b = a.b ? static_cast<const T*>(a.b) + row * a.ldb : nullptr;
   const T* gate = static_cast<const T*>(a.gate) + row * a.gate_stride;
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_forward_kern
   T* r = static_cast<T*>(a.r) + row * a.ldr;
   T* y = static_cast<T*>(a.y) + row * a.ldy;
   const long long n = a.n, per = (long long)THREADS * VEC * CH;
-  const long long passes = HELD ? 1 : (n + per - 1) / per;
+  const long long passes = (n + per - 1) / per;
   const float inv_n = 1.0f / (float)n;
   float vx[CH][VEC], vb[CH][VEC];
   float rb = 0.0f, sum[1];
@@ -130,14 +131,12 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_forward_kern
     }
     bn_sum<THREADS, 1>(sum, slots[0], lane, wave);
     rb = 1.0f / sqrtf(sum[0] * inv_n + a.eps);
-  } else if constexpr (HELD) {
-    load(0);
   }
   float rr = 0.0f;
   if (w_pre) {
     sum[0] = 0.0f;
     for (long long pass = 0; pass < passes; pass++) {
-      if constexpr (!HELD) load(pass);
+      load(pass);
       if (b) join(pass);
 #pragma unroll
       for (int c = 0; c < CH; c++)
@@ -148,8 +147,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_forward_kern
     rr = 1.0f / sqrtf(sum[0] * inv_n + a.eps);
   }
   for (long long pass = 0; pass < passes; pass++) {
-    if constexpr (!HELD) load(pass);
-    if (b && (!HELD || !w_pre)) join(pass);
+    load(pass);
+    if (b) join(pass);
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       const long long at = pass * per + ((long long)c * THREADS + t) * VEC;
@@ -166,29 +165,22 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_forward_kern
   }
 }
 
-// One round of sums per row: with e = w_pre dy and f = scale gate w_post,
-//   mean(r e), mean(r^2), mean(b^2), and the three parts of sum(b f dx), dx = dr + rr e - r rr^3 mean(r e):
-//   sum(b f dr), sum(b f e), sum(b f r).
-// A workgroup takes every gridDim-th row and keeps the sums over its rows of the columns its threads hold, which go
-// out as one partial per workgroup and are summed, in their order, by bn_columns_kernel: the same bits
-// every time.  With one gate per channel dgate and dw_post are both multiples of sum dx b / rms(b).
-template <typename T, int THREADS, int CH, bool HELD, bool TOKEN_GATE>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_backward_kernel(BnArgs a) {
+template <typename T, bool TOKEN_GATE>
+__global__ __launch_bounds__(BN_LONG) void bn_backward_long_kernel(BnArgs a) {
+  constexpr int THREADS = BN_LONG, CH = 2;
   constexpr int VEC = BN_VEC<T>;
-  constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
   __shared__ float slots[2][6][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t = THREADS < 256 ? lane : threadIdx.x;
+  const int t = threadIdx.x;
   const long long n = a.n, per = (long long)THREADS * VEC * CH;
-  const long long passes = HELD ? 1 : (n + per - 1) / per;
+  const long long passes = (n + per - 1) / per;
   const float inv_n = 1.0f / (float)n;
   const T* w_post = static_cast<const T*>(a.w_post);
   const T* w_pre = static_cast<const T*>(a.w_pre);
-  const long long worker = (long long)blockIdx.x * ROWS + (ROWS > 1 ? wave : 0);
-  const long long workers = (long long)gridDim.x * ROWS;
+  const long long worker = blockIdx.x;
+  const long long workers = gridDim.x;
   float* partial = a.partial + worker * n;
   const long long plane = workers * n;
-  float s_post[CH][VEC] = {}, s_pre[CH][VEC] = {};
   int turn = 0;
 
   for (long long row = worker; row < a.tokens; row += workers, turn ^= 1) {
@@ -241,7 +233,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_backward_ker
     const float kr = w_pre ? rr * rr * rr * (sum[0] * inv_n) : 0.0f;
     const float kb = rb * rb * rb * ((sum[3] + rr * sum[4] - kr * sum[5]) * inv_n);
     for (long long pass = 0; pass < passes; pass++) {
-      if constexpr (!HELD) load(pass);
+      load(pass);
 #pragma unroll
       for (int c = 0; c < CH; c++) {
         const long long at = pass * per + ((long long)c * THREADS + t) * VEC;
@@ -268,55 +260,296 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void bn_backward_ker
           if (a.db) bn_store<T, VEC>(static_cast<T*>(a.db) + row * a.lddb + at, n - at, db);
           if (TOKEN_GATE && a.dgate) bn_store<T, VEC>(static_cast<T*>(a.dgate) + row * a.dgate_stride + at, n - at, dg);
         }
-        if constexpr (HELD) {
-#pragma unroll
-          for (int i = 0; i < VEC; i++) { s_post[c][i] += post[i]; s_pre[c][i] += pre[i]; }
-        } else {
-          // too many columns for registers: the sums live in the worker's own partials
-          for (int i = 0; i < VEC && at + i < n; i++) {
-            const bool fresh = row == worker;
-            if (a.want_post || a.want_gate) partial[at + i] = post[i] + (fresh ? 0.0f : partial[at + i]);
-            if (a.want_pre) partial[plane + at + i] = pre[i] + (fresh ? 0.0f : partial[plane + at + i]);
-          }
+        // too many columns for registers: the sums live in the worker's own partials
+        for (int i = 0; i < VEC && at + i < n; i++) {
+          const bool fresh = row == worker;
+          if (a.want_post || a.want_gate) partial[at + i] = post[i] + (fresh ? 0.0f : partial[at + i]);
+          if (a.want_pre) partial[plane + at + i] = pre[i] + (fresh ? 0.0f : partial[plane + at + i]);
         }
       }
     }
   }
-  if constexpr (HELD) {
+}
+
+// ------------------------------------------------------------------ held rows
+// 16 bytes of a row as they lie in memory, zeros past its end; and as numbers.
+template <typename T>
+__device__ __forceinline__ u32x4 bn_raw(const T* p, long long valid) {
+  constexpr int VEC = BN_VEC<T>;
+  u32x4 r;
+  if (valid >= VEC) {
+    __builtin_memcpy(&r, p, 16);
+  } else {
+    T t[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; i++) t[i] = i < valid ? p[i] : (T)0.0f;
+    __builtin_memcpy(&r, t, 16);
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void bn_numbers(u32x4 raw, float (&out)[BN_VEC<T>]) {
+  T t[BN_VEC<T>];
+  __builtin_memcpy(t, &raw, 16);
+#pragma unroll
+  for (int i = 0; i < BN_VEC<T>; i++) out[i] = (float)t[i];
+}
+
+// The pieces a thread holds of a row of an array (nothing where the array is absent), or of a vector.
+template <typename T, int THREADS, int CH>
+struct BnPieces {
+  u32x4 raw[CH];
+  __device__ __forceinline__ void load(const T* row, long long n, int t) {
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      const long long at = ((long long)c * THREADS + t) * BN_VEC<T>;
+      raw[c] = bn_raw(row + at, row ? n - at : 0);
+    }
+  }
+};
+
+template <int THREADS> constexpr int BN_GROUP = THREADS < 256 ? 256 : THREADS;   // threads of a workgroup
+template <int THREADS> constexpr int BN_ROWS = BN_GROUP<THREADS> / THREADS;      // rows it has in hand
+
+template <typename T, int THREADS, int CH, bool AHEAD>
+__global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a) {
+  constexpr int VEC = BN_VEC<T>, ROWS = BN_ROWS<THREADS>;
+  using Pieces = BnPieces<T, THREADS, CH>;
+  __shared__ float slots[2][2][1][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int t = threadIdx.x % THREADS;
+  const long long n = a.n, workers = (long long)gridDim.x * ROWS;
+  const float inv_n = 1.0f / (float)n;
+  const T *b = static_cast<const T*>(a.b), *gate = static_cast<const T*>(a.gate);
+  const bool block = b != nullptr, pre = a.w_pre != nullptr, token_gate = a.gate_stride != 0;
+  const T* x = static_cast<const T*>(a.x);
+  const T *p_post = static_cast<const T*>(a.w_post), *p_pre = static_cast<const T*>(a.w_pre);
+  Pieces w_post, w_pre, channel_gate, nx, nb, ng;
+  // a piece of a vector: held, or read again
+  auto piece = [&](const Pieces& held, const T* from, int c, float (&out)[VEC]) {
+    const long long at = ((long long)c * THREADS + t) * VEC;
+    bn_numbers<T>(AHEAD ? held.raw[c] : bn_raw(from + at, from ? n - at : 0), out);
+  };
+  auto fetch = [&](long long row) {
+    nx.load(x + row * a.ldx, n, t);
+    if (block) nb.load(b + row * a.ldb, n, t);
+    if (block && token_gate) ng.load(gate + row * a.gate_stride, n, t);
+  };
+  long long row = (long long)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / THREADS : 0);
+  if (row >= a.tokens) return;                 // (with THREADS > 64 the whole workgroup)
+  fetch(row);
+  if (AHEAD) {
+    w_post.load(p_post, n, t);
+    w_pre.load(p_pre, n, t);
+    channel_gate.load(token_gate ? nullptr : gate, n, t);
+  }
+  for (int turn = 0; row < a.tokens; row += workers, turn ^= 1) {
+    const Pieces cx = nx, cb = nb, cg = ng;
+    if (AHEAD && row + workers < a.tokens) fetch(row + workers);
+    float v[CH][VEC], sum[1] = {0.0f};
+#pragma unroll
+    for (int c = 0; c < CH; c++) bn_numbers<T>(cx.raw[c], v[c]);
+    if (block) {
+#pragma unroll
+      for (int c = 0; c < CH; c++) {
+        float f[VEC];
+        bn_numbers<T>(cb.raw[c], f);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) sum[0] += f[i] * f[i];
+      }
+      bn_sum<THREADS, 1>(sum, slots[turn][0], lane, wave);
+      const float rb = 1.0f / sqrtf(sum[0] * inv_n + a.eps);
+#pragma unroll
+      for (int c = 0; c < CH; c++) {
+        float f[VEC], g[VEC], w[VEC];
+        bn_numbers<T>(cb.raw[c], f);
+        if (token_gate) bn_numbers<T>(cg.raw[c], g);
+        else piece(channel_gate, gate, c, g);
+        piece(w_post, p_post, c, w);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) v[c][i] += a.scale * g[i] * (f[i] * rb * w[i]);
+      }
+    }
+    float rr = 0.0f;
+    if (pre) {
+      sum[0] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < CH; c++)
+#pragma unroll
+        for (int i = 0; i < VEC; i++) sum[0] += v[c][i] * v[c][i];
+      bn_sum<THREADS, 1>(sum, slots[turn][1], lane, wave);
+      rr = 1.0f / sqrtf(sum[0] * inv_n + a.eps);
+    }
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       const long long at = ((long long)c * THREADS + t) * VEC;
       if (at >= n) break;
-      if (a.want_post || a.want_gate) bn_store<float, VEC>(partial + at, n - at, s_post[c]);
-      if (a.want_pre) bn_store<float, VEC>(partial + plane + at, n - at, s_pre[c]);
+      if (block) bn_store<T, VEC>(static_cast<T*>(a.r) + row * a.ldr + at, n - at, v[c]);
+      if (pre) {
+        float w[VEC];
+        piece(w_pre, p_pre, c, w);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) w[i] *= v[c][i] * rr;
+        bn_store<T, VEC>(static_cast<T*>(a.y) + row * a.ldy + at, n - at, w);
+      }
     }
-  } else if (worker >= a.tokens) {
-    for (long long j = t; j < n; j += THREADS) partial[j] = partial[plane + j] = 0.0f;
+    if (!AHEAD && row + workers < a.tokens) fetch(row + workers);
   }
 }
 
-// The sums over workers: 32 columns x 8 groups of workers per workgroup, joined in LDS in a fixed order.
+// One round of sums per row: with e = w_pre dy and f = scale gate w_post,
+//   mean(r e), mean(r^2), mean(b^2), and the three parts of sum(b f dx), dx = dr + rr e - r rr^3 mean(r e):
+//   sum(b f dr), sum(b f e), sum(b f r).
+// A worker (a row's threads) takes every workers-th row and keeps the sums over its rows of the columns its threads
+// hold, which go out as one partial per worker and are summed, in their order, by bn_columns_kernel: the same bits
+// every time.  With one gate per channel dgate and dw_post are both multiples of sum dx b / rms(b).
+template <typename T, int THREADS, int CH, bool AHEAD, bool TOKEN_GATE>
+__global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a) {
+  constexpr int VEC = BN_VEC<T>, ROWS = BN_ROWS<THREADS>;
+  using Pieces = BnPieces<T, THREADS, CH>;
+  __shared__ float slots[2][6][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int t = threadIdx.x % THREADS;
+  const long long n = a.n;
+  const float inv_n = 1.0f / (float)n;
+  const long long worker = (long long)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / THREADS : 0), workers = (long long)gridDim.x * ROWS;
+  const T *r = static_cast<const T*>(a.x), *b = static_cast<const T*>(a.b), *dr = static_cast<const T*>(a.dr), *dy = static_cast<const T*>(a.dy);
+  const T* gate = static_cast<const T*>(a.gate);
+  const bool block = b != nullptr, pre = a.w_pre != nullptr;
+  const T *p_post = static_cast<const T*>(a.w_post), *p_pre = static_cast<const T*>(a.w_pre);
+  Pieces w_post, w_pre, channel_gate, nr, nb = {}, nd = {}, ny = {}, ng = {};
+  auto piece = [&](const Pieces& held, const T* from, int c, float (&out)[VEC]) {
+    const long long at = ((long long)c * THREADS + t) * VEC;
+    bn_numbers<T>(AHEAD ? held.raw[c] : bn_raw(from + at, from ? n - at : 0), out);
+  };
+  auto fetch = [&](long long row) {
+    nr.load(r + row * a.ldx, n, t);
+    if (block) nb.load(b + row * a.ldb, n, t);
+    if (dr) nd.load(dr + row * a.lddr, n, t);
+    if (pre) ny.load(dy + row * a.lddy, n, t);
+    if (TOKEN_GATE && block) ng.load(gate + row * a.gate_stride, n, t);
+  };
+  // the sums of a thread's own columns: in registers, or in LDS where rows are long and registers few
+  constexpr bool IN_LDS = THREADS >= 512;
+  __shared__ float lds_sums[IN_LDS ? 2 * CH * VEC * THREADS : 1];
+  float s_post[IN_LDS ? 1 : CH][VEC] = {}, s_pre[IN_LDS ? 1 : CH][VEC] = {};
+  auto add = [&](int which, float (&held)[VEC], int c, int i, float x) {
+    if (IN_LDS) lds_sums[((which * CH + c) * VEC + i) * THREADS + t] += x;
+    else held[i] += x;
+  };
+  if (IN_LDS)
+    for (int i = 0; i < 2 * CH * VEC; i++) lds_sums[i * THREADS + t] = 0.0f;
+  if (worker < a.tokens) fetch(worker);
+  if (AHEAD) {
+    w_post.load(p_post, n, t);
+    w_pre.load(p_pre, n, t);
+    if (!TOKEN_GATE) channel_gate.load(gate, n, t);
+  }
+  int turn = 0;
+  for (long long row = worker; row < a.tokens; row += workers, turn ^= 1) {
+    const Pieces cr = nr, cb = nb, cd = nd, cy = ny, cg = ng;
+    if (AHEAD && row + workers < a.tokens) fetch(row + workers);
+    float sum[6] = {};
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      float vr[VEC], vb[VEC], vd[VEC], vy[VEC], g[VEC], wp[VEC], wq[VEC];
+      bn_numbers<T>(cr.raw[c], vr);
+      bn_numbers<T>(cb.raw[c], vb);
+      bn_numbers<T>(cd.raw[c], vd);
+      bn_numbers<T>(cy.raw[c], vy);
+      if (TOKEN_GATE) bn_numbers<T>(cg.raw[c], g);
+      else piece(channel_gate, gate, c, g);
+      piece(w_post, p_post, c, wp);
+      piece(w_pre, p_pre, c, wq);
+#pragma unroll
+      for (int i = 0; i < VEC; i++) {
+        const float e = wq[i] * vy[i], bf = vb[i] * (wp[i] * (a.scale * g[i]));
+        sum[0] += vr[i] * e;
+        sum[1] += vr[i] * vr[i];
+        sum[2] += vb[i] * vb[i];
+        sum[3] += bf * vd[i];
+        sum[4] += bf * e;
+        sum[5] += bf * vr[i];
+      }
+    }
+    bn_sum<THREADS, 6>(sum, slots[turn], lane, wave);
+    const float rr = pre ? 1.0f / sqrtf(sum[1] * inv_n + a.eps) : 0.0f;
+    const float rb = 1.0f / sqrtf(sum[2] * inv_n + a.eps);
+    const float kr = pre ? rr * rr * rr * (sum[0] * inv_n) : 0.0f;
+    const float kb = rb * rb * rb * ((sum[3] + rr * sum[4] - kr * sum[5]) * inv_n);
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      const long long at = ((long long)c * THREADS + t) * VEC;
+      if (at >= n) break;
+      float vr[VEC], vd[VEC], vy[VEC], wq[VEC], dx[VEC];
+      bn_numbers<T>(cr.raw[c], vr);
+      bn_numbers<T>(cd.raw[c], vd);
+      bn_numbers<T>(cy.raw[c], vy);
+      piece(w_pre, p_pre, c, wq);
+#pragma unroll
+      for (int i = 0; i < VEC; i++) {
+        dx[i] = vd[i] + (rr * (wq[i] * vy[i]) - kr * vr[i]);
+        add(1, s_pre[IN_LDS ? 0 : c], c, i, vy[i] * (vr[i] * rr));
+      }
+      if (a.dx) bn_store<T, VEC>(static_cast<T*>(a.dx) + row * a.lddx + at, n - at, dx);
+      if (block) {
+        float vb[VEC], g[VEC], wp[VEC], db[VEC], dg[VEC];
+        bn_numbers<T>(cb.raw[c], vb);
+        if (TOKEN_GATE) bn_numbers<T>(cg.raw[c], g);
+        else piece(channel_gate, gate, c, g);
+        piece(w_post, p_post, c, wp);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) {
+          const float sdx = a.scale * dx[i], bh = vb[i] * rb;
+          db[i] = rb * (sdx * g[i] * wp[i]) - kb * vb[i];
+          dg[i] = sdx * wp[i] * bh;
+          add(0, s_post[IN_LDS ? 0 : c], c, i, TOKEN_GATE ? sdx * g[i] * bh : sdx * bh);
+        }
+        if (a.db) bn_store<T, VEC>(static_cast<T*>(a.db) + row * a.lddb + at, n - at, db);
+        if (TOKEN_GATE && a.dgate) bn_store<T, VEC>(static_cast<T*>(a.dgate) + row * a.dgate_stride + at, n - at, dg);
+      }
+    }
+    if (!AHEAD && row + workers < a.tokens) fetch(row + workers);
+  }
+  float* partial = a.partial + worker * n;
+  const long long plane = workers * n;
+#pragma unroll
+  for (int c = 0; c < CH; c++) {
+    const long long at = ((long long)c * THREADS + t) * VEC;
+    if (at >= n) break;
+    float post[VEC], own[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; i++) {
+      post[i] = IN_LDS ? lds_sums[(c * VEC + i) * THREADS + t] : s_post[IN_LDS ? 0 : c][i];
+      own[i] = IN_LDS ? lds_sums[((CH + c) * VEC + i) * THREADS + t] : s_pre[IN_LDS ? 0 : c][i];
+    }
+    if (a.want_post || a.want_gate) bn_store<float, VEC>(partial + at, n - at, post);
+    if (a.want_pre) bn_store<float, VEC>(partial + plane + at, n - at, own);
+  }
+}
+
+// The sums over workers: 32 columns x 32 groups of workers per workgroup, joined in LDS in a fixed order.
 template <typename T>
-__global__ __launch_bounds__(256) void bn_columns_kernel(BnArgs a, int workers, bool token_gate, float* dw_post, float* dgate, float* dw_pre) {
-  __shared__ float part[2][8][32];
+__global__ __launch_bounds__(1024) void bn_columns_kernel(BnArgs a, int workers, bool token_gate, float* dw_post, float* dgate, float* dw_pre) {
+  __shared__ float part[2][32][33];
   const int cx = threadIdx.x & 31, gy = threadIdx.x >> 5;
   const long long col = (long long)blockIdx.x * 32 + cx;
   const bool post = a.want_post || a.want_gate;
-  float s0 = 0.0f, s1 = 0.0f;
-  if (col < a.n) {
-    const float* p = a.partial + col;
-    const long long plane = (long long)workers * a.n;
-    for (int w = gy; w < workers; w += 8) {
-      if (post) s0 += p[w * a.n];
-      if (a.want_pre) s1 += p[plane + w * a.n];
-    }
+  float s[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    if (col >= a.n || !(k == 0 ? post : a.want_pre != 0)) continue;
+    const float* p = a.partial + k * (long long)workers * a.n + col;
+#pragma unroll 8
+    for (int w = gy; w < workers; w += 32) s[k] += p[w * a.n];
   }
-  part[0][gy][cx] = s0;
-  part[1][gy][cx] = s1;
+  part[0][gy][cx] = s[0];
+  part[1][gy][cx] = s[1];
   __syncthreads();
   if (gy == 0 && col < a.n) {
-    s0 = s1 = 0.0f;
-    for (int i = 0; i < 8; i++) { s0 += part[0][i][cx]; s1 += part[1][i][cx]; }
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; i++) { s0 += part[0][i][cx]; s1 += part[1][i][cx]; }
     if (a.want_pre) dw_pre[col] = s1;
     if (token_gate) {
       if (a.want_post) dw_post[col] = s0;
@@ -329,36 +562,53 @@ __global__ __launch_bounds__(256) void bn_columns_kernel(BnArgs a, int workers, 
 }
 
 // ------------------------------------------------------------------ plan
-constexpr int BN_WORKERS = 512;      // workgroups of the backward pass (two per compute unit)
 constexpr long long BN_MAX_DIM = 1LL << 30;
+// Most workgroups of a pass: as many as are resident at once (two of 256 threads with 200 registers, one larger one,
+// per compute unit), so that the next row's loads always have a row to hide behind and partial sums stay few.
+constexpr long long bn_most_groups(int threads) { return threads <= 256 ? 512 : 256; }
 
-// f(threads per row, pieces per thread, held) for rows of n elements
+// f(threads per row, pieces per thread, next row ahead) for rows of n elements; 0 pieces: too long for registers.
+// 16-bit pieces are twice the numbers of fp32 ones, so a thread holds half as many.
 template <typename T, typename F>
 void bn_shape(long long n, F&& f) {
   const long long pieces = (n + BN_VEC<T> - 1) / BN_VEC<T>;
+  constexpr int WIDE = sizeof(T) == 4 ? 2 : 1;
   using std::integral_constant;
-#define BN_CASE(TH, CHUNKS, H) f(integral_constant<int, TH>{}, integral_constant<int, CHUNKS>{}, integral_constant<bool, H>{})
-  if (pieces <= 64) BN_CASE(64, 1, true);
+#define BN_CASE(TH, CHUNKS, AHEAD) f(integral_constant<int, TH>{}, integral_constant<int, CHUNKS>{}, integral_constant<bool, AHEAD>{})
+  if (pieces <= 16) BN_CASE(16, 1, true);
+  else if (pieces <= 32) BN_CASE(16, 2, true);
+  else if (pieces <= 64) BN_CASE(64, 1, true);
   else if (pieces <= 128) BN_CASE(64, 2, true);
   else if (pieces <= 256) BN_CASE(256, 1, true);
   else if (pieces <= 512) BN_CASE(256, 2, true);
-  else if (pieces <= 1024) BN_CASE(1024, 1, true);
-  else if (pieces <= 2048) BN_CASE(1024, 2, true);
-  else BN_CASE(1024, 2, false);
+  else if (pieces <= 1024) BN_CASE(512 / WIDE, 2 * WIDE, true);
+  else if (pieces <= 2048) BN_CASE(512, 4, false);
+  else {
+    if constexpr (WIDE == 2) {
+      if (pieces <= 4096) {
+        BN_CASE(512, 8, false);
+        return;
+      }
+    }
+    BN_CASE(BN_LONG, 0, false);
+  }
 #undef BN_CASE
 }
 
-long long bn_row_groups(int threads, long long tokens) {
+long long bn_groups(int threads, long long tokens) {
   const int rows = threads < 256 ? 256 / threads : 1;
-  return (tokens + rows - 1) / rows;
+  const long long groups = (tokens + rows - 1) / rows, most = bn_most_groups(threads);
+  return groups < most ? groups : most;
 }
 
 template <typename T>
 int run_forward(const BnArgs& a, hipStream_t stream) {
-  bn_shape<T>(a.n, [&](auto th, auto ch, auto held) {
+  bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
     mark(stream);
-    launch(bn_forward_kernel<T, th.value, ch.value, held.value>, dim3((unsigned)bn_row_groups(th.value, a.tokens)),
-           dim3(th.value < 256 ? 256 : th.value), stream, a);
+    if constexpr (ch.value == 0)
+      launch(bn_forward_long_kernel<T>, dim3((unsigned)a.tokens), dim3(BN_LONG), stream, a);
+    else
+      launch(bn_forward_kernel<T, th.value, ch.value, ahead.value>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
   });
   mark(stream);
   return launch_status();
@@ -366,19 +616,23 @@ int run_forward(const BnArgs& a, hipStream_t stream) {
 
 template <typename T>
 int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate, float* dw_pre, hipStream_t stream) {
-  bn_shape<T>(a.n, [&](auto th, auto ch, auto held) {
-    long long groups = bn_row_groups(th.value, a.tokens);
-    if (groups > BN_WORKERS) groups = BN_WORKERS;
-    const int workers = (int)groups * (th.value < 256 ? 256 / th.value : 1);
-    const dim3 block(th.value < 256 ? 256 : th.value);
+  bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
+    const long long groups = bn_groups(th.value, a.tokens);
+    const dim3 grid((unsigned)groups), block(BN_GROUP<th.value>);
     if (groups > 0) {
       mark(stream);
-      if (token_gate) launch(bn_backward_kernel<T, th.value, ch.value, held.value, true>, dim3((unsigned)groups), block, stream, a);
-      else launch(bn_backward_kernel<T, th.value, ch.value, held.value, false>, dim3((unsigned)groups), block, stream, a);
+      if constexpr (ch.value == 0) {
+        if (token_gate) launch(bn_backward_long_kernel<T, true>, grid, block, stream, a);
+        else launch(bn_backward_long_kernel<T, false>, grid, block, stream, a);
+      } else {
+        if (token_gate) launch(bn_backward_kernel<T, th.value, ch.value, ahead.value, true>, grid, block, stream, a);
+        else launch(bn_backward_kernel<T, th.value, ch.value, ahead.value, false>, grid, block, stream, a);
+      }
     }
     if (a.want_post || a.want_gate || a.want_pre) {
       mark(stream);
-      launch(bn_columns_kernel<T>, dim3((unsigned)((a.n + 31) / 32)), dim3(256), stream, a, workers, token_gate, dw_post, dgate, dw_pre);
+      launch(bn_columns_kernel<T>, dim3((unsigned)((a.n + 31) / 32)), dim3(1024), stream, a, (int)groups * BN_ROWS<th.value>, token_gate,
+             dw_post, dgate, dw_pre);
     }
   });
   mark(stream);
@@ -424,12 +678,15 @@ BnArgs bn_start(const mlproj_norm_block* k) {
 }
 
 size_t bn_workspace(long long tokens, long long n) {
-  // as many workers as the smallest rows take: four per workgroup
-  const long long workers = tokens < 4 * BN_WORKERS ? (tokens + 3) / 4 * 4 : 4 * BN_WORKERS;
-  const long long few = tokens < BN_WORKERS ? tokens : BN_WORKERS;
-  // rows of at most 128 pieces take a wavefront each (1024 16-bit elements), longer ones a workgroup
-  const long long w = n <= 1024 ? workers : few;
-  return (size_t)(w > 0 ? w : 1) * n * 2 * sizeof(float) + 256;
+  // the most workers any storage type has: a row takes at least the threads of its 16-bit form
+  long long workers = 1;
+  auto count = [&](auto th, auto, auto) {
+    const long long w = bn_groups(th.value, tokens) * BN_ROWS<th.value>;
+    workers = w > workers ? w : workers;
+  };
+  bn_shape<bf16_t>(n, count);
+  bn_shape<float>(n, count);
+  return (size_t)workers * n * 2 * sizeof(float) + 256;
 }
 
 }  // namespace
