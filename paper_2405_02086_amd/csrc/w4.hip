@@ -36,54 +36,64 @@ __device__ __forceinline__ f16x8 w4_widen(unsigned v, f16_t) {
   return r;
 }
 
-// A workgroup computes 16 columns (of one matrix, or of both) for up to 16 MT tokens; its wavefronts share out the row
-// blocks and join their sums in LDS, in their order.  A wavefront's load of a block is 1 KiB in one instruction, already in the
-// layout of the matrix cores' second operand, and the hardware widens two codes per instruction; a group's sum
-// leaves the matrix cores unscaled, in the lane that holds its column's scale.  fp32 tokens are cut into three
-// bf16 parts (ffstaged.h), which with weights of two significant bits loses nothing.
-// Bound by HBM: n m / 2 bytes of codes and 2 n m / group of scales.
-template <typename T, bool GATED, int MT, int WAVES, int GROUP>
+// A workgroup computes CB x 16 columns (of one matrix, or of both) for up to 16 MT tokens; its wavefronts share out the
+// row blocks, U at a time, and join their sums in LDS, in their order.  A wavefront's load of a block is 1 KiB in one
+// instruction, already in the layout of the matrix cores' second operand, and the hardware widens two codes per instruction; a
+// group's sum leaves the matrix cores unscaled, in the lane that holds its column's scale.  fp32 tokens are cut into
+// three bf16 parts (ffstaged.h), which with weights of two significant bits loses nothing.
+//
+// Bound by HBM at one token: n m / 2 bytes of codes and 2 n m / group of scales; at 16 tokens by the tokens themselves, which
+// every workgroup reads from L2 (128 rows of 16 tokens are 4 KiB, of a column block 1 KiB).  So: one column block per
+// workgroup and 16 wavefronts while that is what fills the chip, two where there are columns enough, four (and 32
+// tokens) where the tokens dominate.  us, with 1 x 16 / 2 x 8 / 4 x 8 (column blocks x wavefronts): one token 16384 ->
+// 4096 10.8 / 14 / 22, one token 4096 -> 2 x 16384 19 / 14.0 (4.9 TB/s) / 16.4, 16 tokens 4096 -> 2 x 16384 27 / 17.5 / 17.0,
+// 16 tokens 16384 -> 8192 38 / 23 / 27; 64 tokens 4096 -> 2 x 16384 84 / 52 / 44, with 32 tokens at a time 36.
+template <typename T, bool GATED, int MT, int CB, int U, int WAVES, int GROUP>
 __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
   using E = typename FfParts<T>::type;
   using F = typename FfFrag<E>::type;
-  constexpr int P = FfParts<T>::count, MATS = GATED ? 2 : 1, PER = W4_ROWS / GROUP;
-  constexpr int U = MT == 1 ? 4 : MT == 2 ? 2 : 1;        // row blocks in flight per wavefront
-  __shared__ float sums[WAVES][MATS][MT][64][4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long cb = blockIdx.x, t0 = (long long)blockIdx.y * (16 * MT);
+  constexpr int P = FfParts<T>::count, MATS = GATED ? 2 : 1, PER = W4_ROWS / GROUP, SETS = CB * MATS;
+  __shared__ float sums[WAVES][SETS][MT][64][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long cb0 = (long long)blockIdx.x * CB, t0 = (long long)blockIdx.y * (16 * MT);
+  const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
   const T* x = static_cast<const T*>(a.x);
-  f32x4 acc[MATS][MT] = {};
+  f32x4 acc[SETS][MT] = {};
   for (int kb = wave; kb < a.kblocks; kb += WAVES * U) {
-    u32x4 w[U][MATS];
-    bf16_t s[U][MATS][PER];
+    u32x4 w[U][SETS];
+    bf16_t s[U][SETS][PER];
     F xf[U][MT][P][4];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      // past the end: the last block again, with tokens of zeros
-      const bool there = kb + u * WAVES < a.kblocks;
-      const long long k = there ? kb + u * WAVES : a.kblocks - 1;
+      // past the end: the last block again, not used
+      const int k = kb + u * WAVES < a.kblocks ? kb + u * WAVES : a.kblocks - 1;
 #pragma unroll
-      for (int i = 0; i < MATS; i++) {
-        w[u][i] = *reinterpret_cast<const u32x4*>(a.codes[i] + (cb * a.kblocks + k) * W4_BYTES + lane * 16);
-        __builtin_memcpy(s[u][i], a.scales[i] + ((cb * a.kblocks + k) * 16 + (lane & 15)) * PER, PER * 2);
+      for (int i = 0; i < SETS; i++) {
+        const long long cb = cb0 + i % CB < cbs ? cb0 + i % CB : cbs - 1, at = cb * a.kblocks + k;
+        w[u][i] = *reinterpret_cast<const u32x4*>(a.codes[i / CB] + at * W4_BYTES + lane * 16);
+        __builtin_memcpy(s[u][i], a.scales[i / CB] + (at * 16 + (lane & 15)) * PER, PER * 2);
       }
+      const bool whole = (k + 1) * W4_ROWS <= a.n;
 #pragma unroll
       for (int mt = 0; mt < MT; mt++) {
+        // (rows past the tokens are the last one again: what they come to is not stored)
         const long long t = t0 + mt * 16 + (lane & 15);
+        const T* row = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-          const long long at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
+          const int at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
           u32x4 parts[P];
-          fs_parts(ff_load8(x + t * a.ldx + at, t < a.tokens && there ? a.n - at : 0), parts);
+          fs_parts(ff_load8(row + at, whole ? 8 : a.n - at), parts);
 #pragma unroll
           for (int p = 0; p < P; p++) __builtin_memcpy(&xf[u][mt][p][q], &parts[p], 16);
         }
       }
     }
 #pragma unroll
-    for (int u = 0; u < U; u++)
+    for (int u = 0; u < U; u++) {
+      if (kb + u * WAVES >= a.kblocks) break;
 #pragma unroll
-      for (int i = 0; i < MATS; i++) {
+      for (int i = 0; i < SETS; i++) {
         f32x4 part[MT] = {};
 #pragma unroll
         for (int q = 0; q < 4; q++) {
@@ -102,22 +112,23 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
           }
         }
       }
+    }
   }
 #pragma unroll
-  for (int i = 0; i < MATS; i++)
+  for (int i = 0; i < SETS; i++)
 #pragma unroll
     for (int mt = 0; mt < MT; mt++) *reinterpret_cast<f32x4*>(sums[wave][i][mt][lane]) = acc[i][mt];
   __syncthreads();
-  // entry e of a tile: token e / 16, column e % 16; it is value (e / 16) % 4 of lane 16 (e / 64) + e % 16
-  for (int e = threadIdx.x; e < MT * 256; e += WAVES * 64) {
-    const int mt = e >> 8, in = e & 255, src = (in >> 6) * 16 + (in & 15), v = (in >> 4) & 3;
-    const long long t = t0 + e / 16, col = cb * W4_COLS + (in & 15);
+  // entry e of a set: token e / 16, column e % 16; it is value (e / 16) % 4 of lane 16 (e / 64) + e % 16
+  for (int e = threadIdx.x; e < CB * MT * 256; e += WAVES * 64) {
+    const int c = e / (MT * 256), f = e % (MT * 256), mt = f >> 8, in = f & 255, src = (in >> 6) * 16 + (in & 15), v = (in >> 4) & 3;
+    const long long t = t0 + f / 16, col = (cb0 + c) * W4_COLS + (in & 15);
     if (t >= a.tokens || col >= a.m) continue;
     float r[MATS] = {};
 #pragma unroll
     for (int i = 0; i < MATS; i++)
 #pragma unroll
-      for (int k = 0; k < WAVES; k++) r[i] += sums[k][i][mt][src][v];
+      for (int k = 0; k < WAVES; k++) r[i] += sums[k][i * CB + c][mt][src][v];
     float out = r[0];
     if constexpr (GATED) {
       f32x4 value, slope;
@@ -186,30 +197,35 @@ int w4_array(const void* p, bool needed, long long row, long long ld, int es) {
   return aligned(p, es) ? MLPROJ_OK : MLPROJ_ERR_ALIGNMENT;
 }
 
-template <typename T, bool GATED, int MT, int WAVES>
-void w4_launch_group(const W4Args& a, int group, dim3 grid, hipStream_t stream) {
+template <typename T, bool GATED, int MT, int CB, int U, int WAVES>
+void w4_launch(const W4Args& a, int group, hipStream_t stream) {
+  const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
+  const dim3 grid((unsigned)((cbs + CB - 1) / CB), (unsigned)((a.tokens + 16 * MT - 1) / (16 * MT))), block(WAVES * 64);
   mark(stream);
-  const dim3 block(WAVES * 64);
-  if (group == 32) launch(w4_kernel<T, GATED, MT, WAVES, 32>, grid, block, stream, a);
-  else if (group == 64) launch(w4_kernel<T, GATED, MT, WAVES, 64>, grid, block, stream, a);
-  else launch(w4_kernel<T, GATED, MT, WAVES, 128>, grid, block, stream, a);
+  if (group == 32) launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 32>, grid, block, stream, a);
+  else if (group == 64) launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 64>, grid, block, stream, a);
+  else launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 128>, grid, block, stream, a);
 }
 
 template <typename T, bool GATED>
 int w4_run(const W4Args& a, int group, hipStream_t stream) {
-  const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
-  const int mt = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
   // a grid has at most 65535 workgroups along y: more tokens than they take go out in several launches
-  constexpr long long MOST = 65535LL * 64;
+  constexpr long long MOST = 65535LL * 16;
   W4Args b = a;
   for (long long t = 0; t < a.tokens; t += MOST) {
     b.tokens = a.tokens - t < MOST ? a.tokens - t : MOST;
     b.x = static_cast<const T*>(a.x) + t * a.ldx;
     b.y = static_cast<T*>(a.y) + t * a.ldy;
-    const dim3 grid((unsigned)cbs, (unsigned)((b.tokens + 16 * mt - 1) / (16 * mt)));
-    if (mt == 1) w4_launch_group<T, GATED, 1, 8>(b, group, grid, stream);
-    else if (mt == 2) w4_launch_group<T, GATED, 2, 8>(b, group, grid, stream);
-    else w4_launch_group<T, GATED, 4, 8>(b, group, grid, stream);
+    const long long cbs = (a.m + W4_COLS - 1) / W4_COLS, groups = cbs * ((b.tokens + 15) / 16);
+    if (sizeof(T) == 2 && b.tokens > 16 && cbs * ((b.tokens + 31) / 32) >= 1024) {
+      if constexpr (sizeof(T) == 2) w4_launch<T, GATED, 2, 4, 1, 8>(b, group, stream);
+    } else if (groups >= 1024 && b.tokens >= 8) {
+      w4_launch<T, GATED, 1, 4, 1, 8>(b, group, stream);
+    } else if (groups >= 512) {
+      w4_launch<T, GATED, 1, 2, 2, 8>(b, group, stream);
+    } else {
+      w4_launch<T, GATED, 1, 1, 2, 16>(b, group, stream);
+    }
   }
   mark(stream);
   return launch_status();
