@@ -46,14 +46,22 @@ __device__ __forceinline__ f16x8 w4_widen(unsigned v, f16_t) {
 // every workgroup reads from L2 (128 rows of 16 tokens are 4 KiB, of a column block 1 KiB).  So: one column block per
 // workgroup and 16 wavefronts while that is what fills the chip, two where there are columns enough, four (and 32
 // tokens) where the tokens dominate.  us, with 1 x 16 / 2 x 8 / 4 x 8 (column blocks x wavefronts): one token 16384 ->
-// 4096 10.8 / 14 / 22, one token 4096 -> 2 x 16384 19 / 14.0 (4.9 TB/s) / 16.4, 16 tokens 4096 -> 2 x 16384 27 / 17.5 / 17.0,
-// 16 tokens 16384 -> 8192 38 / 23 / 27; 64 tokens 4096 -> 2 x 16384 84 / 52 / 44, with 32 tokens at a time 36.
-template <typename T, bool GATED, int MT, int CB, int U, int WAVES, int GROUP>
+// 4096 10.8 / 14 / 22, one token 4096 -> 2 x 16384 18 / 14 / 17, 16 tokens 4096 -> 2 x 16384 24 / 17 / 17, 16 tokens 16384
+// -> 8192 26 / 20 / 24; 64 tokens 4096 -> 2 x 16384 65 / 44 / 49, with 32 tokens at a time 34.
+//
+// A row block's tokens are loaded in whole rows, 256 bytes (fp32: 512) of one after the other, and turned into operands through
+// a corner of LDS that belongs to the wavefront (VIA_LDS): loading operands straight, lane l token l % 16, every four
+// lanes touch four cache lines, and at 16 tokens the lookups cost more than the weights (16384 -> 4096, groups of 32: 18.7
+// us).  With at most four tokens the lines are few and the straight way is shorter.
+template <typename T, bool GATED, int MT, int CB, int U, int WAVES, int GROUP, bool VIA_LDS>
 __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
   using E = typename FfParts<T>::type;
   using F = typename FfFrag<E>::type;
   constexpr int P = FfParts<T>::count, MATS = GATED ? 2 : 1, PER = W4_ROWS / GROUP, SETS = CB * MATS;
-  __shared__ float sums[WAVES][SETS][MT][64][4];
+  // tokens in whole rows: 16-byte pieces of a row, rows a load covers, loads
+  constexpr int VEC = 16 / sizeof(T), PIECES = W4_ROWS / VEC, ROWS = 64 / PIECES, XLOADS = 16 * MT / ROWS;
+  constexpr int HELD = VIA_LDS ? 16 * MT * PIECES : 0, SUMS = SETS * MT * 64;      // 16-byte pieces per row block, per wavefront
+  __shared__ u32x4 lds[WAVES * (U * HELD > SUMS ? U * HELD : SUMS)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long cb0 = (long long)blockIdx.x * CB, t0 = (long long)blockIdx.y * (16 * MT);
   const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
@@ -62,7 +70,8 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
   for (int kb = wave; kb < a.kblocks; kb += WAVES * U) {
     u32x4 w[U][SETS];
     bf16_t s[U][SETS][PER];
-    F xf[U][MT][P][4];
+    F xf[U][VIA_LDS ? 1 : MT][P][4];
+    u32x4 xr[U][VIA_LDS ? XLOADS : 1];
 #pragma unroll
     for (int u = 0; u < U; u++) {
       // past the end: the last block again, not used
@@ -74,50 +83,99 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
         __builtin_memcpy(s[u][i], a.scales[i / CB] + (at * 16 + (lane & 15)) * PER, PER * 2);
       }
       const bool whole = (k + 1) * W4_ROWS <= a.n;
+      // (rows past the tokens are the last one again: what they come to is not stored)
+      if constexpr (VIA_LDS) {
 #pragma unroll
-      for (int mt = 0; mt < MT; mt++) {
-        // (rows past the tokens are the last one again: what they come to is not stored)
-        const long long t = t0 + mt * 16 + (lane & 15);
-        const T* row = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx;
+        for (int j = 0; j < XLOADS; j++) {
+          const long long t = t0 + j * ROWS + lane / PIECES;
+          const int at = k * W4_ROWS + lane % PIECES * VEC;
+          const T* from = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx + at;
+          if (whole) {
+            __builtin_memcpy(&xr[u][j], from, 16);
+          } else {
+            T v[VEC];
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-          const int at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
-          u32x4 parts[P];
-          fs_parts(ff_load8(row + at, whole ? 8 : a.n - at), parts);
+            for (int i = 0; i < VEC; i++) v[i] = at + i < a.n ? from[i] : (T)0.0f;
+            __builtin_memcpy(&xr[u][j], v, 16);
+          }
+        }
+      } else {
 #pragma unroll
-          for (int p = 0; p < P; p++) __builtin_memcpy(&xf[u][mt][p][q], &parts[p], 16);
+        for (int mt = 0; mt < MT; mt++) {
+          const long long t = t0 + mt * 16 + (lane & 15);
+          const T* row = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx;
+#pragma unroll
+          for (int q = 0; q < 4; q++) {
+            const int at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
+            u32x4 parts[P];
+            fs_parts(ff_load8(row + at, whole ? 8 : a.n - at), parts);
+#pragma unroll
+            for (int p = 0; p < P; p++) __builtin_memcpy(&xf[u][mt][p][q], &parts[p], 16);
+          }
         }
       }
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
       if (kb + u * WAVES >= a.kblocks) break;
+      u32x4* mine = lds + (wave * U + u) * HELD;
+      if constexpr (VIA_LDS) {
+        // (pieces permuted by the row's number: eight rows' pieces spread over all banks)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-      for (int i = 0; i < SETS; i++) {
-        f32x4 part[MT] = {};
+        for (int j = 0; j < XLOADS; j++) {
+          const int r = j * ROWS + lane / PIECES;
+          mine[r * PIECES + (lane % PIECES ^ (r & 7))] = xr[u][j];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      f32x4 part[SETS][MT] = {};
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
+      for (int q = 0; q < 4; q++) {
+        F xq[MT][P];
+#pragma unroll
+        for (int mt = 0; mt < MT; mt++) {
+          if constexpr (VIA_LDS) {
+            FfVec8<T> v;
+            constexpr int EACH = 8 / VEC;
+            const int r = mt * 16 + (lane & 15);
+#pragma unroll
+            for (int e = 0; e < EACH; e++) {
+              const u32x4 piece = mine[r * PIECES + (((q * 4 + (lane >> 4)) * EACH + e) ^ (r & 7))];
+              __builtin_memcpy(&v.v[e * VEC], &piece, 16);
+            }
+            u32x4 parts[P];
+            fs_parts(v, parts);
+#pragma unroll
+            for (int p = 0; p < P; p++) __builtin_memcpy(&xq[mt][p], &parts[p], 16);
+          } else {
+#pragma unroll
+            for (int p = 0; p < P; p++) xq[mt][p] = xf[u][VIA_LDS ? 0 : mt][p][q];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < SETS; i++) {
           const F wf = w4_widen(w[u][i][q], E{});
 #pragma unroll
-          for (int mt = 0; mt < MT; mt++)
+          for (int mt = 0; mt < MT; mt++) {
 #pragma unroll
-            for (int p = P - 1; p >= 0; p--) part[mt] = ff_mfma(xf[u][mt][p][q], wf, part[mt]);
-          if ((q + 1) * 32 % GROUP == 0) {
-            const float scale = (float)s[u][i][q * 32 / GROUP];
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++) {
-              acc[i][mt] += scale * part[mt];
-              part[mt] = f32x4{};
+            for (int p = P - 1; p >= 0; p--) part[i][mt] = ff_mfma(xq[mt][p], wf, part[i][mt]);
+            if ((q + 1) * 32 % GROUP == 0) {
+              acc[i][mt] += (float)s[u][i][q * 32 / GROUP] * part[i][mt];
+              part[i][mt] = f32x4{};
             }
           }
         }
       }
     }
   }
+  if (VIA_LDS) __syncthreads();                 // the sums take the tokens' place
+  f32x4* sums = reinterpret_cast<f32x4*>(lds);
 #pragma unroll
   for (int i = 0; i < SETS; i++)
 #pragma unroll
-    for (int mt = 0; mt < MT; mt++) *reinterpret_cast<f32x4*>(sums[wave][i][mt][lane]) = acc[i][mt];
+    for (int mt = 0; mt < MT; mt++) sums[((wave * SETS + i) * MT + mt) * 64 + lane] = acc[i][mt];
   __syncthreads();
   // entry e of a set: token e / 16, column e % 16; it is value (e / 16) % 4 of lane 16 (e / 64) + e % 16
   for (int e = threadIdx.x; e < CB * MT * 256; e += WAVES * 64) {
@@ -128,7 +186,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
 #pragma unroll
     for (int i = 0; i < MATS; i++)
 #pragma unroll
-      for (int k = 0; k < WAVES; k++) r[i] += sums[k][i * CB + c][mt][src][v];
+      for (int k = 0; k < WAVES; k++) r[i] += sums[((k * SETS + i * CB + c) * MT + mt) * 64 + src][v];
     float out = r[0];
     if constexpr (GATED) {
       f32x4 value, slope;
@@ -197,14 +255,14 @@ int w4_array(const void* p, bool needed, long long row, long long ld, int es) {
   return aligned(p, es) ? MLPROJ_OK : MLPROJ_ERR_ALIGNMENT;
 }
 
-template <typename T, bool GATED, int MT, int CB, int U, int WAVES>
+template <typename T, bool GATED, int MT, int CB, int U, int WAVES, bool VIA_LDS>
 void w4_launch(const W4Args& a, int group, hipStream_t stream) {
   const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
   const dim3 grid((unsigned)((cbs + CB - 1) / CB), (unsigned)((a.tokens + 16 * MT - 1) / (16 * MT))), block(WAVES * 64);
   mark(stream);
-  if (group == 32) launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 32>, grid, block, stream, a);
-  else if (group == 64) launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 64>, grid, block, stream, a);
-  else launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 128>, grid, block, stream, a);
+  if (group == 32) launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 32, VIA_LDS>, grid, block, stream, a);
+  else if (group == 64) launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 64, VIA_LDS>, grid, block, stream, a);
+  else launch(w4_kernel<T, GATED, MT, CB, U, WAVES, 128, VIA_LDS>, grid, block, stream, a);
 }
 
 template <typename T, bool GATED>
@@ -218,13 +276,15 @@ int w4_run(const W4Args& a, int group, hipStream_t stream) {
     b.y = static_cast<T*>(a.y) + t * a.ldy;
     const long long cbs = (a.m + W4_COLS - 1) / W4_COLS, groups = cbs * ((b.tokens + 15) / 16);
     if (sizeof(T) == 2 && b.tokens > 16 && cbs * ((b.tokens + 31) / 32) >= 1024) {
-      if constexpr (sizeof(T) == 2) w4_launch<T, GATED, 2, 4, 1, 8>(b, group, stream);
+      if constexpr (sizeof(T) == 2) w4_launch<T, GATED, 2, 4, 1, 8, false>(b, group, stream);
     } else if (groups >= 1024 && b.tokens >= 8) {
-      w4_launch<T, GATED, 1, 4, 1, 8>(b, group, stream);
+      w4_launch<T, GATED, 1, 4, 1, 8, false>(b, group, stream);
     } else if (groups >= 512) {
-      w4_launch<T, GATED, 1, 2, 2, 8>(b, group, stream);
+      if (b.tokens > 4) w4_launch<T, GATED, 1, 2, 1, 8, true>(b, group, stream);
+      else w4_launch<T, GATED, 1, 2, 2, 8, false>(b, group, stream);
     } else {
-      w4_launch<T, GATED, 1, 1, 2, 16>(b, group, stream);
+      if (b.tokens > 4) w4_launch<T, GATED, 1, 1, 1, 16, true>(b, group, stream);
+      else w4_launch<T, GATED, 1, 1, 2, 16, false>(b, group, stream);
     }
   }
   mark(stream);
