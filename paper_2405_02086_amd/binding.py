@@ -590,9 +590,12 @@ def _storage(dtype):
     return _STORAGES[dtype]
 
 
+# (One token through a norm is 4 us on the GPU: here too, what a call costs is marshalling, and most tensors are contiguous.)
 def _matrix(t, shape, like, what):
     """A device matrix of `shape` and `like`'s dtype whose rows are contiguous; returns its row stride."""
-    assert t.is_cuda and t.dtype is like.dtype and t.shape == shape, what
+    assert t.dtype is like.dtype and t.is_cuda and t.shape == shape, what
+    if t.is_contiguous():
+        return shape[1]
     rows, cols = shape
     assert cols <= 1 or t.stride(1) == 1, what + ": the entries of a row must be neighbours"
     return t.stride(0) if rows > 1 else max(cols, t.stride(0))
@@ -600,7 +603,9 @@ def _matrix(t, shape, like, what):
 
 def _result(t, shape, like, what):
     if t is None:
-        t = _import_torch().empty(shape, dtype=like.dtype, device=like.device)
+        if like.shape == shape and like.is_contiguous():
+            return _torch.empty_like(like), shape[1]
+        return like.new_empty(shape), shape[1]
     return t, _matrix(t, shape, like, what)
 
 
@@ -628,6 +633,7 @@ def gated_ff(X, Wg, Wu, act="silu", mask=None, H=None, g_out=None, u_out=None, w
     """H = mask * act(X Wg) * (X Wu): X is tokens x n, the weights n x m, all of one type (fp32, bf16, fp16), rows any
     distance apart.  act: "silu", "gelu" (with erf) or "relu"; mask: the kept-column mask of a projection.
     g_out, u_out: tensors that also receive X Wg and X Wu, for gated_ff_backward."""
+    storage = _storage(X.dtype)
     block, tokens, n, m = _gated_block(X, Wg, Wu, mask)
     H, ldh = _result(H, (tokens, m), X, "H")
     ldg = 0
@@ -637,7 +643,7 @@ def gated_ff(X, Wg, Wu, act="silu", mask=None, H=None, g_out=None, u_out=None, w
         assert _matrix(u_out, (tokens, m), X, "u_out") == ldg, "g_out and u_out: one row stride"
     if workspace is None:
         workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, False, mask is not None), device=X.device)
-    st = lib().gated_ff_forward(_storage(X.dtype), _ACTS[act], ctypes.byref(block), H.data_ptr(), ldh, _ptr(g_out), _ptr(u_out),
+    st = lib().gated_ff_forward(storage, _ACTS[act], ctypes.byref(block), H.data_ptr(), ldh, _ptr(g_out), _ptr(u_out),
                                 ldg, workspace.buf.data_ptr(), workspace.nbytes, _stream(stream))
     if st != 0:
         _check(st, "gated_ff_forward")
@@ -648,6 +654,7 @@ def gated_ff_backward(dH, X, Wg, Wu, act="silu", mask=None, G=None, U=None, dX=N
                       stream=None, need_dx=True, need_dw=True):
     """(dX, dWg, dWu) of gated_ff for the gradient dH of its result.  G, U: what the forward call wrote to g_out and
     u_out; without them they are computed again.  need_dx, need_dw: leave out what is not needed (None comes back)."""
+    storage = _storage(X.dtype)
     block, tokens, n, m = _gated_block(X, Wg, Wu, mask)
     ldh = _matrix(dH, (tokens, m), X, "dH")
     assert (G is None) == (U is None), "G and U: both or neither"
@@ -663,7 +670,7 @@ def gated_ff_backward(dH, X, Wg, Wu, act="silu", mask=None, G=None, U=None, dX=N
         assert ld == lddw, "dWg and dWu: one row stride"
     if workspace is None:
         workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, True, mask is not None), device=X.device)
-    st = lib().gated_ff_backward(_storage(X.dtype), _ACTS[act], ctypes.byref(block), dH.data_ptr(), ldh, _ptr(G), _ptr(U), ldg,
+    st = lib().gated_ff_backward(storage, _ACTS[act], ctypes.byref(block), dH.data_ptr(), ldh, _ptr(G), _ptr(U), ldg,
                                  _ptr(dX) if need_dx else None, lddx, _ptr(dWg) if need_dw else None,
                                  _ptr(dWu) if need_dw else None, lddw, workspace.buf.data_ptr(), workspace.nbytes,
                                  _stream(stream))
@@ -672,27 +679,26 @@ def gated_ff_backward(dH, X, Wg, Wu, act="silu", mask=None, G=None, U=None, dX=N
     return (dX if need_dx else None, dWg if need_dw else None, dWu if need_dw else None)
 
 
-def _vector(t, n, like, what):
-    assert t.is_cuda and t.dtype is like.dtype and t.is_contiguous() and t.shape == (n,), what
+def _vector(t, shape, like, what):
+    assert t.dtype is like.dtype and t.is_cuda and t.shape == shape and t.is_contiguous(), what
     return t.data_ptr()
 
 
 def _norm_block(z, b, w_post, gate, w_pre, scale, eps):
-    tokens, n = z.shape
-    block = NormBlock(tokens, n)
-    block.scale, block.eps = scale, eps
-    token_gate = False
-    if b is not None:
-        block.b, block.ldb = b.data_ptr(), _matrix(b, (tokens, n), z, "b")
-        block.w_post = _vector(w_post, n, z, "w_post: n entries")
-        token_gate = gate.dim() == 2
-        if token_gate:
-            block.gate, block.gate_stride = gate.data_ptr(), _matrix(gate, (tokens, n), z, "gate")
-        else:
-            block.gate = _vector(gate, n, z, "gate: n entries, or tokens x n")
-    if w_pre is not None:
-        block.w_pre = _vector(w_pre, n, z, "w_pre: n entries")
-    return block, tokens, n, token_gate
+    shape = z.shape
+    tokens, n = shape
+    row = (n,)
+    pre = None if w_pre is None else _vector(w_pre, row, z, "w_pre: n entries")
+    if b is None:
+        return NormBlock(tokens, n, None, 0, None, None, 0, pre, scale, eps), shape, False
+    ldb = _matrix(b, shape, z, "b")
+    post = _vector(w_post, row, z, "w_post: n entries")
+    token_gate = gate.dim() == 2
+    if token_gate:
+        stride, at = _matrix(gate, shape, z, "gate"), gate.data_ptr()
+    else:
+        stride, at = 0, _vector(gate, row, z, "gate: n entries, or tokens x n")
+    return NormBlock(tokens, n, b.data_ptr(), ldb, post, at, stride, pre, scale, eps), shape, token_gate
 
 
 def block_norm(x, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e-6, r=None, y=None, stream=None):
@@ -700,18 +706,25 @@ def block_norm(x, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e-
     a vector of n entries or a tokens x n matrix.  Without b, r is x itself; without w_pre there is no y.
     r may be x and y may be b (in place)."""
     assert x.dim() == 2
-    block, tokens, n, _ = _norm_block(x, b, w_post, gate, w_pre, scale, eps)
+    storage = _storage(x.dtype)
+    block, shape, _ = _norm_block(x, b, w_post, gate, w_pre, scale, eps)
+    ldx = _matrix(x, shape, x, "x")
+    at_r = at_y = None
     ldr = ldy = 0
-    if b is not None:
-        r, ldr = _result(r, (tokens, n), x, "r")
-    if w_pre is not None:
-        y, ldy = _result(y, (tokens, n), x, "y")
-    st = lib().block_norm_forward(_storage(x.dtype), ctypes.byref(block), x.data_ptr(), _matrix(x, (tokens, n), x, "x"),
-                                  None if b is None else r.data_ptr(), ldr, None if w_pre is None else y.data_ptr(), ldy,
-                                  _stream(stream))
+    if b is None:
+        r = x
+    else:
+        r, ldr = _result(r, shape, x, "r")
+        at_r = r.data_ptr()
+    if w_pre is None:
+        y = None
+    else:
+        y, ldy = _result(y, shape, x, "y")
+        at_y = y.data_ptr()
+    st = lib().block_norm_forward(storage, ctypes.byref(block), x.data_ptr(), ldx, at_r, ldr, at_y, ldy, _stream(stream))
     if st != 0:
         _check(st, "block_norm_forward")
-    return (x if b is None else r), (None if w_pre is None else y)
+    return r, y
 
 
 def block_norm_workspace_bytes(tokens, n):
@@ -725,32 +738,35 @@ def block_norm_backward(dr, dy, r, b=None, w_post=None, gate=None, w_pre=None, s
     """(dx, db, dw_post, dgate, dw_pre) of block_norm for the gradients dr (None: zeros) and dy (None without w_pre) of
     its results; r is what it returned.  The gradients of vectors are fp32 sums over the tokens, dgate of a
     tokens x n gate is a matrix like it; what has no input is None.  dx may be dr, db may be b or dy."""
-    torch = _import_torch()
     assert r.dim() == 2
-    block, tokens, n, token_gate = _norm_block(r, b, w_post, gate, w_pre, scale, eps)
+    storage = _storage(r.dtype)
+    f32 = _torch.float32
+    block, shape, token_gate = _norm_block(r, b, w_post, gate, w_pre, scale, eps)
+    tokens, n = shape
+    ldr = _matrix(r, shape, r, "r")
     lddr = lddy = lddb = ldg = 0
+    at_dy = at_db = at_post = at_gate = at_pre = dw_post = dgate = dw_pre = None
     if dr is not None:
-        lddr = _matrix(dr, (tokens, n), r, "dr")
-    if w_pre is not None:
-        lddy = _matrix(dy, (tokens, n), r, "dy")
-    dx, lddx = _result(dx, (tokens, n), r, "dx")
-    dw_post = dgate = dw_pre = None
-    if b is not None:
-        db, lddb = _result(db, (tokens, n), r, "db")
-        if token_gate:
-            dgate, ldg = _result(None, (tokens, n), r, "dgate")
-            dw_post = torch.empty(n, dtype=torch.float32, device=r.device)
-        else:
-            dw_post, dgate = torch.empty(2, n, dtype=torch.float32, device=r.device)
-    else:
+        lddr = _matrix(dr, shape, r, "dr")
+    dx, lddx = _result(dx, shape, r, "dx")
+    if b is None:
         db = None
+    else:
+        db, lddb = _result(db, shape, r, "db")
+        dw_post = r.new_empty(n, dtype=f32)
+        if token_gate:
+            dgate, ldg = _result(None, shape, r, "dgate")
+        else:
+            dgate = r.new_empty(n, dtype=f32)
+        at_db, at_post, at_gate = db.data_ptr(), dw_post.data_ptr(), dgate.data_ptr()
     if w_pre is not None:
-        dw_pre = torch.empty(n, dtype=torch.float32, device=r.device)
+        lddy = _matrix(dy, shape, r, "dy")
+        dw_pre = r.new_empty(n, dtype=f32)
+        at_dy, at_pre = dy.data_ptr(), dw_pre.data_ptr()
     if workspace is None:
         workspace = Workspace(block_norm_workspace_bytes(tokens, n), device=r.device)
-    st = lib().block_norm_backward(_storage(r.dtype), ctypes.byref(block), r.data_ptr(), _matrix(r, (tokens, n), r, "r"),
-                                   _ptr(dr), lddr, None if w_pre is None else dy.data_ptr(), lddy, dx.data_ptr(), lddx,
-                                   _ptr(db), lddb, _ptr(dw_post), _ptr(dgate), ldg, _ptr(dw_pre), workspace.buf.data_ptr(),
+    st = lib().block_norm_backward(storage, ctypes.byref(block), r.data_ptr(), ldr, _ptr(dr), lddr, at_dy, lddy, dx.data_ptr(),
+                                   lddx, at_db, lddb, at_post, at_gate, ldg, at_pre, workspace.buf.data_ptr(),
                                    workspace.nbytes, _stream(stream))
     if st != 0:
         _check(st, "block_norm_backward")
@@ -792,10 +808,10 @@ def w4_pack(W, group=128, stream=None):
 
 def w4_matvec(x, W, y=None, stream=None):
     """y = x W for few tokens (x: tokens x n) and a packed W."""
-    tokens = x.shape[0]
+    storage, tokens = _storage(x.dtype), x.shape[0]
     ldx = _matrix(x, (tokens, W.n), x, "x")
     y, ldy = _result(y, (tokens, W.m), x, "y")
-    st = lib().w4_matvec(_storage(x.dtype), W._ref, x.data_ptr(), ldx, tokens, y.data_ptr(), ldy, _stream(stream))
+    st = lib().w4_matvec(storage, W._ref, x.data_ptr(), ldx, tokens, y.data_ptr(), ldy, _stream(stream))
     if st != 0:
         _check(st, "w4_matvec")
     return y
@@ -803,10 +819,10 @@ def w4_matvec(x, W, y=None, stream=None):
 
 def w4_gated_matvec(x, Wg, Wu, act="silu", h=None, stream=None):
     """h = act(x Wg) * (x Wu) for few tokens and packed weights of one size and group."""
-    tokens = x.shape[0]
+    storage, tokens = _storage(x.dtype), x.shape[0]
     ldx = _matrix(x, (tokens, Wg.n), x, "x")
     h, ldh = _result(h, (tokens, Wg.m), x, "h")
-    st = lib().w4_gated_matvec(_storage(x.dtype), _ACTS[act], Wg._ref, Wu._ref, x.data_ptr(), ldx, tokens, h.data_ptr(), ldh,
+    st = lib().w4_gated_matvec(storage, _ACTS[act], Wg._ref, Wu._ref, x.data_ptr(), ldx, tokens, h.data_ptr(), ldh,
                                _stream(stream))
     if st != 0:
         _check(st, "w4_gated_matvec")
