@@ -36,7 +36,7 @@ struct FfProduct {
   long long lda, ldb;          // elements between rows
   long long M, N, K;           // N: columns of each of the two products
   int segs;
-  bool filled;                 // B is the workspace's: its rows may be read up to ldb
+  bool a_filled, b_filled;     // the workspace's: rows may be read up to their whole 16-byte pieces, past K they hold zeros
   int act;
   void *C0, *C1;
   long long ldc;

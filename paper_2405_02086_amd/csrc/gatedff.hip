@@ -22,12 +22,13 @@ static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // ------------------------------------------------------------------ plan of a product
 // Which tiles a product takes and into how many shares its sum is cut.  Three kinds of tiles: direct 256 x 256 (one workgroup
-// per compute unit), direct 128 x 128 (two), staged 128 x 128 (three).  What a 32-deep step of a tile takes with every place
+// per compute unit), direct 128 x 128 (two), staged 128 x 128 (three; fp32: two).  What a 32-deep step of a tile takes with every place
 // taken, the price of a workgroup beside its steps and the price of joining shares were measured (4096 x 4096 x 16384
 // and 1000 x 1000 x 20000, bf16 and fp32); the plan is the cheapest of them.
 struct FfPlan {
   int kind;      // 0: direct 256, 1: direct 128, 2: staged, 3: few tokens
   int splits;
+  double us;
 };
 // (forward: A's rows and B's columns run along memory, as in the forward product)
 struct FfKind {
@@ -35,33 +36,28 @@ struct FfKind {
   double step_us, tile_us;
 };
 static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool forward, bool direct, int es) {
-  static const FfKind kinds[3] = {{256, 256, 1, 0.86, 9.0}, {128, 128, 2, 0.53, 5.0}, {128, 128, 3, 1.3, 5.0}};
+  static const FfKind kinds[4] = {{256, 256, 1, 0.86, 9.0}, {128, 128, 2, 0.53, 5.0}, {128, 128, 3, 2.0, 5.0}, {128, 128, 2, 3.1, 5.0}};
   if (es == 4 && forward && M <= FK_TOKENS) {
     // shares until there are two workgroups per compute unit or a wavefront has one step left
     int splits = 1;
     const long long groups = ff_cdiv(N, FK_COLS) * ff_cdiv(M, 16);
     while (groups * splits < 512 && steps > FK_WAVES * splits && splits < 64) splits *= 2;
-    return {3, splits};
+    return {3, splits, 0.0};
   }
-  FfPlan best{2, 1};
-  double least = 1e30;
+  FfPlan best{2, 1, 1e30};
   for (int kind = direct ? 0 : 2; kind <= (direct ? 1 : 2); kind++) {
-    const FfKind& k = kinds[kind];
-    const double step_us = k.step_us * (kind == 2 && es == 4 ? 4.0 : 1.0);
+    const FfKind& k = kinds[kind == 2 && es == 4 ? 3 : kind];
     const long long tiles = ff_cdiv(M, k.rows) * ff_cdiv(N, dual ? k.cols / 2 : k.cols);
     const double planes = 4.0 * M * N * (dual ? 2 : 1);
     for (int splits = 1; splits <= 64; splits *= 2) {
       if (splits > 1 && (steps / splits < 2 || planes * splits > 512e6)) break;
       const double units = 256.0 * k.places, groups = (double)tiles * splits;
-      // workgroups in turn on the fullest place; a place shared with empty ones is faster, at best as fast as half of them
+      // workgroups in turn on the fullest place; a direct tile beside an empty place is faster
       const double turns = ff_cdiv((long long)groups, (long long)units);
-      const double share = groups < units / 2 && k.places > 1 ? 0.65 : 1.0;
-      double us = turns * ((double)ff_cdiv(steps, splits) * step_us * share + k.tile_us);
+      const double share = groups < units / 2 && kind == 1 ? 0.65 : 1.0;
+      double us = turns * ((double)ff_cdiv(steps, splits) * k.step_us * share + k.tile_us);
       if (splits > 1) us += 4.0 + 0.3 * splits + planes * (splits + splits) / 4.0e6;
-      if (us < least) {
-        least = us;
-        best = {kind, splits};
-      }
+      if (us < best.us) best = {kind, splits, us};
     }
   }
   return best;
@@ -77,13 +73,29 @@ static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, 
   return most;
 }
 
+// Whether 16-bit operands whose rows are not in whole 16-byte pieces are copied into rows that are (ff_pad_kernel), for
+// the direct tiles: where that is cheaper than the staged tiles by the plan.  Copies go at 4 TB/s, read and written.
+static bool ff_pads(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
+  if (es != 2 || (n % 8 == 0 && (m % 8 == 0 || masked))) return false;
+  auto us = [&](bool direct) {
+    double t = ff_plan(tokens, m, ff_steps(n, 1), true, true, direct, es).us;
+    if (backward) t += ff_plan(tokens, n, ff_steps(m, 2), false, false, direct, es).us + ff_plan(n, m, ff_steps(tokens, 1), true, false, direct, es).us;
+    return t;
+  };
+  const double elements = (double)tokens * n + (masked ? 0.0 : 2.0 * n * m);
+  return us(true) + 5.0 + elements * 2 * es / 4.0e6 < us(false);
+}
+
 // ------------------------------------------------------------------ workspace
 struct FfLayout {
+  long long ldn;               // row length of a padded X: n in whole 16-byte pieces
+  size_t X;                    // padded: a copy of X; the weights' copies take W
   long long ldd;               // row length of packed and intermediate arrays: m in whole 16-byte pieces
   size_t partial;              // shares of sums, of one product at a time
   size_t dG, dU;               // backward: gradients at the pre-activations, tokens x ldd
   size_t position, kept, W[2], in[3], out[3];   // masked: where the channels went; packed weights, inputs and results
-  size_t shares, bytes;
+  size_t bytes;                // a workspace for masked calls serves the others too
+  bool pads;
 };
 FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
   FfLayout L{};
@@ -94,6 +106,7 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
     return at;
   };
   L.ldd = ff_cdiv(m, 8) * 8;
+  L.ldn = ff_cdiv(n, 8) * 8;
   // (the packed channels' products run over ldd of them)
   const long long widest = masked ? L.ldd : m;
   size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, true, es);
@@ -102,37 +115,39 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
     shares = shares > x ? shares : x;
     shares = shares > w ? shares : w;
   }
-  if (masked) {      // a workspace for masked calls serves the others too
-    const size_t plain = ff_layout(es, tokens, n, m, backward, false).shares;
-    shares = shares > plain ? shares : plain;
-  }
-  L.shares = shares;
   L.partial = take(shares);
   const size_t plane = (size_t)tokens * L.ldd * es, weights = (size_t)n * L.ldd * es;
   if (backward) {
     L.dG = take(plane);
     L.dU = take(plane);
   }
+  L.pads = ff_pads(es, tokens, n, m, backward, masked);
+  if (L.pads) L.X = take((size_t)tokens * L.ldn * es);
+  if (L.pads || masked)
+    for (size_t& w : L.W) w = take(weights);
   if (masked) {
     L.position = take((size_t)(m + 1) * 4);
     L.kept = take(4);
-    for (size_t& w : L.W) w = take(weights);
     if (backward)
       for (size_t& i : L.in) i = take(plane);
     for (int i = 0; i < (backward ? 2 : 3); i++) L.out[i] = take(backward ? weights : plane);
   }
   L.bytes = o + 256;
+  if (masked) {
+    const size_t plain = ff_layout(es, tokens, n, m, backward, false).bytes;
+    L.bytes = L.bytes > plain ? L.bytes : plain;
+  }
   return L;
 }
 
 // ------------------------------------------------------------------ launches
 // Whether a product's operands can go straight into LDS: 16-bit elements, rows, starts and row lengths in whole
 // 16-byte pieces, and a tile's rows within a buffer resource's 2 GiB.
-// (A row's last piece may reach past N where B is the workspace's, whose rows are filled up.)
+// (The last piece of a row may reach past the matrix where the rows are the workspace's.  Past K there are zeros.)
 template <bool A_KC, bool B_KC, typename T>
 bool ff_direct(const FfProduct& p) {
   if (sizeof(T) != 2) return false;
-  const long long a_row = A_KC ? p.K : p.M, b_row = B_KC ? p.K : (p.filled ? 0 : p.N);
+  const long long a_row = p.a_filled ? 0 : A_KC ? p.K : p.M, b_row = p.b_filled ? 0 : B_KC ? p.K : p.N;
   for (const void* q : {p.A0, p.A1, p.B0, p.B1})
     if (!aligned(q, 16)) return false;
   return a_row % 8 == 0 && b_row % 8 == 0 && p.lda % 8 == 0 && p.ldb % 8 == 0 && p.lda < (1 << 22) && p.ldb < (1 << 22) &&
@@ -251,11 +266,51 @@ struct FfMove {
   }
 };
 
-// A block's weights and the channels its products run over: the caller's, or the kept ones in packed form.
+// Copies of matrices in rows of whole 16-byte pieces, filled up with zeros; without `from` only the filling: the pieces
+// from the last whole one on.
+struct FfPad {
+  const void* from[5];
+  void* to[5];
+  long long ld_from[5], ld_to[5], rows[5], cols[5];
+  long long first[5];          // number of the first thread of a matrix
+  int count;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void ff_pad_kernel(FfPad a) {
+  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  int i = 0;
+  while (i + 1 < a.count && id >= a.first[i + 1]) i++;
+  const long long pieces = a.from[i] ? a.ld_to[i] / 8 : 1, at = id - a.first[i];
+  const long long row = at >> 32 ? at / pieces : (unsigned)at / (unsigned)pieces;
+  const long long col = a.from[i] ? (at - row * pieces) * 8 : a.ld_to[i] - 8;
+  if (row >= a.rows[i]) return;
+  FfVec8<T> v = {};
+  if (a.from[i]) v = ff_load8(static_cast<const T*>(a.from[i]) + row * a.ld_from[i] + col, a.cols[i] - col);
+  __builtin_memcpy(static_cast<T*>(a.to[i]) + row * a.ld_to[i] + col, &v, sizeof(v));
+}
+struct FfPadder {
+  FfPad a{};
+  long long threads = 0;
+  void add(const void* from, long long ld_from, void* to, long long ld_to, long long rows, long long cols) {
+    const int i = a.count++;
+    a.from[i] = from; a.ld_from[i] = ld_from; a.to[i] = to; a.ld_to[i] = ld_to; a.rows[i] = rows; a.cols[i] = cols;
+    a.first[i] = threads;
+    threads += rows * (from ? ld_to / 8 : 1);
+  }
+  template <typename T>
+  void go(hipStream_t stream) {
+    if (threads == 0) return;
+    mark(stream);
+    launch(ff_pad_kernel<T>, dim3((unsigned)ff_cdiv(threads, 256)), dim3(256), stream, a);
+  }
+};
+
+// A block's weights and the channels its products run over: the caller's, copies in filled rows, or the kept ones in packed form.
 struct FfChannels {
   const void *Wg, *Wu;
   long long ldw, m;            // m: how many there can be
   int *position = nullptr, *kept = nullptr;
+  bool filled = false;         // the weights are the workspace's, rows filled up with zeros
 };
 FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, hipStream_t stream) {
   FfChannels c{b->Wg, b->Wu, b->ldw, b->m};
@@ -266,7 +321,36 @@ FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws,
   launch(ff_index_kernel, dim3(1), dim3(FC_THREADS), stream, b->mask, b->m, c.position, c.kept);
   c.Wg = ws + L.W[0]; c.Wu = ws + L.W[1];
   c.ldw = c.m = L.ldd;
+  c.filled = true;
   return c;
+}
+
+// X, and copies of it and of the weights where the plan pads (weights: unless they are packed anyway, or not read).
+struct FfInput {
+  const void* at;
+  long long ld;
+  bool filled;
+};
+template <typename T>
+FfInput ff_input(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, bool weights, FfChannels& ch, hipStream_t stream) {
+  FfInput X{b->X, b->ldx, false};
+  if (!L.pads) return X;
+  FfPadder pad;
+  if (b->n % 8) {
+    pad.add(b->X, b->ldx, ws + L.X, L.ldn, b->tokens, b->n);
+    X = {ws + L.X, L.ldn, true};
+  }
+  if (!pack && weights) {
+    pad.add(b->Wg, b->ldw, ws + L.W[0], L.ldd, b->n, b->m);
+    pad.add(b->Wu, b->ldw, ws + L.W[1], L.ldd, b->n, b->m);
+    ch.Wg = ws + L.W[0]; ch.Wu = ws + L.W[1]; ch.ldw = L.ldd; ch.filled = true;
+    if (L.dU && b->m % 8) {      // dG and dU are summed over as well: whole pieces there too
+      pad.add(nullptr, 0, ws + L.dG, L.ldd, b->tokens, 0);
+      pad.add(nullptr, 0, ws + L.dU, L.ldd, b->tokens, 0);
+    }
+  }
+  pad.go<T>(stream);
+  return X;
 }
 
 template <typename T>
@@ -275,17 +359,18 @@ int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, vo
   const bool pack = b->mask && b->tokens > FF_PACK_TOKENS;
   const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, false, pack);
   char* ws = static_cast<char*>(workspace);
-  const FfChannels ch = ff_channels(b, L, ws, pack, stream);
+  FfChannels ch = ff_channels(b, L, ws, pack, stream);
   if (pack) {
     FfMove<T, true> in(b->m, ch.position, ch.kept);
     in.add(b->Wg, b->ldw, ws + L.W[0], L.ldd, b->n);
     in.add(b->Wu, b->ldw, ws + L.W[1], L.ldd, b->n);
     in.go(stream);
   }
+  const FfInput X = ff_input<T>(b, L, ws, pack, true, ch, stream);
   FfProduct p{};
   p.segs = 1; p.act = act;
-  p.A0 = b->X; p.lda = b->ldx;
-  p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
+  p.A0 = X.at; p.lda = X.ld; p.a_filled = X.filled;
+  p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw; p.b_filled = ch.filled;
   p.M = b->tokens; p.N = ch.m; p.K = b->n;
   p.C0 = H; p.ldc = ldh;
   p.G = G; p.U = U; p.ldg = ldg;
@@ -325,7 +410,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
   const bool pack = b->mask != nullptr;
   const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, true, pack);
   char* ws = static_cast<char*>(workspace);
-  const FfChannels ch = ff_channels(b, L, ws, pack, stream);
+  FfChannels ch = ff_channels(b, L, ws, pack, stream);
   if (pack) {
     // what runs over the channels: the weights where a product reads them, dH and the saved pre-activations
     void *W[2] = {ws + L.W[0], ws + L.W[1]}, *in[3] = {ws + L.in[0], ws + L.in[1], ws + L.in[2]};
@@ -344,6 +429,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     planes.go(stream);
     dH = in[0]; ldh = L.ldd;
   }
+  const FfInput X = ff_input<T>(b, L, ws, pack, dX || !G, ch, stream);
   T *dG = reinterpret_cast<T*>(ws + L.dG), *dU = reinterpret_cast<T*>(ws + L.dU);
   {
     FfProduct p{};
@@ -357,16 +443,16 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
       mark(stream);
       launch(ff_slopes_kernel<T>, dim3((unsigned)ff_cdiv(ff_cdiv(ch.m, 4) * b->tokens, 256)), dim3(256), stream, p);
     } else {
-      p.A0 = b->X; p.lda = b->ldx;
-      p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
+      p.A0 = X.at; p.lda = X.ld; p.a_filled = X.filled;
+      p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw; p.b_filled = ch.filled;
       ff_product<T, true, false, true, FF_GRAD>(p, ws + L.partial, stream);
     }
   }
   if (dX) {
     FfProduct p{};
     p.segs = 2;
-    p.A0 = dG; p.A1 = dU; p.lda = L.ldd;
-    p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw;
+    p.A0 = dG; p.A1 = dU; p.lda = L.ldd; p.a_filled = ch.filled;
+    p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw; p.b_filled = ch.filled;
     p.M = b->tokens; p.N = b->n; p.K = ch.m;
     p.C0 = dX; p.ldc = lddx;
     p.kept = ch.kept;
@@ -376,10 +462,9 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     void* packed[2] = {ws + L.out[0], ws + L.out[1]};
     FfProduct p{};
     p.segs = 1;
-    p.A0 = b->X; p.lda = b->ldx;
-    p.B0 = dG; p.B1 = dU; p.ldb = L.ldd;
+    p.A0 = X.at; p.lda = X.ld; p.a_filled = X.filled;
+    p.B0 = dG; p.B1 = dU; p.ldb = L.ldd; p.b_filled = true;
     p.M = b->n; p.N = ch.m; p.K = b->tokens;
-    p.filled = true;
     p.C0 = pack ? packed[0] : dWg; p.C1 = pack ? packed[1] : dWu; p.ldc = pack ? L.ldd : lddw;
     p.kept = ch.kept;
     ff_product<T, false, false, true, FF_STORE>(p, ws + L.partial, stream);
