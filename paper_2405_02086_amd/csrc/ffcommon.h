@@ -45,7 +45,7 @@ struct FfProduct {
   long long ldg, ldh;
   const unsigned char* keep;   // one byte per column of the result, or null
   const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
-  float* partial;              // PARTIAL: [splits][products][M][N]
+  float* partial;              // PARTIAL: [splits][products][M][N in whole quads]
   int splits;
 };
 
@@ -153,16 +153,11 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
   const bool whole = col + 4 <= N;
   const int count = whole ? 4 : (int)(N - col);
   if constexpr (EPI == FF_PARTIAL) {
-    float* at = p.partial + ((long long)blockIdx.y * (DUAL ? 2 : 1) * p.M + row) * p.N + col;
-    if (whole) {
-      ff_store4(at, v0);
-      if constexpr (DUAL) ff_store4(at + p.M * p.N, v1);
-    } else {
-      for (int i = 0; i < count; i++) {
-        at[i] = v0[i];
-        if constexpr (DUAL) at[p.M * p.N + i] = v1[i];
-      }
-    }
+    // (rows of whole quads: what lies past N is written and never read)
+    const long long ld = (p.N + 3) / 4 * 4, plane = p.M * ld;
+    float* at = p.partial + (long long)blockIdx.y * (DUAL ? 2 : 1) * plane + row * ld + col;
+    ff_store4(at, v0);
+    if constexpr (DUAL) ff_store4(at + plane, v1);
     return;
   }
   f32x4 o0 = v0, o1 = v1;
@@ -178,11 +173,11 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
         o1[i] = (float)d.v[i] * value[i];
       }
     }
-    if (p.keep) {
+  }
+  if (p.keep) {
 #pragma unroll
-      for (int i = 0; i < 4; i++)
-        if (i < count && !p.keep[col + i]) o0[i] = o1[i] = v0[i] = v1[i] = 0.0f;
-    }
+    for (int i = 0; i < 4; i++)
+      if (i < count && !p.keep[col + i]) o0[i] = o1[i] = v0[i] = v1[i] = 0.0f;
   }
   T* c0 = static_cast<T*>(p.C0) + row * p.ldc + col;
   T* c1 = (DUAL && EPI != FF_FWD) ? static_cast<T*>(p.C1) + row * p.ldc + col : nullptr;

@@ -202,35 +202,41 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
   }
 }
 
-// Joins the shares of K: sums the partial products in their order and finishes them.
-template <typename T, bool DUAL, int EPI>
+// Joins the shares of K: sums the partial products in their order and finishes them.  GROUPS threads share a quad's sum where
+// the shares are many and the quads few, each a run of shares; their sums are added in order.
+template <typename T, bool DUAL, int EPI, int GROUPS>
 __global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p) {
-  const long long quads = (p.N + 3) / 4, plane = p.M * p.N;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= quads * p.M) return;
+  constexpr int QUADS = 256 / GROUPS, PLANES = DUAL ? 2 : 1;
+  __shared__ f32x4 sums[GROUPS > 1 ? GROUPS : 1][PLANES][QUADS];
+  const long long quads = (p.N + 3) / 4, plane = p.M * quads * 4;
+  const int in = threadIdx.x % QUADS, group = threadIdx.x / QUADS;
+  const long long i = (long long)blockIdx.x * QUADS + in;
   const long long row = i / quads, col = i % quads * 4;
   const long long N = p.kept && DUAL ? *p.kept : p.N;
-  if (col >= N) return;
-  f32x4 v0 = {}, v1 = {};
-  const float* at = p.partial + row * p.N + col;
-  constexpr int PLANES = DUAL ? 2 : 1;
-  if (col + 4 <= p.N) {
+  const bool there = i < quads * p.M && col < N;
+  f32x4 v[2] = {};
+  if (there) {
+    const float* at = p.partial + i * 4;
+    const int last = p.splits * (group + 1) / GROUPS;
 #pragma unroll 8
-    for (int s = 0; s < p.splits; s++) {
-      v0 += ff_load4(at + s * PLANES * plane);
-      if constexpr (DUAL) v1 += ff_load4(at + (s * PLANES + 1) * plane);
-    }
-  } else {
-    for (int c = 0; c < p.N - col; c++)
-#pragma unroll 8
-      for (int s = 0; s < p.splits; s++) {
-        v0[c] += at[s * PLANES * plane + c];
-        if constexpr (DUAL) v1[c] += at[(s * PLANES + 1) * plane + c];
-      }
+    for (int s = p.splits * group / GROUPS; s < last; s++)
+#pragma unroll
+      for (int k = 0; k < PLANES; k++) v[k] += ff_load4(at + (s * PLANES + k) * plane);
   }
+  if constexpr (GROUPS > 1) {
+#pragma unroll
+    for (int k = 0; k < PLANES; k++) sums[group][k][in] = v[k];
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; g++)
+#pragma unroll
+      for (int k = 0; k < PLANES; k++) v[k] += sums[g][k][in];
+  }
+  if (!there) return;
   FfVec4<T> d = {};
   if constexpr (EPI == FF_GRAD) d = ff_upstream<T>(p, row, col, N);
-  ff_finish<EPI, DUAL, T>(p, row, col, N, v0, v1, d);
+  ff_finish<EPI, DUAL, T>(p, row, col, N, v[0], v[1], d);
 }
 
 }  // namespace mlproj

@@ -11,9 +11,6 @@ namespace mlproj {
 namespace {
 
 constexpr long long FF_MAX_DIM = 1LL << 30;
-// A masked forward call of more tokens than this packs its kept channels first; fewer read every weight once
-// anyway, which is all that packing would do.
-constexpr long long FF_PACK_TOKENS = 64;
 // fp32 forward products of at most this many tokens go without tiles (ffskinny.h).
 constexpr long long FK_TOKENS = 32;
 
@@ -30,13 +27,13 @@ struct FfPlan {
   int splits;
   double us;
 };
-// (forward: A's rows and B's columns run along memory, as in the forward product)
 struct FfKind {
   int rows, cols, places;      // of the tile; workgroups per compute unit
-  double step_us, tile_us;
+  double step_us, tile_us[4];  // by epilogue
 };
-static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool forward, bool direct, int es) {
-  static const FfKind kinds[4] = {{256, 256, 1, 0.86, 9.0}, {128, 128, 2, 0.53, 5.0}, {128, 128, 3, 2.0, 5.0}, {128, 128, 2, 3.1, 5.0}};
+static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int epi, bool direct, int es) {
+  static const FfKind kinds[4] = {{256, 256, 1, 0.78, {12, 14, 24, 12}}, {128, 128, 2, 0.53, {5, 6, 8, 5}}, {128, 128, 3, 2.0, {5, 6, 8, 5}}, {128, 128, 2, 3.1, {5, 6, 8, 5}}};
+  const bool forward = epi == FF_FWD || epi == FF_GRAD;
   if (es == 4 && forward && M <= FK_TOKENS) {
     // shares until there are two workgroups per compute unit or a wavefront has one step left
     int splits = 1;
@@ -55,35 +52,45 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, bool
       // workgroups in turn on the fullest place; a direct tile beside an empty place is faster
       const double turns = ff_cdiv((long long)groups, (long long)units);
       const double share = groups < units / 2 && kind == 1 ? 0.65 : 1.0;
-      double us = turns * ((double)ff_cdiv(steps, splits) * k.step_us * share + k.tile_us);
-      if (splits > 1) us += 4.0 + 0.3 * splits + planes * (splits + splits) / 4.0e6;
+      double us = turns * ((double)ff_cdiv(steps, splits) * k.step_us * share + k.tile_us[splits > 1 ? FF_PARTIAL : epi]);
+      if (splits > 1) us += 4.0 + 0.05 * splits + planes * (splits + splits) / 4.0e6;
       if (us < best.us) best = {kind, splits, us};
     }
   }
   return best;
 }
 static long long ff_steps(long long K, int segs) { return ff_cdiv(K, 32) * segs; }
-static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, bool forward, int es) {
+static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, int epi, int es) {
   size_t most = 0;
   for (int direct = 0; direct < 2; direct++) {
-    const FfPlan plan = ff_plan(M, N, ff_steps(K, segs), dual, forward, direct, es);
-    const size_t bytes = plan.splits > 1 ? (size_t)plan.splits * (dual ? 2 : 1) * M * N * 4 : 0;
+    const FfPlan plan = ff_plan(M, N, ff_steps(K, segs), dual, epi, direct, es);
+    const size_t bytes = plan.splits > 1 ? (size_t)plan.splits * (dual ? 2 : 1) * M * (ff_cdiv(N, 4) * 4) * 4 : 0;
     if (bytes > most) most = bytes;
   }
   return most;
 }
 
+// What a call's products take, all of them, by the plan.
+static double ff_products_us(int es, long long tokens, long long n, long long m, bool backward, bool direct) {
+  double us = ff_plan(tokens, m, ff_steps(n, 1), true, backward ? FF_GRAD : FF_FWD, direct, es).us;
+  if (backward) us += ff_plan(tokens, n, ff_steps(m, 2), false, FF_STORE, direct, es).us + ff_plan(n, m, ff_steps(tokens, 1), true, FF_STORE, direct, es).us;
+  return us;
+}
 // Whether 16-bit operands whose rows are not in whole 16-byte pieces are copied into rows that are (ff_pad_kernel), for
 // the direct tiles: where that is cheaper than the staged tiles by the plan.  Copies go at 4 TB/s, read and written.
 static bool ff_pads(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
   if (es != 2 || (n % 8 == 0 && (m % 8 == 0 || masked))) return false;
-  auto us = [&](bool direct) {
-    double t = ff_plan(tokens, m, ff_steps(n, 1), true, true, direct, es).us;
-    if (backward) t += ff_plan(tokens, n, ff_steps(m, 2), false, false, direct, es).us + ff_plan(n, m, ff_steps(tokens, 1), true, false, direct, es).us;
-    return t;
-  };
   const double elements = (double)tokens * n + (masked ? 0.0 : 2.0 * n * m);
-  return us(true) + 5.0 + elements * 2 * es / 4.0e6 < us(false);
+  return ff_products_us(es, tokens, n, m, backward, true) + 5.0 + elements * 2 * es / 4.0e6 < ff_products_us(es, tokens, n, m, backward, false);
+}
+// Whether a masked call packs its kept channels: where half of its products (the host does not know how many were kept) take
+// longer than moving weights, planes and results, and the launches that does.  Otherwise pruned channels are computed
+// and replaced by zeros (backward: the weights' too, in a copy).
+static bool ff_packs(int es, long long tokens, long long n, long long m, bool backward) {
+  const double weights = 2.0 * n * m * es, plane = (double)tokens * m * es;
+  const double moves = backward ? 25.0 + (1.5 * weights + 1.5 * plane + 1.5 * weights) / 4.0e6 - (5.0 + 2.0 * weights / 4.0e6)
+                                : 20.0 + (1.5 * weights + 2.0 * plane) / 4.0e6;
+  return 0.5 * ff_products_us(es, tokens, n, m, backward, es == 2) > moves;
 }
 
 // ------------------------------------------------------------------ workspace
@@ -94,10 +101,13 @@ struct FfLayout {
   size_t partial;              // shares of sums, of one product at a time
   size_t dG, dU;               // backward: gradients at the pre-activations, tokens x ldd
   size_t position, kept, W[2], in[3], out[3];   // masked: where the channels went; packed weights, inputs and results
-  size_t bytes;                // a workspace for masked calls serves the others too
+  size_t bytes;
   bool pads;
 };
-FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
+// How a call deals with its mask: it has none, zeros in the epilogue (backward: and in a copy of the weights), packed channels.
+enum FfMask { MASK_NONE, MASK_EPILOGUE, MASK_PACK };
+FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool backward, FfMask masked) {
+  const bool packed = masked == MASK_PACK, cleaned = masked == MASK_EPILOGUE && backward;
   FfLayout L{};
   size_t o = 0;
   auto take = [&](size_t bytes) {
@@ -108,10 +118,10 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
   L.ldd = ff_cdiv(m, 8) * 8;
   L.ldn = ff_cdiv(n, 8) * 8;
   // (the packed channels' products run over ldd of them)
-  const long long widest = masked ? L.ldd : m;
-  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, true, es);
+  const long long widest = packed ? L.ldd : m;
+  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, backward ? FF_GRAD : FF_FWD, es);
   if (backward) {
-    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, false, es), w = ff_partial_bytes(n, widest, tokens, 1, true, false, es);
+    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, FF_STORE, es), w = ff_partial_bytes(n, widest, tokens, 1, true, FF_STORE, es);
     shares = shares > x ? shares : x;
     shares = shares > w ? shares : w;
   }
@@ -121,11 +131,11 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
     L.dG = take(plane);
     L.dU = take(plane);
   }
-  L.pads = ff_pads(es, tokens, n, m, backward, masked);
+  L.pads = ff_pads(es, tokens, n, m, backward, packed);
   if (L.pads) L.X = take((size_t)tokens * L.ldn * es);
-  if (L.pads || masked)
+  if (L.pads || packed || cleaned)
     for (size_t& w : L.W) w = take(weights);
-  if (masked) {
+  if (packed) {
     L.position = take((size_t)(m + 1) * 4);
     L.kept = take(4);
     if (backward)
@@ -133,11 +143,11 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
     for (int i = 0; i < (backward ? 2 : 3); i++) L.out[i] = take(backward ? weights : plane);
   }
   L.bytes = o + 256;
-  if (masked) {
-    const size_t plain = ff_layout(es, tokens, n, m, backward, false).bytes;
-    L.bytes = L.bytes > plain ? L.bytes : plain;
-  }
   return L;
+}
+
+static FfMask ff_mask(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
+  return !masked ? MASK_NONE : ff_packs(es, tokens, n, m, backward) ? MASK_PACK : MASK_EPILOGUE;
 }
 
 // ------------------------------------------------------------------ launches
@@ -182,7 +192,7 @@ void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_product(FfProduct p, void* partial, hipStream_t stream) {
   if (p.M == 0) return;
-  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, A_KC && !B_KC, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
+  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, EPI, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
   p.splits = plan.splits;
   p.partial = static_cast<float*>(partial);
   if (p.splits == 1) {
@@ -191,7 +201,9 @@ void ff_product(FfProduct p, void* partial, hipStream_t stream) {
   }
   ff_launch<T, A_KC, B_KC, DUAL, FF_PARTIAL>(p, plan.kind, stream);
   mark(stream);
-  launch(ff_join_kernel<T, DUAL, EPI>, dim3((unsigned)ff_cdiv(ff_cdiv(p.N, 4) * p.M, 256)), dim3(256), stream, p);
+  const long long quads = ff_cdiv(p.N, 4) * p.M;
+  if (p.splits >= 16) launch(ff_join_kernel<T, DUAL, EPI, 8>, dim3((unsigned)ff_cdiv(quads, 32)), dim3(256), stream, p);
+  else launch(ff_join_kernel<T, DUAL, EPI, 1>, dim3((unsigned)ff_cdiv(quads, 256)), dim3(256), stream, p);
 }
 
 // dG and dU from saved pre-activations.
@@ -273,6 +285,7 @@ struct FfPad {
   void* to[5];
   long long ld_from[5], ld_to[5], rows[5], cols[5];
   long long first[5];          // number of the first thread of a matrix
+  const unsigned char* mask[5];  // columns to be replaced by zeros, or null
   int count;
 };
 template <typename T>
@@ -286,14 +299,19 @@ __global__ __launch_bounds__(256) void ff_pad_kernel(FfPad a) {
   if (row >= a.rows[i]) return;
   FfVec8<T> v = {};
   if (a.from[i]) v = ff_load8(static_cast<const T*>(a.from[i]) + row * a.ld_from[i] + col, a.cols[i] - col);
+  if (a.mask[i])
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+      if (col + j < a.cols[i] && !a.mask[i][col + j]) v.v[j] = (T)0.0f;
   __builtin_memcpy(static_cast<T*>(a.to[i]) + row * a.ld_to[i] + col, &v, sizeof(v));
 }
 struct FfPadder {
   FfPad a{};
   long long threads = 0;
-  void add(const void* from, long long ld_from, void* to, long long ld_to, long long rows, long long cols) {
+  void add(const void* from, long long ld_from, void* to, long long ld_to, long long rows, long long cols, const unsigned char* mask = nullptr) {
     const int i = a.count++;
     a.from[i] = from; a.ld_from[i] = ld_from; a.to[i] = to; a.ld_to[i] = ld_to; a.rows[i] = rows; a.cols[i] = cols;
+    a.mask[i] = mask;
     a.first[i] = threads;
     threads += rows * (from ? ld_to / 8 : 1);
   }
@@ -325,24 +343,24 @@ FfChannels ff_channels(const mlproj_gated_block* b, const FfLayout& L, char* ws,
   return c;
 }
 
-// X, and copies of it and of the weights where the plan pads (weights: unless they are packed anyway, or not read).
+// X, and copies: of X where the plan pads; of the weights where it pads (unless they are packed anyway, or not read), or where
+// pruned columns have to be zeros (`clean`).
 struct FfInput {
   const void* at;
   long long ld;
   bool filled;
 };
 template <typename T>
-FfInput ff_input(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, bool weights, FfChannels& ch, hipStream_t stream) {
+FfInput ff_input(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool pack, bool weights, bool clean, FfChannels& ch, hipStream_t stream) {
   FfInput X{b->X, b->ldx, false};
-  if (!L.pads) return X;
   FfPadder pad;
-  if (b->n % 8) {
+  if (L.pads && b->n % 8) {
     pad.add(b->X, b->ldx, ws + L.X, L.ldn, b->tokens, b->n);
     X = {ws + L.X, L.ldn, true};
   }
-  if (!pack && weights) {
-    pad.add(b->Wg, b->ldw, ws + L.W[0], L.ldd, b->n, b->m);
-    pad.add(b->Wu, b->ldw, ws + L.W[1], L.ldd, b->n, b->m);
+  if (!pack && weights && (L.pads || clean)) {
+    pad.add(b->Wg, b->ldw, ws + L.W[0], L.ldd, b->n, b->m, clean ? b->mask : nullptr);
+    pad.add(b->Wu, b->ldw, ws + L.W[1], L.ldd, b->n, b->m, clean ? b->mask : nullptr);
     ch.Wg = ws + L.W[0]; ch.Wu = ws + L.W[1]; ch.ldw = L.ldd; ch.filled = true;
     if (L.dU && b->m % 8) {      // dG and dU are summed over as well: whole pieces there too
       pad.add(nullptr, 0, ws + L.dG, L.ldd, b->tokens, 0);
@@ -356,8 +374,9 @@ FfInput ff_input(const mlproj_gated_block* b, const FfLayout& L, char* ws, bool 
 template <typename T>
 int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, void* G, void* U, long long ldg,
                 void* workspace, hipStream_t stream) {
-  const bool pack = b->mask && b->tokens > FF_PACK_TOKENS;
-  const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, false, pack);
+  const FfMask masked = ff_mask(sizeof(T), b->tokens, b->n, b->m, false, b->mask != nullptr);
+  const bool pack = masked == MASK_PACK;
+  const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, false, masked);
   char* ws = static_cast<char*>(workspace);
   FfChannels ch = ff_channels(b, L, ws, pack, stream);
   if (pack) {
@@ -366,7 +385,7 @@ int run_forward(int act, const mlproj_gated_block* b, void* H, long long ldh, vo
     in.add(b->Wu, b->ldw, ws + L.W[1], L.ldd, b->n);
     in.go(stream);
   }
-  const FfInput X = ff_input<T>(b, L, ws, pack, true, ch, stream);
+  const FfInput X = ff_input<T>(b, L, ws, pack, true, false, ch, stream);
   FfProduct p{};
   p.segs = 1; p.act = act;
   p.A0 = X.at; p.lda = X.ld; p.a_filled = X.filled;
@@ -407,8 +426,9 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     mark(stream);
     return launch_status();
   }
-  const bool pack = b->mask != nullptr;
-  const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, true, pack);
+  const FfMask masked = ff_mask(sizeof(T), b->tokens, b->n, b->m, true, b->mask != nullptr);
+  const bool pack = masked == MASK_PACK, clean = masked == MASK_EPILOGUE && dX;
+  const FfLayout L = ff_layout(sizeof(T), b->tokens, b->n, b->m, true, masked);
   char* ws = static_cast<char*>(workspace);
   FfChannels ch = ff_channels(b, L, ws, pack, stream);
   if (pack) {
@@ -429,7 +449,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     planes.go(stream);
     dH = in[0]; ldh = L.ldd;
   }
-  const FfInput X = ff_input<T>(b, L, ws, pack, dX || !G, ch, stream);
+  const FfInput X = ff_input<T>(b, L, ws, pack, dX || !G, clean, ch, stream);
   T *dG = reinterpret_cast<T*>(ws + L.dG), *dU = reinterpret_cast<T*>(ws + L.dU);
   {
     FfProduct p{};
@@ -438,6 +458,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.C0 = dG; p.C1 = dU; p.ldc = L.ldd;
     p.dH = dH; p.ldh = ldh;
     p.kept = ch.kept;
+    p.keep = pack ? nullptr : b->mask;
     if (G) {
       p.G = const_cast<void*>(G); p.U = const_cast<void*>(U); p.ldg = ldg;
       mark(stream);
@@ -465,6 +486,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     p.A0 = X.at; p.lda = X.ld; p.a_filled = X.filled;
     p.B0 = dG; p.B1 = dU; p.ldb = L.ldd; p.b_filled = true;
     p.M = b->n; p.N = ch.m; p.K = b->tokens;
+    p.keep = pack ? nullptr : b->mask;
     p.C0 = pack ? packed[0] : dWg; p.C1 = pack ? packed[1] : dWu; p.ldc = pack ? L.ldd : lddw;
     p.kept = ch.kept;
     ff_product<T, false, false, true, FF_STORE>(p, ws + L.partial, stream);
@@ -484,7 +506,12 @@ int ff_workspace(int storage, long long tokens, long long n, long long m, int ba
   if (storage < MLPROJ_STORE_F32 || storage > MLPROJ_STORE_F16) return MLPROJ_ERR_BAD_VARIANT;
   if (tokens < 0 || n <= 0 || m <= 0 || (backward | 1) != 1 || (masked | 1) != 1) return MLPROJ_ERR_BAD_DIMENSION;
   if (tokens > FF_MAX_DIM || n > FF_MAX_DIM || m > FF_MAX_DIM || tokens * m > (1LL << 38) || tokens * n > (1LL << 38) || n * m > (1LL << 38)) return MLPROJ_ERR_TOO_LARGE;
-  *out = ff_layout(storage == MLPROJ_STORE_F32 ? 4 : 2, tokens, n, m, backward != 0, masked != 0).bytes;
+  const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
+  *out = ff_layout(es, tokens, n, m, backward != 0, MASK_NONE).bytes;
+  if (masked) {      // serves calls without a mask as well
+    const size_t with = ff_layout(es, tokens, n, m, backward != 0, ff_mask(es, tokens, n, m, backward != 0, true)).bytes;
+    *out = *out > with ? *out : with;
+  }
   return MLPROJ_OK;
 }
 
