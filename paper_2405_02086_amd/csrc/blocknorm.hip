@@ -401,7 +401,7 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
 //   mean(r e), mean(r^2), mean(b^2), and the three parts of sum(b f dx), dx = dr + rr e - r rr^3 mean(r e):
 //   sum(b f dr), sum(b f e), sum(b f r).
 // A worker (a row's threads) takes every workers-th row and keeps the sums over its rows of the columns its threads
-// hold, which go out as one partial per worker and are summed, in their order, by bn_columns_kernel: the same bits
+// hold, which go out as one partial per workgroup and are summed, in their order, by bn_columns_kernel: the same bits
 // every time.  With one gate per channel dgate and dw_post are both multiples of sum dx b / rms(b).
 template <typename T, int THREADS, int CH, bool AHEAD, bool TOKEN_GATE>
 __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a) {
@@ -511,8 +511,29 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
     }
     if (!AHEAD && row + workers < a.tokens) fetch(row + workers);
   }
-  float* partial = a.partial + worker * n;
-  const long long plane = workers * n;
+  float* partial = a.partial + blockIdx.x * n;
+  const long long plane = gridDim.x * n;
+  if constexpr (ROWS > 1) {
+    // the workgroup's workers first, in their order
+    __shared__ float rows[2][ROWS][CH * VEC * THREADS];
+#pragma unroll
+    for (int c = 0; c < CH; c++)
+#pragma unroll
+      for (int i = 0; i < VEC; i++) {
+        const int at = (c * THREADS + t) * VEC + i;
+        rows[0][threadIdx.x / THREADS][at] = s_post[c][i];
+        rows[1][threadIdx.x / THREADS][at] = s_pre[c][i];
+      }
+    __syncthreads();
+    for (int j = threadIdx.x; j < n; j += 256) {
+      float post = 0.0f, own = 0.0f;
+#pragma unroll
+      for (int r = 0; r < ROWS; r++) { post += rows[0][r][j]; own += rows[1][r][j]; }
+      if (a.want_post || a.want_gate) partial[j] = post;
+      if (a.want_pre) partial[plane + j] = own;
+    }
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < CH; c++) {
     const long long at = ((long long)c * THREADS + t) * VEC;
@@ -528,7 +549,7 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
   }
 }
 
-// The sums over workers: 32 columns x 32 groups of workers per workgroup, joined in LDS in a fixed order.
+// The sums over workgroups: 32 columns x 32 groups of them per workgroup here, joined in LDS in a fixed order.
 template <typename T>
 __global__ __launch_bounds__(1024) void bn_columns_kernel(BnArgs a, int workers, bool token_gate, float* dw_post, float* dgate, float* dw_pre) {
   __shared__ float part[2][32][33];
@@ -631,7 +652,7 @@ int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate,
     }
     if (a.want_post || a.want_gate || a.want_pre) {
       mark(stream);
-      launch(bn_columns_kernel<T>, dim3((unsigned)((a.n + 31) / 32)), dim3(1024), stream, a, (int)groups * BN_ROWS<th.value>, token_gate,
+      launch(bn_columns_kernel<T>, dim3((unsigned)((a.n + 31) / 32)), dim3(1024), stream, a, (int)groups, token_gate,
              dw_post, dgate, dw_pre);
     }
   });
@@ -678,15 +699,15 @@ BnArgs bn_start(const mlproj_norm_block* k) {
 }
 
 size_t bn_workspace(long long tokens, long long n) {
-  // the most workers any storage type has: a row takes at least the threads of its 16-bit form
-  long long workers = 1;
+  // the most workgroups any storage type has
+  long long most = 1;
   auto count = [&](auto th, auto, auto) {
-    const long long w = bn_groups(th.value, tokens) * BN_ROWS<th.value>;
-    workers = w > workers ? w : workers;
+    const long long groups = bn_groups(th.value, tokens);
+    most = groups > most ? groups : most;
   };
   bn_shape<bf16_t>(n, count);
   bn_shape<float>(n, count);
-  return (size_t)workers * n * 2 * sizeof(float) + 256;
+  return (size_t)most * n * 2 * sizeof(float) + 256;
 }
 
 }  // namespace

@@ -69,7 +69,7 @@ struct FcArrays {
 // caller's (PACK), or the caller's out of packed ones with zeros where a channel was pruned.  Both sides of memory see
 // whole 16-byte pieces of consecutive columns; the single elements are picked from LDS.  Bound by HBM: 4096 x 16384 bf16
 // at 40 % kept, two matrices, 375 MB.
-constexpr int FC_COLS = 2048, FC_ROWS = 4;
+constexpr int FC_COLS = 2048, FC_ROWS = 4, FC_GROUPS = 1024;
 template <typename T, bool PACK>
 __global__ __launch_bounds__(256) void ff_move_kernel(FcArrays a) {
   __shared__ T held[FC_ROWS][FC_COLS + 8];
@@ -100,16 +100,18 @@ __global__ __launch_bounds__(256) void ff_move_kernel(FcArrays a) {
   int pick[8];
 #pragma unroll
   for (int i = 0; i < 8; i++) pick[i] = PACK ? (t8 + i < packed ? source[t8 + i] : -1) : place[i];
-  for (long long r0 = (long long)group * FC_ROWS; r0 < rows; r0 += (long long)a.groups[which] * FC_ROWS) {
-    FfVec8<T> v[FC_ROWS];
+  FfVec8<T> v[FC_ROWS];
+  auto fetch = [&](long long r0) {
 #pragma unroll
-    for (int r = 0; r < FC_ROWS; r++) {
-      const long long left = r0 + r < rows ? in - t8 : 0;
-      v[r] = ff_load8(from + (r0 + r) * ld_from + t8, left);
-    }
+    for (int r = 0; r < FC_ROWS; r++) v[r] = ff_load8(from + (r0 + r) * ld_from + t8, r0 + r < rows ? in - t8 : 0);
+  };
+  const long long stride = (long long)a.groups[which] * FC_ROWS;
+  fetch((long long)group * FC_ROWS);
+  for (long long r0 = (long long)group * FC_ROWS; r0 < rows; r0 += stride) {
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < FC_ROWS; r++) *reinterpret_cast<FfVec8<T>*>(&held[r][t8]) = v[r];
+    if (r0 + stride < rows) fetch(r0 + stride);
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < FC_ROWS; r++) {

@@ -88,8 +88,8 @@ static bool ff_pads(int es, long long tokens, long long n, long long m, bool bac
 // and replaced by zeros (backward: the weights' too, in a copy).
 static bool ff_packs(int es, long long tokens, long long n, long long m, bool backward) {
   const double weights = 2.0 * n * m * es, plane = (double)tokens * m * es;
-  const double moves = backward ? 25.0 + (1.5 * weights + 1.5 * plane + 1.5 * weights) / 4.0e6 - (5.0 + 2.0 * weights / 4.0e6)
-                                : 20.0 + (1.5 * weights + 2.0 * plane) / 4.0e6;
+  const double moves = backward ? 45.0 + (1.5 * weights + 1.5 * plane + 1.5 * weights) / 4.0e6 - (5.0 + 2.0 * weights / 4.0e6)
+                                : 28.0 + (1.5 * weights + 2.0 * plane) / 4.0e6;
   return 0.5 * ff_products_us(es, tokens, n, m, backward, es == 2) > moves;
 }
 
@@ -267,12 +267,18 @@ struct FfMove {
   void add(const void* from, long long ld_from, void* to, long long ld_to, long long rows) {
     const int i = a.count++;
     a.from[i] = from; a.ld_from[i] = ld_from; a.to[i] = to; a.ld_to[i] = ld_to; a.rows[i] = rows;
-    const long long groups = ff_cdiv(rows, FC_ROWS);
-    a.groups[i] = (int)(groups < 4096 ? groups : 4096);
   }
   void go(hipStream_t stream) {
+    // about four workgroups per compute unit: each reads its columns' places once, for many rows
+    const long long segments = ff_cdiv(a.cols, FC_COLS);
+    long long most = FC_GROUPS / (segments * a.count);
+    if (most < 1) most = 1;
     int groups = 0;
-    for (int i = 0; i < a.count; i++) groups += a.groups[i];
+    for (int i = 0; i < a.count; i++) {
+      const long long all = ff_cdiv(a.rows[i], FC_ROWS);
+      a.groups[i] = (int)(all < most ? all : most);
+      groups += a.groups[i];
+    }
     mark(stream);
     launch(ff_move_kernel<T, PACK>, dim3((unsigned)ff_cdiv(a.cols, FC_COLS), (unsigned)groups), dim3(256), stream, a);
   }
