@@ -25,6 +25,7 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 //   FWD      C0 = keep * act(G) * U; G and U too where the caller wants them
 //   GRAD     C0 = keep * act'(G) * U * dH, C1 = keep * act(G) * dH
 //   PARTIAL  the sums over this workgroup's share of K, in fp32, for the join kernel
+enum : int { FF_WHOLE = 0, FF_TURNS = 1, FF_REST = 2 };
 enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3 };
 
 // One product C = A B (M x N, summed over K), or two that share A: C0 = A B0, C1 = A B1.
@@ -47,6 +48,7 @@ struct FfProduct {
   const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
   float* partial;              // PARTIAL: [splits][products][M][N in whole quads]
   int splits;
+  int part;                    // direct tiles: FF_WHOLE, or a product shared between two launches (ffdirect.h)
 };
 
 // ------------------------------------------------------------------ elements

@@ -26,6 +26,7 @@ struct FfPlan {
   int kind;      // 0: direct 256, 1: direct 128, 2: staged, 3: few tokens
   int splits;
   double us;
+  bool parts;    // direct 256: whole turns, and the rest in smaller tiles
 };
 struct FfKind {
   int rows, cols, places;      // of the tile; workgroups per compute unit
@@ -39,9 +40,9 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int 
     int splits = 1;
     const long long groups = ff_cdiv(N, FK_COLS) * ff_cdiv(M, 16);
     while (groups * splits < 512 && steps > FK_WAVES * splits && splits < 64) splits *= 2;
-    return {3, splits, 0.0};
+    return {3, splits, 0.0, false};
   }
-  FfPlan best{2, 1, 1e30};
+  FfPlan best{2, 1, 1e30, false};
   for (int kind = direct ? 0 : 2; kind <= (direct ? 1 : 2); kind++) {
     const FfKind& k = kinds[kind == 2 && es == 4 ? 3 : kind];
     const long long tiles = ff_cdiv(M, k.rows) * ff_cdiv(N, dual ? k.cols / 2 : k.cols);
@@ -54,7 +55,14 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int 
       const double share = groups < units / 2 && kind == 1 ? 0.65 : 1.0;
       double us = turns * ((double)ff_cdiv(steps, splits) * k.step_us * share + k.tile_us[splits > 1 ? FF_PARTIAL : epi]);
       if (splits > 1) us += 4.0 + 0.05 * splits + planes * (splits + splits) / 4.0e6;
-      if (us < best.us) best = {kind, splits, us};
+      if (us < best.us) best = {kind, splits, us, false};
+      if (kind == 0 && splits == 1 && tiles > 256) {
+        const FfKind& small = kinds[1];
+        const long long rest = tiles % 256 * 4;
+        const double in_parts = tiles / 256 * (steps * k.step_us + k.tile_us[epi]) + 4.0 +
+                                ff_cdiv(rest, 512) * (steps * small.step_us * (rest < 256 ? 0.65 : 1.0) + small.tile_us[epi]);
+        if (in_parts < best.us) best = {0, 1, in_parts, true};
+      }
     }
   }
   return best;
@@ -181,7 +189,7 @@ void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
       return;
     }
     if (kind == 1) {
-      const long long tiles = ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
+      const long long tiles = p.part == FF_REST ? 4 * (FD_TURN - 1) : ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
       launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)tiles, p.splits), dim3(256), stream, p);
       return;
     }
@@ -195,6 +203,14 @@ void ff_product(FfProduct p, void* partial, hipStream_t stream) {
   const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, EPI, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
   p.splits = plan.splits;
   p.partial = static_cast<float*>(partial);
+  // (packed channels: how many tiles there will be is not known here, so both launches go out wherever they are many)
+  if (plan.kind == 0 && p.splits == 1 && (plan.parts || (p.kept && DUAL && ff_cdiv(p.M, 256) * ff_cdiv(p.N, 128) > 256))) {
+    p.part = FF_TURNS;
+    ff_launch<T, A_KC, B_KC, DUAL, EPI>(p, 0, stream);
+    p.part = FF_REST;
+    ff_launch<T, A_KC, B_KC, DUAL, EPI>(p, 1, stream);
+    return;
+  }
   if (p.splits == 1) {
     ff_launch<T, A_KC, B_KC, DUAL, EPI>(p, plan.kind, stream);
     return;
