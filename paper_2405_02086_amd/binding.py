@@ -131,6 +131,8 @@ def lib():
     block, norm, w4 = ctypes.POINTER(GatedBlock), ctypes.POINTER(NormBlock), ctypes.POINTER(PackedW4)
     L.mlproj_gated_ff_workspace_bytes.restype = c_i
     L.mlproj_gated_ff_workspace_bytes.argtypes = [c_i, c_ll, c_ll, c_ll, c_i, c_i, ctypes.POINTER(c_sz)]
+    L.mlproj_gated_ff_route.restype = c_i
+    L.mlproj_gated_ff_route.argtypes = [c_i, c_i, c_ll, c_ll, c_ll]
     L.gated_ff_forward.restype = c_i
     L.gated_ff_forward.argtypes = [c_i, c_i, block, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_sz, c_vp]
     L.gated_ff_backward.restype = c_i
@@ -189,7 +191,7 @@ EXPORTS = (
     "bilevel_proj_stored", "bilevel_proj_batch", "trilevel_proj_stored", "mlproj_set_l11_sweeps",
     "multilevel_proj_stored", "bilevel_proj_weighted", "multilevel_proj_weighted", "mlproj_set_search_spin_limit",
     "bilevel_proj_l1inf_no_alloc", "mlproj_stripe_of_workgroup", "mlproj_multilevel_one_pass",
-    "mlproj_gated_ff_workspace_bytes", "gated_ff_forward", "gated_ff_backward",
+    "mlproj_gated_ff_workspace_bytes", "mlproj_gated_ff_route", "gated_ff_forward", "gated_ff_backward",
     "block_norm_forward", "mlproj_block_norm_workspace_bytes", "block_norm_backward",
     "mlproj_w4_bytes", "w4_pack", "w4_matvec", "w4_gated_matvec",
 )
@@ -615,6 +617,14 @@ def gated_ff_workspace_bytes(tokens, n, m, dtype, backward=False, masked=True):
     _check(lib().mlproj_gated_ff_workspace_bytes(_storage(dtype), tokens, n, m, int(backward), int(masked), ctypes.byref(out)),
            "mlproj_gated_ff_workspace_bytes")
     return out.value
+
+
+def gated_ff_route(dtype, product, tokens, n, m):
+    """How a product of a block with aligned rows is computed: {"kind", "packed", "parts", "shares"} (see mlproj.h)."""
+    r = lib().mlproj_gated_ff_route(_storage(dtype), product, tokens, n, m)
+    if r < 0:
+        _check(r, "mlproj_gated_ff_route")
+    return {"kind": r & 15, "packed": bool(r & 16), "parts": bool(r & 32), "shares": r >> 8}
 
 
 def _gated_block(X, Wg, Wu, mask):

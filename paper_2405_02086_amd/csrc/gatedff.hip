@@ -549,6 +549,19 @@ int mlproj_gated_ff_workspace_bytes(int storage, long long tokens, long long n, 
   return ff_workspace(storage, tokens, n, m, backward, masked, bytes_out);
 }
 
+int mlproj_gated_ff_route(int storage, int product, long long tokens, long long n, long long m) {
+  size_t bytes;
+  FF_TRY(ff_workspace(storage, tokens, n, m, 1, 1, &bytes));
+  if (product < 0 || product > 3) return MLPROJ_ERR_BAD_VARIANT;
+  const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
+  const bool direct = es == 2, backward = product > 0;
+  FfPlan plan;
+  if (product < 2) plan = ff_plan(tokens, m, ff_steps(n, 1), true, backward ? FF_GRAD : FF_FWD, direct, es);
+  else if (product == 2) plan = ff_plan(tokens, n, ff_steps(m, 2), false, FF_STORE, direct, es);
+  else plan = ff_plan(n, m, ff_steps(tokens, 1), true, FF_STORE, direct, es);
+  return plan.kind + 16 * ff_packs(es, tokens, n, m, backward) + 32 * plan.parts + 256 * plan.splits;
+}
+
 int gated_ff_forward(int storage, int activation, const mlproj_gated_block* b, void* H, long long ldh, void* G, void* U,
                      long long ldg, void* workspace, size_t workspace_bytes, void* stream) {
   FF_TRY(ff_check(storage, activation, b));

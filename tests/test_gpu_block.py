@@ -451,3 +451,125 @@ def test_w4_larger_and_no_tokens(mp):
         close(mp.w4_matvec(X, W), y, sum_bound(n, dtype) * (np.abs(x) @ np.abs(w)) + stored(y, dtype), "y")
         assert torch.equal(mp.w4_matvec(X, W), mp.w4_matvec(X, W))
     assert mp.w4_matvec(torch.empty(0, 1000, device="cuda"), W).shape == (0, 4100)
+
+
+# ---------------------------------------------------------------- routes, larger sizes, graphs, the example
+
+def blocks_close(got, want, e, what, side=64):
+    """Every side x side block of a result is as near the 64-bit one as two roundings of its entries allow (each at most e
+    of an entry or of the terms it is summed from, whose errors add up as a norm): a tile that went wrong stands out."""
+    got, want = got.double(), want
+    rows, cols = want.shape
+    pad = (-rows % side, -cols % side)
+    def norms(t):
+        t = torch.nn.functional.pad(t, (0, pad[1], 0, pad[0]))
+        return t.view(t.shape[0] // side, side, t.shape[1] // side, side).square().sum((1, 3)).sqrt()
+    off, size = norms(got - want), norms(want)
+    bad = ~(off <= 4 * e * size + 1e-30)
+    assert not bad.any(), "%s: blocks off: %s" % (what, bad.nonzero()[:5].tolist())
+
+
+def exact_block(X, Wg, Wu, dH, act, mask):
+    x, wg, wu = X.double(), Wg.double(), Wu.double()
+    k = mask.double() if mask is not None else 1.0
+    g, u = x @ wg, x @ wu
+    if act == "silu":
+        s = torch.sigmoid(g)
+        a, slope = g * s, s * (1 + g * (1 - s))
+    else:
+        a, slope = torch.relu(g), (g > 0).double()
+    dg, du = dH.double() * u * slope * k, dH.double() * a * k
+    return {"H": a * u * k, "G": g * k, "U": u * k, "dX": dg @ (wg * k).t() + du @ (wu * k).t(), "dWg": x.t() @ dg, "dWu": x.t() @ du}
+
+
+# sizes whose products take: whole turns and a rest of smaller tiles (packed or not), shares of the sum in every kind of tile, ...
+ROUTES = [(4200, 512, 4200, 0, {"kind": 0, "parts": True}), (2100, 2056, 8200, 1, {"kind": 0, "parts": True, "packed": True}),
+          (2304, 2048, 4400, 2, {"kind": 0, "packed": True}), (1100, 2048, 9000, 3, {"kind": 0, "parts": True}),
+          (300, 8192, 64, 1, {"kind": 1}), (1000, 1000, 10000, 2, {"kind": 1}), (2048, 1024, 1536, 0, {"kind": 1, "shares": 1})]
+
+
+@pytest.mark.parametrize("case", range(len(ROUTES)))
+@pytest.mark.parametrize("masked", [False, True])
+def test_gated_ff_routes(mp, case, masked):
+    tokens, n, m, product, route = ROUTES[case]
+    dtype = "bf16" if case % 2 else "f16"
+    got = mp.gated_ff_route(TYPES[dtype], product, tokens, n, m)
+    assert {k: got[k] for k in route} == route
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(40 + case)
+    new = lambda r, c, s=1.0: (torch.randn(r, c, generator=gen, device="cuda") * s).to(TYPES[dtype])  # noqa: E731
+    X, Wg, Wu, dH = new(tokens, n), new(n, m, n ** -0.5), new(n, m, n ** -0.5), new(tokens, m)
+    mask = (torch.rand(m, generator=gen, device="cuda") < 0.55).to(torch.uint8) if masked else None
+    act = ("silu", "relu")[case % 2] if case != 1 else "silu"
+    want = exact_block(X, Wg, Wu, dH, act, mask)
+    G, U = torch.empty(2, tokens, m, dtype=TYPES[dtype], device="cuda")
+    H = mp.gated_ff(X, Wg, Wu, act=act, mask=mask, g_out=G, u_out=U)
+    for name, t in (("H", H), ("G", G), ("U", U)):
+        blocks_close(t, want[name], ROUND[dtype], name)
+    # a relu whose argument rounds to the other side of 0 changes whole entries of its gradient, but only where both are tiny
+    for name, t in zip(("dX", "dWg", "dWu"), mp.gated_ff_backward(dH, X, Wg, Wu, act=act, mask=mask)):
+        blocks_close(t, want[name], ROUND[dtype], name)
+
+
+def test_gated_ff_fp32_larger(mp):
+    for tokens, n, m in ((700, 1000, 1100), (40, 3000, 700), (1500, 264, 2056)):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(tokens)
+        new = lambda r, c, s=1.0: torch.randn(r, c, generator=gen, device="cuda") * s  # noqa: E731
+        X, Wg, Wu, dH = new(tokens, n), new(n, m, n ** -0.5), new(n, m, n ** -0.5), new(tokens, m)
+        for mask in (None, (torch.rand(m, generator=gen, device="cuda") < 0.5).to(torch.uint8)):
+            want = exact_block(X, Wg, Wu, dH, "silu", mask)
+            # fp32 sums of up to 4000 terms: sqrt(4000) roundings of 2^-24 in a random walk, and the function's 16
+            e = 100 * U32
+            blocks_close(mp.gated_ff(X, Wg, Wu, mask=mask), want["H"], e, "H")
+            for name, t in zip(("dX", "dWg", "dWu"), mp.gated_ff_backward(dH, X, Wg, Wu, mask=mask)):
+                blocks_close(t, want[name], e, name)
+
+
+def test_block_calls_can_be_captured_in_a_hip_graph(mp):
+    rng = np.random.default_rng(16)
+    for tokens, n, m, dtype in ((1, 2000, 520, "bf16"), (300, 700, 1000, "bf16"), (20, 300, 200, "f32"), (2100, 1032, 4168, "f16")):
+        X, x, Wg, wg, Wu, wu, mask, dmask = ff_case(mp, rng, tokens, n, m, dtype, 0.5, False)
+        dH, _ = matrix(rng, tokens, m, dtype)
+        w = torch.ones(n, dtype=TYPES[dtype], device="cuda")
+        packed = mp.w4_pack(Wg)
+        H, h4 = torch.empty_like(dH), torch.empty_like(dH)
+        outs = [torch.empty_like(X), torch.empty_like(Wg), torch.empty_like(Wu)]
+        r, y = torch.empty_like(X), torch.empty_like(X)
+        ws = mp.Workspace(mp.gated_ff_workspace_bytes(tokens, n, m, TYPES[dtype], True))
+        wf = mp.Workspace(mp.gated_ff_workspace_bytes(tokens, n, m, TYPES[dtype]))
+
+        def calls():
+            mp.gated_ff(X, Wg, Wu, mask=dmask, H=H, workspace=wf)
+            mp.gated_ff_backward(dH, X, Wg, Wu, mask=dmask, dX=outs[0], dWg=outs[1], dWu=outs[2], workspace=ws)
+            mp.block_norm(X, X, w, w, w, r=r, y=y)
+            mp.w4_gated_matvec(X, packed, packed, h=h4)
+
+        calls()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls()
+        for turn in range(3):
+            X.copy_(matrix(rng, tokens, n, dtype)[0])
+            calls()
+            want = [t.clone() for t in (H, *outs, r, y, h4)]
+            for t in (H, *outs, r, y, h4):
+                t.fill_(3.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(want, (H, *outs, r, y, h4)):
+                assert torch.equal(a, b)
+
+
+def test_the_example_learns_prunes_and_answers_in_four_bits(mp):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "pruned_block.py")
+    spec = importlib.util.spec_from_file_location("pruned_block", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    out = example.main()
+    assert out["last_loss"] < 0.75 * out["first_loss"]
+    assert 0 < out["kept"] < out["channels"]
+    assert out["four_bit_error"] < 0.2
