@@ -76,13 +76,13 @@ class PrunedBlock:
         return mp.block_norm(x, b, w["w_post"], w["gate"], w["w_out"], scale=self.scale)[1]
 
 
-def main(n=256, m=512, relevant=48, tokens=512, steps=60, rate=4.0, seed=0):
+def main(n=256, m=512, relevant=48, tokens=512, steps=60, rate=16.0, radius=0.03, seed=0):
     """Trains; returns what `python examples/pruned_block.py` prints."""
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
     teacher = PrunedBlock(n, m, gen, kept=relevant)
     block = PrunedBlock(n, m, gen)
-    eta = 0.25 * float(block.master["Wg"].abs().amax(0).sum())
+    eta = radius * float(block.master["Wg"].abs().amax(0).sum())
     losses = []
     for _ in range(steps):
         x = torch.randn(tokens, n, generator=gen, device="cuda").to(torch.bfloat16)

@@ -6,9 +6,9 @@ namespace mlproj {
 namespace {
 
 // ------------------------------------------------------------------ rows in registers
-// A row's entries are dealt in 16-byte pieces: piece i of a row belongs to thread i % THREADS of the row's
+// A row's entries are dealt in pieces of 16 bytes (bn_shape has the exception): piece i of a row belongs to thread i % THREADS of the row's
 // threads (16, a wavefront, or a workgroup of 256 or 512), CH of them per thread, and stays in its registers from the
-// one load to the one store.  Loads take any address; the last piece of a row is filled up element by element.
+// one load to the one store.  The last piece of a row is filled up element by element.
 // Both directions are bound by HBM: forward reads x and b and writes r and y once, backward reads four
 // arrays and writes two.  A row group takes many rows: the vectors (weights, a gate per channel) stay in registers
 // too, and the next row's loads go out before the present row is reduced, as far as there are registers for it.
@@ -272,38 +272,46 @@ __global__ __launch_bounds__(BN_LONG) void bn_backward_long_kernel(BnArgs a) {
 }
 
 // ------------------------------------------------------------------ held rows
-// 16 bytes of a row as they lie in memory, zeros past its end; and as numbers.
-template <typename T>
-__device__ __forceinline__ u32x4 bn_raw(const T* p, long long valid) {
-  constexpr int VEC = BN_VEC<T>;
-  u32x4 r;
-  if (valid >= VEC) {
-    __builtin_memcpy(&r, p, 16);
+// A piece is VEC neighbouring entries: 16 bytes, or, where fp32 rows do not start on 16 bytes, a single entry: a
+// wavefront's single entries are neighbours, which the memory system takes at full rate from any start, while
+// unaligned 16-byte accesses go at half.
+// As it lies in memory, zeros past the row's end; and as numbers.
+template <typename T, int VEC> struct BnRaw { using type = u32x4; };
+template <typename T> struct BnRaw<T, 1> { using type = T; };
+template <typename T, int VEC>
+__device__ __forceinline__ typename BnRaw<T, VEC>::type bn_raw(const T* p, long long valid) {
+  if constexpr (VEC == 1) {
+    return valid > 0 ? *p : (T)0.0f;
   } else {
-    T t[VEC];
+    u32x4 r;
+    if (valid >= VEC) {
+      __builtin_memcpy(&r, p, 16);
+    } else {
+      T t[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; i++) t[i] = i < valid ? p[i] : (T)0.0f;
-    __builtin_memcpy(&r, t, 16);
+      for (int i = 0; i < VEC; i++) t[i] = i < valid ? p[i] : (T)0.0f;
+      __builtin_memcpy(&r, t, 16);
+    }
+    return r;
   }
-  return r;
 }
-template <typename T>
-__device__ __forceinline__ void bn_numbers(u32x4 raw, float (&out)[BN_VEC<T>]) {
-  T t[BN_VEC<T>];
-  __builtin_memcpy(t, &raw, 16);
+template <typename T, int VEC>
+__device__ __forceinline__ void bn_numbers(typename BnRaw<T, VEC>::type raw, float (&out)[VEC]) {
+  T t[VEC];
+  __builtin_memcpy(t, &raw, sizeof(t));
 #pragma unroll
-  for (int i = 0; i < BN_VEC<T>; i++) out[i] = (float)t[i];
+  for (int i = 0; i < VEC; i++) out[i] = (float)t[i];
 }
 
 // The pieces a thread holds of a row of an array (nothing where the array is absent), or of a vector.
-template <typename T, int THREADS, int CH>
+template <typename T, int THREADS, int CH, int VEC>
 struct BnPieces {
-  u32x4 raw[CH];
+  typename BnRaw<T, VEC>::type raw[CH];
   __device__ __forceinline__ void load(const T* row, long long n, int t) {
 #pragma unroll
     for (int c = 0; c < CH; c++) {
-      const long long at = ((long long)c * THREADS + t) * BN_VEC<T>;
-      raw[c] = bn_raw(row + at, row ? n - at : 0);
+      const long long at = ((long long)c * THREADS + t) * VEC;
+      raw[c] = bn_raw<T, VEC>(row + at, row ? n - at : 0);
     }
   }
 };
@@ -311,10 +319,10 @@ struct BnPieces {
 template <int THREADS> constexpr int BN_GROUP = THREADS < 256 ? 256 : THREADS;   // threads of a workgroup
 template <int THREADS> constexpr int BN_ROWS = BN_GROUP<THREADS> / THREADS;      // rows it has in hand
 
-template <typename T, int THREADS, int CH, bool AHEAD>
+template <typename T, int THREADS, int CH, int VEC, bool AHEAD>
 __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a) {
-  constexpr int VEC = BN_VEC<T>, ROWS = BN_ROWS<THREADS>;
-  using Pieces = BnPieces<T, THREADS, CH>;
+  constexpr int ROWS = BN_ROWS<THREADS>;
+  using Pieces = BnPieces<T, THREADS, CH, VEC>;
   __shared__ float slots[2][2][1][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = threadIdx.x % THREADS;
@@ -328,7 +336,7 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
   // a piece of a vector: held, or read again
   auto piece = [&](const Pieces& held, const T* from, int c, float (&out)[VEC]) {
     const long long at = ((long long)c * THREADS + t) * VEC;
-    bn_numbers<T>(AHEAD ? held.raw[c] : bn_raw(from + at, from ? n - at : 0), out);
+    bn_numbers<T, VEC>(AHEAD ? held.raw[c] : bn_raw<T, VEC>(from + at, from ? n - at : 0), out);
   };
   auto fetch = [&](long long row) {
     nx.load(x + row * a.ldx, n, t);
@@ -348,12 +356,12 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
     if (AHEAD && row + workers < a.tokens) fetch(row + workers);
     float v[CH][VEC], sum[1] = {0.0f};
 #pragma unroll
-    for (int c = 0; c < CH; c++) bn_numbers<T>(cx.raw[c], v[c]);
+    for (int c = 0; c < CH; c++) bn_numbers<T, VEC>(cx.raw[c], v[c]);
     if (block) {
 #pragma unroll
       for (int c = 0; c < CH; c++) {
         float f[VEC];
-        bn_numbers<T>(cb.raw[c], f);
+        bn_numbers<T, VEC>(cb.raw[c], f);
 #pragma unroll
         for (int i = 0; i < VEC; i++) sum[0] += f[i] * f[i];
       }
@@ -362,8 +370,8 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
 #pragma unroll
       for (int c = 0; c < CH; c++) {
         float f[VEC], g[VEC], w[VEC];
-        bn_numbers<T>(cb.raw[c], f);
-        if (token_gate) bn_numbers<T>(cg.raw[c], g);
+        bn_numbers<T, VEC>(cb.raw[c], f);
+        if (token_gate) bn_numbers<T, VEC>(cg.raw[c], g);
         else piece(channel_gate, gate, c, g);
         piece(w_post, p_post, c, w);
 #pragma unroll
@@ -403,10 +411,10 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
 // A worker (a row's threads) takes every workers-th row and keeps the sums over its rows of the columns its threads
 // hold, which go out as one partial per workgroup and are summed, in their order, by bn_columns_kernel: the same bits
 // every time.  With one gate per channel dgate and dw_post are both multiples of sum dx b / rms(b).
-template <typename T, int THREADS, int CH, bool AHEAD, bool TOKEN_GATE>
+template <typename T, int THREADS, int CH, int VEC, bool AHEAD, bool TOKEN_GATE>
 __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a) {
-  constexpr int VEC = BN_VEC<T>, ROWS = BN_ROWS<THREADS>;
-  using Pieces = BnPieces<T, THREADS, CH>;
+  constexpr int ROWS = BN_ROWS<THREADS>;
+  using Pieces = BnPieces<T, THREADS, CH, VEC>;
   __shared__ float slots[2][6][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = threadIdx.x % THREADS;
@@ -420,7 +428,7 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
   Pieces w_post, w_pre, channel_gate, nr, nb = {}, nd = {}, ny = {}, ng = {};
   auto piece = [&](const Pieces& held, const T* from, int c, float (&out)[VEC]) {
     const long long at = ((long long)c * THREADS + t) * VEC;
-    bn_numbers<T>(AHEAD ? held.raw[c] : bn_raw(from + at, from ? n - at : 0), out);
+    bn_numbers<T, VEC>(AHEAD ? held.raw[c] : bn_raw<T, VEC>(from + at, from ? n - at : 0), out);
   };
   auto fetch = [&](long long row) {
     nr.load(r + row * a.ldx, n, t);
@@ -453,11 +461,11 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       float vr[VEC], vb[VEC], vd[VEC], vy[VEC], g[VEC], wp[VEC], wq[VEC];
-      bn_numbers<T>(cr.raw[c], vr);
-      bn_numbers<T>(cb.raw[c], vb);
-      bn_numbers<T>(cd.raw[c], vd);
-      bn_numbers<T>(cy.raw[c], vy);
-      if (TOKEN_GATE) bn_numbers<T>(cg.raw[c], g);
+      bn_numbers<T, VEC>(cr.raw[c], vr);
+      bn_numbers<T, VEC>(cb.raw[c], vb);
+      bn_numbers<T, VEC>(cd.raw[c], vd);
+      bn_numbers<T, VEC>(cy.raw[c], vy);
+      if (TOKEN_GATE) bn_numbers<T, VEC>(cg.raw[c], g);
       else piece(channel_gate, gate, c, g);
       piece(w_post, p_post, c, wp);
       piece(w_pre, p_pre, c, wq);
@@ -482,9 +490,9 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
       const long long at = ((long long)c * THREADS + t) * VEC;
       if (at >= n) break;
       float vr[VEC], vd[VEC], vy[VEC], wq[VEC], dx[VEC];
-      bn_numbers<T>(cr.raw[c], vr);
-      bn_numbers<T>(cd.raw[c], vd);
-      bn_numbers<T>(cy.raw[c], vy);
+      bn_numbers<T, VEC>(cr.raw[c], vr);
+      bn_numbers<T, VEC>(cd.raw[c], vd);
+      bn_numbers<T, VEC>(cy.raw[c], vy);
       piece(w_pre, p_pre, c, wq);
 #pragma unroll
       for (int i = 0; i < VEC; i++) {
@@ -494,8 +502,8 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
       if (a.dx) bn_store<T, VEC>(static_cast<T*>(a.dx) + row * a.lddx + at, n - at, dx);
       if (block) {
         float vb[VEC], g[VEC], wp[VEC], db[VEC], dg[VEC];
-        bn_numbers<T>(cb.raw[c], vb);
-        if (TOKEN_GATE) bn_numbers<T>(cg.raw[c], g);
+        bn_numbers<T, VEC>(cb.raw[c], vb);
+        if (TOKEN_GATE) bn_numbers<T, VEC>(cg.raw[c], g);
         else piece(channel_gate, gate, c, g);
         piece(w_post, p_post, c, wp);
 #pragma unroll
@@ -588,14 +596,26 @@ constexpr long long BN_MAX_DIM = 1LL << 30;
 // per compute unit), so that the next row's loads always have a row to hide behind and partial sums stay few.
 constexpr long long bn_most_groups(int threads) { return threads <= 256 ? 512 : 256; }
 
-// f(threads per row, pieces per thread, next row ahead) for rows of n elements; 0 pieces: too long for registers.
-// 16-bit pieces are twice the numbers of fp32 ones, so a thread holds half as many.
+// f(threads per row, pieces per thread, entries per piece, next row ahead) for rows of n entries, whose starts are `wide` (on 16
+// bytes) or not; 0 pieces: too long for registers.  Single entries are for fp32 rows of up to 4096: 16-bit ones take a register
+// each as well, twice what they hold, and lose (64M entries in rows of 3003, backward: fp32 312 -> 203 us, bf16 283 ->
+// 1113; fp32 rows of 5001 312 -> 607).
 template <typename T, typename F>
-void bn_shape(long long n, F&& f) {
+void bn_shape(long long n, bool wide, F&& f) {
   const long long pieces = (n + BN_VEC<T> - 1) / BN_VEC<T>;
   constexpr int WIDE = sizeof(T) == 4 ? 2 : 1;
   using std::integral_constant;
-#define BN_CASE(TH, CHUNKS, AHEAD) f(integral_constant<int, TH>{}, integral_constant<int, CHUNKS>{}, integral_constant<bool, AHEAD>{})
+  auto call = [&](auto th, auto ch, auto ahead) {
+    constexpr int V = BN_VEC<T>;
+    if constexpr (WIDE == 2 && ahead.value) {
+      if (!wide) {
+        f(th, integral_constant<int, ch.value * V>{}, integral_constant<int, 1>{}, ahead);
+        return;
+      }
+    }
+    f(th, ch, integral_constant<int, V>{}, ahead);
+  };
+#define BN_CASE(TH, CHUNKS, AHEAD) call(integral_constant<int, TH>{}, integral_constant<int, CHUNKS>{}, integral_constant<bool, AHEAD>{})
   if (pieces <= 16) BN_CASE(16, 1, true);
   else if (pieces <= 32) BN_CASE(16, 2, true);
   else if (pieces <= 64) BN_CASE(64, 1, true);
@@ -611,9 +631,18 @@ void bn_shape(long long n, F&& f) {
         return;
       }
     }
-    BN_CASE(BN_LONG, 0, false);
+    f(integral_constant<int, BN_LONG>{}, integral_constant<int, 0>{}, integral_constant<int, 1>{}, integral_constant<bool, false>{});
   }
 #undef BN_CASE
+}
+// Whether every array's rows start on 16 bytes.
+template <typename T>
+bool bn_wide(const BnArgs& a) {
+  const void* arrays[] = {a.x, a.b, a.r, a.y, a.dr, a.dy, a.dx, a.db, a.dgate, a.gate_stride ? a.gate : nullptr};
+  const long long strides[] = {a.ldx, a.ldb, a.ldr, a.ldy, a.lddr, a.lddy, a.lddx, a.lddb, a.dgate_stride, a.gate_stride};
+  for (int i = 0; i < 10; i++)
+    if (arrays[i] && (!aligned(arrays[i], 16) || (a.tokens > 1 && strides[i] % BN_VEC<T> != 0))) return false;
+  return true;
 }
 
 long long bn_groups(int threads, long long tokens) {
@@ -624,12 +653,12 @@ long long bn_groups(int threads, long long tokens) {
 
 template <typename T>
 int run_forward(const BnArgs& a, hipStream_t stream) {
-  bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
+  bn_shape<T>(a.n, bn_wide<T>(a), [&](auto th, auto ch, auto vec, auto ahead) {
     mark(stream);
     if constexpr (ch.value == 0)
       launch(bn_forward_long_kernel<T>, dim3((unsigned)a.tokens), dim3(BN_LONG), stream, a);
     else
-      launch(bn_forward_kernel<T, th.value, ch.value, ahead.value>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
+      launch(bn_forward_kernel<T, th.value, ch.value, vec.value, ahead.value>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
   });
   mark(stream);
   return launch_status();
@@ -637,7 +666,7 @@ int run_forward(const BnArgs& a, hipStream_t stream) {
 
 template <typename T>
 int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate, float* dw_pre, hipStream_t stream) {
-  bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
+  bn_shape<T>(a.n, bn_wide<T>(a), [&](auto th, auto ch, auto vec, auto ahead) {
     const long long groups = bn_groups(th.value, a.tokens);
     const dim3 grid((unsigned)groups), block(BN_GROUP<th.value>);
     if (groups > 0) {
@@ -646,8 +675,8 @@ int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate,
         if (token_gate) launch(bn_backward_long_kernel<T, true>, grid, block, stream, a);
         else launch(bn_backward_long_kernel<T, false>, grid, block, stream, a);
       } else {
-        if (token_gate) launch(bn_backward_kernel<T, th.value, ch.value, ahead.value, true>, grid, block, stream, a);
-        else launch(bn_backward_kernel<T, th.value, ch.value, ahead.value, false>, grid, block, stream, a);
+        if (token_gate) launch(bn_backward_kernel<T, th.value, ch.value, vec.value, ahead.value, true>, grid, block, stream, a);
+        else launch(bn_backward_kernel<T, th.value, ch.value, vec.value, ahead.value, false>, grid, block, stream, a);
       }
     }
     if (a.want_post || a.want_gate || a.want_pre) {
@@ -701,12 +730,12 @@ BnArgs bn_start(const mlproj_norm_block* k) {
 size_t bn_workspace(long long tokens, long long n) {
   // the most workgroups any storage type has
   long long most = 1;
-  auto count = [&](auto th, auto, auto) {
+  auto count = [&](auto th, auto, auto, auto) {
     const long long groups = bn_groups(th.value, tokens);
     most = groups > most ? groups : most;
   };
-  bn_shape<bf16_t>(n, count);
-  bn_shape<float>(n, count);
+  bn_shape<bf16_t>(n, true, count);
+  bn_shape<float>(n, true, count);
   return (size_t)most * n * 2 * sizeof(float) + 256;
 }
 
