@@ -47,7 +47,8 @@ struct FfProduct {
   const unsigned char* keep;   // one byte per column of the result, or null
   const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
   float* partial;              // PARTIAL: [splits][products][M][N in whole quads]
-  int splits;
+  int splits;                  // shares of the sum, and the one a workgroup has (set in the kernels)
+  int share;
   int part;                    // direct tiles: FF_WHOLE, or a product shared between two launches (ffdirect.h)
 };
 
@@ -86,6 +87,54 @@ __device__ __forceinline__ FfVec8<T> ff_load8(const T* p, long long valid) {
     for (int i = 0; i < 8; i++) r.v[i] = i < valid ? p[i] : (T)0.0f;
   }
   return r;
+}
+
+// ------------------------------------------------------------------ tiles
+// The tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn; each XCD takes a run of consecutive tiles, and
+// tiles are numbered down FF_BAND tile rows before the next column, so that what runs on an XCD at one time shares rows of A
+// and columns of B in its L2.  Shares of a sum go to different XCDs (with fewer than 8 shares, several XCDs divide a
+// share's tiles), so that each of them reads a part of K only.
+//
+// A product of 3.25 turns of 256 x 256 tiles on 256 compute units takes as long as one of 4.  It can go out in two launches:
+// FF_TURNS takes the whole turns, FF_REST the remaining tiles cut into four of 128 x 128, which a quarter of the units
+// would have taken whole.  More than FF_LEFT remaining tiles would be more than one turn of small ones: then they stay
+// whole.  (The number of tiles may be known on the device only, where channels are packed.)
+constexpr int FF_BAND = 4, FF_TURN = 256, FF_LEFT = 128;
+__host__ __device__ inline long long ff_in_turns(long long tiles) {
+  const long long rest = tiles % FF_TURN;
+  return rest > FF_LEFT ? tiles : tiles - rest;
+}
+__device__ __forceinline__ void ff_place(long long v, long long tiles_m, long long tiles_n, long long* tm, long long* tn) {
+  const long long band = v / (FF_BAND * tiles_n), in = v % (FF_BAND * tiles_n);
+  const long long rows = tiles_m - band * FF_BAND < FF_BAND ? tiles_m - band * FF_BAND : FF_BAND;
+  *tm = band * FF_BAND + in % rows;
+  *tn = in / rows;
+}
+// First row and column of the workgroup's tile of BM x COLS, and its share of the sum (p.share); false: there is none.
+template <int BM, int COLS>
+__device__ __forceinline__ bool ff_tile(FfProduct& p, long long N, long long* row0, long long* col0) {
+  long long tm, tn;
+  p.share = 0;
+  if (p.part == FF_REST) {        // a quarter of a tile of twice the size
+    const long long tiles_m = (p.M + 2 * BM - 1) / (2 * BM), tiles_n = (N + 2 * COLS - 1) / (2 * COLS);
+    const long long v = ff_in_turns(tiles_m * tiles_n) + (blockIdx.x >> 2);
+    if (v >= tiles_m * tiles_n) return false;
+    ff_place(v, tiles_m, tiles_n, &tm, &tn);
+    *row0 = (2 * tm + (blockIdx.x >> 1 & 1)) * BM;
+    *col0 = (2 * tn + (blockIdx.x & 1)) * COLS;
+    return *row0 < p.M && *col0 < N;
+  }
+  const long long tiles_m = (p.M + BM - 1) / BM, tiles_n = (N + COLS - 1) / COLS;
+  const long long all = p.part == FF_TURNS ? ff_in_turns(tiles_m * tiles_n) : tiles_m * tiles_n;
+  p.share = blockIdx.x % p.splits;
+  const long long id = blockIdx.x / p.splits;
+  if (id >= all) return false;
+  const long long xcds = p.splits < 8 ? 8 / p.splits : 1;         // that divide the share's tiles (splits: a power of two)
+  const long long xcd = id % xcds, each = all / xcds, more = all % xcds;
+  ff_place(xcd * each + (xcd < more ? xcd : more) + id / xcds, tiles_m, tiles_n, &tm, &tn);
+  *row0 = tm * BM;
+  *col0 = tn * COLS;
+  return true;
 }
 
 // ------------------------------------------------------------------ activation
@@ -157,7 +206,7 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
   if constexpr (EPI == FF_PARTIAL) {
     // (rows of whole quads: what lies past N is written and never read)
     const long long ld = (p.N + 3) / 4 * 4, plane = p.M * ld;
-    float* at = p.partial + (long long)blockIdx.y * (DUAL ? 2 : 1) * plane + row * ld + col;
+    float* at = p.partial + (long long)p.share * (DUAL ? 2 : 1) * plane + row * ld + col;
     ff_store4(at, v0);
     if constexpr (DUAL) ff_store4(at + plane, v1);
     return;

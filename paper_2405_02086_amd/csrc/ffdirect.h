@@ -98,43 +98,6 @@ __device__ __forceinline__ F fd_frag(const unsigned char* lds, const FdFrom& fro
   return r;
 }
 
-// The tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn; each XCD takes a run of consecutive tiles, and
-// tiles are numbered down FD_BAND tile rows before the next column, so that what runs on an XCD at one time shares rows of A
-// and columns of B in its L2.
-//
-// A product of 3.25 turns of 256 x 256 tiles on 256 compute units takes as long as one of 4.  It can go out in two launches:
-// FF_TURNS takes the whole turns, FF_REST the remaining tiles cut into four of 128 x 128, which a quarter of the units
-// would have taken whole.  (The number of tiles may be known on the device only, where channels are packed.)
-constexpr int FD_BAND = 4, FD_TURN = 256;
-__device__ __forceinline__ void fd_place(long long v, long long tiles_m, long long tiles_n, long long* tm, long long* tn) {
-  const long long band = v / (FD_BAND * tiles_n), in = v % (FD_BAND * tiles_n);
-  const long long rows = tiles_m - band * FD_BAND < FD_BAND ? tiles_m - band * FD_BAND : FD_BAND;
-  *tm = band * FD_BAND + in % rows;
-  *tn = in / rows;
-}
-// First row and column of the workgroup's tile of BM x COLS; false: there is none.
-template <int BM, int COLS>
-__device__ __forceinline__ bool fd_tile(int part, long long M, long long N, long long* row0, long long* col0) {
-  long long tm, tn;
-  if (part == FF_REST) {          // BM = 128: a quarter of a tile of twice the size
-    const long long tiles_m = (M + 2 * BM - 1) / (2 * BM), tiles_n = (N + 2 * COLS - 1) / (2 * COLS);
-    const long long v = tiles_m * tiles_n / FD_TURN * FD_TURN + (blockIdx.x >> 2);
-    if (v >= tiles_m * tiles_n) return false;
-    fd_place(v, tiles_m, tiles_n, &tm, &tn);
-    *row0 = (2 * tm + (blockIdx.x >> 1 & 1)) * BM;
-    *col0 = (2 * tn + (blockIdx.x & 1)) * COLS;
-    return *row0 < M && *col0 < N;
-  }
-  const long long tiles_m = (M + BM - 1) / BM, tiles_n = (N + COLS - 1) / COLS, id = blockIdx.x;
-  const long long all = part == FF_TURNS ? tiles_m * tiles_n / FD_TURN * FD_TURN : tiles_m * tiles_n;
-  if (id >= all) return false;
-  const long long xcd = id & 7, each = all >> 3, more = all & 7;
-  fd_place(xcd * each + (xcd < more ? xcd : more) + (id >> 3), tiles_m, tiles_n, &tm, &tn);
-  *row0 = tm * BM;
-  *col0 = tn * COLS;
-  return true;
-}
-
 // The order of a step's instructions: its LDS reads spread evenly between its matrix instructions.
 template <int DONE, int MFMAS, int READS>
 __device__ __forceinline__ void fd_schedule() {
@@ -163,9 +126,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p)
   const long long K = p.kept && SUMS_CHANNELS ? *p.kept : p.K;
   constexpr int COLS = DUAL ? BW : BN;
   long long row0, col0;
-  if (!fd_tile<BM, COLS>(p.part, p.M, N, &row0, &col0)) return;
+  if (!ff_tile<BM, COLS>(p, N, &row0, &col0)) return;
   const int ksteps = (int)((K + FD_K - 1) / FD_K), all = ksteps * p.segs;
-  const int first = (int)((long long)all * blockIdx.y / p.splits), last = (int)((long long)all * (blockIdx.y + 1) / p.splits);
+  const int first = (int)((long long)all * p.share / p.splits), last = (int)((long long)all * (p.share + 1) / p.splits);
 
   FdPart<A_KC, AW, THREADS> pa[AP];
   FdPart<B_KC, BW, THREADS> pb[2];

@@ -38,6 +38,7 @@ __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
   // workgroup 8 i + x runs on XCD x: columns x, x + 8, ... there, each with all its tokens in turn
   const long long mine = blockIdx.x >> 3, tn = mine / tiles_m * 8 + (blockIdx.x & 7), row0 = mine % tiles_m * 16;
   if (tn >= tiles_n) return;
+  p.share = blockIdx.y;
   const long long col0 = tn * FK_COLS, col = col0 + c * CW;
   const float* X = static_cast<const float*>(p.A0);
   const float* B[2] = {static_cast<const float*>(p.B0), static_cast<const float*>(p.B1)};

@@ -97,13 +97,12 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   constexpr int COLS = DUAL ? 64 : 128;                    // columns of each product in a tile
-  const long long tiles_n = (p.N + COLS - 1) / COLS;
   const long long N = p.kept && !(B_KC && A_KC) ? *p.kept : p.N;
   const long long K = p.kept && (B_KC && A_KC) ? *p.kept : p.K;
-  const long long row0 = blockIdx.x / tiles_n * FS_M, col0 = blockIdx.x % tiles_n * COLS;
-  if (col0 >= N) return;
+  long long row0, col0;
+  if (!ff_tile<FS_M, COLS>(p, N, &row0, &col0)) return;
   const long long ksteps = (K + FS_K - 1) / FS_K, all = ksteps * p.segs;
-  const long long first = all * blockIdx.y / p.splits, last = all * (blockIdx.y + 1) / p.splits;
+  const long long first = all * p.share / p.splits, last = all * (p.share + 1) / p.splits;
 
   FfVec8<T> ra[2], rb[2];
   auto fetch = [&](long long step) {

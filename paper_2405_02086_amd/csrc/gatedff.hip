@@ -33,7 +33,7 @@ struct FfKind {
   double step_us, tile_us[4];  // by epilogue
 };
 static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int epi, bool direct, int es) {
-  static const FfKind kinds[4] = {{256, 256, 1, 0.78, {12, 14, 24, 12}}, {128, 128, 2, 0.53, {5, 6, 8, 5}}, {128, 128, 3, 2.0, {5, 6, 8, 5}}, {128, 128, 2, 3.1, {5, 6, 8, 5}}};
+  static const FfKind kinds[4] = {{256, 256, 1, 0.78, {12, 14, 24, 12}}, {128, 128, 2, 0.57, {5, 6, 8, 5}}, {128, 128, 3, 2.0, {5, 6, 8, 5}}, {128, 128, 2, 3.1, {5, 6, 8, 5}}};
   const bool forward = epi == FF_FWD || epi == FF_GRAD;
   if (es == 4 && forward && M <= FK_TOKENS) {
     // shares until there are two workgroups per compute unit or a wavefront has one step left
@@ -50,17 +50,19 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int 
     for (int splits = 1; splits <= 64; splits *= 2) {
       if (splits > 1 && (steps / splits < 2 || planes * splits > 512e6)) break;
       const double units = 256.0 * k.places, groups = (double)tiles * splits;
-      // workgroups in turn on the fullest place; a direct tile beside an empty place is faster
+      // workgroups in turn on the fullest place.  A direct 128 x 128 tile that has its compute unit to itself takes two thirds of
+      // the time; where both operands run along K (dX) two of them are no faster than one after the other, because
+      // each step uses half of every cache line it loads.
       const double turns = ff_cdiv((long long)groups, (long long)units);
-      const double share = groups < units / 2 && kind == 1 ? 0.65 : 1.0;
-      double us = turns * ((double)ff_cdiv(steps, splits) * k.step_us * share + k.tile_us[splits > 1 ? FF_PARTIAL : epi]);
-      if (splits > 1) us += 4.0 + 0.05 * splits + planes * (splits + splits) / 4.0e6;
+      const double step_us = kind != 1 ? k.step_us : groups <= units / 2 ? 0.37 : dual ? k.step_us : 0.75;
+      double us = turns * ((double)ff_cdiv(steps, splits) * step_us + k.tile_us[splits > 1 ? FF_PARTIAL : epi]);
+      if (splits > 1) us += 4.0 + 0.05 * splits + planes * (splits + splits) / 8.0e6;
       if (us < best.us) best = {kind, splits, us, false};
-      if (kind == 0 && splits == 1 && tiles > 256) {
+      if (kind == 0 && splits == 1 && tiles > 256 && ff_in_turns(tiles) < tiles) {
         const FfKind& small = kinds[1];
         const long long rest = tiles % 256 * 4;
         const double in_parts = tiles / 256 * (steps * k.step_us + k.tile_us[epi]) + 4.0 +
-                                ff_cdiv(rest, 512) * (steps * small.step_us * (rest < 256 ? 0.65 : 1.0) + small.tile_us[epi]);
+                                (steps * (rest <= 256 ? 0.37 : dual ? small.step_us : 0.75) + small.tile_us[epi]);
         if (in_parts < best.us) best = {0, 1, in_parts, true};
       }
     }
@@ -185,17 +187,17 @@ void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
     if (kind == 0) {
       const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)tiles, p.splits), dim3(512), stream, p);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)(tiles * p.splits)), dim3(512), stream, p);
       return;
     }
     if (kind == 1) {
-      const long long tiles = p.part == FF_REST ? 4 * (FD_TURN - 1) : ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)tiles, p.splits), dim3(256), stream, p);
+      const long long tiles = p.part == FF_REST ? 4 * FF_LEFT : ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)(tiles * p.splits)), dim3(256), stream, p);
       return;
     }
   }
   const long long tiles = ff_cdiv(p.M, FS_M) * ff_cdiv(p.N, DUAL ? 64 : 128);
-  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)tiles, p.splits), dim3(FS_THREADS), stream, p);
+  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)(tiles * p.splits)), dim3(FS_THREADS), stream, p);
 }
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_product(FfProduct p, void* partial, hipStream_t stream) {
