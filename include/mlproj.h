@@ -456,9 +456,9 @@ int mlproj_gated_ff_workspace_bytes(int storage, long long tokens, long long n, 
 
 /* TEST AND TUNING AID: how the library would compute one of a block's products from 16-byte aligned rows --
  * product 0: forward, 1: the backward call's X Wg and X Wu, 2: dX, 3: dWg and dWu -- as kind + 16 * masked_packed + 32 *
- * in_two_launches + 256 * shares: kind 0 / 1 tiles of 256 x 256 / 128 x 128 straight into LDS, 2 tiles staged through
- * registers, 3 no tiles (few fp32 tokens); masked_packed: a masked call packs its kept channels first; shares: of the
- * sum, added by a second kernel.  The route depends on nothing but these arguments and alignment.  Host only.      */
+ * in_two_launches + 64 * low_tiles + 256 * shares: kind 0 / 1 tiles of 256 x 256 / 128 x 128 (low_tiles: 64 x 128) straight
+ * into LDS, 2 tiles staged through registers, 3 no tiles (few fp32 tokens); masked_packed: a masked call packs its kept
+ * channels first; shares: of the sum, added by a second kernel.  The route depends on nothing but these arguments and alignment.  Host only.      */
 int mlproj_gated_ff_route(int storage, int product, long long tokens, long long n, long long m);
 
 /* H = mask * act(X Wg) * (X Wu), tokens x m.  G, U (both or neither): also X Wg and X Wu, for a later

@@ -620,11 +620,12 @@ def gated_ff_workspace_bytes(tokens, n, m, dtype, backward=False, masked=True):
 
 
 def gated_ff_route(dtype, product, tokens, n, m):
-    """How a product of a block with aligned rows is computed: {"kind", "packed", "parts", "shares"} (see mlproj.h)."""
+    """How a product of a block with aligned rows is computed: {"kind", "packed", "parts", "low", "shares"} (see
+    mlproj.h)."""
     r = lib().mlproj_gated_ff_route(_storage(dtype), product, tokens, n, m)
     if r < 0:
         _check(r, "mlproj_gated_ff_route")
-    return {"kind": r & 15, "packed": bool(r & 16), "parts": bool(r & 32), "shares": r >> 8}
+    return {"kind": r & 15, "packed": bool(r & 16), "parts": bool(r & 32), "low": bool(r & 64), "shares": r >> 8}
 
 
 def _gated_block(X, Wg, Wu, mask):

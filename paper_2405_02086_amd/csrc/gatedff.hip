@@ -1,5 +1,7 @@
 // mlproj: the gated feed-forward block whose hidden channels the projection prunes, forward and backward:
-// argument checks, plans and the C ABI.  Kernels: ffcommon.h, ffstaged.h.
+// argument checks, plans, copies of operands and the C ABI.  The products' kernels: ffdirect.h (16-bit elements, tiles straight
+// into LDS), ffstaged.h (fp32 and other alignments; joins), ffskinny.h (few fp32 tokens), what they share: ffcommon.h;
+// moving kept channels: ffcompact.h.
 #include "ffcommon.h"
 #include "ffcompact.h"
 #include "ffdirect.h"
@@ -18,24 +20,35 @@ static long long ff_cdiv(long long a, long long b) { return (a + b - 1) / b; }
 static size_t ff_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // ------------------------------------------------------------------ plan of a product
-// Which tiles a product takes and into how many shares its sum is cut.  Three kinds of tiles: direct 256 x 256 (one workgroup
-// per compute unit), direct 128 x 128 (two), staged 128 x 128 (three; fp32: two).  What a 32-deep step of a tile takes with every place
-// taken, the price of a workgroup beside its steps and the price of joining shares were measured (4096 x 4096 x 16384
-// and 1000 x 1000 x 20000, bf16 and fp32); the plan is the cheapest of them.
+// Which tiles a product takes and into how many shares its sum is cut: the cheapest by what was measured, which is a
+// 32-deep step of a tile by how many workgroups the compute unit holds, a tile beside its steps (more where others
+// on the unit want the same), and joining shares.  Fitted to the four products of 59 blocks, 1 x 440 -> 2048 to 8192 x
+// 2048 -> 8192, each in every tile and with every number of shares: the plan's choice takes 0.6 % more than the best
+// one on average, 14 % at most.  256 x 256 tiles (one workgroup per compute unit) have the fastest steps, 64 x 128 (three)
+// fill the chip where there are few tiles: 303 x 256 -> 1272 backward products take 7, 10 and 6 us in them, in 128 x 128
+// (two) 10, 12 and 8, in 256 x 256 18, 20 and 16; 4096 x 4096 -> 4096 forward takes 359, 269 and 215 us.
 struct FfPlan {
-  int kind;      // 0: direct 256, 1: direct 128, 2: staged, 3: few tokens
+  int kind;      // 0: direct 256 x 256, 1: direct 128 x 128, 2: staged, 3: few tokens, 4: direct 64 x 128
   int splits;
   double us;
   bool parts;    // direct 256: whole turns, and the rest in smaller tiles
 };
 struct FfKind {
   int rows, cols, places;      // of the tile; workgroups per compute unit
-  double step_us, tile_us[4];  // by epilogue
+  double step[2][3];           // us; one product or two, workgroups on the unit
+  double tile[4], crowd;       // by epilogue; more by this share for each further workgroup
+  double turn(bool dual, int epi, long long steps, long long on_unit) const {
+    return steps * step[dual][on_unit - 1] + tile[epi] * (1.0 + crowd * (on_unit - 1));
+  }
 };
 static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int epi, bool direct, int es) {
-  static const FfKind kinds[4] = {{256, 256, 1, 0.78, {12, 14, 24, 12}}, {128, 128, 2, 0.57, {5, 6, 8, 5}}, {128, 128, 3, 2.0, {5, 6, 8, 5}}, {128, 128, 2, 3.1, {5, 6, 8, 5}}};
-  const bool forward = epi == FF_FWD || epi == FF_GRAD;
-  if (es == 4 && forward && M <= FK_TOKENS) {
+  static const FfKind tile256 = {256, 256, 1, {{0.66}, {0.66}}, {8.2, 8.5, 18.6, 2.3}, 0.0};
+  static const FfKind tile128 = {128, 128, 2, {{0.30, 0.59}, {0.24, 0.50}}, {1.9, 1.7, 4.1, 0.5}, 1.9};
+  static const FfKind tile64 = {64, 128, 3, {{0.18, 0.42, 0.70}, {0.16, 0.44, 0.57}}, {1.1, 0.9, 1.7, 0.5}, 1.4};
+  static const FfKind staged = {128, 128, 3, {{0.81, 1.27, 0.85}, {1.46, 1.40, 1.33}}, {3.0, 0.5, 1.7, 0.1}, 1.9};
+  static const FfKind staged32 = {128, 128, 2, {{3.1, 3.1}, {3.1, 3.1}}, {2.0, 3.0, 5.0, 2.0}, 0.0};
+  constexpr double LAUNCH = 3.6;
+  if (es == 4 && (epi == FF_FWD || epi == FF_GRAD) && M <= FK_TOKENS) {
     // shares until there are two workgroups per compute unit or a wavefront has one step left
     int splits = 1;
     const long long groups = ff_cdiv(N, FK_COLS) * ff_cdiv(M, 16);
@@ -43,29 +56,30 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int 
     return {3, splits, 0.0, false};
   }
   FfPlan best{2, 1, 1e30, false};
-  for (int kind = direct ? 0 : 2; kind <= (direct ? 1 : 2); kind++) {
-    const FfKind& k = kinds[kind == 2 && es == 4 ? 3 : kind];
+  const double planes = 4.0 * M * N * (dual ? 2 : 1);
+  auto consider = [&](int kind, const FfKind& k) {
     const long long tiles = ff_cdiv(M, k.rows) * ff_cdiv(N, dual ? k.cols / 2 : k.cols);
-    const double planes = 4.0 * M * N * (dual ? 2 : 1);
     for (int splits = 1; splits <= 64; splits *= 2) {
       if (splits > 1 && (steps / splits < 2 || planes * splits > 512e6)) break;
-      const double units = 256.0 * k.places, groups = (double)tiles * splits;
-      // workgroups in turn on the fullest place.  A direct 128 x 128 tile that has its compute unit to itself takes two thirds of
-      // the time; where both operands run along K (dX) two of them are no faster than one after the other, because
-      // each step uses half of every cache line it loads.
-      const double turns = ff_cdiv((long long)groups, (long long)units);
-      const double step_us = kind != 1 ? k.step_us : groups <= units / 2 ? 0.37 : dual ? k.step_us : 0.75;
-      double us = turns * ((double)ff_cdiv(steps, splits) * step_us + k.tile_us[splits > 1 ? FF_PARTIAL : epi]);
-      if (splits > 1) us += 4.0 + 0.05 * splits + planes * (splits + splits) / 8.0e6;
+      const long long groups = tiles * splits, units = 256 * k.places, rest = groups % units, each = ff_cdiv(steps, splits);
+      const int out = splits > 1 ? FF_PARTIAL : epi;
+      double us = LAUNCH + (double)(groups / units) * k.turn(dual, out, each, k.places);
+      if (rest) us += k.turn(dual, out, each, ff_cdiv(rest, 256));
+      if (splits > 1) us += 3.0 + planes * 2 * splits / 5.7e6;
       if (us < best.us) best = {kind, splits, us, false};
-      if (kind == 0 && splits == 1 && tiles > 256 && ff_in_turns(tiles) < tiles) {
-        const FfKind& small = kinds[1];
-        const long long rest = tiles % 256 * 4;
-        const double in_parts = tiles / 256 * (steps * k.step_us + k.tile_us[epi]) + 4.0 +
-                                (steps * (rest <= 256 ? 0.37 : dual ? small.step_us : 0.75) + small.tile_us[epi]);
-        if (in_parts < best.us) best = {0, 1, in_parts, true};
-      }
     }
+    if (kind == 0 && tiles > 256 && ff_in_turns(tiles) < tiles) {
+      const long long left = tiles % 256 * 4;
+      const double us = 2 * LAUNCH + (double)(tiles / 256) * k.turn(dual, epi, steps, 1) + tile128.turn(dual, epi, steps, ff_cdiv(left, 256));
+      if (us < best.us) best = {0, 1, us, true};
+    }
+  };
+  if (direct) {
+    consider(0, tile256);
+    consider(1, tile128);
+    consider(4, tile64);
+  } else {
+    consider(2, es == 4 ? staged32 : staged);
   }
   return best;
 }
@@ -188,6 +202,11 @@ void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
     if (kind == 0) {
       const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
       launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)(tiles * p.splits)), dim3(512), stream, p);
+      return;
+    }
+    if (kind == 4) {
+      const long long tiles = ff_cdiv(p.M, 64) * ff_cdiv(p.N, DUAL ? 64 : 128);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 64, 128, 2, 2>, dim3((unsigned)(tiles * p.splits)), dim3(256), stream, p);
       return;
     }
     if (kind == 1) {
@@ -561,7 +580,8 @@ int mlproj_gated_ff_route(int storage, int product, long long tokens, long long 
   if (product < 2) plan = ff_plan(tokens, m, ff_steps(n, 1), true, backward ? FF_GRAD : FF_FWD, direct, es);
   else if (product == 2) plan = ff_plan(tokens, n, ff_steps(m, 2), false, FF_STORE, direct, es);
   else plan = ff_plan(n, m, ff_steps(tokens, 1), true, FF_STORE, direct, es);
-  return plan.kind + 16 * ff_packs(es, tokens, n, m, backward) + 32 * plan.parts + 256 * plan.splits;
+  const bool low = plan.kind == 4;
+  return (low ? 1 : plan.kind) + 16 * ff_packs(es, tokens, n, m, backward) + 32 * plan.parts + 64 * low + 256 * plan.splits;
 }
 
 int gated_ff_forward(int storage, int activation, const mlproj_gated_block* b, void* H, long long ldh, void* G, void* U,

@@ -100,12 +100,13 @@ def test_gated_ff_routes(lib):
     kind = lambda r: r & 15       # noqa: E731
     shares = lambda r: r >> 8     # noqa: E731
     packed = lambda r: bool(r & 16)   # noqa: E731
+    low = lambda r: bool(r & 64)      # noqa: E731
     for storage in (1, 2):
         big = route(storage, 0, 4096, 4096, 16384)
-        assert kind(big) == 0 and shares(big) == 1 and packed(big)
+        assert kind(big) == 0 and not low(big) and shares(big) == 1 and packed(big)
         small = route(storage, 0, 16, 256, 128)
-        assert kind(small) == 1 and shares(small) == 1 and not packed(small)
-        assert shares(route(storage, 0, 1, 4096, 16384)) > 1
+        assert kind(small) == 1 and low(small) and shares(small) == 1 and not packed(small)
+        assert shares(route(storage, 0, 11, 7448, 1256)) > 1
         assert shares(route(storage, 2, 1000, 1000, 10000)) > 1
     assert kind(route(0, 0, 32, 256, 128)) == 3 and kind(route(0, 0, 33, 256, 128)) == 2
     assert kind(route(0, 2, 16, 256, 128)) == 2

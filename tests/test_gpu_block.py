@@ -485,7 +485,10 @@ def exact_block(X, Wg, Wu, dH, act, mask):
 # sizes whose products take: whole turns and a rest of smaller tiles (packed or not), shares of the sum in every kind of tile, ...
 ROUTES = [(4200, 512, 4200, 0, {"kind": 0, "parts": True}), (2100, 2056, 8200, 1, {"kind": 0, "parts": True, "packed": True}),
           (2304, 2048, 4400, 2, {"kind": 0, "packed": True}), (1100, 2048, 9000, 3, {"kind": 0, "parts": True}),
-          (300, 8192, 64, 1, {"kind": 1}), (1000, 1000, 10000, 2, {"kind": 0, "shares": 16}), (3617, 1032, 4096, 1, {"packed": True}), (2048, 1024, 1536, 0, {"kind": 1, "shares": 1})]
+          (300, 8192, 64, 1, {"kind": 1}), (1000, 1000, 10000, 2, {"kind": 0, "shares": 16}), (3617, 1032, 4096, 1, {"packed": True}), (2048, 1024, 1536, 0, {"kind": 1, "shares": 1}),
+          (1024, 4096, 512, 0, {"kind": 1, "low": True, "shares": 2}), (514, 4096, 2048, 1, {"kind": 1, "low": False, "shares": 1}),
+          (1300, 776, 2056, 2, {"kind": 1, "low": True, "shares": 1}), (310, 824, 6432, 2, {"kind": 1, "low": False, "shares": 8}),
+          (2500, 800, 2400, 3, {"kind": 1, "low": True, "shares": 1})]
 
 
 @pytest.mark.parametrize("case", range(len(ROUTES)))
