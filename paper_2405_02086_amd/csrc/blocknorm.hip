@@ -6,12 +6,13 @@ namespace mlproj {
 namespace {
 
 // ------------------------------------------------------------------ rows in registers
-// A row's entries are dealt in pieces of 16 bytes (bn_shape has the exception): piece i of a row belongs to thread i % THREADS of the row's
-// threads (16, a wavefront, or a workgroup of 256 or 512), CH of them per thread, and stays in its registers from the
-// one load to the one store.  The last piece of a row is filled up element by element.
+// A row's entries are dealt in pieces of 16 bytes: piece i of a row belongs to thread i % THREADS of the row's threads (16, a
+// wavefront, or a workgroup of 256 or 512), CH of them per thread, and stays in its registers from the one load to the one store.
 // Both directions are bound by HBM: forward reads x and b and writes r and y once, backward reads four
 // arrays and writes two.  A row group takes many rows: the vectors (weights, a gate per channel) stay in registers
 // too, and the next row's loads go out before the present row is reduced, as far as there are registers for it.
+// 64M entries, bf16, one gate per channel: rows of 4096 take 99 us forward (5.4 TB/s) and 166 backward (4.9), of 8192 98 and
+// 164, of 3000 114 and 178, of 3003 (rows no longer start on 16 bytes) 151 and 208, of 16384 (no room for the next row) 135 and 236.
 template <typename T> constexpr int BN_VEC = 16 / sizeof(T);
 
 struct BnArgs {
@@ -272,46 +273,76 @@ __global__ __launch_bounds__(BN_LONG) void bn_backward_long_kernel(BnArgs a) {
 }
 
 // ------------------------------------------------------------------ held rows
-// A piece is VEC neighbouring entries: 16 bytes, or, where fp32 rows do not start on 16 bytes, a single entry: a
-// wavefront's single entries are neighbours, which the memory system takes at full rate from any start, while
-// unaligned 16-byte accesses go at half.
-// As it lies in memory, zeros past the row's end; and as numbers.
-template <typename T, int VEC> struct BnRaw { using type = u32x4; };
-template <typename T> struct BnRaw<T, 1> { using type = T; };
-template <typename T, int VEC>
-__device__ __forceinline__ typename BnRaw<T, VEC>::type bn_raw(const T* p, long long valid) {
-  if constexpr (VEC == 1) {
-    return valid > 0 ? *p : (T)0.0f;
-  } else {
-    u32x4 r;
-    if (valid >= VEC) {
-      __builtin_memcpy(&r, p, 16);
-    } else {
-      T t[VEC];
+// A piece is 16 bytes of neighbouring entries, as it lies in memory, zeros past the row's end; and as numbers.  (fp32 rows
+// that do not start on 16 bytes went entry by entry before partial pieces stopped being waited for: rows of 2047, 2049 or 4095
+// are 2 to 8 % faster that way, rows of 513, 1001 or 3003 16 to 30 % slower, and a second set of kernels is not worth it.)
+// (A piece wholly past the end must not take the path of a partial one: its entries, put together one by one, are waited for
+// there, and with them the next row's loads.  64M entries in rows of 5000 bf16, backward: 304 -> 204 us.)
+template <typename T>
+__device__ __forceinline__ u32x4 bn_raw(const T* p, long long valid) {
+  constexpr int VEC = BN_VEC<T>;
+  u32x4 r = {};
+  if (valid >= VEC) {
+    __builtin_memcpy(&r, p, 16);
+  } else if (valid > 0) {
+    T t[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; i++) t[i] = i < valid ? p[i] : (T)0.0f;
-      __builtin_memcpy(&r, t, 16);
-    }
-    return r;
+    for (int i = 0; i < VEC; i++) t[i] = i < valid ? p[i] : (T)0.0f;
+    __builtin_memcpy(&r, t, 16);
   }
+  return r;
 }
 template <typename T, int VEC>
-__device__ __forceinline__ void bn_numbers(typename BnRaw<T, VEC>::type raw, float (&out)[VEC]) {
+__device__ __forceinline__ void bn_numbers(u32x4 raw, float (&out)[VEC]) {
   T t[VEC];
   __builtin_memcpy(t, &raw, sizeof(t));
 #pragma unroll
   for (int i = 0; i < VEC; i++) out[i] = (float)t[i];
 }
 
-// The pieces a thread holds of a row of an array (nothing where the array is absent), or of a vector.
-template <typename T, int THREADS, int CH, int VEC>
+// The pieces a thread holds of a row of an array (nothing where the array is absent), or of a vector.  `fetch` loads
+// without waiting for anything: of a last piece that is not whole the row's last 16 bytes, which `settle` moves into place
+// (64M entries in rows of 2047 bf16, backward: 317 -> 196 us).
+template <typename T, int THREADS, int CH>
 struct BnPieces {
-  typename BnRaw<T, VEC>::type raw[CH];
+  static constexpr int VEC = BN_VEC<T>;
+  u32x4 raw[CH];
   __device__ __forceinline__ void load(const T* row, long long n, int t) {
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       const long long at = ((long long)c * THREADS + t) * VEC;
-      raw[c] = bn_raw<T, VEC>(row + at, row ? n - at : 0);
+      raw[c] = bn_raw<T>(row + at, row ? n - at : 0);
+    }
+  }
+  template <bool AHEAD>
+  __device__ __forceinline__ void fetch(const T* row, long long n, int t) {
+    if (!AHEAD || n < VEC) {
+      load(row, n, t);
+      return;
+    }
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+      const long long at = ((long long)c * THREADS + t) * VEC, first = at < n - VEC ? at : n - VEC;
+      raw[c] = {};
+      if (at < n) __builtin_memcpy(&raw[c], row + first, 16);
+    }
+  }
+  template <bool AHEAD>
+  __device__ __forceinline__ void settle(long long n, int t) {
+    if constexpr (AHEAD) {
+      if (n < VEC || n % VEC == 0) return;
+#pragma unroll
+      for (int c = 0; c < CH; c++) {
+        const long long valid = n - ((long long)c * THREADS + t) * VEC;
+        if (valid <= 0 || valid >= VEC) continue;
+        // (VEC - valid) entries to the front: by two dwords, one, and half of one
+        const int off = (int)(VEC - valid) * (int)sizeof(T);
+        u32x4 w = raw[c];
+        if (off & 8) w = u32x4{w[2], w[3], 0, 0};
+        if (off & 4) w = u32x4{w[1], w[2], w[3], 0};
+        if (off & 2) w = u32x4{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16), __builtin_amdgcn_alignbit(w[3], w[2], 16), w[3] >> 16};
+        raw[c] = w;
+      }
     }
   }
 };
@@ -319,10 +350,11 @@ struct BnPieces {
 template <int THREADS> constexpr int BN_GROUP = THREADS < 256 ? 256 : THREADS;   // threads of a workgroup
 template <int THREADS> constexpr int BN_ROWS = BN_GROUP<THREADS> / THREADS;      // rows it has in hand
 
-template <typename T, int THREADS, int CH, int VEC, bool AHEAD>
+template <typename T, int THREADS, int CH, bool AHEAD>
 __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a) {
   constexpr int ROWS = BN_ROWS<THREADS>;
-  using Pieces = BnPieces<T, THREADS, CH, VEC>;
+  using Pieces = BnPieces<T, THREADS, CH>;
+  constexpr int VEC = BN_VEC<T>;
   __shared__ float slots[2][2][1][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = threadIdx.x % THREADS;
@@ -336,12 +368,12 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
   // a piece of a vector: held, or read again
   auto piece = [&](const Pieces& held, const T* from, int c, float (&out)[VEC]) {
     const long long at = ((long long)c * THREADS + t) * VEC;
-    bn_numbers<T, VEC>(AHEAD ? held.raw[c] : bn_raw<T, VEC>(from + at, from ? n - at : 0), out);
+    bn_numbers<T, VEC>(AHEAD ? held.raw[c] : bn_raw<T>(from + at, from ? n - at : 0), out);
   };
   auto fetch = [&](long long row) {
-    nx.load(x + row * a.ldx, n, t);
-    if (block) nb.load(b + row * a.ldb, n, t);
-    if (block && token_gate) ng.load(gate + row * a.gate_stride, n, t);
+    nx.template fetch<AHEAD>(x + row * a.ldx, n, t);
+    if (block) nb.template fetch<AHEAD>(b + row * a.ldb, n, t);
+    if (block && token_gate) ng.template fetch<AHEAD>(gate + row * a.gate_stride, n, t);
   };
   long long row = (long long)blockIdx.x * ROWS + (ROWS > 1 ? threadIdx.x / THREADS : 0);
   if (row >= a.tokens) return;                 // (with THREADS > 64 the whole workgroup)
@@ -352,8 +384,11 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
     channel_gate.load(token_gate ? nullptr : gate, n, t);
   }
   for (int turn = 0; row < a.tokens; row += workers, turn ^= 1) {
-    const Pieces cx = nx, cb = nb, cg = ng;
+    Pieces cx = nx, cb = nb, cg = ng;
     if (AHEAD && row + workers < a.tokens) fetch(row + workers);
+    cx.template settle<AHEAD>(n, t);
+    cb.template settle<AHEAD>(n, t);
+    if (token_gate) cg.template settle<AHEAD>(n, t);
     float v[CH][VEC], sum[1] = {0.0f};
 #pragma unroll
     for (int c = 0; c < CH; c++) bn_numbers<T, VEC>(cx.raw[c], v[c]);
@@ -411,10 +446,11 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
 // A worker (a row's threads) takes every workers-th row and keeps the sums over its rows of the columns its threads
 // hold, which go out as one partial per workgroup and are summed, in their order, by bn_columns_kernel: the same bits
 // every time.  With one gate per channel dgate and dw_post are both multiples of sum dx b / rms(b).
-template <typename T, int THREADS, int CH, int VEC, bool AHEAD, bool TOKEN_GATE>
+template <typename T, int THREADS, int CH, bool AHEAD, bool TOKEN_GATE>
 __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a) {
   constexpr int ROWS = BN_ROWS<THREADS>;
-  using Pieces = BnPieces<T, THREADS, CH, VEC>;
+  using Pieces = BnPieces<T, THREADS, CH>;
+  constexpr int VEC = BN_VEC<T>;
   __shared__ float slots[2][6][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = threadIdx.x % THREADS;
@@ -428,14 +464,14 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
   Pieces w_post, w_pre, channel_gate, nr, nb = {}, nd = {}, ny = {}, ng = {};
   auto piece = [&](const Pieces& held, const T* from, int c, float (&out)[VEC]) {
     const long long at = ((long long)c * THREADS + t) * VEC;
-    bn_numbers<T, VEC>(AHEAD ? held.raw[c] : bn_raw<T, VEC>(from + at, from ? n - at : 0), out);
+    bn_numbers<T, VEC>(AHEAD ? held.raw[c] : bn_raw<T>(from + at, from ? n - at : 0), out);
   };
   auto fetch = [&](long long row) {
-    nr.load(r + row * a.ldx, n, t);
-    if (block) nb.load(b + row * a.ldb, n, t);
-    if (dr) nd.load(dr + row * a.lddr, n, t);
-    if (pre) ny.load(dy + row * a.lddy, n, t);
-    if (TOKEN_GATE && block) ng.load(gate + row * a.gate_stride, n, t);
+    nr.template fetch<AHEAD>(r + row * a.ldx, n, t);
+    if (block) nb.template fetch<AHEAD>(b + row * a.ldb, n, t);
+    if (dr) nd.template fetch<AHEAD>(dr + row * a.lddr, n, t);
+    if (pre) ny.template fetch<AHEAD>(dy + row * a.lddy, n, t);
+    if (TOKEN_GATE && block) ng.template fetch<AHEAD>(gate + row * a.gate_stride, n, t);
   };
   // the sums of a thread's own columns: in registers, or in LDS where rows are long and registers few
   constexpr bool IN_LDS = THREADS >= 512;
@@ -455,8 +491,10 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
   }
   int turn = 0;
   for (long long row = worker; row < a.tokens; row += workers, turn ^= 1) {
-    const Pieces cr = nr, cb = nb, cd = nd, cy = ny, cg = ng;
+    Pieces cr = nr, cb = nb, cd = nd, cy = ny, cg = ng;
     if (AHEAD && row + workers < a.tokens) fetch(row + workers);
+    for (Pieces* p : {&cr, &cb, &cd, &cy}) p->template settle<AHEAD>(n, t);
+    if (TOKEN_GATE) cg.template settle<AHEAD>(n, t);
     float sum[6] = {};
 #pragma unroll
     for (int c = 0; c < CH; c++) {
@@ -481,6 +519,11 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
       }
     }
     bn_sum<THREADS, 6>(sum, slots[turn], lane, wave);
+    // Below, 16-bit entries are widened again: kept wide since the sums they would take twice the registers, more than there
+    // are in rows past 8192 (4096 rows of 16384 bf16, gate per channel: 412 -> 234 us).  The statement keeps the compiler from it.
+    if constexpr (sizeof(T) == 2 && !AHEAD)
+#pragma unroll
+      for (int c = 0; c < CH; c++) asm volatile("" : "+v"(cr.raw[c]), "+v"(cb.raw[c]), "+v"(cd.raw[c]), "+v"(cy.raw[c]), "+v"(cg.raw[c]));
     const float rr = pre ? 1.0f / sqrtf(sum[1] * inv_n + a.eps) : 0.0f;
     const float rb = 1.0f / sqrtf(sum[2] * inv_n + a.eps);
     const float kr = pre ? rr * rr * rr * (sum[0] * inv_n) : 0.0f;
@@ -596,26 +639,13 @@ constexpr long long BN_MAX_DIM = 1LL << 30;
 // per compute unit), so that the next row's loads always have a row to hide behind and partial sums stay few.
 constexpr long long bn_most_groups(int threads) { return threads <= 256 ? 512 : 256; }
 
-// f(threads per row, pieces per thread, entries per piece, next row ahead) for rows of n entries, whose starts are `wide` (on 16
-// bytes) or not; 0 pieces: too long for registers.  Single entries are for fp32 rows of up to 4096: 16-bit ones take a register
-// each as well, twice what they hold, and lose (64M entries in rows of 3003, backward: fp32 312 -> 203 us, bf16 283 ->
-// 1113; fp32 rows of 5001 312 -> 607).
+// f(threads per row, pieces per thread, next row ahead) for rows of n entries; 0 pieces: too long for registers.
 template <typename T, typename F>
-void bn_shape(long long n, bool wide, F&& f) {
+void bn_shape(long long n, F&& f) {
   const long long pieces = (n + BN_VEC<T> - 1) / BN_VEC<T>;
   constexpr int WIDE = sizeof(T) == 4 ? 2 : 1;
   using std::integral_constant;
-  auto call = [&](auto th, auto ch, auto ahead) {
-    constexpr int V = BN_VEC<T>;
-    if constexpr (WIDE == 2 && ahead.value) {
-      if (!wide) {
-        f(th, integral_constant<int, ch.value * V>{}, integral_constant<int, 1>{}, ahead);
-        return;
-      }
-    }
-    f(th, ch, integral_constant<int, V>{}, ahead);
-  };
-#define BN_CASE(TH, CHUNKS, AHEAD) call(integral_constant<int, TH>{}, integral_constant<int, CHUNKS>{}, integral_constant<bool, AHEAD>{})
+#define BN_CASE(TH, CHUNKS, AHEAD) f(integral_constant<int, TH>{}, integral_constant<int, CHUNKS>{}, integral_constant<bool, AHEAD>{})
   if (pieces <= 16) BN_CASE(16, 1, true);
   else if (pieces <= 32) BN_CASE(16, 2, true);
   else if (pieces <= 64) BN_CASE(64, 1, true);
@@ -631,18 +661,9 @@ void bn_shape(long long n, bool wide, F&& f) {
         return;
       }
     }
-    f(integral_constant<int, BN_LONG>{}, integral_constant<int, 0>{}, integral_constant<int, 1>{}, integral_constant<bool, false>{});
+    f(integral_constant<int, BN_LONG>{}, integral_constant<int, 0>{}, integral_constant<bool, false>{});
   }
 #undef BN_CASE
-}
-// Whether every array's rows start on 16 bytes.
-template <typename T>
-bool bn_wide(const BnArgs& a) {
-  const void* arrays[] = {a.x, a.b, a.r, a.y, a.dr, a.dy, a.dx, a.db, a.dgate, a.gate_stride ? a.gate : nullptr};
-  const long long strides[] = {a.ldx, a.ldb, a.ldr, a.ldy, a.lddr, a.lddy, a.lddx, a.lddb, a.dgate_stride, a.gate_stride};
-  for (int i = 0; i < 10; i++)
-    if (arrays[i] && (!aligned(arrays[i], 16) || (a.tokens > 1 && strides[i] % BN_VEC<T> != 0))) return false;
-  return true;
 }
 
 long long bn_groups(int threads, long long tokens) {
@@ -653,12 +674,12 @@ long long bn_groups(int threads, long long tokens) {
 
 template <typename T>
 int run_forward(const BnArgs& a, hipStream_t stream) {
-  bn_shape<T>(a.n, bn_wide<T>(a), [&](auto th, auto ch, auto vec, auto ahead) {
+  bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
     mark(stream);
     if constexpr (ch.value == 0)
       launch(bn_forward_long_kernel<T>, dim3((unsigned)a.tokens), dim3(BN_LONG), stream, a);
     else
-      launch(bn_forward_kernel<T, th.value, ch.value, vec.value, ahead.value>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
+      launch(bn_forward_kernel<T, th.value, ch.value, ahead.value>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
   });
   mark(stream);
   return launch_status();
@@ -666,7 +687,7 @@ int run_forward(const BnArgs& a, hipStream_t stream) {
 
 template <typename T>
 int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate, float* dw_pre, hipStream_t stream) {
-  bn_shape<T>(a.n, bn_wide<T>(a), [&](auto th, auto ch, auto vec, auto ahead) {
+  bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
     const long long groups = bn_groups(th.value, a.tokens);
     const dim3 grid((unsigned)groups), block(BN_GROUP<th.value>);
     if (groups > 0) {
@@ -675,8 +696,8 @@ int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate,
         if (token_gate) launch(bn_backward_long_kernel<T, true>, grid, block, stream, a);
         else launch(bn_backward_long_kernel<T, false>, grid, block, stream, a);
       } else {
-        if (token_gate) launch(bn_backward_kernel<T, th.value, ch.value, vec.value, ahead.value, true>, grid, block, stream, a);
-        else launch(bn_backward_kernel<T, th.value, ch.value, vec.value, ahead.value, false>, grid, block, stream, a);
+        if (token_gate) launch(bn_backward_kernel<T, th.value, ch.value, ahead.value, true>, grid, block, stream, a);
+        else launch(bn_backward_kernel<T, th.value, ch.value, ahead.value, false>, grid, block, stream, a);
       }
     }
     if (a.want_post || a.want_gate || a.want_pre) {
@@ -730,12 +751,12 @@ BnArgs bn_start(const mlproj_norm_block* k) {
 size_t bn_workspace(long long tokens, long long n) {
   // the most workgroups any storage type has
   long long most = 1;
-  auto count = [&](auto th, auto, auto, auto) {
+  auto count = [&](auto th, auto, auto) {
     const long long groups = bn_groups(th.value, tokens);
     most = groups > most ? groups : most;
   };
-  bn_shape<bf16_t>(n, true, count);
-  bn_shape<float>(n, true, count);
+  bn_shape<bf16_t>(n, count);
+  bn_shape<float>(n, count);
   return (size_t)most * n * 2 * sizeof(float) + 256;
 }
 
