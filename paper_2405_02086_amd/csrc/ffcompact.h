@@ -10,7 +10,9 @@ namespace mlproj {
 // What the projection leaves of a weight matrix is a set of whole columns, scattered over its rows.  They are packed
 // side by side in their order; their number is known on the device only, so kernels are launched for m columns and
 // workgroups past the kept ones leave at once.  The number is filled up to a multiple of 8 with columns of zeros,
-// which keeps packed rows in whole 16-byte pieces.
+// which keeps packed rows in whole 16-byte pieces.  Bound by HBM and, where a wavefront's lanes scatter, by its
+// requests: 4096 x 4096 -> 16384 bf16 backward with 40 % kept spends 11 + 88 + 48 + 124 us of 1420 here (index; weights and
+// dH packed; gradients out, zeros included); without a mask it takes 2840.
 // position[c], c = 0 .. m: where the caller's column c went, p, or ~p if it was pruned, with p the number of
 // kept columns before it either way.
 constexpr int FC_THREADS = 1024, FC_OWN = 16;

@@ -13,7 +13,7 @@ namespace mlproj {
 // cutting into bf16 parts, no LDS, no barrier until the wavefronts, which share out the rows, add their sums in a
 // tree (in a fixed order).  Loads take any address.  Workgroups of the same columns and other tokens run on one
 // XCD next to one another and share the weights in its L2.
-// us, staged tiles / this: 16 x 4096 -> 16384 216 / 109 (4.9 TB/s), 16 x 256 -> 128 24 / 7; at 64 tokens the tiles win, 247
+// us, staged tiles / this: 16 x 4096 -> 16384 216 / 108 (5 TB/s), 16 x 256 -> 128 24 / 7; at 64 tokens the tiles win, 192
 // against 315.  (16-bit pieces turned into operands by byte permutes were no faster than the tiles: one token through
 // 4097 x 16383 bf16 110 against 112.)
 constexpr int FK_WAVES = 8, FK_COLS = 64;
@@ -34,7 +34,8 @@ __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
   constexpr int CW = 4, VALUES = 2 * CW * 4;
   __shared__ float sums[FK_WAVES / 2][VALUES][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
-  const long long tiles_n = (p.N + FK_COLS - 1) / FK_COLS, tiles_m = (p.M + 15) / 16;
+  const long long N = p.kept ? *p.kept : p.N;
+  const long long tiles_n = (N + FK_COLS - 1) / FK_COLS, tiles_m = (p.M + 15) / 16;
   // workgroup 8 i + x runs on XCD x: columns x, x + 8, ... there, each with all its tokens in turn
   const long long mine = blockIdx.x >> 3, tn = mine / tiles_m * 8 + (blockIdx.x & 7), row0 = mine % tiles_m * 16;
   if (tn >= tiles_n) return;
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
 #pragma unroll
     for (int i = 0; i < 2; i++)
 #pragma unroll
-      for (int s = 0; s < 8; s++) w[i][s] = fk_load(B[i] + (k0 + s) * p.ldb + col, k0 + s < p.K ? p.N - col : 0);
+      for (int s = 0; s < 8; s++) w[i][s] = fk_load(B[i] + (k0 + s) * p.ldb + col, k0 + s < p.K ? N - col : 0);
     const FfVec8<float> x = ff_load8(X + (row0 + c) * p.lda + k0, row0 + c < p.M ? p.K - k0 : 0);
 #pragma unroll
     for (int i = 0; i < 2; i++)
@@ -82,15 +83,15 @@ __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
   for (int e = threadIdx.x; e < rows * (FK_COLS / 4); e += FK_WAVES * 64) {
     const int t = e / (FK_COLS / 4), in = e % (FK_COLS / 4) * 4;
     const long long at = col0 + in;
-    if (at >= p.N) continue;
+    if (at >= N) continue;
     f32x4 v[2];
 #pragma unroll
     for (int i = 0; i < 2; i++)
 #pragma unroll
       for (int q = 0; q < 4; q++) v[i][q] = sums[0][(i * CW + (in + q) % CW) * 4 + t % 4][t / 4 * 16 + (in + q) / CW];
     FfVec4<float> d = {};
-    if constexpr (EPI == FF_GRAD) d = ff_upstream<float>(p, row0 + t, at, p.N);
-    ff_finish<EPI, true, float>(p, row0 + t, at, p.N, v[0], v[1], d);
+    if constexpr (EPI == FF_GRAD) d = ff_upstream<float>(p, row0 + t, at, N);
+    ff_finish<EPI, true, float>(p, row0 + t, at, N, v[0], v[1], d);
   }
 }
 

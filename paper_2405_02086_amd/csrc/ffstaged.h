@@ -12,12 +12,16 @@ namespace mlproj {
 // columns of both), each wavefront 64 x 64 of them, in steps of 32 along K.  The next step's operands are
 // loaded into registers while the matrix cores work on the present one in LDS.  Loads take any address, and
 // what lies outside the matrix is filled with zeros element by element, so nothing is asked of sizes,
-// strides or alignment.
+// strides or alignment.  16-bit elements come here only where copying them into aligned rows costs more than it saves
+// (ff_pads): a step of a tile takes two to three times the direct tiles' (2047 x 2047 -> 4095 bf16 forward 169 us here, 81 with copies,
+// the copies included).
 //
 // fp32 goes through the bf16 matrix cores: an element is cut into three bf16 parts of 8 significant bits each
 // (x = p0 + p1 + p2 exactly, by truncation), and a product of two elements is summed from the six products of
 // parts that reach 2^-16 of it.  What is left out is 2^-24 of a product on average (2^-21 at most), and the sums are
-// fp32 throughout.  Six bf16 products cost 6/16 of what the chip's fp32 matrix instructions would.
+// fp32 throughout.  Six bf16 products cost 6/16 of what the chip's fp32 matrix instructions would.  Bound by the vector
+// instructions that cut: 2048 x 2048 -> 4096 fp32 runs at 192 TFLOP/s forward and 195 backward, the library's plain products at
+// 150 to 154.  Largest error of G over 7467 x 488 -> 1024: 3.3e-7 rms, the library's 4.0e-7.
 // (A part past the range of bf16's exponent, below 2^-126, is lost: an absolute error no sum can see.  The remainder of an
 // infinity is a NaN, so an infinity makes the sums that it is part of NaN.)
 constexpr int FS_M = 128, FS_N = 128, FS_K = 32, FS_THREADS = 256;

@@ -53,7 +53,7 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int 
     int splits = 1;
     const long long groups = ff_cdiv(N, FK_COLS) * ff_cdiv(M, 16);
     while (groups * splits < 512 && steps > FK_WAVES * splits && splits < 64) splits *= 2;
-    return {3, splits, 0.0, false};
+    return {3, splits, LAUNCH + 32.0 * steps * N * 2 * 4 / 4.9e6, false};      // the weights, once
   }
   FfPlan best{2, 1, 1e30, false};
   const double planes = 4.0 * M * N * (dual ? 2 : 1);

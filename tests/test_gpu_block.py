@@ -529,6 +529,24 @@ def test_gated_ff_fp32_larger(mp):
                 blocks_close(t, want[name], e, name)
 
 
+def test_gated_ff_fp32_few_tokens_packed(mp):
+    tokens, n, m = 9, 4096, 12004
+    assert mp.gated_ff_route(torch.float32, 1, tokens, n, m)["packed"] and mp.gated_ff_route(torch.float32, 1, tokens, n, m)["kind"] == 3
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    new = lambda r, c, s=1.0: torch.randn(r, c, generator=gen, device="cuda") * s  # noqa: E731
+    X, Wg, Wu, dH = new(tokens, n), new(n, m, n ** -0.5), new(n, m, n ** -0.5), new(tokens, m)
+    for keep in (0.0, 0.4, 1.0):
+        mask = (torch.rand(m, generator=gen, device="cuda") < keep).to(torch.uint8)
+        got = mp.gated_ff_backward(dH, X, Wg, Wu, mask=mask)
+        if not keep:
+            assert not any(t.any() for t in got)
+            continue
+        want = exact_block(X, Wg, Wu, dH, "silu", mask)
+        for name, t in zip(("dX", "dWg", "dWu"), got):
+            blocks_close(t, want[name], 100 * U32, name)
+
+
 def test_block_calls_can_be_captured_in_a_hip_graph(mp):
     rng = np.random.default_rng(16)
     for tokens, n, m, dtype in ((1, 2000, 520, "bf16"), (300, 700, 1000, "bf16"), (20, 300, 200, "f32"), (2100, 1032, 4168, "f16")):
