@@ -520,8 +520,10 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
     }
     bn_sum<THREADS, 6>(sum, slots[turn], lane, wave);
     // Below, 16-bit entries are widened again: kept wide since the sums they would take twice the registers, more than there
-    // are in rows past 8192 (4096 rows of 16384 bf16, gate per channel: 412 -> 234 us).  The statement keeps the compiler from it.
-    if constexpr (sizeof(T) == 2 && !AHEAD)
+    // are in rows past 8192 (4096 rows of 16384 bf16, gate per channel: 412 -> 234 us), or than two workgroups of a compute unit
+    // have (64M entries in rows of 1024 bf16: 180 -> 165 us).  The statement keeps the compiler from it; elsewhere it costs
+    // up to 6 %.
+    if constexpr (sizeof(T) == 2 && (!AHEAD || THREADS == 64))
 #pragma unroll
       for (int c = 0; c < CH; c++) asm volatile("" : "+v"(cr.raw[c]), "+v"(cb.raw[c]), "+v"(cd.raw[c]), "+v"(cy.raw[c]), "+v"(cg.raw[c]));
     const float rr = pre ? 1.0f / sqrtf(sum[1] * inv_n + a.eps) : 0.0f;
@@ -635,7 +637,7 @@ __global__ __launch_bounds__(1024) void bn_columns_kernel(BnArgs a, int workers,
 
 // ------------------------------------------------------------------ plan
 constexpr long long BN_MAX_DIM = 1LL << 30;
-// Most workgroups of a pass: as many as are resident at once (two of 256 threads with 200 registers, one larger one,
+// Most workgroups of a pass: as many as are resident at once (two of 256 threads with up to 256 registers, one larger one,
 // per compute unit), so that the next row's loads always have a row to hide behind and partial sums stay few.
 constexpr long long bn_most_groups(int threads) { return threads <= 256 ? 512 : 256; }
 
