@@ -94,9 +94,12 @@ __global__ __launch_bounds__(256) void ff_move_kernel(FcArrays a) {
     if (PACK && p >= 0) source[p - p0] = (short)(t8 + i);
   }
   if (PACK) __syncthreads();
-  // the last segment also writes the columns of zeros that fill the packed rows up
+  // the last segment also writes the columns of zeros that fill the packed rows up: behind a segment that was kept whole
+  // up to seven of them lie past the eight columns per thread and are written on their own (`past`)
   const int filled = PACK ? (c1 == a.cols ? *a.kept - p0 : packed) : wide;
   const int in = PACK ? wide : packed, out = filled;
+  const int past_row = threadIdx.x / 8, past = FC_COLS + threadIdx.x % 8;
+  const bool writes_past = PACK && past_row < FC_ROWS && past < out;
   from += PACK ? c0 : p0;
   to += PACK ? p0 : c0;
   int pick[8];
@@ -130,6 +133,7 @@ __global__ __launch_bounds__(256) void ff_move_kernel(FcArrays a) {
           if (t8 + i < out) at[i] = w.v[i];
       }
     }
+    if (writes_past && r0 + past_row < rows) to[(r0 + past_row) * ld_to + past] = (T)0.0f;
   }
 }
 

@@ -594,3 +594,35 @@ def test_the_example_learns_prunes_and_answers_in_four_bits(mp):
     assert out["last_loss"] < 0.75 * out["first_loss"]
     assert 0 < out["kept"] < out["channels"]
     assert out["four_bit_error"] < 0.2
+
+
+# ---------------------------------------------------------------- lightly pruned blocks whose channels are packed
+
+FILLS = [("bf16", 1024, 1032, 4096, 1), ("bf16", 1024, 1032, 4096, 3), ("f16", 1024, 1032, 4095, 1), ("bf16", 512, 2048, 6144, 7),
+         ("f32", 256, 512, 4096, 1), ("f32", 256, 512, 6144, 3)]
+
+
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("case", range(len(FILLS)))
+def test_packed_channels_are_filled_up_with_zeros(mp, case, saved):
+    """Only the first few channels are pruned, so that the kept ones end inside a piece behind a full last segment of columns.
+    The workspace holds NaN: what is summed over and not written shows."""
+    dtype, tokens, n, m, pruned = FILLS[case]
+    assert mp.gated_ff_route(TYPES[dtype], 1, tokens, n, m)["packed"]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(60 + case)
+    new = lambda r, c, s=1.0: (torch.randn(r, c, generator=gen, device="cuda") * s).to(TYPES[dtype])  # noqa: E731
+    X, Wg, Wu, dH = new(tokens, n), new(n, m, n ** -0.5), new(n, m, n ** -0.5), new(tokens, m)
+    mask = torch.ones(m, dtype=torch.uint8, device="cuda")
+    mask[:pruned] = 0
+    want = exact_block(X, Wg, Wu, dH, "silu", mask)
+    G = U = None
+    if saved:
+        G, U = want["G"].to(TYPES[dtype]), want["U"].to(TYPES[dtype])
+    ws = mp.Workspace(mp.gated_ff_workspace_bytes(tokens, n, m, TYPES[dtype], True))
+    ws.buf.fill_(255)
+    # two roundings (dG and dU, the result), saved pre-activations a third; fp32: sums of 2 m terms in a random walk
+    e = 120 * U32 if dtype == "f32" else 1.5 * ROUND[dtype]
+    for name, t in zip(("dX", "dWg", "dWu"), mp.gated_ff_backward(dH, X, Wg, Wu, mask=mask, G=G, U=U, workspace=ws)):
+        assert torch.isfinite(t).all(), name
+        blocks_close(t, want[name], e, name)
