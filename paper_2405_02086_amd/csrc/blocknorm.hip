@@ -628,9 +628,10 @@ __global__ __launch_bounds__(1024) void bn_columns_kernel(BnArgs a, int workers,
     if (token_gate) {
       if (a.want_post) dw_post[col] = s0;
     } else {
-      // s0 = sum of scale dx b / rms(b)
-      if (a.want_post) dw_post[col] = s0 * (float)static_cast<const T*>(a.gate)[col];
-      if (a.want_gate) dgate[col] = s0 * (float)static_cast<const T*>(a.w_post)[col];
+      // s0 = sum of scale dx b / rms(b); without tokens the gate need not be there, and may hold anything
+      const bool some = workers > 0;
+      if (a.want_post) dw_post[col] = some ? s0 * (float)static_cast<const T*>(a.gate)[col] : 0.0f;
+      if (a.want_gate) dgate[col] = some ? s0 * (float)static_cast<const T*>(a.w_post)[col] : 0.0f;
     }
   }
 }

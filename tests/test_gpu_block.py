@@ -626,3 +626,21 @@ def test_packed_channels_are_filled_up_with_zeros(mp, case, saved):
     for name, t in zip(("dX", "dWg", "dWu"), mp.gated_ff_backward(dH, X, Wg, Wu, mask=mask, G=G, U=U, workspace=ws)):
         assert torch.isfinite(t).all(), name
         blocks_close(t, want[name], e, name)
+
+
+def test_block_norm_without_tokens_reads_nothing(mp):
+    """Sums over no tokens are zeros whatever the vectors hold, and the gate need not be there."""
+    import ctypes
+    for dtype in TYPES.values():
+        e = torch.empty(0, 72, dtype=dtype, device="cuda")
+        bad = torch.full((72,), float("nan"), dtype=dtype, device="cuda")
+        for t in mp.block_norm_backward(e, e, e, e, bad, bad, bad)[2:]:
+            assert not t.any()
+        ws = mp.Workspace(mp.block_norm_workspace_bytes(0, 72))
+        sums = torch.full((3, 72), 7.0, device="cuda")
+        block = mp.NormBlock(0, 72, None, 0, bad.data_ptr(), None, 0, bad.data_ptr(), 1.0, 1e-6)
+        st = mp.lib().block_norm_backward(mp._storage(dtype), ctypes.byref(block), None, 0, None, 0, None, 0, None, 0, None, 0,
+                                          sums[0].data_ptr(), sums[1].data_ptr(), 0, sums[2].data_ptr(), ws.buf.data_ptr(), ws.nbytes,
+                                          torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert st == 0 and not sums.any()
