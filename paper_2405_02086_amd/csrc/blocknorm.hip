@@ -744,8 +744,10 @@ int bn_inputs(const mlproj_norm_block* k, int es) {
 
 BnArgs bn_start(const mlproj_norm_block* k) {
   BnArgs a{};
-  a.b = k->w_post ? k->b : nullptr; a.ldb = k->ldb;
-  a.w_post = k->w_post; a.gate = k->gate; a.gate_stride = k->gate_stride; a.w_pre = k->w_pre;
+  const bool block = k->w_post != nullptr;     // without it b and gate are not used: the kernels go by these pointers
+  a.b = block ? k->b : nullptr; a.ldb = k->ldb;
+  a.w_post = k->w_post; a.w_pre = k->w_pre;
+  a.gate = block ? k->gate : nullptr; a.gate_stride = block ? k->gate_stride : 0;
   a.tokens = k->tokens; a.n = k->n;
   a.scale = k->scale; a.eps = k->eps;
   return a;

@@ -644,3 +644,25 @@ def test_block_norm_without_tokens_reads_nothing(mp):
                                           torch.cuda.current_stream().cuda_stream)
         torch.cuda.synchronize()
         assert st == 0 and not sums.any()
+
+
+def test_block_norm_without_a_block_does_not_use_its_gate(mp):
+    """w_post = NULL: b and gate may be anything, at any address."""
+    import ctypes
+    rng = np.random.default_rng(18)
+    for n in (40, 3000, 9000, 17000):
+        X, _ = matrix(rng, 5, n, "bf16")
+        DY, _ = matrix(rng, 5, n, "bf16")
+        w = matrix(rng, 1, n, "bf16")[0][0]
+        unused = torch.full((2 * n + 16,), 255, dtype=torch.uint8, device="cuda")
+        _, want = mp.block_norm(X, w_pre=w)
+        dx, _, _, _, dw = mp.block_norm_backward(None, DY, X, w_pre=w)
+        ws = mp.Workspace(mp.block_norm_workspace_bytes(5, n))
+        block = mp.NormBlock(5, n, None, 0, None, unused.data_ptr() + 1, 0, w.data_ptr(), 1.0, 1e-6)
+        y, dx2, dw2 = torch.empty_like(X), torch.empty_like(X), torch.empty_like(dw)
+        stream = torch.cuda.current_stream().cuda_stream
+        assert mp.lib().block_norm_forward(1, ctypes.byref(block), X.data_ptr(), n, None, 0, y.data_ptr(), n, stream) == 0
+        assert mp.lib().block_norm_backward(1, ctypes.byref(block), X.data_ptr(), n, None, 0, DY.data_ptr(), n, dx2.data_ptr(), n, None, 0,
+                                            None, None, 0, dw2.data_ptr(), ws.buf.data_ptr(), ws.nbytes, stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(dx, dx2) and torch.equal(dw, dw2)
