@@ -250,13 +250,34 @@ def _stream(stream):
     return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
+# What a call allocates itself (scratch, results) it allocates on the stream that it runs on: the allocator hands out and takes
+# back memory in the order of the stream it was asked on, and the scratch is given back while the kernels are still to run.
+def _empty_like(t, stream=None):
+    torch = _import_torch()
+    if stream is None:
+        return torch.empty_like(t)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
+
+
+def _new_empty(like, shape, dtype=None, stream=None):
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with _import_torch().cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 class Workspace:
-    """Device scratch for one call at a time; needs no initialisation."""
+    """Device scratch for one call at a time, allocated on `stream` (default: the current one); needs no initialisation."""
 
     def __init__(self, nbytes, device="cuda", stream=None):
-        import torch
+        torch = _import_torch()
         nbytes = (int(nbytes) + 255) // 256 * 256
-        self.buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream is None:
+            self.buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(stream):
+                self.buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
         assert self.buf.data_ptr() % 256 == 0
         self.nbytes = nbytes
 
@@ -273,12 +294,12 @@ class Workspace:
                 "inner_sweeps": sweeps, "inner_pending": pending, "inner_finished": finished}
 
 
-def _prep(Y, X):
+def _prep(Y, X, stream=None):
     torch = _import_torch()
     f32 = torch.float32
     assert Y.is_cuda and Y.dtype is f32 and Y.is_contiguous(), "Y: contiguous fp32 device tensor"
     if X is None:
-        return torch.empty_like(Y)
+        return _empty_like(Y, stream)
     assert X.is_cuda and X.dtype is f32 and X.is_contiguous() and X.shape == Y.shape
     return X
 
@@ -286,7 +307,7 @@ def _prep(Y, X):
 def _bilevel(name, variant, Y, eta, X, workspace, v_out, u_out, stream):
     assert Y.dim() == 2
     n, m = Y.shape
-    X = _prep(Y, X)
+    X = _prep(Y, X, stream)
     if workspace is None:
         workspace = Workspace.for_call(variant, n, m, device=Y.device, stream=stream)
     st = getattr(lib(), name)(Y.data_ptr(), X.data_ptr(), n, m, eta, workspace.buf.data_ptr(), workspace.nbytes,
@@ -339,7 +360,7 @@ def bilevel_apply(variant, Y, X, workspace, u_out=None, stream=None):
 def trilevel_proj_l1infinf(Y, eta, X=None, workspace=None, v_out=None, u_out=None, stream=None):
     assert Y.dim() == 3
     d0, d1, d2 = Y.shape
-    X = _prep(Y, X)
+    X = _prep(Y, X, stream)
     if workspace is None:
         workspace = Workspace.for_call(L1INFINF, d0, d1, d2, device=Y.device, stream=stream)
     st = lib().trilevel_proj_l1infinf(_ptr(Y), _ptr(X), d0, d1, d2, ctypes.c_float(eta),
@@ -357,7 +378,7 @@ def bilevel_proj_pq(p, q, Y, eta, X=None, workspace=None, v_out=None, u_out=None
     """BP^{p,q}: p in {1, 2, "inf"} (outer), q in {"inf", 1, 2} (per column)."""
     assert Y.dim() == 2
     n, m = Y.shape
-    X = _prep(Y, X)
+    X = _prep(Y, X, stream)
     variant = {"inf": L1INF, 1: L11, 2: L12}[q]
     if workspace is None:
         workspace = Workspace.for_call(variant, n, m, device=Y.device, stream=stream)
@@ -379,7 +400,7 @@ def bilevel_proj_stored(Y, eta, q, p=1, X=None, workspace=None, v_out=None, u_ou
     assert Y.is_cuda and Y.dim() == 2 and Y.is_contiguous() and Y.dtype in storages
     n, m = Y.shape
     if X is None:
-        X = torch.empty_like(Y)
+        X = _empty_like(Y, stream)
     assert X.is_cuda and X.dtype == Y.dtype and X.is_contiguous() and X.shape == Y.shape
     assert mask_out is None or (mask_out.dtype == torch.uint8 and mask_out.numel() >= m)
     variant = {"inf": L1INF, 1: L11, 2: L12}[q]
@@ -402,7 +423,7 @@ def bilevel_proj_weighted(Y, eta, q, weights, X=None, workspace=None, v_out=None
     n, m = Y.shape
     assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == m
     if X is None:
-        X = torch.empty_like(Y)
+        X = _empty_like(Y, stream)
     assert X.is_cuda and X.dtype == Y.dtype and X.is_contiguous() and X.shape == Y.shape
     assert mask_out is None or (mask_out.dtype == torch.uint8 and mask_out.numel() >= m)
     variant = {"inf": L1INF, 1: L11, 2: L12}[q]
@@ -422,7 +443,7 @@ def trilevel_proj_stored(Y, eta, X=None, workspace=None, v_out=None, u_out=None,
     assert Y.is_cuda and Y.dim() == 3 and Y.is_contiguous() and Y.dtype in storages
     d0, d1, d2 = Y.shape
     if X is None:
-        X = torch.empty_like(Y)
+        X = _empty_like(Y, stream)
     assert X.is_cuda and X.dtype == Y.dtype and X.is_contiguous() and X.shape == Y.shape
     if workspace is None:
         workspace = Workspace.for_call("tri", d0, d1, d2, device=Y.device, stream=stream)
@@ -437,9 +458,9 @@ class PreparedBatch:
     """The argument block of a bilevel_proj_batch call, marshalled once: a training loop projects
     the same buffers after every step, and filling the block costs more host time than the
     call.  Calling the object enqueues the batch; `.X` lists the output tensors.  It keeps every
-    tensor it points to alive."""
+    tensor it points to alive.  `stream`: what it allocates itself is for calls on that stream."""
 
-    def __init__(self, Ys, etas, q, p=1, Xs=None, workspaces=None, v_outs=None, u_outs=None, mask_outs=None):
+    def __init__(self, Ys, etas, q, p=1, Xs=None, workspaces=None, v_outs=None, u_outs=None, mask_outs=None, stream=None):
         import torch
         storages = {torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float16: STORE_F16}
         count = len(Ys)
@@ -456,10 +477,10 @@ class PreparedBatch:
             n, m = Y.shape
             X = pick(Xs, i)
             if X is None:
-                X = torch.empty_like(Y)
+                X = _empty_like(Y, stream)
             assert X.is_cuda and X.dtype == Y.dtype and X.is_contiguous() and X.shape == Y.shape
             # every problem needs a workspace of its own
-            ws = pick(workspaces, i) or Workspace.for_call(self.variant, n, m, device=Y.device)
+            ws = pick(workspaces, i) or Workspace.for_call(self.variant, n, m, device=Y.device, stream=stream)
             self.keep.append(ws)
             self.X.append(X)
             pr = self.problems[i]
@@ -482,8 +503,9 @@ def bilevel_proj_batch(Ys, etas, q, p=1, Xs=None, workspaces=None, v_outs=None, 
     """Independent BP^{p,q} projections of the matrices in Ys (same dtype, any shapes) with radii
     etas, through bilevel_proj_batch; returns the list of X tensors.  Optional lists give the
     per-problem X, workspace, v_out, u_out and mask_out."""
-    return PreparedBatch(Ys, etas, q, p=p, Xs=Xs, workspaces=workspaces, v_outs=v_outs, u_outs=u_outs,
-                         mask_outs=mask_outs)(stream)
+    batch = PreparedBatch(Ys, etas, q, p=p, Xs=Xs, workspaces=workspaces, v_outs=v_outs, u_outs=u_outs,
+                          mask_outs=mask_outs, stream=stream)
+    return batch(stream)
 
 
 NORM_INF, NORM_L1, NORM_L2 = 0, 1, 2
@@ -501,11 +523,11 @@ def multilevel_workspace_bytes(shape):
 def multilevel_proj(Y, norms, eta, X=None, workspace=None, v_out=None, u_out=None, stream=None, p=1):
     """norms: inner norms, innermost (last axis) first, each "inf", 1 or 2; groups on axis 0;
     p: outermost norm (1, 2 or "inf")."""
-    X = _prep(Y, X)
+    X = _prep(Y, X, stream)
     shape = tuple(Y.shape)
     assert len(norms) == len(shape) - 1
     if workspace is None:
-        workspace = Workspace(multilevel_workspace_bytes(shape), device=Y.device)
+        workspace = Workspace(multilevel_workspace_bytes(shape), device=Y.device, stream=stream)
     dims = (ctypes.c_longlong * len(shape))(*shape)
     nrm = (ctypes.c_int * len(norms))(*[_NORMS[q] for q in norms])
     if p == 1:
@@ -524,12 +546,12 @@ def multilevel_proj_stored(Y, norms, eta, p=1, X=None, workspace=None, v_out=Non
     storages = {torch.float32: STORE_F32, torch.bfloat16: STORE_BF16, torch.float16: STORE_F16}
     assert Y.is_cuda and Y.is_contiguous() and Y.dtype in storages
     if X is None:
-        X = torch.empty_like(Y)
+        X = _empty_like(Y, stream)
     assert X.is_cuda and X.dtype == Y.dtype and X.is_contiguous() and X.shape == Y.shape
     shape = tuple(Y.shape)
     assert len(norms) == len(shape) - 1
     if workspace is None:
-        workspace = Workspace(multilevel_workspace_bytes(shape), device=Y.device)
+        workspace = Workspace(multilevel_workspace_bytes(shape), device=Y.device, stream=stream)
     dims = (ctypes.c_longlong * len(shape))(*shape)
     nrm = (ctypes.c_int * len(norms))(*[_NORMS[q] for q in norms])
     st = lib().multilevel_proj_stored(storages[Y.dtype], _OUTERS[p], _ptr(Y), _ptr(X), len(shape), dims, nrm,
@@ -548,11 +570,11 @@ def multilevel_proj_weighted(Y, norms, eta, weights, X=None, workspace=None, v_o
     shape = tuple(Y.shape)
     assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == shape[0]
     if X is None:
-        X = torch.empty_like(Y)
+        X = _empty_like(Y, stream)
     assert X.is_cuda and X.dtype == Y.dtype and X.is_contiguous() and X.shape == Y.shape
     assert len(norms) == len(shape) - 1
     if workspace is None:
-        workspace = Workspace(multilevel_workspace_bytes(shape), device=Y.device)
+        workspace = Workspace(multilevel_workspace_bytes(shape), device=Y.device, stream=stream)
     dims = (ctypes.c_longlong * len(shape))(*shape)
     nrm = (ctypes.c_int * len(norms))(*[_NORMS[q] for q in norms])
     st = lib().multilevel_proj_weighted(storages[Y.dtype], _ptr(Y), _ptr(X), len(shape), dims, nrm,
@@ -570,10 +592,12 @@ def norm_l1q(Y, variant, workspace=None, v_out=None, stream=None):
     v = _VARIANTS.get(variant, variant)
     if workspace is None:
         workspace = Workspace.for_call(v, n, m, device=Y.device, stream=stream)
-    out = torch.empty(1, dtype=torch.float64, device=Y.device)
+    out = _new_empty(Y, 1, torch.float64, stream)
     st = lib().mlproj_norm_l1q(_ptr(Y), n, m, v, _ptr(workspace.buf), workspace.nbytes, _ptr(out),
                                _ptr(v_out), _stream(stream))
     _check(st, "mlproj_norm_l1q")
+    if stream is not None:
+        stream.synchronize()      # (item() waits for the current stream)
     return float(out.item())
 
 
@@ -603,11 +627,11 @@ def _matrix(t, shape, like, what):
     return t.stride(0) if rows > 1 else max(cols, t.stride(0))
 
 
-def _result(t, shape, like, what):
+def _result(t, shape, like, what, stream):
     if t is None:
         if like.shape == shape and like.is_contiguous():
-            return _torch.empty_like(like), shape[1]
-        return like.new_empty(shape), shape[1]
+            return _torch.empty_like(like) if stream is None else _empty_like(like, stream), shape[1]
+        return _new_empty(like, shape, None, stream), shape[1]
     return t, _matrix(t, shape, like, what)
 
 
@@ -646,14 +670,14 @@ def gated_ff(X, Wg, Wu, act="silu", mask=None, H=None, g_out=None, u_out=None, w
     g_out, u_out: tensors that also receive X Wg and X Wu, for gated_ff_backward."""
     storage = _storage(X.dtype)
     block, tokens, n, m = _gated_block(X, Wg, Wu, mask)
-    H, ldh = _result(H, (tokens, m), X, "H")
+    H, ldh = _result(H, (tokens, m), X, "H", stream)
     ldg = 0
     assert (g_out is None) == (u_out is None), "g_out and u_out: both or neither"
     if g_out is not None:
         ldg = _matrix(g_out, (tokens, m), X, "g_out")
         assert _matrix(u_out, (tokens, m), X, "u_out") == ldg, "g_out and u_out: one row stride"
     if workspace is None:
-        workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, False, mask is not None), device=X.device)
+        workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, False, mask is not None), device=X.device, stream=stream)
     st = lib().gated_ff_forward(storage, _ACTS[act], ctypes.byref(block), H.data_ptr(), ldh, _ptr(g_out), _ptr(u_out),
                                 ldg, workspace.buf.data_ptr(), workspace.nbytes, _stream(stream))
     if st != 0:
@@ -674,13 +698,13 @@ def gated_ff_backward(dH, X, Wg, Wu, act="silu", mask=None, G=None, U=None, dX=N
         ldg = _matrix(G, (tokens, m), X, "G")
         assert _matrix(U, (tokens, m), X, "U") == ldg, "G and U: one row stride"
     if need_dx:
-        dX, lddx = _result(dX, (tokens, n), X, "dX")
+        dX, lddx = _result(dX, (tokens, n), X, "dX", stream)
     if need_dw:
-        dWg, lddw = _result(dWg, (n, m), X, "dWg")
-        dWu, ld = _result(dWu, (n, m), X, "dWu")
+        dWg, lddw = _result(dWg, (n, m), X, "dWg", stream)
+        dWu, ld = _result(dWu, (n, m), X, "dWu", stream)
         assert ld == lddw, "dWg and dWu: one row stride"
     if workspace is None:
-        workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, True, mask is not None), device=X.device)
+        workspace = Workspace(gated_ff_workspace_bytes(tokens, n, m, X.dtype, True, mask is not None), device=X.device, stream=stream)
     st = lib().gated_ff_backward(storage, _ACTS[act], ctypes.byref(block), dH.data_ptr(), ldh, _ptr(G), _ptr(U), ldg,
                                  _ptr(dX) if need_dx else None, lddx, _ptr(dWg) if need_dw else None,
                                  _ptr(dWu) if need_dw else None, lddw, workspace.buf.data_ptr(), workspace.nbytes,
@@ -725,12 +749,12 @@ def block_norm(x, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e-
     if b is None:
         r = x
     else:
-        r, ldr = _result(r, shape, x, "r")
+        r, ldr = _result(r, shape, x, "r", stream)
         at_r = r.data_ptr()
     if w_pre is None:
         y = None
     else:
-        y, ldy = _result(y, shape, x, "y")
+        y, ldy = _result(y, shape, x, "y", stream)
         at_y = y.data_ptr()
     st = lib().block_norm_forward(storage, ctypes.byref(block), x.data_ptr(), ldx, at_r, ldr, at_y, ldy, _stream(stream))
     if st != 0:
@@ -759,23 +783,23 @@ def block_norm_backward(dr, dy, r, b=None, w_post=None, gate=None, w_pre=None, s
     at_dy = at_db = at_post = at_gate = at_pre = dw_post = dgate = dw_pre = None
     if dr is not None:
         lddr = _matrix(dr, shape, r, "dr")
-    dx, lddx = _result(dx, shape, r, "dx")
+    dx, lddx = _result(dx, shape, r, "dx", stream)
     if b is None:
         db = None
     else:
-        db, lddb = _result(db, shape, r, "db")
-        dw_post = r.new_empty(n, dtype=f32)
+        db, lddb = _result(db, shape, r, "db", stream)
+        dw_post = _new_empty(r, n, f32, stream)
         if token_gate:
-            dgate, ldg = _result(None, shape, r, "dgate")
+            dgate, ldg = _result(None, shape, r, "dgate", stream)
         else:
-            dgate = r.new_empty(n, dtype=f32)
+            dgate = _new_empty(r, n, f32, stream)
         at_db, at_post, at_gate = db.data_ptr(), dw_post.data_ptr(), dgate.data_ptr()
     if w_pre is not None:
         lddy = _matrix(dy, shape, r, "dy")
-        dw_pre = r.new_empty(n, dtype=f32)
+        dw_pre = _new_empty(r, n, f32, stream)
         at_dy, at_pre = dy.data_ptr(), dw_pre.data_ptr()
     if workspace is None:
-        workspace = Workspace(block_norm_workspace_bytes(tokens, n), device=r.device)
+        workspace = Workspace(block_norm_workspace_bytes(tokens, n), device=r.device, stream=stream)
     st = lib().block_norm_backward(storage, ctypes.byref(block), r.data_ptr(), ldr, _ptr(dr), lddr, at_dy, lddy, dx.data_ptr(),
                                    lddx, at_db, lddb, at_post, at_gate, ldg, at_pre, workspace.buf.data_ptr(),
                                    workspace.nbytes, _stream(stream))
@@ -811,8 +835,8 @@ def w4_pack(W, group=128, stream=None):
     n, m = W.shape
     ldw = _matrix(W, (n, m), W, "W")
     code_bytes, scale_bytes = w4_bytes(n, m, group)
-    packed = W4(n, m, group, torch.empty(code_bytes, dtype=torch.uint8, device=W.device),
-                torch.empty(scale_bytes // 2, dtype=torch.bfloat16, device=W.device))
+    packed = W4(n, m, group, _new_empty(W, code_bytes, torch.uint8, stream),
+                _new_empty(W, scale_bytes // 2, torch.bfloat16, stream))
     _check(lib().w4_pack(_storage(W.dtype), W.data_ptr(), ldw, packed._ref, _stream(stream)), "w4_pack")
     return packed
 
@@ -821,7 +845,7 @@ def w4_matvec(x, W, y=None, stream=None):
     """y = x W for few tokens (x: tokens x n) and a packed W."""
     storage, tokens = _storage(x.dtype), x.shape[0]
     ldx = _matrix(x, (tokens, W.n), x, "x")
-    y, ldy = _result(y, (tokens, W.m), x, "y")
+    y, ldy = _result(y, (tokens, W.m), x, "y", stream)
     st = lib().w4_matvec(storage, W._ref, x.data_ptr(), ldx, tokens, y.data_ptr(), ldy, _stream(stream))
     if st != 0:
         _check(st, "w4_matvec")
@@ -832,7 +856,7 @@ def w4_gated_matvec(x, Wg, Wu, act="silu", h=None, stream=None):
     """h = act(x Wg) * (x Wu) for few tokens and packed weights of one size and group."""
     storage, tokens = _storage(x.dtype), x.shape[0]
     ldx = _matrix(x, (tokens, Wg.n), x, "x")
-    h, ldh = _result(h, (tokens, Wg.m), x, "h")
+    h, ldh = _result(h, (tokens, Wg.m), x, "h", stream)
     st = lib().w4_gated_matvec(storage, _ACTS[act], Wg._ref, Wu._ref, x.data_ptr(), ldx, tokens, h.data_ptr(), ldh,
                                _stream(stream))
     if st != 0:

@@ -193,3 +193,34 @@ def test_w4_refusals(lib):
     assert lib.w4_gated_matvec(1, 3, R(ok), R(ok), P, 100, 2, P, 40, None) == VARIANT
     assert lib.w4_gated_matvec(1, 0, R(ok), R(packed(m=41)), P, 100, 2, P, 48, None) == DIM
     assert lib.w4_gated_matvec(1, 0, R(ok), R(packed(group=32)), P, 100, 2, P, 48, None) == DIM
+
+
+def test_what_a_call_allocates_belongs_to_its_stream(monkeypatch):
+    """Scratch is given back when a call returns, before its kernels ran: it has to come from the call's stream."""
+    import contextlib
+    import types
+    import torch
+    current, seen = ["default"], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        current.append(stream)
+        yield
+        current.pop()
+
+    def empty(*args, **kw):
+        seen.append(current[-1])
+        return types.SimpleNamespace(data_ptr=lambda: 256)
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch, "empty_like", empty)
+    like = types.SimpleNamespace(shape=(2, 3), is_contiguous=lambda: True, new_empty=empty)
+    binding._import_torch()
+    binding.Workspace(1000)
+    binding.Workspace(1000, stream="side")
+    binding._result(None, (2, 3), like, "same", None)
+    binding._result(None, (2, 3), like, "same", "side")
+    binding._result(None, (2, 4), like, "other", None)
+    binding._result(None, (2, 4), like, "other", "side")
+    assert seen == ["default", "side"] * 3

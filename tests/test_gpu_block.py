@@ -666,3 +666,48 @@ def test_block_norm_without_a_block_does_not_use_its_gate(mp):
                                             None, None, 0, dw2.data_ptr(), ws.buf.data_ptr(), ws.nbytes, stream) == 0
         torch.cuda.synchronize()
         assert torch.equal(y, want) and torch.equal(dx, dx2) and torch.equal(dw, dw2)
+
+
+def pools(tensors):
+    """The streams whose memory the tensors lie in."""
+    at = {}
+    for seg in torch.cuda.memory_snapshot():
+        for t in tensors:
+            if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+                at[t.data_ptr()] = seg["stream"]
+    return [at[t.data_ptr()] for t in tensors]
+
+
+def test_calls_given_a_stream_allocate_on_it(mp, monkeypatch):
+    """Every call with stream=, results and scratch alike, and a norm that is read back."""
+    side = torch.cuda.Stream()
+    scratch = []
+    init = mp.Workspace.__init__
+
+    def noted(self, *args, **kw):
+        init(self, *args, **kw)
+        scratch.append(self.buf)
+
+    monkeypatch.setattr(mp.Workspace, "__init__", noted)
+    rng = np.random.default_rng(19)
+    X, Wg = matrix(rng, 20, 72, "bf16")[0], matrix(rng, 72, 136, "bf16")[0]
+    dH, w, Y = matrix(rng, 20, 136, "bf16")[0], matrix(rng, 1, 72, "bf16")[0][0], matrix(rng, 40, 24, "f32")[0]
+    cube, weights = matrix(rng, 6, 20, "f32")[0].view(6, 4, 5), torch.ones(24, device="cuda")
+    torch.cuda.synchronize()
+    kw = dict(stream=side)
+    packed = mp.w4_pack(Wg, **kw)
+    H = mp.gated_ff(X, Wg, Wg, **kw)
+    outs = [packed.codes, packed.scales, H, *mp.gated_ff_backward(dH, X, Wg, Wg, **kw), *mp.block_norm(X, X, w, w, w, **kw),
+            *mp.block_norm_backward(None, X, X, X, w, w, w, **kw), *mp.block_norm_backward(None, X, X, X, w, X, w, **kw),
+            mp.w4_matvec(X, packed, **kw), mp.w4_gated_matvec(X, packed, packed, **kw),
+            mp.bilevel_proj_l1inf(Y, 1.0, **kw), mp.bilevel_proj_pq(2, 1, Y, 1.0, **kw), mp.bilevel_proj_stored(X, 1.0, "inf", **kw),
+            mp.bilevel_proj_weighted(Y, 1.0, 2, weights, **kw), mp.trilevel_proj_l1infinf(cube, 1.0, **kw),
+            mp.trilevel_proj_stored(cube, 1.0, **kw), *mp.bilevel_proj_batch([Y, Y], [1.0, 2.0], 2, **kw),
+            mp.multilevel_proj(cube, [2, "inf"], 1.0, **kw), mp.multilevel_proj_stored(cube, [2, "inf"], 1.0, **kw),
+            mp.multilevel_proj_weighted(cube, [2, "inf"], 1.0, weights[:6], **kw)]
+    norm = mp.norm_l1q(Y, "l12", **kw)
+    assert abs(norm - float(Y.double().norm(dim=0).sum())) < 1e-4 * norm
+    assert len(scratch) > 10
+    assert set(pools(outs + scratch)) == {side.cuda_stream}
+    torch.cuda.synchronize()
+    assert torch.equal(H, mp.gated_ff(X, Wg, Wg))
