@@ -776,6 +776,13 @@ def block_norm_backward(dr, dy, r, b=None, w_post=None, gate=None, w_pre=None, s
     assert r.dim() == 2
     storage = _storage(r.dtype)
     f32 = _torch.float32
+    if b is not None and gate.dim() == 2 and gate.stride(0) == 0 and gate.shape[0] > 1:
+        # one row seen by all tokens: to the library a stride of 0 is a gate per channel, whose gradient is one row as well
+        if stream is None:
+            gate = gate.contiguous()
+        else:
+            with _torch.cuda.stream(stream):
+                gate = gate.contiguous()
     block, shape, token_gate = _norm_block(r, b, w_post, gate, w_pre, scale, eps)
     tokens, n = shape
     ldr = _matrix(r, shape, r, "r")

@@ -711,3 +711,22 @@ def test_calls_given_a_stream_allocate_on_it(mp, monkeypatch):
     assert set(pools(outs + scratch)) == {side.cuda_stream}
     torch.cuda.synchronize()
     assert torch.equal(H, mp.gated_ff(X, Wg, Wg))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 40, 1000, 17000])
+def test_block_norm_gate_shared_by_all_tokens_as_a_view(mp, dtype, n):
+    """A tokens x n gate whose rows are one row (stride 0) has a gradient of its own for every token."""
+    rng = np.random.default_rng(20)
+    (R, _), (B, _), (WP, _), (G, _), (WQ, _) = norm_case(rng, 7, n, dtype, False, 0)
+    DR, DY = matrix(rng, 7, n, dtype)[0], matrix(rng, 7, n, dtype)[0]
+    shared = G[None].expand(7, n)
+    assert shared.stride(0) == 0
+    whole = shared.contiguous()
+    for a, b in zip(mp.block_norm(R, B, WP, shared, WQ), mp.block_norm(R, B, WP, whole, WQ)):
+        assert torch.equal(a, b)
+    want = mp.block_norm_backward(DR, DY, R, B, WP, whole, WQ)
+    got = mp.block_norm_backward(DR, DY, R, B, WP, shared, WQ)
+    assert got[3].shape == (7, n) and got[3].dtype == TYPES[dtype]
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
