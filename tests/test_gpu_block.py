@@ -730,3 +730,38 @@ def test_block_norm_gate_shared_by_all_tokens_as_a_view(mp, dtype, n):
     assert got[3].shape == (7, n) and got[3].dtype == TYPES[dtype]
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def gelu_tail_bounds(g, dtype):
+    """Phi(g) for negative g and the relative error its computation may have.  16 bits: that of Abramowitz and Stegun 7.1.26 as a
+    form of Phi(-|g|), here in 64 bits, the roundings of its terms and of the exponential's argument; fp32: those of erfc's
+    argument, g^2 times over, and 16 of the function's."""
+    from scipy import special
+    phi, x = special.ndtr(g), np.abs(g) * np.sqrt(0.5)
+    if dtype == "f32":
+        return phi, (3 * g * g + 16) * U32
+    c = np.array([0.254829592, -0.284496736, 1.421413741, -1.453152027, 1.061405429])
+    t = 1 / (1 + 0.3275911 * x)
+    terms = c[:, None] * t[None] ** np.arange(1, 6)[:, None]
+    formula = 0.5 * terms.sum(0) * np.exp(-x * x)
+    return phi, np.abs(formula / phi - 1) + (12 * np.abs(terms).sum(0) / terms.sum(0) + 3 * g * g + 16) * U32
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gelu_keeps_its_digits_where_it_fades_out(mp, dtype):
+    """One token per pre-activation g from -6 to 0, G = g and U = 2^13 exactly: gelu(g) and its slope to their own digits."""
+    g = np.concatenate([-np.linspace(0.03, 6, 700), -np.arange(1, 24) / 4.0])
+    g = torch.from_numpy(g).to(TYPES[dtype]).double().numpy()
+    u = 2.0 ** 13
+    X = torch.from_numpy(np.stack([g, np.ones_like(g)], 1)).to(TYPES[dtype]).cuda()
+    Wg = torch.tensor([[1.0], [0.0]], dtype=TYPES[dtype], device="cuda")
+    Wu = torch.tensor([[0.0], [u]], dtype=TYPES[dtype], device="cuda")
+    phi, rel = gelu_tail_bounds(g, dtype)
+    density = np.exp(-0.5 * g * g) / np.sqrt(2 * np.pi)
+    H = g * phi * u
+    close(mp.gated_ff(X, Wg, Wu, act="gelu"), H[:, None], (rel * np.abs(H) + 4 * U32 * np.abs(H) + stored(H, dtype))[:, None], "H")
+    # dG = U slope is the first column of dX, rounded once more as an operand
+    slope = phi + g * density
+    dX = mp.gated_ff_backward(torch.ones(len(g), 1, dtype=TYPES[dtype], device="cuda"), X, Wg, Wu, act="gelu", need_dw=False)[0]
+    e = u * (rel * phi + np.abs(g) * density * (3 * g * g + 16) * U32 + 4 * U32 * np.abs(slope))
+    close(dX[:, 0], slope * u, e + 2.01 * stored(slope * u, dtype), "dG")
