@@ -540,7 +540,8 @@ typedef struct mlproj_w4 {
 int mlproj_w4_bytes(long long n, long long m, int group, size_t* codes_out /* host */, size_t* scales_out /* host */);
 
 /* Packs W (n x m): the scale of a group is its largest magnitude / 6, rounded to bf16, and a code is the entry
- * over the scale, rounded to the nearest value, ties to the smaller magnitude.  A group of zeros (a pruned column) has scale 0.
+ * over the scale, rounded to the nearest value, ties to the smaller magnitude.  A group of zeros (a pruned column) has scale 0,
+ * one with a NaN or an infinity a scale of NaN or infinity and codes of 0: its products are NaN.
  * `packed`: codes and scales are written.                                                     */
 int w4_pack(int storage, const void* W /* device, n x m */, long long ldw, const mlproj_w4* packed /* host */, void* stream);
 

@@ -210,7 +210,10 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const T* W, long long ldw,
   const T* w = W + row0 * ldw + col;
   const long long rows = col >= m || row0 >= n ? 0 : (n - row0 < group ? n - row0 : group);
   float top = 0.0f;
-  for (long long r = 0; r < rows; r++) top = fmaxf(top, fabsf((float)w[r * ldw]));
+  for (long long r = 0; r < rows; r++) {
+    const float size = fabsf((float)w[r * ldw]);
+    top = size > top || size != size ? size : top;       // a NaN stays: the scale is NaN then, and with it the products
+  }
   const bf16_t rounded = (bf16_t)(top / 6.0f);
   const float scale = (float)rounded;
   const long long block = (col / W4_COLS) * kblocks + kb;

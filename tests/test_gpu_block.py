@@ -765,3 +765,21 @@ def test_gelu_keeps_its_digits_where_it_fades_out(mp, dtype):
     dX = mp.gated_ff_backward(torch.ones(len(g), 1, dtype=TYPES[dtype], device="cuda"), X, Wg, Wu, act="gelu", need_dw=False)[0]
     e = u * (rel * phi + np.abs(g) * density * (3 * g * g + 16) * U32 + 4 * U32 * np.abs(slope))
     close(dX[:, 0], slope * u, e + 2.01 * stored(slope * u, dtype), "dG")
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_w4_pack_does_not_lose_a_nan(mp, dtype, group):
+    """A group that holds a NaN (or an infinity, for which 4 bits have no code) makes its column's products NaN and no others."""
+    rng = np.random.default_rng(21)
+    W, _ = matrix(rng, 200, 40, dtype, 0.1)
+    W[:, 7] = 0
+    X, _ = matrix(rng, 3, 200, dtype)
+    clean = mp.w4_matvec(X, mp.w4_pack(W, group))
+    bad = W.clone()
+    bad[130, 3], bad[0, 7], bad[199, 20], bad[50, 39] = float("nan"), float("nan"), float("inf"), float("-inf")
+    got = mp.w4_matvec(X, mp.w4_pack(bad, group))
+    off = torch.zeros(40, dtype=torch.bool, device="cuda")
+    off[[3, 7, 20, 39]] = True
+    assert torch.isnan(got[:, off]).all()
+    assert torch.equal(got[:, ~off], clean[:, ~off])
