@@ -36,8 +36,9 @@ template <typename E> struct FfFrag;
 template <> struct FfFrag<bf16_t> { using type = bf16x8; };
 template <> struct FfFrag<f16_t> { using type = f16x8; };
 
-// Eight elements as the 16 bytes of each of their parts.
-template <typename T>
+// Eight elements as the 16 bytes of each of their parts.  INFINITIES: an infinity is its first part alone; otherwise what
+// remains of it is a NaN.
+template <typename T, bool INFINITIES = false>
 __device__ __forceinline__ void fs_parts(const FfVec8<T>& x, u32x4 (&out)[FfParts<T>::count]) {
   if constexpr (FfParts<T>::count == 1) {
     __builtin_memcpy(&out[0], &x, 16);
@@ -49,7 +50,7 @@ __device__ __forceinline__ void fs_parts(const FfVec8<T>& x, u32x4 (&out)[FfPart
       for (int j = 0; j < 2; j++) {
         const float a = x.v[2 * i + j];
         const unsigned a0 = __builtin_bit_cast(unsigned, a) & 0xffff0000u;
-        const float r1 = a - __builtin_bit_cast(float, a0);
+        const float r1 = INFINITIES && __builtin_isinf(a) ? 0.0f : a - __builtin_bit_cast(float, a0);
         const unsigned a1 = __builtin_bit_cast(unsigned, r1) & 0xffff0000u;
         w[0][j] = a0;
         w[1][j] = a1;

@@ -40,7 +40,9 @@ __device__ __forceinline__ f16x8 w4_widen(unsigned v, f16_t) {
 // row blocks, U at a time, and join their sums in LDS, in their order.  A wavefront's load of a block is 1 KiB in one
 // instruction, already in the layout of the matrix cores' second operand, and the hardware widens two codes per instruction; a
 // group's sum leaves the matrix cores unscaled, in the lane that holds its column's scale.  fp32 tokens are cut into
-// three bf16 parts (ffstaged.h), which with weights of two significant bits loses nothing.
+// three bf16 parts (ffstaged.h), which with weights of two significant bits loses nothing.  Cut that way an infinity leaves a NaN; keeping
+// it apart costs a call of one token 15 %, so a workgroup does that only in a second run, if a NaN came out of the first (to look
+// for one costs 4 %).
 //
 // Bound by HBM at one token: n m / 2 bytes of codes and 2 n m / group of scales; at 16 tokens by the tokens themselves, which
 // every workgroup reads from L2 (128 rows of 16 tokens are 4 KiB, of a column block 1 KiB).  So: one column block per
@@ -67,107 +69,126 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Args a) {
   const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
   const T* x = static_cast<const T*>(a.x);
   f32x4 acc[SETS][MT] = {};
-  for (int kb = wave; kb < a.kblocks; kb += WAVES * U) {
-    u32x4 w[U][SETS];
-    bf16_t s[U][SETS][PER];
-    F xf[U][VIA_LDS ? 1 : MT][P][4];
-    u32x4 xr[U][VIA_LDS ? XLOADS : 1];
+  auto run = [&](auto infinities) {
+    for (int kb = wave; kb < a.kblocks; kb += WAVES * U) {
+      u32x4 w[U][SETS];
+      bf16_t s[U][SETS][PER];
+      F xf[U][VIA_LDS ? 1 : MT][P][4];
+      u32x4 xr[U][VIA_LDS ? XLOADS : 1];
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      // past the end: the last block again, not used
-      const int k = kb + u * WAVES < a.kblocks ? kb + u * WAVES : a.kblocks - 1;
+      for (int u = 0; u < U; u++) {
+        // past the end: the last block again, not used
+        const int k = kb + u * WAVES < a.kblocks ? kb + u * WAVES : a.kblocks - 1;
 #pragma unroll
-      for (int i = 0; i < SETS; i++) {
-        const long long cb = cb0 + i % CB < cbs ? cb0 + i % CB : cbs - 1, at = cb * a.kblocks + k;
-        w[u][i] = *reinterpret_cast<const u32x4*>(a.codes[i / CB] + at * W4_BYTES + lane * 16);
-        __builtin_memcpy(s[u][i], a.scales[i / CB] + (at * 16 + (lane & 15)) * PER, PER * 2);
-      }
-      const bool whole = (k + 1) * W4_ROWS <= a.n;
-      // (rows past the tokens are the last one again: what they come to is not stored)
-      if constexpr (VIA_LDS) {
+        for (int i = 0; i < SETS; i++) {
+          const long long cb = cb0 + i % CB < cbs ? cb0 + i % CB : cbs - 1, at = cb * a.kblocks + k;
+          w[u][i] = *reinterpret_cast<const u32x4*>(a.codes[i / CB] + at * W4_BYTES + lane * 16);
+          __builtin_memcpy(s[u][i], a.scales[i / CB] + (at * 16 + (lane & 15)) * PER, PER * 2);
+        }
+        const bool whole = (k + 1) * W4_ROWS <= a.n;
+        // (rows past the tokens are the last one again: what they come to is not stored)
+        if constexpr (VIA_LDS) {
 #pragma unroll
-        for (int j = 0; j < XLOADS; j++) {
-          const long long t = t0 + j * ROWS + lane / PIECES;
-          const int at = k * W4_ROWS + lane % PIECES * VEC;
-          const T* from = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx + at;
-          if (whole) {
-            __builtin_memcpy(&xr[u][j], from, 16);
-          } else {
-            T v[VEC];
+          for (int j = 0; j < XLOADS; j++) {
+            const long long t = t0 + j * ROWS + lane / PIECES;
+            const int at = k * W4_ROWS + lane % PIECES * VEC;
+            const T* from = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx + at;
+            if (whole) {
+              __builtin_memcpy(&xr[u][j], from, 16);
+            } else {
+              T v[VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; i++) v[i] = at + i < a.n ? from[i] : (T)0.0f;
-            __builtin_memcpy(&xr[u][j], v, 16);
+              for (int i = 0; i < VEC; i++) v[i] = at + i < a.n ? from[i] : (T)0.0f;
+              __builtin_memcpy(&xr[u][j], v, 16);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int mt = 0; mt < MT; mt++) {
+            const long long t = t0 + mt * 16 + (lane & 15);
+            const T* row = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+              const int at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
+              u32x4 parts[P];
+              fs_parts<T, infinities.value>(ff_load8(row + at, whole ? 8 : a.n - at), parts);
+#pragma unroll
+              for (int p = 0; p < P; p++) __builtin_memcpy(&xf[u][mt][p][q], &parts[p], 16);
+            }
           }
         }
-      } else {
+      }
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++) {
-          const long long t = t0 + mt * 16 + (lane & 15);
-          const T* row = x + (t < a.tokens ? t : a.tokens - 1) * a.ldx;
+      for (int u = 0; u < U; u++) {
+        if (kb + u * WAVES >= a.kblocks) break;
+        u32x4* mine = lds + (wave * U + u) * HELD;
+        if constexpr (VIA_LDS) {
+          // (pieces permuted by the row's number: eight rows' pieces spread over all banks)
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-          for (int q = 0; q < 4; q++) {
-            const int at = k * W4_ROWS + q * 32 + (lane >> 4) * 8;
-            u32x4 parts[P];
-            fs_parts(ff_load8(row + at, whole ? 8 : a.n - at), parts);
+          for (int j = 0; j < XLOADS; j++) {
+            const int r = j * ROWS + lane / PIECES;
+            mine[r * PIECES + (lane % PIECES ^ (r & 7))] = xr[u][j];
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+        }
+        f32x4 part[SETS][MT] = {};
 #pragma unroll
-            for (int p = 0; p < P; p++) __builtin_memcpy(&xf[u][mt][p][q], &parts[p], 16);
+        for (int q = 0; q < 4; q++) {
+          F xq[MT][P];
+#pragma unroll
+          for (int mt = 0; mt < MT; mt++) {
+            if constexpr (VIA_LDS) {
+              FfVec8<T> v;
+              constexpr int EACH = 8 / VEC;
+              const int r = mt * 16 + (lane & 15);
+#pragma unroll
+              for (int e = 0; e < EACH; e++) {
+                const u32x4 piece = mine[r * PIECES + (((q * 4 + (lane >> 4)) * EACH + e) ^ (r & 7))];
+                __builtin_memcpy(&v.v[e * VEC], &piece, 16);
+              }
+              u32x4 parts[P];
+              fs_parts<T, infinities.value>(v, parts);
+#pragma unroll
+              for (int p = 0; p < P; p++) __builtin_memcpy(&xq[mt][p], &parts[p], 16);
+            } else {
+#pragma unroll
+              for (int p = 0; p < P; p++) xq[mt][p] = xf[u][VIA_LDS ? 0 : mt][p][q];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < SETS; i++) {
+            const F wf = w4_widen(w[u][i][q], E{});
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+#pragma unroll
+              for (int p = P - 1; p >= 0; p--) part[i][mt] = ff_mfma(xq[mt][p], wf, part[i][mt]);
+              if ((q + 1) * 32 % GROUP == 0) {
+                acc[i][mt] += (float)s[u][i][q * 32 / GROUP] * part[i][mt];
+                part[i][mt] = f32x4{};
+              }
+            }
           }
         }
       }
     }
+  };
+  run(std::false_type{});
+  if constexpr (P > 1) {
+    bool nan = false;
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      if (kb + u * WAVES >= a.kblocks) break;
-      u32x4* mine = lds + (wave * U + u) * HELD;
-      if constexpr (VIA_LDS) {
-        // (pieces permuted by the row's number: eight rows' pieces spread over all banks)
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int i = 0; i < SETS; i++)
 #pragma unroll
-        for (int j = 0; j < XLOADS; j++) {
-          const int r = j * ROWS + lane / PIECES;
-          mine[r * PIECES + (lane % PIECES ^ (r & 7))] = xr[u][j];
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-      }
-      f32x4 part[SETS][MT] = {};
+      for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        F xq[MT][P];
+        for (int v = 0; v < 4; v++) nan = nan || acc[i][mt][v] != acc[i][mt][v];
+    if (__syncthreads_or(nan)) {
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++) {
-          if constexpr (VIA_LDS) {
-            FfVec8<T> v;
-            constexpr int EACH = 8 / VEC;
-            const int r = mt * 16 + (lane & 15);
+      for (int i = 0; i < SETS; i++)
 #pragma unroll
-            for (int e = 0; e < EACH; e++) {
-              const u32x4 piece = mine[r * PIECES + (((q * 4 + (lane >> 4)) * EACH + e) ^ (r & 7))];
-              __builtin_memcpy(&v.v[e * VEC], &piece, 16);
-            }
-            u32x4 parts[P];
-            fs_parts(v, parts);
-#pragma unroll
-            for (int p = 0; p < P; p++) __builtin_memcpy(&xq[mt][p], &parts[p], 16);
-          } else {
-#pragma unroll
-            for (int p = 0; p < P; p++) xq[mt][p] = xf[u][VIA_LDS ? 0 : mt][p][q];
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < SETS; i++) {
-          const F wf = w4_widen(w[u][i][q], E{});
-#pragma unroll
-          for (int mt = 0; mt < MT; mt++) {
-#pragma unroll
-            for (int p = P - 1; p >= 0; p--) part[i][mt] = ff_mfma(xq[mt][p], wf, part[i][mt]);
-            if ((q + 1) * 32 % GROUP == 0) {
-              acc[i][mt] += (float)s[u][i][q * 32 / GROUP] * part[i][mt];
-              part[i][mt] = f32x4{};
-            }
-          }
-        }
-      }
+        for (int mt = 0; mt < MT; mt++) acc[i][mt] = f32x4{};
+      run(std::true_type{});
     }
   }
   if (VIA_LDS) __syncthreads();                 // the sums take the tokens' place

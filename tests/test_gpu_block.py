@@ -783,3 +783,22 @@ def test_w4_pack_does_not_lose_a_nan(mp, dtype, group):
     off[[3, 7, 20, 39]] = True
     assert torch.isnan(got[:, off]).all()
     assert torch.equal(got[:, ~off], clean[:, ~off])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [1, 5, 33])
+def test_w4_products_of_infinite_tokens(mp, dtype, tokens):
+    """An infinity in a token is one in its products, by the sign of the weight, and NaN where the weight is 0."""
+    rng = np.random.default_rng(22)
+    for n, m in ((100, 40), (700, 300)):
+        W, w = w4_matrix(mp, rng, n, m, 64)
+        X, x = matrix(rng, tokens, n, dtype)
+        X[tokens // 2, 65] = x[tokens // 2, 65] = float("inf")
+        with np.errstate(invalid="ignore"):
+            want = x @ w
+        got = values(mp.w4_matvec(X, W))
+        row = tokens // 2
+        assert np.isinf(want[row]).any() and np.isnan(want[row]).any()
+        assert np.array_equal(got[row], want[row], equal_nan=True)
+        rest = np.arange(tokens) != row
+        assert np.isfinite(got[rest]).all()
