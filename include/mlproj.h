@@ -422,8 +422,8 @@ int mlproj_multilevel_one_pass(int storage, int fibre_norm, long long d0, long l
  * length of a row (so the gate and up weights may be the halves of one n x 2m matrix).  Arrays are
  * aligned to their element size and nothing more is asked; 16-byte aligned rows are fastest.
  * `storage` is a mlproj_storage and applies to every matrix and vector of a call unless said
- * otherwise; arithmetic and sums are fp32 throughout, and results are rounded to nearest-even
- * once, on store.  `tokens` may be 0: then nothing is read, and sums over tokens are zeros.
+ * otherwise; arithmetic and sums are fp32 throughout (infinities and NaN among them are what sums
+ * in fp32 make of them), and results are rounded to nearest-even once, on store.  `tokens` may be 0: then nothing is read, and sums over tokens are zeros.
  * Calls enqueue on `stream`, keep no state and need no cleared workspace, as everywhere above.
  * Outputs must not overlap inputs or one another except where said.
  * --------------------------------------------------------------------------------------------- */

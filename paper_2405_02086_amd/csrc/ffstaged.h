@@ -22,8 +22,8 @@ namespace mlproj {
 // fp32 throughout.  Six bf16 products cost 6/16 of what the chip's fp32 matrix instructions would.  Bound by the vector
 // instructions that cut: 2048 x 2048 -> 4096 fp32 runs at 192 TFLOP/s forward and 195 backward, the library's plain products at
 // 150 to 154.  Largest error of G over 7467 x 488 -> 1024: 3.3e-7 rms, the library's 4.0e-7.
-// (A part past the range of bf16's exponent, below 2^-126, is lost: an absolute error no sum can see.  The remainder of an
-// infinity is a NaN, so an infinity makes the sums that it is part of NaN.)
+// (A part past the range of bf16's exponent, below 2^-126, is lost: an absolute error no sum can see.  What remains of an
+// infinity is a NaN, and so are the sums that it is part of: fs_again.)
 constexpr int FS_M = 128, FS_N = 128, FS_K = 32, FS_THREADS = 256;
 
 template <typename T> struct FfParts { static constexpr int count = 1; using type = T; };
@@ -90,6 +90,59 @@ __device__ __forceinline__ F fs_frag(const unsigned char* tile, int idx, int lan
     __builtin_memcpy(&r, half, 16);
   }
   return r;
+}
+
+// Sums in fp32 that came out as NaN, again: with the fp32 matrix instructions, whose infinities are infinities, straight from
+// memory.  Each wavefront does that for the 16 columns at a time of its part of the tile in which there are any (and the channel
+// is not pruned); the others keep their bits.  Two to four times a tile's time, for
+// tiles with infinities or NaN alone (2048 x 2048 -> 4096 forward with one NaN token: 360 -> 1300 us); looking for them costs calls of
+// few steps 2 to 7 %, others nothing that was measured.
+template <bool A_KC, bool B_KC, bool DUAL>
+__device__ __forceinline__ void fs_again(const FfProduct& p, long long row0, long long col0, long long N, long long K, long long ksteps,
+                                         long long first, long long last, int lane, f32x4 (&acc)[4][4]) {
+  const int g = lane >> 4, c = lane & 15;
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    const long long left = col0 + (j & 1) * 16 + (DUAL || j < 2 ? 0 : 64);      // of these sixteen columns; a lane's results: four of them
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+      for (int v = 0; v < 4; v++) {
+        const long long at = left + g * 4 + v;
+        if (acc[i][j][v] != acc[i][j][v] && at < N && row0 + i * 16 + c < p.M) nan = nan || !p.keep || p.keep[at];
+      }
+    if (!__any(nan)) continue;
+    f32x4 sum[4] = {};
+    const long long col = left + c;
+    for (long long step = first; step < last; step++) {
+      const int seg = step >= ksteps;
+      const long long k0 = (step - (seg ? ksteps : 0)) * FS_K + 8 * g;
+      const float* A = static_cast<const float*>(seg ? p.A1 : p.A0);
+      const float* B = static_cast<const float*>((DUAL ? j >= 2 : seg) ? p.B1 : p.B0);
+      FfVec8<float> b, a[4];
+      if constexpr (B_KC) b = ff_load8(B + col * p.ldb + k0, col < N ? K - k0 : 0);
+      else
+#pragma unroll
+        for (int s = 0; s < 8; s++) b.v[s] = col < N && k0 + s < K ? B[(k0 + s) * p.ldb + col] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const long long row = row0 + i * 16 + c;
+        if constexpr (A_KC) a[i] = ff_load8(A + row * p.lda + k0, row < p.M ? K - k0 : 0);
+        else
+#pragma unroll
+          for (int s = 0; s < 8; s++) a[i].v[s] = row < p.M && k0 + s < K ? A[(k0 + s) * p.lda + row] : 0.0f;
+      }
+#pragma unroll
+      for (int s = 0; s < 8; s++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) sum[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(b.v[s], a[i].v[s], sum[i], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+      for (int v = 0; v < 4; v++) acc[i][j][v] = acc[i][j][v] != acc[i][j][v] ? sum[i][v] : acc[i][j][v];
+  }
 }
 
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
@@ -177,6 +230,14 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
         for (int i = 0; i < 4; i++)
 #pragma unroll
           for (int j = 0; j < 4; j++) acc[i][j] = ff_mfma(b[sum - ka][j], a[ka][i], acc[i][j]);
+  }
+
+  if constexpr (P > 1) {
+    // an infinity of A is a row of NaN, one of B a column: one entry of each shows them all
+    bool nan = __builtin_isunordered(acc[0][0][0], acc[1][0][0]) || __builtin_isunordered(acc[2][0][0], acc[3][0][0]);
+#pragma unroll
+    for (int j = 0; j < 4; j++) nan = nan || __builtin_isunordered(acc[0][j][0], acc[0][j][1]) || __builtin_isunordered(acc[0][j][2], acc[0][j][3]);
+    if (__any(nan)) fs_again<A_KC, B_KC, DUAL>(p, row0 + wm * 64, col0 + wn * 32, N, K, ksteps, first, last, lane, acc);
   }
 
   FfVec4<T> d[4][2] = {};

@@ -802,3 +802,39 @@ def test_w4_products_of_infinite_tokens(mp, dtype, tokens):
         assert np.array_equal(got[row], want[row], equal_nan=True)
         rest = np.arange(tokens) != row
         assert np.isfinite(got[rest]).all()
+
+
+@pytest.mark.parametrize("tokens", [5, 40, 300])
+def test_gated_ff_fp32_infinities_are_the_definition_s(mp, tokens):
+    """Infinities of either sign in tokens, weights and gradients come out as sums in fp32 have them, at any number of tokens: the
+    signs of infinities and the places of NaN are those of the 64-bit form, and what they do not reach keeps its bits."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(23)
+    new = lambda r, c, s=1.0: torch.randn(r, c, generator=gen, device="cuda") * s  # noqa: E731
+    n, m, inf = 200, 333, float("inf")
+    X, Wg, Wu, dH = new(tokens, n), new(n, m, 0.1), new(n, m, 0.1), new(tokens, m)
+    X[3, 5], X[4, 100], X[4, 199], Wu[7, 40], Wg[7, 41] = inf, -inf, inf, -inf, inf
+    G, U = torch.empty(2, tokens, m, device="cuda")
+    H = mp.gated_ff(X, Wg, Wu, act="relu", g_out=G, u_out=U)
+    for got, W in ((G, Wg), (U, Wu)):
+        with np.errstate(invalid="ignore"):
+            want = values(X) @ values(W)
+        assert np.isinf(want[3]).all() and np.isinf(want[:3, 40 if W is Wu else 41]).all() and np.isnan(want[4]).any()
+        special = ~np.isfinite(want)
+        assert np.array_equal(values(got)[special], want[special], equal_nan=True)
+        assert np.isfinite(values(got)[~special]).all()
+    clean = mp.gated_ff(X.nan_to_num(0.5, 0.5, 0.5), Wg.nan_to_num(0.1, 0.1, 0.1), Wu.nan_to_num(0.1, 0.1, 0.1), act="relu")
+    rows = [t for t in range(tokens) if t not in (3, 4)]
+    cols = [c for c in range(m) if c not in (40, 41)]
+    assert torch.equal(H[rows][:, cols], clean[rows][:, cols])
+    # gradients: one infinity in dH, weights and tokens finite
+    X, Wg, Wu = X.nan_to_num(0.5, 0.5, 0.5), Wg.nan_to_num(0.1, 0.1, 0.1), Wu.nan_to_num(0.1, 0.1, 0.1)
+    dH[2, 50] = -inf
+    got = mp.gated_ff_backward(dH, X, Wg, Wu, act="silu")
+    with np.errstate(invalid="ignore"):
+        want = bo.gated_ff_backward(values(dH), values(X), values(Wg), values(Wu), "silu")
+    for t, w in zip(got, want):
+        special = ~np.isfinite(w)
+        assert special.any()
+        assert np.array_equal(values(t)[special], w[special], equal_nan=True)
+        assert np.isfinite(values(t)[~special]).all()
