@@ -84,10 +84,25 @@ static FfPlan ff_plan(long long M, long long N, long long steps, bool dual, int 
   return best;
 }
 static long long ff_steps(long long K, int segs) { return ff_cdiv(K, 32) * segs; }
-static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, int epi, int es) {
+// Workgroups (along x) of a product's launch and their threads.
+struct FfGrid { long long groups; int threads; };
+static FfGrid ff_grid(int kind, long long M, long long N, bool dual, int splits) {
+  const int half = dual ? 2 : 1;
+  switch (kind) {
+    case 0: return {ff_cdiv(M, 256) * ff_cdiv(N, 256 / half) * splits, 512};
+    case 3: return {ff_cdiv(ff_cdiv(N, FK_COLS), 8) * 8 * ff_cdiv(M, 16), FK_WAVES * 64};      // (shares along y)
+    case 4: return {ff_cdiv(M, 64) * ff_cdiv(N, 128 / half) * splits, 256};
+    default: return {ff_cdiv(M, 128) * ff_cdiv(N, 128 / half) * splits, 256};                  // 1: direct, 2: staged
+  }
+}
+// A launch has less than 2^32 threads along an axis.
+constexpr long long FF_MOST_THREADS = (1LL << 32) - 1;
+static size_t ff_partial_bytes(long long M, long long N, long long K, int segs, bool dual, int epi, int es, bool* fits) {
   size_t most = 0;
   for (int direct = 0; direct < 2; direct++) {
     const FfPlan plan = ff_plan(M, N, ff_steps(K, segs), dual, epi, direct, es);
+    const FfGrid grid = ff_grid(plan.kind, M, N, dual, plan.splits);
+    if ((es == 2 || !direct) && grid.groups > FF_MOST_THREADS / grid.threads) *fits = false;
     const size_t bytes = plan.splits > 1 ? (size_t)plan.splits * (dual ? 2 : 1) * M * (ff_cdiv(N, 4) * 4) * 4 : 0;
     if (bytes > most) most = bytes;
   }
@@ -127,6 +142,7 @@ struct FfLayout {
   size_t position, kept, W[2], in[3], out[3];   // masked: where the channels went; packed weights, inputs and results
   size_t bytes;
   bool pads;
+  bool fits;                   // every product's launch has a grid
 };
 // How a call deals with its mask: it has none, zeros in the epilogue (backward: and in a copy of the weights), packed channels.
 enum FfMask { MASK_NONE, MASK_EPILOGUE, MASK_PACK };
@@ -143,12 +159,14 @@ FfLayout ff_layout(int es, long long tokens, long long n, long long m, bool back
   L.ldn = ff_cdiv(n, 8) * 8;
   // (the packed channels' products run over ldd of them)
   const long long widest = packed ? L.ldd : m;
-  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, backward ? FF_GRAD : FF_FWD, es);
+  L.fits = true;
+  size_t shares = ff_partial_bytes(tokens, widest, n, 1, true, backward ? FF_GRAD : FF_FWD, es, &L.fits);
   if (backward) {
-    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, FF_STORE, es), w = ff_partial_bytes(n, widest, tokens, 1, true, FF_STORE, es);
+    const size_t x = ff_partial_bytes(tokens, n, widest, 2, false, FF_STORE, es, &L.fits), w = ff_partial_bytes(n, widest, tokens, 1, true, FF_STORE, es, &L.fits);
     shares = shares > x ? shares : x;
     shares = shares > w ? shares : w;
   }
+  if (tokens == 0) L.fits = true;      // (no product is launched)
   L.partial = take(shares);
   const size_t plane = (size_t)tokens * L.ldd * es, weights = (size_t)n * L.ldd * es;
   if (backward) {
@@ -191,32 +209,29 @@ bool ff_direct(const FfProduct& p) {
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
   mark(stream);
+  const FfGrid g = ff_grid(kind, p.M, p.N, DUAL, p.splits);
+  const dim3 grid(p.part == FF_REST ? 4 * FF_LEFT : (unsigned)g.groups, kind == 3 ? p.splits : 1), block(g.threads);
   if constexpr (sizeof(T) == 4 && A_KC && !B_KC) {
     if (kind == 3) {
-      const dim3 grid((unsigned)(ff_cdiv(ff_cdiv(p.N, FK_COLS), 8) * 8 * ff_cdiv(p.M, 16)), p.splits);
-      launch(ff_skinny_kernel<EPI>, grid, dim3(FK_WAVES * 64), stream, p);
+      launch(ff_skinny_kernel<EPI>, grid, block, stream, p);
       return;
     }
   }
   if constexpr (sizeof(T) == 2) {
     if (kind == 0) {
-      const long long tiles = ff_cdiv(p.M, 256) * ff_cdiv(p.N, DUAL ? 128 : 256);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, dim3((unsigned)(tiles * p.splits)), dim3(512), stream, p);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 256, 256, 2, 4>, grid, block, stream, p);
       return;
     }
     if (kind == 4) {
-      const long long tiles = ff_cdiv(p.M, 64) * ff_cdiv(p.N, DUAL ? 64 : 128);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 64, 128, 2, 2>, dim3((unsigned)(tiles * p.splits)), dim3(256), stream, p);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 64, 128, 2, 2>, grid, block, stream, p);
       return;
     }
     if (kind == 1) {
-      const long long tiles = p.part == FF_REST ? 4 * FF_LEFT : ff_cdiv(p.M, 128) * ff_cdiv(p.N, DUAL ? 64 : 128);
-      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, dim3((unsigned)(tiles * p.splits)), dim3(256), stream, p);
+      launch(ff_direct_kernel<T, A_KC, B_KC, DUAL, EPI, 128, 128, 2, 2>, grid, block, stream, p);
       return;
     }
   }
-  const long long tiles = ff_cdiv(p.M, FS_M) * ff_cdiv(p.N, DUAL ? 64 : 128);
-  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, dim3((unsigned)(tiles * p.splits)), dim3(FS_THREADS), stream, p);
+  launch(ff_staged_kernel<T, A_KC, B_KC, DUAL, EPI>, grid, block, stream, p);
 }
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_product(FfProduct p, void* partial, hipStream_t stream) {
@@ -243,30 +258,38 @@ void ff_product(FfProduct p, void* partial, hipStream_t stream) {
   else launch(ff_join_kernel<T, DUAL, EPI, 1>, dim3((unsigned)ff_cdiv(quads, 256)), dim3(256), stream, p);
 }
 
+// Elementwise kernels: at most this many workgroups, which go on in strides of the grid where there is more to do than one
+// launch may have threads.
+constexpr long long FF_MOST_GROUPS = 1 << 16;
+static dim3 ff_strided_grid(long long threads) {
+  const long long groups = ff_cdiv(threads, 256);
+  return dim3((unsigned)(groups < FF_MOST_GROUPS ? groups : FF_MOST_GROUPS));
+}
+
 // dG and dU from saved pre-activations.
 template <typename T>
 __global__ __launch_bounds__(256) void ff_slopes_kernel(FfProduct p) {
   const long long quads = (p.N + 3) / 4, N = p.kept ? *p.kept : p.N;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= quads * p.M) return;
-  const long long row = i / quads, col = i % quads * 4;
-  if (col >= N) return;
-  f32x4 g = {}, u = {};
-  const T* pg = static_cast<const T*>(p.G) + row * p.ldg + col;
-  const T* pu = static_cast<const T*>(p.U) + row * p.ldg + col;
-  if (col + 4 <= N) {
-    g = ff_load4(pg);
-    u = ff_load4(pu);
-  } else {
-    for (int c = 0; c < N - col; c++) { g[c] = (float)pg[c]; u[c] = (float)pu[c]; }
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < quads * p.M; i += (long long)gridDim.x * 256) {
+    const long long row = i / quads, col = i % quads * 4;
+    if (col >= N) continue;
+    f32x4 g = {}, u = {};
+    const T* pg = static_cast<const T*>(p.G) + row * p.ldg + col;
+    const T* pu = static_cast<const T*>(p.U) + row * p.ldg + col;
+    if (col + 4 <= N) {
+      g = ff_load4(pg);
+      u = ff_load4(pu);
+    } else {
+      for (int c = 0; c < N - col; c++) { g[c] = (float)pg[c]; u[c] = (float)pu[c]; }
+    }
+    ff_finish<FF_GRAD, true, T>(p, row, col, N, g, u, ff_upstream<T>(p, row, col, N));
   }
-  ff_finish<FF_GRAD, true, T>(p, row, col, N, g, u, ff_upstream<T>(p, row, col, N));
 }
 // Zeros into what an empty batch leaves.
 template <typename T>
 __global__ __launch_bounds__(256) void ff_zero_kernel(T* a, T* b, long long rows, long long cols, long long ld) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i < rows * cols) a[i / cols * ld + i % cols] = b[i / cols * ld + i % cols] = (T)0.0f;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (long long)gridDim.x * 256)
+    a[i / cols * ld + i % cols] = b[i / cols * ld + i % cols] = (T)0.0f;
 }
 
 int ff_check(int storage, int act, const mlproj_gated_block* b) {
@@ -328,41 +351,41 @@ struct FfPad {
   void* to[5];
   long long ld_from[5], ld_to[5], rows[5], cols[5];
   long long first[5];          // number of the first thread of a matrix
+  long long threads;           // of all
   const unsigned char* mask[5];  // columns to be replaced by zeros, or null
   int count;
 };
 template <typename T>
 __global__ __launch_bounds__(256) void ff_pad_kernel(FfPad a) {
-  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   int i = 0;
-  while (i + 1 < a.count && id >= a.first[i + 1]) i++;
-  const long long pieces = a.from[i] ? a.ld_to[i] / 8 : 1, at = id - a.first[i];
-  const long long row = at >> 32 ? at / pieces : (unsigned)at / (unsigned)pieces;
-  const long long col = a.from[i] ? (at - row * pieces) * 8 : a.ld_to[i] - 8;
-  if (row >= a.rows[i]) return;
-  FfVec8<T> v = {};
-  if (a.from[i]) v = ff_load8(static_cast<const T*>(a.from[i]) + row * a.ld_from[i] + col, a.cols[i] - col);
-  if (a.mask[i])
+  for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < a.threads; id += (long long)gridDim.x * 256) {
+    while (i + 1 < a.count && id >= a.first[i + 1]) i++;
+    const long long pieces = a.from[i] ? a.ld_to[i] / 8 : 1, at = id - a.first[i];
+    const long long row = at >> 32 ? at / pieces : (unsigned)at / (unsigned)pieces;
+    const long long col = a.from[i] ? (at - row * pieces) * 8 : a.ld_to[i] - 8;
+    FfVec8<T> v = {};
+    if (a.from[i]) v = ff_load8(static_cast<const T*>(a.from[i]) + row * a.ld_from[i] + col, a.cols[i] - col);
+    if (a.mask[i])
 #pragma unroll
-    for (int j = 0; j < 8; j++)
-      if (col + j < a.cols[i] && !a.mask[i][col + j]) v.v[j] = (T)0.0f;
-  __builtin_memcpy(static_cast<T*>(a.to[i]) + row * a.ld_to[i] + col, &v, sizeof(v));
+      for (int j = 0; j < 8; j++)
+        if (col + j < a.cols[i] && !a.mask[i][col + j]) v.v[j] = (T)0.0f;
+    __builtin_memcpy(static_cast<T*>(a.to[i]) + row * a.ld_to[i] + col, &v, sizeof(v));
+  }
 }
 struct FfPadder {
   FfPad a{};
-  long long threads = 0;
   void add(const void* from, long long ld_from, void* to, long long ld_to, long long rows, long long cols, const unsigned char* mask = nullptr) {
     const int i = a.count++;
     a.from[i] = from; a.ld_from[i] = ld_from; a.to[i] = to; a.ld_to[i] = ld_to; a.rows[i] = rows; a.cols[i] = cols;
     a.mask[i] = mask;
-    a.first[i] = threads;
-    threads += rows * (from ? ld_to / 8 : 1);
+    a.first[i] = a.threads;
+    a.threads += rows * (from ? ld_to / 8 : 1);
   }
   template <typename T>
   void go(hipStream_t stream) {
-    if (threads == 0) return;
+    if (a.threads == 0) return;
     mark(stream);
-    launch(ff_pad_kernel<T>, dim3((unsigned)ff_cdiv(threads, 256)), dim3(256), stream, a);
+    launch(ff_pad_kernel<T>, ff_strided_grid(a.threads), dim3(256), stream, a);
   }
 };
 
@@ -464,7 +487,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
   if (b->tokens == 0) {
     if (dWg) {
       mark(stream);
-      launch(ff_zero_kernel<T>, dim3((unsigned)ff_cdiv(b->n * b->m, 256)), dim3(256), stream, static_cast<T*>(dWg), static_cast<T*>(dWu), b->n, b->m, lddw);
+      launch(ff_zero_kernel<T>, ff_strided_grid(b->n * b->m), dim3(256), stream, static_cast<T*>(dWg), static_cast<T*>(dWu), b->n, b->m, lddw);
     }
     mark(stream);
     return launch_status();
@@ -505,7 +528,7 @@ int run_backward(int act, const mlproj_gated_block* b, const void* dH, long long
     if (G) {
       p.G = const_cast<void*>(G); p.U = const_cast<void*>(U); p.ldg = ldg;
       mark(stream);
-      launch(ff_slopes_kernel<T>, dim3((unsigned)ff_cdiv(ff_cdiv(ch.m, 4) * b->tokens, 256)), dim3(256), stream, p);
+      launch(ff_slopes_kernel<T>, ff_strided_grid(ff_cdiv(ch.m, 4) * b->tokens), dim3(256), stream, p);
     } else {
       p.A0 = X.at; p.lda = X.ld; p.a_filled = X.filled;
       p.B0 = ch.Wg; p.B1 = ch.Wu; p.ldb = ch.ldw; p.b_filled = ch.filled;
@@ -550,10 +573,13 @@ int ff_workspace(int storage, long long tokens, long long n, long long m, int ba
   if (tokens < 0 || n <= 0 || m <= 0 || (backward | 1) != 1 || (masked | 1) != 1) return MLPROJ_ERR_BAD_DIMENSION;
   if (tokens > FF_MAX_DIM || n > FF_MAX_DIM || m > FF_MAX_DIM || tokens * m > (1LL << 38) || tokens * n > (1LL << 38) || n * m > (1LL << 38)) return MLPROJ_ERR_TOO_LARGE;
   const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
-  *out = ff_layout(es, tokens, n, m, backward != 0, MASK_NONE).bytes;
+  const FfLayout plain = ff_layout(es, tokens, n, m, backward != 0, MASK_NONE);
+  if (!plain.fits) return MLPROJ_ERR_TOO_LARGE;
+  *out = plain.bytes;
   if (masked) {      // serves calls without a mask as well
-    const size_t with = ff_layout(es, tokens, n, m, backward != 0, ff_mask(es, tokens, n, m, backward != 0, true)).bytes;
-    *out = *out > with ? *out : with;
+    const FfLayout with = ff_layout(es, tokens, n, m, backward != 0, ff_mask(es, tokens, n, m, backward != 0, true));
+    if (!with.fits) return MLPROJ_ERR_TOO_LARGE;
+    *out = *out > with.bytes ? *out : with.bytes;
   }
   return MLPROJ_OK;
 }

@@ -224,3 +224,21 @@ def test_what_a_call_allocates_belongs_to_its_stream(monkeypatch):
     binding._result(None, (2, 4), like, "other", None)
     binding._result(None, (2, 4), like, "other", "side")
     assert seen == ["default", "side"] * 3
+
+
+def test_gated_ff_sizes_past_one_launch_are_too_large(lib):
+    """Products whose tiles would be 2^32 threads or more are refused as sizes, not at their launch."""
+    out = ctypes.c_size_t(0)
+    ask = lib.mlproj_gated_ff_workspace_bytes
+    top = 1 << 30
+    for storage in (0, 1, 2):
+        assert ask(storage, 1, 1, top, 0, 0, ctypes.byref(out)) == LARGE
+        assert ask(storage, 1, 1, top, 1, 1, ctypes.byref(out)) == LARGE
+        assert ask(storage, 1, 1, top >> 3, 0, 0, ctypes.byref(out)) == OK
+        assert ask(storage, 0, 1 << 16, 1 << 17, 1, 0, ctypes.byref(out)) == OK
+        assert ask(storage, 0, 1, top, 1, 1, ctypes.byref(out)) == OK
+        assert ask(storage, 1 << 18, 64, 1 << 16, 1, 1, ctypes.byref(out)) == OK
+    big = block(tokens=1, n=1, m=top, ldx=1, ldw=top)
+    assert forward(lib, big, ldh=top) == LARGE
+    assert backward(lib, big, ldh=top, lddx=1, lddw=top) == LARGE
+    assert forward(lib, block(tokens=32, n=1, m=1 << 28, ldx=1, ldw=1 << 28), storage=0, ldh=1 << 28) == LARGE

@@ -838,3 +838,37 @@ def test_gated_ff_fp32_infinities_are_the_definition_s(mp, tokens):
         assert special.any()
         assert np.array_equal(values(t)[special], w[special], equal_nan=True)
         assert np.isfinite(values(t)[~special]).all()
+
+
+def test_gated_ff_without_tokens_of_more_entries_than_a_launch_has_threads(mp):
+    """2^32 entries in each gradient."""
+    n, m = 1 << 16, 1 << 16
+    X, dH = torch.empty(0, n, dtype=torch.bfloat16, device="cuda"), torch.empty(0, m, dtype=torch.bfloat16, device="cuda")
+    W = torch.empty(n, m, dtype=torch.bfloat16, device="cuda")
+    dWg, dWu = torch.empty_like(W), torch.empty_like(W)
+    for t in (dWg, dWu):
+        t.view(torch.int16).fill_(0x4040)
+    mp.gated_ff_backward(dH, X, W, W, dWg=dWg, dWu=dWu, need_dx=False)
+    for t in (dWg, dWu):
+        for rows in t.view(torch.int16).split(1 << 13):
+            assert not rows.any()
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_gated_ff_elementwise_passes_of_several_strides(mp, masked):
+    """Slopes of 2^26 + entries and copies of 2^27 +: more than their grids have threads at a time."""
+    tokens, n, m = 8200, 9, 8331
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(25)
+    new = lambda r, c, s=1.0: (torch.randn(r, c, generator=gen, device="cuda") * s).to(torch.bfloat16)  # noqa: E731
+    X, Wg, Wu, dH = new(tokens, n), new(n, m, 0.3), new(n, m, 0.3), new(tokens, m)
+    mask = (torch.rand(m, generator=gen, device="cuda") < 0.5).to(torch.uint8) if masked else None
+    want = exact_block(X, Wg, Wu, dH, "silu", mask)
+    G, U = want["G"].to(torch.bfloat16), want["U"].to(torch.bfloat16)
+    for name, t in zip(("dX", "dWg", "dWu"), mp.gated_ff_backward(dH, X, Wg, Wu, mask=mask, G=G, U=U)):
+        blocks_close(t, want[name], 1.5 * ROUND["bf16"], name)
+    tokens, n, m = 20, 16411, 8201
+    X, Wg, Wu = new(tokens, n), new(n, m, 0.01), new(n, m, 0.01)
+    got = mp.gated_ff(X, Wg, Wu, mask=mask[:m].contiguous() if masked else None)
+    h = torch.nn.functional.silu(X.double() @ Wg.double()) * (X.double() @ Wu.double())
+    blocks_close(got, h * mask[:m] if masked else h, ROUND["bf16"], "H")
