@@ -602,37 +602,42 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_backward_kernel(BnArgs a
   }
 }
 
-// The sums over workgroups: 32 columns x 32 groups of them per workgroup here, joined in LDS in a fixed order.
+// The sums over workgroups: 32 columns x 32 groups of them per workgroup here, joined in LDS in a fixed order.  Rows of more columns
+// than a launch has threads for: the next ones a grid further on.
+constexpr long long BN_MOST_COLUMN_GROUPS = 1 << 21;
 template <typename T>
 __global__ __launch_bounds__(1024) void bn_columns_kernel(BnArgs a, int workers, bool token_gate, float* dw_post, float* dgate, float* dw_pre) {
   __shared__ float part[2][32][33];
   const int cx = threadIdx.x & 31, gy = threadIdx.x >> 5;
-  const long long col = (long long)blockIdx.x * 32 + cx;
   const bool post = a.want_post || a.want_gate;
-  float s[2] = {0.0f, 0.0f};
+  for (long long first = (long long)blockIdx.x * 32; first < a.n; first += (long long)gridDim.x * 32) {
+    const long long col = first + cx;
+    float s[2] = {0.0f, 0.0f};
 #pragma unroll
-  for (int k = 0; k < 2; k++) {
-    if (col >= a.n || !(k == 0 ? post : a.want_pre != 0)) continue;
-    const float* p = a.partial + k * (long long)workers * a.n + col;
+    for (int k = 0; k < 2; k++) {
+      if (col >= a.n || !(k == 0 ? post : a.want_pre != 0)) continue;
+      const float* p = a.partial + k * (long long)workers * a.n + col;
 #pragma unroll 8
-    for (int w = gy; w < workers; w += 32) s[k] += p[w * a.n];
-  }
-  part[0][gy][cx] = s[0];
-  part[1][gy][cx] = s[1];
-  __syncthreads();
-  if (gy == 0 && col < a.n) {
-    float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; i++) { s0 += part[0][i][cx]; s1 += part[1][i][cx]; }
-    if (a.want_pre) dw_pre[col] = s1;
-    if (token_gate) {
-      if (a.want_post) dw_post[col] = s0;
-    } else {
-      // s0 = sum of scale dx b / rms(b); without tokens the gate need not be there, and may hold anything
-      const bool some = workers > 0;
-      if (a.want_post) dw_post[col] = some ? s0 * (float)static_cast<const T*>(a.gate)[col] : 0.0f;
-      if (a.want_gate) dgate[col] = some ? s0 * (float)static_cast<const T*>(a.w_post)[col] : 0.0f;
+      for (int w = gy; w < workers; w += 32) s[k] += p[w * a.n];
     }
+    part[0][gy][cx] = s[0];
+    part[1][gy][cx] = s[1];
+    __syncthreads();
+    if (gy == 0 && col < a.n) {
+      float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 32; i++) { s0 += part[0][i][cx]; s1 += part[1][i][cx]; }
+      if (a.want_pre) dw_pre[col] = s1;
+      if (token_gate) {
+        if (a.want_post) dw_post[col] = s0;
+      } else {
+        // s0 = sum of scale dx b / rms(b); without tokens the gate need not be there, and may hold anything
+        const bool some = workers > 0;
+        if (a.want_post) dw_post[col] = some ? s0 * (float)static_cast<const T*>(a.gate)[col] : 0.0f;
+        if (a.want_gate) dgate[col] = some ? s0 * (float)static_cast<const T*>(a.w_post)[col] : 0.0f;
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -705,7 +710,8 @@ int run_backward(const BnArgs& a, bool token_gate, float* dw_post, float* dgate,
     }
     if (a.want_post || a.want_gate || a.want_pre) {
       mark(stream);
-      launch(bn_columns_kernel<T>, dim3((unsigned)((a.n + 31) / 32)), dim3(1024), stream, a, (int)groups, token_gate,
+      const long long columns = (a.n + 31) / 32;
+      launch(bn_columns_kernel<T>, dim3((unsigned)(columns < BN_MOST_COLUMN_GROUPS ? columns : BN_MOST_COLUMN_GROUPS)), dim3(1024), stream, a, (int)groups, token_gate,
              dw_post, dgate, dw_pre);
     }
   });
@@ -717,7 +723,8 @@ int bn_check(int storage, const mlproj_norm_block* b) {
   if (!b) return MLPROJ_ERR_NULL_POINTER;
   if (storage < MLPROJ_STORE_F32 || storage > MLPROJ_STORE_F16) return MLPROJ_ERR_BAD_VARIANT;
   if (b->tokens < 0 || b->n <= 0) return MLPROJ_ERR_BAD_DIMENSION;
-  if (b->tokens > BN_MAX_DIM || b->n > BN_MAX_DIM || (b->tokens > 0 && b->n > (1LL << 38) / b->tokens)) return MLPROJ_ERR_TOO_LARGE;
+  // (rows too long for registers have a workgroup of 512 threads each: past 2^14 entries, 2^37 in all are less than 2^23 of them)
+  if (b->tokens > BN_MAX_DIM || b->n > BN_MAX_DIM || (b->tokens > 0 && b->n > (1LL << 37) / b->tokens)) return MLPROJ_ERR_TOO_LARGE;
   if (!(b->eps >= 0.0f) || b->eps > 3.0e38f || !(b->scale - b->scale == 0.0f)) return MLPROJ_ERR_BAD_VALUE;
   return MLPROJ_OK;
 }

@@ -242,3 +242,11 @@ def test_gated_ff_sizes_past_one_launch_are_too_large(lib):
     assert forward(lib, big, ldh=top) == LARGE
     assert backward(lib, big, ldh=top, lddx=1, lddw=top) == LARGE
     assert forward(lib, block(tokens=32, n=1, m=1 << 28, ldx=1, ldw=1 << 28), storage=0, ldh=1 << 28) == LARGE
+
+
+def test_block_norm_sizes_past_one_launch_are_too_large(lib):
+    """2^23 rows of more than 2^14 entries would be 2^32 threads."""
+    for tokens, n in ((1 << 23, 16385), (1 << 30, 129)):
+        k = norm(tokens=tokens, n=n, ldb=n)
+        assert norm_forward(lib, k, ldx=n, ldr=n, ldy=n) == LARGE
+        assert norm_backward(lib, k, ldr=n, lddr=n, lddy=n, lddx=n, lddb=n) == LARGE

@@ -872,3 +872,18 @@ def test_gated_ff_elementwise_passes_of_several_strides(mp, masked):
     got = mp.gated_ff(X, Wg, Wu, mask=mask[:m].contiguous() if masked else None)
     h = torch.nn.functional.silu(X.double() @ Wg.double()) * (X.double() @ Wu.double())
     blocks_close(got, h * mask[:m] if masked else h, ROUND["bf16"], "H")
+
+
+def test_block_norm_backward_of_more_columns_than_a_launch_has_threads_for(mp):
+    """One row of 2^27 + 40 entries: the kernel that finishes the column sums gives 32 threads to each."""
+    n = (1 << 27) + 40
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(26)
+    r, dy = (torch.randn(1, n, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    w = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    dx, _, _, _, dw = mp.block_norm_backward(None, dy, r, w_pre=w)
+    rms = (r.float().square().double().mean() + 1e-6).sqrt()
+    want = (dy.double() * r.double())[0] / rms
+    # one term per sum: the root's error, of 2^27 terms summed by 512 threads and a tree, and the products'
+    assert (dw.double() - want).abs().le(want.abs() * ((1 << 18) + 64) * U32).all()
+    assert torch.isfinite(dx).all() and dw[-40:].any() and dw[:40].any()
