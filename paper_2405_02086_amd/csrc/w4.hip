@@ -279,6 +279,10 @@ int w4_array(const void* p, bool needed, long long row, long long ld, int es) {
   return aligned(p, es) ? MLPROJ_OK : MLPROJ_ERR_ALIGNMENT;
 }
 
+// Column blocks that a launch of less than 2^32 threads takes: workgroups of so many have 512 threads and two blocks, or four
+// with at least 8 tokens (w4_run).
+bool w4_fits(long long m, long long tokens) { return (m + W4_COLS - 1) / W4_COLS <= (tokens >= 8 ? (1LL << 25) - 4 : (1LL << 24) - 2); }
+
 template <typename T, bool GATED, int MT, int CB, int U, int WAVES, bool VIA_LDS>
 void w4_launch(const W4Args& a, int group, hipStream_t stream) {
   const long long cbs = (a.m + W4_COLS - 1) / W4_COLS;
@@ -329,6 +333,7 @@ int w4_product(int storage, int act, const mlproj_w4* g, const mlproj_w4* u, con
   W4_TRY(w4_array(x, tokens > 0, g->n, ldx, es));
   W4_TRY(w4_array(y, tokens > 0, g->m, ldy, es));
   if (tokens == 0) return MLPROJ_OK;
+  if (!w4_fits(g->m, tokens)) return MLPROJ_ERR_TOO_LARGE;
   W4Args a{};
   a.codes[0] = static_cast<const unsigned char*>(g->codes);
   a.scales[0] = static_cast<const bf16_t*>(g->scales);
@@ -370,6 +375,7 @@ int w4_pack(int storage, const void* W, long long ldw, const mlproj_w4* packed, 
   const long long columns = (packed->m + W4_COLS - 1) / W4_COLS * W4_COLS;
   const int kblocks = (int)((packed->n + W4_ROWS - 1) / W4_ROWS);
   const long long threads = columns * kblocks * (W4_ROWS / packed->group);
+  if ((threads + 255) / 256 >= 1LL << 24) return MLPROJ_ERR_TOO_LARGE;      // 2^32 threads in a launch
   const dim3 grid((unsigned)((threads + 255) / 256));
   unsigned* codes = static_cast<unsigned*>(const_cast<void*>(packed->codes));
   bf16_t* scales = static_cast<bf16_t*>(const_cast<void*>(packed->scales));

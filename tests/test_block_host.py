@@ -250,3 +250,13 @@ def test_block_norm_sizes_past_one_launch_are_too_large(lib):
         k = norm(tokens=tokens, n=n, ldb=n)
         assert norm_forward(lib, k, ldx=n, ldr=n, ldy=n) == LARGE
         assert norm_backward(lib, k, ldr=n, lddr=n, lddy=n, lddx=n, lddb=n) == LARGE
+
+
+def test_w4_sizes_past_one_launch_are_too_large(lib):
+    R = ctypes.byref
+    wide, wider, widest = packed(m=1 << 28), packed(m=1 << 29), packed(m=1 << 30)
+    for tokens, w in ((1, wide), (7, wide), (8, wider), (64, widest)):
+        assert lib.w4_matvec(1, R(w), P, 100, tokens, P, w.m, None) == LARGE
+        assert lib.w4_gated_matvec(1, 0, R(w), R(w), P, 100, tokens, P, w.m, None) == LARGE
+    assert lib.w4_pack(1, P, 1 << 30, R(packed(m=1 << 30, group=32)), None) == LARGE
+    assert lib.w4_matvec(1, R(wide), None, 100, 0, None, 1 << 28, None) == OK
