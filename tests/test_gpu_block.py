@@ -887,3 +887,89 @@ def test_block_norm_backward_of_more_columns_than_a_launch_has_threads_for(mp):
     # one term per sum: the root's error, of 2^27 terms summed by 512 threads and a tree, and the products'
     assert (dw.double() - want).abs().le(want.abs() * ((1 << 18) + 64) * U32).all()
     assert torch.isfinite(dx).all() and dw[-40:].any() and dw[:40].any()
+
+
+# ---------------------------------------------------------------- every form of the 4-bit launches, rows by the hundreds
+
+def grid_matrix(rng, n, m, group):
+    """A matrix that 4 bits hold exactly: codes times a power of two per column and group, the largest code in every group."""
+    codes = rng.integers(0, 16, (n, m))
+    codes[::group] = 7
+    scale = 2.0 ** rng.integers(-4, 0, (-(-n // group), m))
+    return np.where(codes >= 8, -bo.E2M1[codes & 7], bo.E2M1[codes & 7]) * np.repeat(scale, group, axis=0)[:n]
+
+
+# tokens, n, m: column blocks (an odd number of them) and tokens that reach the launches of one to four column blocks per workgroup
+W4_FORMS = [(1, 300, 8209), (3, 300, 8209), (5, 300, 8209), (4, 700, 200), (9, 700, 200), (8, 257, 16417), (16, 257, 16417), (33, 300, 16417),
+            (64, 300, 16417), (1, 130, 16417)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("case", range(len(W4_FORMS)))
+def test_w4_every_form(mp, case, dtype):
+    tokens, n, m = W4_FORMS[case]
+    rng = np.random.default_rng(27 + case)
+    for group in (32, 64, 128):
+        wg, wu = grid_matrix(rng, n, m, group), grid_matrix(rng, n, m, group)
+        Wg, Wu = (mp.w4_pack(torch.from_numpy(w.astype(np.float32)).cuda(), group) for w in (wg, wu))
+        X, x = matrix(rng, tokens, n, dtype, n ** -0.5, gap=group % 3)
+        c = sum_bound(n, dtype)
+        g, u = x @ wg, x @ wu
+        eg, eu = c * (np.abs(x) @ np.abs(wg)), c * (np.abs(x) @ np.abs(wu))
+        pad = torch.full((tokens + 1, m + 5), 7.0, dtype=TYPES[dtype], device="cuda")
+        mp.w4_matvec(X, Wg, y=pad[:tokens, :m])
+        close(pad[:tokens, :m], g, eg + stored(g, dtype), "y")
+        assert (pad[tokens:] == 7).all() and (pad[:, m:] == 7).all()
+        h, a = bo.activation("silu", g) * u, np.abs(bo.activation("silu", g))
+        eh = (SLOPE * eg + 16 * U32 * (a + np.abs(g))) * (np.abs(u) + eu) + a * eu
+        pad.fill_(7.0)
+        mp.w4_gated_matvec(X, Wg, Wu, h=pad[:tokens, :m])
+        close(pad[:tokens, :m], h, eh + stored(h, dtype), "h")
+        assert (pad[tokens:] == 7).all() and (pad[:, m:] == 7).all()
+
+
+# more rows than are resident at once, for every number of threads that a row has
+NORM_ROWS = [(8300, 40), (8250, 250), (2200, 500), (1100, 1500), (600, 2500), (600, 3003), (300, 5001), (300, 8200), (300, 16390)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("token_gate", [False, True])
+@pytest.mark.parametrize("i", range(len(NORM_ROWS)))
+def test_block_norm_of_many_rows(mp, i, token_gate, dtype):
+    tokens, n = NORM_ROWS[i]
+    rng = np.random.default_rng(500 + i)
+    eps, scale = 1e-5, 0.6
+    (X, x), (B, b), (WP, wp), (G, g), (WQ, wq) = norm_case(rng, tokens, n, dtype, token_gate, i % 2)
+    r, y, er, ey = norm_forward_bounds(x, b, wp, g, wq, scale, eps, dtype)
+    R, Y = mp.block_norm(X, B, WP, G, WQ, scale=scale, eps=eps)
+    close(R, r, er + stored(r, dtype), "r")
+    close(Y, y, ey + stored(y, dtype), "y")
+    Xc, Bc = X.clone(), B.clone()
+    mp.block_norm(Xc, Bc, WP, G, WQ, scale=scale, eps=eps, r=Xc, y=Bc)
+    assert torch.equal(Xc, R) and torch.equal(Bc, Y)
+
+    (DR, dr), (DY, dy) = matrix(rng, tokens, n, dtype, gap=i % 2), matrix(rng, tokens, n, dtype, gap=i % 2)
+    dx, db, dwp, dg, dwq = bo.block_norm_backward(dr, dy, x, b, wp, g, wq, scale, eps)
+    ws = mp.Workspace(mp.block_norm_workspace_bytes(tokens, n))
+    ws.buf.fill_(255)
+    got = mp.block_norm_backward(DR, DY, X, B, WP, G, WQ, scale=scale, eps=eps, workspace=ws)
+    k, over = (n + 64) * U32, (tokens + 16) * U32
+    sr, sb, e, f = bo.rms(x, eps), bo.rms(b, eps), np.abs(wq * dy), np.abs(scale * g * wp)
+    mag = np.abs(dr) + e / sr + np.abs(x) / sr * (np.abs(x) / sr * e).mean(1, keepdims=True) / sr
+    bh = np.abs(b) / sb
+    close(got[0], dx, k * mag + stored(dx, dtype), "dx")
+    close(got[1], db, 4 * k * (f * mag / sb + bh * (bh * f * mag).mean(1, keepdims=True) / sb) + stored(db, dtype), "db")
+    close(got[2], dwp, (4 * k + over) * (np.abs(scale * g) * mag * bh).sum(0) + 1e-37, "dw_post")
+    tg = np.abs(scale * wp) * mag * bh
+    if token_gate:
+        close(got[3], dg, 4 * k * tg + stored(dg, dtype), "dgate")
+    else:
+        close(got[3], dg, (4 * k + over) * tg.sum(0) + 1e-37, "dgate")
+    close(got[4], dwq, (k + over) * np.abs(dy * (x / sr)).sum(0) + 1e-37, "dw_pre")
+    # in place: dx over dr, db over b, then over dy
+    DRc, Bc = DR.clone(), B.clone()
+    for a, c in zip(got, mp.block_norm_backward(DRc, DY, X, Bc, WP, G, WQ, scale=scale, eps=eps, dx=DRc, db=Bc)):
+        assert torch.equal(a, c)
+    DYc = DY.clone()
+    for a, c in zip(got, mp.block_norm_backward(DR, DYc, X, B, WP, G, WQ, scale=scale, eps=eps, db=DYc)):
+        assert torch.equal(a, c)
