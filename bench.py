@@ -30,9 +30,9 @@ if ROOT not in sys.path:
 HBM_PEAK_GBS = 8000.0
 # HBM-side bytes per launch of the map kernel from the rocprofv3 --pmc runs summarised in
 # profiles/ (FETCH_SIZE x 2.0 + WRITE_SIZE x 1.0, in KiB), valid for this library version only.
-TRAFFIC_VERSION = 400   # the library version the counters in profiles/ were taken with
-TRAFFIC_KIB = {"square_4096": 32980.6 * 1.999 + 65608.4, "square_16384": 524929.1 * 1.999 + 1048624.0,
-               "tensor_256x256x256": 32899.7 * 1.999 + 65630.2}
+TRAFFIC_VERSION = 401   # the library version the counters in profiles/ were taken with
+TRAFFIC_KIB = {"square_4096": 32980.8 * 1.999 + 65556.7, "square_16384": 524929.1 * 1.999 + 1048616.2,
+               "tensor_256x256x256": 32899.9 * 1.999 + 65620.3}
 INFINITY_CACHE_BYTES = 256 * 1024 * 1024
 
 

@@ -423,7 +423,9 @@ int mlproj_multilevel_one_pass(int storage, int fibre_norm, long long d0, long l
  * aligned to their element size and nothing more is asked; 16-byte aligned rows are fastest.
  * `storage` is a mlproj_storage and applies to every matrix and vector of a call unless said
  * otherwise; arithmetic and sums are fp32 throughout (infinities and NaN among them are what sums
- * in fp32 make of them), and results are rounded to nearest-even once, on store.  `tokens` may be 0: then nothing is read, and sums over tokens are zeros.
+ * in fp32 make of them), and results are rounded to nearest-even once, on store.  `tokens` may
+ * be 0: then nothing is read, and sums over tokens are zeros.  Sizes past what one launch takes (2^32
+ * threads) are MLPROJ_ERR_TOO_LARGE.
  * Calls enqueue on `stream`, keep no state and need no cleared workspace, as everywhere above.
  * Outputs must not overlap inputs or one another except where said.
  * --------------------------------------------------------------------------------------------- */
@@ -545,7 +547,8 @@ int mlproj_w4_bytes(long long n, long long m, int group, size_t* codes_out /* ho
  * `packed`: codes and scales are written.                                                     */
 int w4_pack(int storage, const void* W /* device, n x m */, long long ldw, const mlproj_w4* packed /* host */, void* stream);
 
-/* y = x W (x: tokens x n, y: tokens x m), made for few tokens: every weight is read once per 64 tokens. */
+/* y = x W (x: tokens x n, y: tokens x m), made for few tokens: every weight is read once per 16 tokens (with 16-bit
+ * storage, more than 16 tokens and many columns once per 32).                                  */
 int w4_matvec(int storage, const mlproj_w4* W /* host */, const void* x /* device */, long long ldx, long long tokens,
               void* y /* device */, long long ldy, void* stream);
 

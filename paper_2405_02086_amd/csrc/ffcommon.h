@@ -23,7 +23,10 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 // What a product leaves behind.
 //   STORE    C0 (and C1, where the tile holds two products side by side)
 //   FWD      C0 = keep * act(G) * U; G and U too where the caller wants them
-//   GRAD     C0 = keep * act'(G) * U * dH, C1 = keep * act(G) * dH
+//   GRAD     C0 = keep * act'(G) * U * dH, C1 = keep * act(G) * dH, rounded to the storage type: they are operands of the matrix
+//            cores in the products that follow.  With 16 bits that is a second rounding behind the one of the results, and errors of
+//            dX, dWg and dWu grow by the root of two (bf16 1.7e-3 -> 2.4e-3 of a result's norm, fp16 2.1e-4 -> 2.9e-4); without it
+//            these products would be in fp32, six times their operations
 //   PARTIAL  the sums over this workgroup's share of K, in fp32, for the join kernel
 enum : int { FF_WHOLE = 0, FF_TURNS = 1, FF_REST = 2 };
 enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3 };

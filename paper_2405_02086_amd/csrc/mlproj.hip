@@ -1087,7 +1087,7 @@ using namespace mlproj;
 
 extern "C" {
 
-int mlproj_version(void) { return 400; }
+int mlproj_version(void) { return 401; }
 
 const char* mlproj_status_string(int status) {
   switch (status) {

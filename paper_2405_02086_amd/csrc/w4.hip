@@ -44,8 +44,10 @@ __device__ __forceinline__ f16x8 w4_widen(unsigned v, f16_t) {
 // it apart costs a call of one token 15 %, so a workgroup does that only in a second run, if a NaN came out of the first (to look
 // for one costs 4 %).
 //
-// Bound by HBM at one token: n m / 2 bytes of codes and 2 n m / group of scales; at 16 tokens by the tokens themselves, which
-// every workgroup reads from L2 (128 rows of 16 tokens are 4 KiB, of a column block 1 KiB).  So: one column block per
+// Bound by HBM at one token where there are columns enough: n m / 2 bytes of codes and 2 n m / group of scales; where there are few, by
+// the rounds of loads that a wavefront waits for (16384 -> 4096, weights in the memory-side cache: one token, four rounds of two
+// blocks, 8.7 us; sixteen, which every workgroup reads from L2, 128 rows of them 4 KiB and of a column block 1 KiB, eight rounds, 10.4).
+// So: one column block per
 // workgroup and 16 wavefronts while that is what fills the chip, two where there are columns enough, four (and 32
 // tokens) where the tokens dominate.  us, with 1 x 16 / 2 x 8 / 4 x 8 (column blocks x wavefronts): one token 16384 ->
 // 4096 10.8 / 14 / 22, one token 4096 -> 2 x 16384 18 / 14 / 17, 16 tokens 4096 -> 2 x 16384 24 / 17 / 17, 16 tokens 16384
