@@ -973,3 +973,22 @@ def test_block_norm_of_many_rows(mp, i, token_gate, dtype):
     DYc = DY.clone()
     for a, c in zip(got, mp.block_norm_backward(DR, DYc, X, B, WP, G, WQ, scale=scale, eps=eps, db=DYc)):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("m", range(4088, 4098))
+def test_packed_channels_of_every_remainder(mp, m):
+    """Widths around two whole segments of columns, one to eight channels pruned ahead of a full last segment."""
+    tokens, n, dtype = 1024, 1032, "bf16"
+    assert mp.gated_ff_route(TYPES[dtype], 1, tokens, n, m)["packed"]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(m)
+    new = lambda r, c, s=1.0: (torch.randn(r, c, generator=gen, device="cuda") * s).to(TYPES[dtype])  # noqa: E731
+    X, Wg, Wu, dH = new(tokens, n), new(n, m, n ** -0.5), new(n, m, n ** -0.5), new(tokens, m)
+    ws = mp.Workspace(mp.gated_ff_workspace_bytes(tokens, n, m, TYPES[dtype], True))
+    for pruned in range(1, 9):
+        mask = torch.ones(m, dtype=torch.uint8, device="cuda")
+        mask[torch.randperm(2000, generator=gen, device="cuda")[:pruned]] = 0
+        ws.buf.fill_(255)
+        want = exact_block(X, Wg, Wu, dH, "silu", mask)
+        for name, t in zip(("dX", "dWg", "dWu"), mp.gated_ff_backward(dH, X, Wg, Wu, mask=mask, workspace=ws)):
+            blocks_close(t, want[name], 1.5 * ROUND[dtype], name)
