@@ -430,11 +430,12 @@ int mlproj_multilevel_one_pass(int storage, int fibre_norm, long long d0, long l
  * Outputs must not overlap inputs or one another except where said.
  * --------------------------------------------------------------------------------------------- */
 
-/* Activation of the gate: g/(1 + e^-g), g Phi(g) (the exact form, with erf), max(g, 0). */
+/* Activation of the gate: g/(1 + e^-g), g Phi(g) (the exact form, with erf), max(g, 0); none (g itself, not for gated blocks). */
 typedef enum mlproj_activation {
   MLPROJ_ACT_SILU = 0,
   MLPROJ_ACT_GELU = 1,
-  MLPROJ_ACT_RELU = 2
+  MLPROJ_ACT_RELU = 2,
+  MLPROJ_ACT_NONE = 3
 } mlproj_activation;
 
 /* The inputs of a gated block.  mask: as bilevel_proj_stored returns it, one byte per hidden
@@ -483,6 +484,56 @@ int gated_ff_backward(int storage, int activation, const mlproj_gated_block* blo
                       void* dX /* device, tokens x n; may be NULL */, long long lddx,
                       void* dWg /* device, n x m; may be NULL */, void* dWu, long long lddw,
                       void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* Dropout whose mask is never stored: it is a function of the place of an entry, computed where it is needed.  Entry (t, c) of
+ * a matrix is kept if word c % 4 of Philox4x32-10 at counter (c / 4, t, low half of o, high half of o) and key (low, high half
+ * of seed) is at least p * 2^32 (rounded to a whole number); kept entries are divided by 1 - p, the others are zeros whatever
+ * they were.  o is `offset`, plus the number in device memory at `step` if there is one: a call that is captured in a graph
+ * reads it at every replay, so that the program advances the mask by advancing that number (and leaves it alone until
+ * the gradient that belongs to it is done).  Calls with different o have independent masks.  0 <= p < 1 (MLPROJ_ERR_BAD_VALUE).
+ * Below, D(v) is v after dropout, and v itself where there is none.                              */
+typedef struct mlproj_dropout {
+  double p;
+  unsigned long long seed, offset;
+  const unsigned long long* step;   /* device; may be NULL                              */
+} mlproj_dropout;
+
+/* y = residual + D(x), rows of n entries.  The gradient is the same call: dx = D(dy).  residual may be NULL; y may be x or
+ * the residual (in place).                                                                   */
+int dropout_forward(int storage, const mlproj_dropout* dropout /* host */, long long tokens, long long n,
+                    const void* x /* device */, long long ldx, const void* residual /* device; may be NULL */, long long ldr,
+                    void* y /* device */, long long ldy, void* stream);
+
+/* A product with what follows it (a block's down product, a projection of any kind), and its gradients. */
+typedef struct mlproj_linear {
+  long long tokens, n, m;
+  const void* X;              /* device, tokens x n                                   */
+  long long ldx;
+  const void* W;              /* device, n x m                                        */
+  long long ldw;
+  const void* bias;           /* device, m; may be NULL                               */
+  const mlproj_dropout* dropout;   /* host; may be NULL                               */
+} mlproj_linear;
+
+int mlproj_linear_workspace_bytes(int storage, long long tokens, long long n, long long m, int backward, size_t* bytes_out /* host */);
+
+/* Z = X W + bias,  Y = residual + D(act(Z)), act any mlproj_activation.  residual may be NULL, and Y may be the
+ * residual (in place, same stride).  Z, where not NULL, is written for a later backward pass.                */
+int linear_forward(int storage, int activation, const mlproj_linear* block /* host */,
+                   const void* residual /* device, tokens x m; may be NULL */, long long ldr,
+                   void* Y /* device, tokens x m */, long long ldy, void* Z /* device, tokens x m; may be NULL */, long long ldz,
+                   void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* Its gradients for a given dY (the residual's is dY itself):
+ *   dZ = act'(Z) D(dY)      (rounded to the storage type as an operand of the products that follow)
+ *   dX = dZ W^T,  dW = X^T dZ,  dbias = sum over tokens of dZ before it is rounded (fp32, m entries)
+ * Z is the forward call's (not read with MLPROJ_ACT_NONE); dropout has to be the forward call's.  dX, dW and dbias may each
+ * be NULL; X is read for dW and W for dX alone, bias is not read.                                */
+int linear_backward(int storage, int activation, const mlproj_linear* block /* host */,
+                    const void* dY /* device, tokens x m */, long long lddy,
+                    const void* Z /* device, tokens x m; may be NULL */, long long ldz,
+                    void* dX /* device, tokens x n; may be NULL */, long long lddx, void* dW /* device, n x m; may be NULL */, long long lddw,
+                    float* dbias /* device, m; may be NULL */, void* workspace /* device */, size_t workspace_bytes, void* stream);
 
 /* The norms around a block, with its gate and residual scale:
  *   r = x + scale * gate * w_post * b / rms(b)      b: the block's output, x: the residual stream

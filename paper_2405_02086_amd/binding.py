@@ -12,7 +12,7 @@ import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmlproj.so")
-SRC_PATHS = [os.path.join(_HERE, "csrc", name) for name in ("mlproj.hip", "heldmulti.hip", "gatedff.hip", "blocknorm.hip", "w4.hip")]
+SRC_PATHS = [os.path.join(_HERE, "csrc", name) for name in ("mlproj.hip", "heldmulti.hip", "gatedff.hip", "linear.hip", "blocknorm.hip", "w4.hip")]
 
 L1INF, L11, L12, L1INFINF = 0, 1, 2, 3
 _VARIANTS = {"l1inf": L1INF, "l11": L11, "l12": L12, "tri": L1INFINF}
@@ -137,6 +137,15 @@ def lib():
     L.gated_ff_forward.argtypes = [c_i, c_i, block, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_sz, c_vp]
     L.gated_ff_backward.restype = c_i
     L.gated_ff_backward.argtypes = [c_i, c_i, block, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_ll, c_vp, c_vp, c_ll, c_vp, c_sz, c_vp]
+    linear, drop = ctypes.POINTER(LinearBlock), ctypes.POINTER(DropoutStruct)
+    L.mlproj_linear_workspace_bytes.restype = c_i
+    L.mlproj_linear_workspace_bytes.argtypes = [c_i, c_ll, c_ll, c_ll, c_i, ctypes.POINTER(c_sz)]
+    L.linear_forward.restype = c_i
+    L.linear_forward.argtypes = [c_i, c_i, linear, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_sz, c_vp]
+    L.linear_backward.restype = c_i
+    L.linear_backward.argtypes = [c_i, c_i, linear, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_vp, c_sz, c_vp]
+    L.dropout_forward.restype = c_i
+    L.dropout_forward.argtypes = [c_i, drop, c_ll, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp]
     L.block_norm_forward.restype = c_i
     L.block_norm_forward.argtypes = [c_i, norm, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp]
     L.mlproj_block_norm_workspace_bytes.restype = c_i
@@ -170,6 +179,18 @@ class GatedBlock(ctypes.Structure):
                 ("ldw", ctypes.c_longlong), ("mask", ctypes.c_void_p)]
 
 
+class DropoutStruct(ctypes.Structure):
+    """mlproj_dropout of include/mlproj.h."""
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_ulonglong), ("offset", ctypes.c_ulonglong), ("step", ctypes.c_void_p)]
+
+
+class LinearBlock(ctypes.Structure):
+    """mlproj_linear of include/mlproj.h."""
+    _fields_ = [("tokens", ctypes.c_longlong), ("n", ctypes.c_longlong), ("m", ctypes.c_longlong),
+                ("X", ctypes.c_void_p), ("ldx", ctypes.c_longlong), ("W", ctypes.c_void_p), ("ldw", ctypes.c_longlong),
+                ("bias", ctypes.c_void_p), ("dropout", ctypes.POINTER(DropoutStruct))]
+
+
 class NormBlock(ctypes.Structure):
     """mlproj_norm_block of include/mlproj.h."""
     _fields_ = [("tokens", ctypes.c_longlong), ("n", ctypes.c_longlong), ("b", ctypes.c_void_p), ("ldb", ctypes.c_longlong),
@@ -192,6 +213,7 @@ EXPORTS = (
     "multilevel_proj_stored", "bilevel_proj_weighted", "multilevel_proj_weighted", "mlproj_set_search_spin_limit",
     "bilevel_proj_l1inf_no_alloc", "mlproj_stripe_of_workgroup", "mlproj_multilevel_one_pass",
     "mlproj_gated_ff_workspace_bytes", "mlproj_gated_ff_route", "gated_ff_forward", "gated_ff_backward",
+    "mlproj_linear_workspace_bytes", "linear_forward", "linear_backward", "dropout_forward",
     "block_norm_forward", "mlproj_block_norm_workspace_bytes", "block_norm_backward",
     "mlproj_w4_bytes", "w4_pack", "w4_matvec", "w4_gated_matvec",
 )
@@ -603,8 +625,8 @@ def norm_l1q(Y, variant, workspace=None, v_out=None, stream=None):
 
 # ---------------------------------------------------------------- the pruned feed-forward block
 
-ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
-_ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU, "relu": ACT_RELU}
+ACT_SILU, ACT_GELU, ACT_RELU, ACT_NONE = 0, 1, 2, 3
+_ACTS = {"silu": ACT_SILU, "gelu": ACT_GELU, "relu": ACT_RELU, "none": ACT_NONE, None: ACT_NONE}
 _STORAGES = {}
 
 
@@ -717,6 +739,102 @@ def gated_ff_backward(dH, X, Wg, Wu, act="silu", mask=None, G=None, U=None, dX=N
 def _vector(t, shape, like, what):
     assert t.dtype is like.dtype and t.is_cuda and t.shape == shape and t.is_contiguous(), what
     return t.data_ptr()
+
+
+class Dropout:
+    """Dropout whose mask is a function of the place of an entry (mlproj_dropout of include/mlproj.h): D(v) keeps an entry
+    with probability 1 - p and divides it by 1 - p.  The same object in a call and in the call of its gradient is the
+    same mask; calls with another `offset` (a number of the layer and the step, say) have independent ones.  step: a device tensor
+    of one int64 that is added to offset when the kernels run, so that a captured graph's replays differ."""
+
+    def __init__(self, p, seed, offset=0, step=None):
+        if step is not None:
+            assert step.is_cuda and step.element_size() == 8 and not step.is_floating_point() and step.numel() == 1, "step: one int64 on the device"
+        self.p, self.seed, self.offset, self.step = p, seed, offset, step
+        self._struct = DropoutStruct(p, seed & 0xffffffffffffffff, offset & 0xffffffffffffffff, _ptr(step))
+        self._ref = ctypes.pointer(self._struct)
+
+
+def dropout(x, drop, residual=None, y=None, stream=None):
+    """y = residual + D(x), rows of x any distance apart; y may be x or residual (in place)."""
+    assert x.dim() == 2
+    storage, shape = _storage(x.dtype), x.shape
+    ldx, ldr = _matrix(x, shape, x, "x"), 0
+    if residual is not None:
+        ldr = _matrix(residual, shape, x, "residual")
+    y, ldy = _result(y, shape, x, "y", stream)
+    st = lib().dropout_forward(storage, drop._ref, shape[0], shape[1], x.data_ptr(), ldx, _ptr(residual), ldr, y.data_ptr(), ldy,
+                               _stream(stream))
+    if st != 0:
+        _check(st, "dropout_forward")
+    return y
+
+
+def dropout_backward(dy, drop, dx=None, stream=None):
+    """dx = D(dy), the gradient of dropout (the residual's is dy itself); dx may be dy."""
+    return dropout(dy, drop, y=dx, stream=stream)
+
+
+def linear_workspace_bytes(tokens, n, m, dtype, backward=False):
+    out = ctypes.c_size_t(0)
+    _check(lib().mlproj_linear_workspace_bytes(_storage(dtype), tokens, n, m, int(backward), ctypes.byref(out)),
+           "mlproj_linear_workspace_bytes")
+    return out.value
+
+
+def linear(X, W, bias=None, residual=None, act=None, dropout=None, Y=None, z_out=None, workspace=None, stream=None):
+    """Y = residual + D(act(X W + bias)): X is tokens x n, W n x m, all of one type (fp32, bf16, fp16), rows any distance
+    apart.  act: None, "silu", "gelu" (with erf) or "relu"; dropout: a Dropout.  z_out: a tensor that also receives
+    X W + bias, for linear_backward.  Y may be the residual (in place)."""
+    assert X.dim() == 2 and W.dim() == 2
+    storage = _storage(X.dtype)
+    tokens, n = X.shape
+    m = W.shape[1]
+    shape = (tokens, m)
+    block = LinearBlock(tokens, n, m, X.data_ptr(), _matrix(X, (tokens, n), X, "X"), W.data_ptr(), _matrix(W, (n, m), X, "W"),
+                        None if bias is None else _vector(bias, (m,), X, "bias: m entries"), None if dropout is None else dropout._ref)
+    ldr = ldz = 0
+    if residual is not None:
+        ldr = _matrix(residual, shape, X, "residual")
+    if z_out is not None:
+        ldz = _matrix(z_out, shape, X, "z_out")
+    Y, ldy = _result(Y, shape, X, "Y", stream)
+    if workspace is None:
+        workspace = Workspace(linear_workspace_bytes(tokens, n, m, X.dtype), device=X.device, stream=stream)
+    st = lib().linear_forward(storage, _ACTS[act], ctypes.byref(block), _ptr(residual), ldr, Y.data_ptr(), ldy, _ptr(z_out), ldz,
+                              workspace.buf.data_ptr(), workspace.nbytes, _stream(stream))
+    if st != 0:
+        _check(st, "linear_forward")
+    return Y
+
+
+def linear_backward(dY, X, W, Z=None, act=None, dropout=None, dX=None, dW=None, workspace=None, stream=None, need_dx=True,
+                    need_dw=True, need_dbias=False):
+    """(dX, dW, dbias) of linear for the gradient dY of its result (the residual's gradient is dY itself).  Z: what the forward
+    call wrote to z_out, needed with an activation; dropout: the forward call's.  dbias is in fp32; what is not needed is
+    None, and then X (for dW) and W (for dX) are not read."""
+    assert X.dim() == 2 and W.dim() == 2
+    storage = _storage(X.dtype)
+    tokens, n = X.shape
+    m = W.shape[1]
+    shape = (tokens, m)
+    block = LinearBlock(tokens, n, m, X.data_ptr(), _matrix(X, (tokens, n), X, "X"), W.data_ptr(), _matrix(W, (n, m), X, "W"), None,
+                        None if dropout is None else dropout._ref)
+    lddy = _matrix(dY, shape, X, "dY")
+    ldz = lddx = lddw = 0
+    assert Z is not None or _ACTS[act] == ACT_NONE, "Z: the pre-activations of the forward call"
+    if Z is not None:
+        ldz = _matrix(Z, shape, X, "Z")
+    dX, lddx = _result(dX, (tokens, n), X, "dX", stream) if need_dx else (None, 0)
+    dW, lddw = _result(dW, (n, m), X, "dW", stream) if need_dw else (None, 0)
+    dbias = _new_empty(X, m, _torch.float32, stream) if need_dbias else None
+    if workspace is None:
+        workspace = Workspace(linear_workspace_bytes(tokens, n, m, X.dtype, True), device=X.device, stream=stream)
+    st = lib().linear_backward(storage, _ACTS[act], ctypes.byref(block), dY.data_ptr(), lddy, _ptr(Z), ldz, _ptr(dX), lddx,
+                               _ptr(dW), lddw, _ptr(dbias), workspace.buf.data_ptr(), workspace.nbytes, _stream(stream))
+    if st != 0:
+        _check(st, "linear_backward")
+    return dX, dW, dbias
 
 
 def _norm_block(z, b, w_post, gate, w_pre, scale, eps):

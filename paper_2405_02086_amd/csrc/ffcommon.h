@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "../../include/mlproj.h"
+#include "dropout.h"
 
 namespace mlproj {
 
@@ -27,9 +28,10 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 //            cores in the products that follow.  With 16 bits that is a second rounding behind the one of the results, and errors of
 //            dX, dWg and dWu grow by the root of two (bf16 1.7e-3 -> 2.4e-3 of a result's norm, fp16 2.1e-4 -> 2.9e-4); without it
 //            these products would be in fp32, six times their operations
+//   LINEAR   Z = v + bias, C0 = residual + D(act(Z)) with D the dropout; Z too where the caller wants it
 //   PARTIAL  the sums over this workgroup's share of K, in fp32, for the join kernel
 enum : int { FF_WHOLE = 0, FF_TURNS = 1, FF_REST = 2 };
-enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3 };
+enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3, FF_LINEAR = 4 };
 
 // One product C = A B (M x N, summed over K), or two that share A: C0 = A B0, C1 = A B1.
 // A: `a_kc` its rows run along K (row-major M x K); otherwise its rows are the K index (K x M).
@@ -44,8 +46,10 @@ struct FfProduct {
   int act;
   void *C0, *C1;
   long long ldc;
-  void *G, *U;                 // FWD: optional outputs
-  const void* dH;              // GRAD
+  void *G, *U;                 // FWD: optional outputs; LINEAR: Z in G
+  const void* dH;              // GRAD; LINEAR: the residual, or null
+  const void* bias;            // LINEAR, or null
+  Dropout drop;                // LINEAR
   long long ldg, ldh;
   const unsigned char* keep;   // one byte per column of the result, or null
   const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
@@ -192,16 +196,27 @@ template <bool EXACT> __device__ __forceinline__ void ff_gate4(int act, f32x4 g,
   }
 }
 
+// With no activation as well; the value alone.
+template <bool EXACT> __device__ __forceinline__ f32x4 ff_value4(int act, f32x4 z) {
+  if (act == MLPROJ_ACT_NONE) return z;
+  f32x4 value, slope;
+  ff_gate4<EXACT>(act, z, value, slope);
+  return value;
+}
+
 // ------------------------------------------------------------------ epilogue
 // Columns col .. col+3 of row `row`, of which those below N exist; v0, v1: their sums in the two products.
 // A pruned channel's outputs are zeros whatever its sums are, NaN included.
-// ff_upstream: GRAD's four entries of dH; all of a thread's are fetched before its first store, which the compiler
-// could not move them across.
+// ff_upstream: GRAD's four entries of dH, LINEAR's of the residual; all of a thread's are fetched before its first store, which the
+// compiler could not move them across.  ff_bias: LINEAR's of the bias.
 template <typename T>
 __device__ __forceinline__ FfVec4<T> ff_upstream(const FfProduct& p, long long row, long long col, long long N) {
   FfVec4<T> d;
   const T* at = static_cast<const T*>(p.dH) + row * p.ldh + col;
-  if (col + 4 <= N) {
+  if (!p.dH) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) d.v[i] = (T)0.0f;
+  } else if (col + 4 <= N) {
     __builtin_memcpy(&d, at, sizeof(d));
   } else {
 #pragma unroll
@@ -209,8 +224,20 @@ __device__ __forceinline__ FfVec4<T> ff_upstream(const FfProduct& p, long long r
   }
   return d;
 }
+template <int EPI> constexpr bool FF_UPSTREAM = EPI == FF_GRAD || EPI == FF_LINEAR;
+template <typename T>
+__device__ __forceinline__ f32x4 ff_bias(const FfProduct& p, long long col, long long N) {
+  f32x4 b = {};
+  if (!p.bias) return b;
+  const T* at = static_cast<const T*>(p.bias) + col;
+  if (col + 4 <= N) return ff_load4(at);
+#pragma unroll
+  for (int i = 0; i < 4; i++) b[i] = col + i < N ? (float)at[i] : 0.0f;
+  return b;
+}
 template <int EPI, bool DUAL, typename T>
-__device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, long long col, long long N, f32x4 v0, f32x4 v1, FfVec4<T> d) {
+__device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, long long col, long long N, f32x4 v0, f32x4 v1, FfVec4<T> d,
+                                          f32x4 bias = {}) {
   const bool whole = col + 4 <= N;
   const int count = whole ? 4 : (int)(N - col);
   if constexpr (EPI == FF_PARTIAL) {
@@ -222,6 +249,13 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
     return;
   }
   f32x4 o0 = v0, o1 = v1;
+  if constexpr (EPI == FF_LINEAR) {
+    v0 += bias;
+    o0 = ff_value4<sizeof(T) == 4>(p.act, v0);
+    if (p.drop.threshold) o0 = dropout4(p.drop, row, col >> 2, o0);
+#pragma unroll
+    for (int i = 0; i < 4; i++) o0[i] += (float)d.v[i];
+  }
   if constexpr (EPI == FF_FWD || EPI == FF_GRAD) {
     f32x4 value, slope;
     ff_gate4<sizeof(T) == 4>(p.act, v0, value, slope);
@@ -241,6 +275,14 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
       if (i < count && !p.keep[col + i]) o0[i] = o1[i] = v0[i] = v1[i] = 0.0f;
   }
   T* c0 = static_cast<T*>(p.C0) + row * p.ldc + col;
+  if constexpr (EPI == FF_LINEAR) {
+    if (p.G) {
+      T* z = static_cast<T*>(p.G) + row * p.ldg + col;
+      if (whole) ff_store4(z, v0);
+      else
+        for (int i = 0; i < count; i++) z[i] = ff_round<T>(v0[i]);
+    }
+  }
   T* c1 = (DUAL && EPI != FF_FWD) ? static_cast<T*>(p.C1) + row * p.ldc + col : nullptr;
   if (whole) {
     ff_store4(c0, o0);

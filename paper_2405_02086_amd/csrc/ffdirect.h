@@ -7,6 +7,7 @@
 #include "ffstaged.h"
 
 namespace mlproj {
+namespace {      // (each translation unit that includes this has its own kernels)
 
 // ------------------------------------------------------------------ tiles straight into LDS
 // A tile is 32 deep.  FD_STAGES of them lie in LDS as a ring: while the matrix cores work on the operands of one, which are in
@@ -223,13 +224,23 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p)
   __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0)
 
   const long long my_row = row0 + wm * RI * 16 + (lane & 15), my_col = col0 + wn * CJ * 16 + (lane >> 4) * 4;
-  FfVec4<T> d[RI][CJ] = {};
-  if constexpr (EPI == FF_GRAD) {
+  constexpr int QUADS = DUAL ? CJ : 2 * CJ;      // of a row's columns in the result
+  auto column = [&](int j) { return my_col + (j < CJ ? j * 16 : BW + (j - CJ) * 16); };
+  FfVec4<T> d[RI][QUADS] = {};
+  f32x4 bias[QUADS] = {};
+  if constexpr (FF_UPSTREAM<EPI>) {
+    if (p.dH)
 #pragma unroll
-    for (int i = 0; i < RI; i++)
+      for (int i = 0; i < RI; i++)
 #pragma unroll
-      for (int j = 0; j < CJ; j++)
-        if (my_row + i * 16 < p.M && my_col + j * 16 < N) d[i][j] = ff_upstream<T>(p, my_row + i * 16, my_col + j * 16, N);
+        for (int j = 0; j < QUADS; j++)
+          if (my_row + i * 16 < p.M && column(j) < N) d[i][j] = ff_upstream<T>(p, my_row + i * 16, column(j), N);
+  }
+  if constexpr (EPI == FF_LINEAR) {
+    dropout_at_step(p.drop);
+#pragma unroll
+    for (int j = 0; j < QUADS; j++)
+      if (column(j) < N) bias[j] = ff_bias<T>(p, column(j), N);
   }
 #pragma unroll
   for (int i = 0; i < RI; i++) {
@@ -241,12 +252,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p)
       if constexpr (DUAL) {
         if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][CJ + j], d[i][j]);
       } else {
-        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, {});
-        if (col + BW < N) ff_finish<EPI, false, T>(p, row, col + BW, N, acc[i][CJ + j], f32x4{}, {});
+        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, d[i][j], bias[j]);
+        if (col + BW < N) ff_finish<EPI, false, T>(p, row, col + BW, N, acc[i][CJ + j], f32x4{}, d[i][CJ + j], bias[CJ + j]);
       }
     }
   }
 }
 
+}  // namespace
 }  // namespace mlproj
 #endif

@@ -1,13 +1,14 @@
-// mlproj: gated fp32 products of few tokens: weights go from memory straight into the matrix cores' operands.
+// mlproj: fp32 products of few tokens: weights go from memory straight into the matrix cores' operands.
 #ifndef MLPROJ_FFSKINNY_H
 #define MLPROJ_FFSKINNY_H
 
 #include "ffcommon.h"
 
 namespace mlproj {
+namespace {      // (each translation unit that includes this has its own kernels)
 
 // ------------------------------------------------------------------ few tokens in fp32
-// G = X Wg and U = X Wu for a few tokens, 16 of them per workgroup: every weight is used for a handful of tokens, so the
+// G = X Wg and U = X Wu (one product alone: X W) for a few tokens, 16 of them per workgroup: every weight is used for a handful of tokens, so the
 // kernel has to keep loads in flight and nothing else.  A wavefront takes 64 columns and 32 rows at a time, a lane
 // four columns of eight rows, and feeds them to the fp32 matrix instructions, whose operands are single elements: no
 // cutting into bf16 parts, no LDS, no barrier until the wavefronts, which share out the rows, add their sums in a
@@ -29,9 +30,9 @@ __device__ __forceinline__ f32x4 fk_load(const float* p, long long valid) {
   return r;
 }
 
-template <int EPI>
+template <int EPI, bool DUAL>
 __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
-  constexpr int CW = 4, VALUES = 2 * CW * 4;
+  constexpr int CW = 4, PRODUCTS = DUAL ? 2 : 1, VALUES = PRODUCTS * CW * 4;
   __shared__ float sums[FK_WAVES / 2][VALUES][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
   const long long N = p.kept ? *p.kept : p.N;
@@ -45,17 +46,17 @@ __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
   const float* B[2] = {static_cast<const float*>(p.B0), static_cast<const float*>(p.B1)};
   const int steps = (int)((p.K + 31) / 32);
   const int first = (int)((long long)steps * blockIdx.y / p.splits), last = (int)((long long)steps * (blockIdx.y + 1) / p.splits);
-  f32x4 acc[2][CW] = {};
+  f32x4 acc[PRODUCTS][CW] = {};
   for (int step = first + wave; step < last; step += FK_WAVES) {
     const long long k0 = (long long)step * 32 + 8 * g;
-    f32x4 w[2][8];
+    f32x4 w[PRODUCTS][8];
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int i = 0; i < PRODUCTS; i++)
 #pragma unroll
       for (int s = 0; s < 8; s++) w[i][s] = fk_load(B[i] + (k0 + s) * p.ldb + col, k0 + s < p.K ? N - col : 0);
     const FfVec8<float> x = ff_load8(X + (row0 + c) * p.lda + k0, row0 + c < p.M ? p.K - k0 : 0);
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int i = 0; i < PRODUCTS; i++)
 #pragma unroll
       for (int s = 0; s < 8; s++)
 #pragma unroll
@@ -78,22 +79,26 @@ __global__ __launch_bounds__(FK_WAVES * 64) void ff_skinny_kernel(FfProduct p) {
 #pragma unroll
     for (int v = 0; v < VALUES; v++) sums[0][v][lane] = value(v);
   __syncthreads();
+  if constexpr (EPI == FF_LINEAR) dropout_at_step(p.drop);
   // four neighbouring columns of a token per thread
   const int rows = p.M - row0 < 16 ? (int)(p.M - row0) : 16;
   for (int e = threadIdx.x; e < rows * (FK_COLS / 4); e += FK_WAVES * 64) {
     const int t = e / (FK_COLS / 4), in = e % (FK_COLS / 4) * 4;
     const long long at = col0 + in;
     if (at >= N) continue;
-    f32x4 v[2];
+    f32x4 v[2] = {};
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int i = 0; i < PRODUCTS; i++)
 #pragma unroll
       for (int q = 0; q < 4; q++) v[i][q] = sums[0][(i * CW + (in + q) % CW) * 4 + t % 4][t / 4 * 16 + (in + q) / CW];
     FfVec4<float> d = {};
-    if constexpr (EPI == FF_GRAD) d = ff_upstream<float>(p, row0 + t, at, N);
-    ff_finish<EPI, true, float>(p, row0 + t, at, N, v[0], v[1], d);
+    f32x4 bias = {};
+    if constexpr (FF_UPSTREAM<EPI>) d = ff_upstream<float>(p, row0 + t, at, N);
+    if constexpr (EPI == FF_LINEAR) bias = ff_bias<float>(p, at, N);
+    ff_finish<EPI, DUAL, float>(p, row0 + t, at, N, v[0], v[1], d, bias);
   }
 }
 
+}  // namespace
 }  // namespace mlproj
 #endif

@@ -6,6 +6,7 @@
 #include "ffcommon.h"
 
 namespace mlproj {
+namespace {      // (each translation unit that includes this has its own kernels)
 
 // ------------------------------------------------------------------ tiles staged through registers
 // A workgroup of four wavefronts computes 128 rows x 128 columns (two products: 128 x 64 of each, the same
@@ -240,15 +241,25 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
     if (__any(nan)) fs_again<A_KC, B_KC, DUAL>(p, row0 + wm * 64, col0 + wn * 32, N, K, ksteps, first, last, lane, acc);
   }
 
-  FfVec4<T> d[4][2] = {};
-  if constexpr (EPI == FF_GRAD) {
+  constexpr int QUADS = DUAL ? 2 : 4;
+  auto column = [&](int j) { return col0 + wn * 32 + (j & 1) * 16 + (j >> 1) * 64 + (lane >> 4) * 4; };
+  FfVec4<T> d[4][QUADS] = {};
+  f32x4 bias[QUADS] = {};
+  if constexpr (FF_UPSTREAM<EPI>) {
+    if (p.dH)
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+      for (int i = 0; i < 4; i++)
 #pragma unroll
-      for (int j = 0; j < 2; j++) {
-        const long long row = row0 + wm * 64 + i * 16 + (lane & 15), col = col0 + wn * 32 + j * 16 + (lane >> 4) * 4;
-        if (row < p.M && col < N) d[i][j] = ff_upstream<T>(p, row, col, N);
-      }
+        for (int j = 0; j < QUADS; j++) {
+          const long long row = row0 + wm * 64 + i * 16 + (lane & 15), col = column(j);
+          if (row < p.M && col < N) d[i][j] = ff_upstream<T>(p, row, col, N);
+        }
+  }
+  if constexpr (EPI == FF_LINEAR) {
+    dropout_at_step(p.drop);
+#pragma unroll
+    for (int j = 0; j < QUADS; j++)
+      if (column(j) < N) bias[j] = ff_bias<T>(p, column(j), N);
   }
 #pragma unroll
   for (int i = 0; i < 4; i++) {
@@ -260,8 +271,8 @@ __global__ __launch_bounds__(FS_THREADS) void ff_staged_kernel(FfProduct p) {
       if constexpr (DUAL) {
         if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][2 + j], d[i][j]);
       } else {
-        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, {});
-        if (col + 64 < N) ff_finish<EPI, false, T>(p, row, col + 64, N, acc[i][2 + j], f32x4{}, {});
+        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, d[i][j], bias[j]);
+        if (col + 64 < N) ff_finish<EPI, false, T>(p, row, col + 64, N, acc[i][2 + j], f32x4{}, d[i][2 + j], bias[2 + j]);
       }
     }
   }
@@ -300,9 +311,15 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p) {
   }
   if (!there) return;
   FfVec4<T> d = {};
-  if constexpr (EPI == FF_GRAD) d = ff_upstream<T>(p, row, col, N);
-  ff_finish<EPI, DUAL, T>(p, row, col, N, v[0], v[1], d);
+  f32x4 bias = {};
+  if constexpr (FF_UPSTREAM<EPI>) d = ff_upstream<T>(p, row, col, N);
+  if constexpr (EPI == FF_LINEAR) {
+    dropout_at_step(p.drop);
+    bias = ff_bias<T>(p, col, N);
+  }
+  ff_finish<EPI, DUAL, T>(p, row, col, N, v[0], v[1], d, bias);
 }
 
+}  // namespace
 }  // namespace mlproj
 #endif
