@@ -223,24 +223,62 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p)
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0)
 
-  const long long my_row = row0 + wm * RI * 16 + (lane & 15), my_col = col0 + wn * CJ * 16 + (lane >> 4) * 4;
-  constexpr int QUADS = DUAL ? CJ : 2 * CJ;      // of a row's columns in the result
-  auto column = [&](int j) { return my_col + (j < CJ ? j * 16 : BW + (j - CJ) * 16); };
-  FfVec4<T> d[RI][QUADS] = {};
-  f32x4 bias[QUADS] = {};
-  if constexpr (FF_UPSTREAM<EPI>) {
-    if (p.dH)
-#pragma unroll
-      for (int i = 0; i < RI; i++)
-#pragma unroll
-        for (int j = 0; j < QUADS; j++)
-          if (my_row + i * 16 < p.M && column(j) < N) d[i][j] = ff_upstream<T>(p, my_row + i * 16, column(j), N);
-  }
   if constexpr (EPI == FF_LINEAR) {
+    // Through LDS, of which each wavefront has a share: the epilogue is long (activation, generator of the dropout), and in a
+    // loop it is there four times and not once for each of the 32 quads of a lane, for which the registers would not do.
+    static_assert(CJ == 2 && !DUAL, "a wavefront's rows are 16 quads");
+    constexpr int WAVES = WM * WN, TILES = RI < 4 ? RI : 4, CHUNK = 4;
+    static_assert(WAVES / 4 * TILES * 16 * 256 <= STAGE, "a wavefront's share");
+    typedef __attribute__((address_space(3))) unsigned char byte_t;
+    typedef __attribute__((address_space(3))) f32x4 quad_t;
+    byte_t* mine = ((wave & 3) == 0 ? (byte_t*)lds0 : (wave & 3) == 1 ? (byte_t*)lds1 : (wave & 3) == 2 ? (byte_t*)lds2 : (byte_t*)lds3) + (wave >> 2) * TILES * 16 * 256;
     dropout_at_step(p.drop);
+    const int quad = lane & 15, c = lane & 15, g = lane >> 4;
+    const long long col = col0 + wn * 32 + (quad >> 2 & 1) * 16 + (quad >> 3) * BW + (quad & 3) * 4, top = row0 + wm * RI * 16;
+    const f32x4 bias = col < N ? ff_bias<T>(p, col, N) : f32x4{};
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < QUADS; j++)
-      if (column(j) < N) bias[j] = ff_bias<T>(p, column(j), N);
+    for (int pass = 0; pass < RI / TILES; pass++) {
+      // row r's quad q lies at place q ^ (r % 16): the 16 rows that a store takes at a time are in different banks
+#pragma unroll
+      for (int i = 0; i < TILES; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+          *(quad_t*)(mine + (i * 16 + c) * 256 + (((j * 4 + g) ^ c) << 4)) = acc[pass * TILES + i][j];
+      const long long first_row = top + pass * TILES * 16 + g;
+      FfVec4<T> d[CHUNK], next[CHUNK];
+      auto fetch = [&](int chunk, FfVec4<T> (&to)[CHUNK]) {
+#pragma unroll
+        for (int u = 0; u < CHUNK; u++) {
+          const long long row = first_row + (chunk * CHUNK + u) * 4;
+          to[u] = {};
+          if (p.dH && row < p.M && col < N) to[u] = ff_upstream<T>(p, row, col, N);
+        }
+      };
+      fetch(0, d);
+#pragma unroll 1
+      for (int chunk = 0; chunk < TILES * 4 / CHUNK; chunk++) {
+        if (chunk + 1 < TILES * 4 / CHUNK) fetch(chunk + 1, next);
+#pragma unroll
+        for (int u = 0; u < CHUNK; u++) {
+          const int r = (chunk * CHUNK + u) * 4 + g;
+          const f32x4 v = *(const quad_t*)(mine + r * 256 + ((quad ^ (r & 15)) << 4));
+          const long long row = first_row + (chunk * CHUNK + u) * 4;
+          if (row < p.M && col < N) ff_finish<EPI, false, T>(p, row, col, N, v, f32x4{}, d[u], bias);
+          d[u] = next[u];
+        }
+      }
+    }
+    return;
+  }
+  const long long my_row = row0 + wm * RI * 16 + (lane & 15), my_col = col0 + wn * CJ * 16 + (lane >> 4) * 4;
+  FfVec4<T> d[RI][CJ] = {};
+  if constexpr (EPI == FF_GRAD) {
+#pragma unroll
+    for (int i = 0; i < RI; i++)
+#pragma unroll
+      for (int j = 0; j < CJ; j++)
+        if (my_row + i * 16 < p.M && my_col + j * 16 < N) d[i][j] = ff_upstream<T>(p, my_row + i * 16, my_col + j * 16, N);
   }
 #pragma unroll
   for (int i = 0; i < RI; i++) {
@@ -252,8 +290,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void ff_direct_kernel(FfProduct p)
       if constexpr (DUAL) {
         if (col < N) ff_finish<EPI, true, T>(p, row, col, N, acc[i][j], acc[i][CJ + j], d[i][j]);
       } else {
-        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, d[i][j], bias[j]);
-        if (col + BW < N) ff_finish<EPI, false, T>(p, row, col + BW, N, acc[i][CJ + j], f32x4{}, d[i][CJ + j], bias[CJ + j]);
+        if (col < N) ff_finish<EPI, false, T>(p, row, col, N, acc[i][j], f32x4{}, {});
+        if (col + BW < N) ff_finish<EPI, false, T>(p, row, col + BW, N, acc[i][CJ + j], f32x4{}, {});
       }
     }
   }
