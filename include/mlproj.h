@@ -575,6 +575,43 @@ int block_norm_backward(int storage, const mlproj_norm_block* block /* host */, 
                         float* dw_pre /* device, n; may be NULL */,
                         void* workspace /* device */, size_t workspace_bytes, void* stream);
 
+/* A matrix in 8 bits: rows of codes in e4m3 (sign, four exponent bits, three fraction bits, no infinities: at most 448),
+ * each times the power of two 2^(byte - 127) of its group, 32 neighbouring entries of its row.  Rows are in whole blocks of 128
+ * entries: past n, codes are zeros (their scales are any but 255).  This is what the matrix cores multiply; a weight matrix n x m that x is
+ * multiplied by (x W) is held by its columns, as m rows of n.
+ *   codes   row i at codes + i * ld bytes; 16-byte aligned, ld a multiple of 16 and at least n in whole blocks
+ *   scales  row i at scales + i * lds bytes; 4-byte aligned, lds a multiple of 4 and at least a byte per group of those    */
+typedef struct mlproj_q8 {
+  long long rows, n;
+  void* codes;                /* device                                               */
+  long long ld;
+  void* scales;               /* device                                               */
+  long long lds;
+} mlproj_q8;
+
+/* Packs a matrix into `packed`: A (rows x n) as it lies (by_columns = 0), or by its columns (1: A is n x rows, as a weight
+ * matrix).  The scale of a group is the smallest power of two (2^-127 at least) with which its largest magnitude is at most 448; codes
+ * are rounded to nearest-even.  A group with a NaN or an infinity is NaN throughout.                */
+int q8_pack(int storage, int by_columns, const void* A /* device */, long long lda, const mlproj_q8* packed /* host */, void* stream);
+
+/* block_norm_forward with y in 8 bits, rounded as q8_pack rounds, from the y that is not rounded to the storage type: tokens
+ * rows of n entries.  w_pre is needed.  `y`: codes and scales are written, whole blocks of them.                 */
+int block_norm8_forward(int storage, const mlproj_norm_block* block /* host */, const void* x /* device */, long long ldx,
+                        void* r /* device */, long long ldr, const mlproj_q8* y /* host */, void* stream);
+
+/* Products with both operands in 8 bits: x is tokens x n, W holds an n x m matrix by its columns (m rows of n); every other
+ * array is of the storage type.  With fp32 storage products and sums are fp32 (entries below 2^-126 count as zeros); with 16 bits they are
+ * the matrix cores' own, whose sums of eight products keep 16 bits beside the largest of them.
+ * q8_linear: y = residual + act(x W + bias); bias and residual may be NULL, y may be the residual (in place, same stride).
+ * q8_gated:  h = act(x Wg) * (x Wu); Wg and Wu of the same size and strides.  A pruned column is a row of zeros.
+ * Strides of packed rows are at most 2^22 here (MLPROJ_ERR_TOO_LARGE).                              */
+int mlproj_q8_workspace_bytes(long long tokens, long long n, long long m, int gated, size_t* bytes_out /* host */);
+int q8_linear(int storage, int activation, const mlproj_q8* x /* host */, const mlproj_q8* W /* host */,
+              const void* bias /* device, m; may be NULL */, const void* residual /* device, tokens x m; may be NULL */, long long ldr,
+              void* y /* device, tokens x m */, long long ldy, void* workspace /* device */, size_t workspace_bytes, void* stream);
+int q8_gated(int storage, int activation, const mlproj_q8* x /* host */, const mlproj_q8* Wg /* host */, const mlproj_q8* Wu /* host */,
+             void* h /* device, tokens x m */, long long ldh, void* workspace /* device */, size_t workspace_bytes, void* stream);
+
 /* A weight matrix in 4 bits.  Every entry is a code: sign bit, two exponent bits, one fraction bit (0, 0.5, 1, 1.5,
  * 2, 3, 4, 6 and their negatives) times the bf16 scale of its group, `group` (32, 64 or 128) neighbouring rows of one
  * column.  Column block c holds columns 16 c .. 16 c + 15 and row block k rows 128 k .. 128 k + 127; past the

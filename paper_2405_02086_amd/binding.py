@@ -12,7 +12,7 @@ import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmlproj.so")
-SRC_PATHS = [os.path.join(_HERE, "csrc", name) for name in ("mlproj.hip", "heldmulti.hip", "gatedff.hip", "linear.hip", "blocknorm.hip", "w4.hip")]
+SRC_PATHS = [os.path.join(_HERE, "csrc", name) for name in ("mlproj.hip", "heldmulti.hip", "gatedff.hip", "linear.hip", "blocknorm.hip", "w4.hip", "q8.hip")]
 
 L1INF, L11, L12, L1INFINF = 0, 1, 2, 3
 _VARIANTS = {"l1inf": L1INF, "l11": L11, "l12": L12, "tri": L1INFINF}
@@ -153,6 +153,17 @@ def lib():
     L.block_norm_backward.restype = c_i
     L.block_norm_backward.argtypes = [c_i, norm, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_vp, c_ll,
                                       c_vp, c_vp, c_sz, c_vp]
+    q8 = ctypes.POINTER(PackedQ8)
+    L.q8_pack.restype = c_i
+    L.q8_pack.argtypes = [c_i, c_i, c_vp, c_ll, q8, c_vp]
+    L.block_norm8_forward.restype = c_i
+    L.block_norm8_forward.argtypes = [c_i, norm, c_vp, c_ll, c_vp, c_ll, q8, c_vp]
+    L.mlproj_q8_workspace_bytes.restype = c_i
+    L.mlproj_q8_workspace_bytes.argtypes = [c_ll, c_ll, c_ll, c_i, ctypes.POINTER(c_sz)]
+    L.q8_linear.restype = c_i
+    L.q8_linear.argtypes = [c_i, c_i, q8, q8, c_vp, c_vp, c_ll, c_vp, c_ll, c_vp, c_sz, c_vp]
+    L.q8_gated.restype = c_i
+    L.q8_gated.argtypes = [c_i, c_i, q8, q8, q8, c_vp, c_ll, c_vp, c_sz, c_vp]
     L.mlproj_w4_bytes.restype = c_i
     L.mlproj_w4_bytes.argtypes = [c_ll, c_ll, c_i, ctypes.POINTER(c_sz), ctypes.POINTER(c_sz)]
     L.w4_pack.restype = c_i
@@ -198,6 +209,12 @@ class NormBlock(ctypes.Structure):
                 ("w_pre", ctypes.c_void_p), ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
+class PackedQ8(ctypes.Structure):
+    """mlproj_q8 of include/mlproj.h."""
+    _fields_ = [("rows", ctypes.c_longlong), ("n", ctypes.c_longlong), ("codes", ctypes.c_void_p), ("ld", ctypes.c_longlong),
+                ("scales", ctypes.c_void_p), ("lds", ctypes.c_longlong)]
+
+
 class PackedW4(ctypes.Structure):
     """mlproj_w4 of include/mlproj.h."""
     _fields_ = [("n", ctypes.c_longlong), ("m", ctypes.c_longlong), ("group", ctypes.c_int), ("codes", ctypes.c_void_p),
@@ -215,6 +232,7 @@ EXPORTS = (
     "mlproj_gated_ff_workspace_bytes", "mlproj_gated_ff_route", "gated_ff_forward", "gated_ff_backward",
     "mlproj_linear_workspace_bytes", "linear_forward", "linear_backward", "dropout_forward",
     "block_norm_forward", "mlproj_block_norm_workspace_bytes", "block_norm_backward",
+    "q8_pack", "block_norm8_forward", "mlproj_q8_workspace_bytes", "q8_linear", "q8_gated",
     "mlproj_w4_bytes", "w4_pack", "w4_matvec", "w4_gated_matvec",
 )
 
@@ -931,6 +949,119 @@ def block_norm_backward(dr, dy, r, b=None, w_post=None, gate=None, w_pre=None, s
     if st != 0:
         _check(st, "block_norm_backward")
     return dx, db, dw_post, dgate, dw_pre
+
+
+class Q8:
+    """A matrix in 8 bits (mlproj_q8 of include/mlproj.h): rows of n entries, each a code times the power of two of its 32
+    neighbours.  codes: a float8_e4m3fn tensor of rows x n filled up with zeros to whole blocks of 128, scales: a float8_e8m0fnu
+    tensor of rows x one per 32 of those; the rows of either may be further apart (codes by multiples of 16, scales of 4)."""
+
+    def __init__(self, n, codes, scales):
+        torch = _import_torch()
+        rows, wide = codes.shape
+        assert codes.is_cuda and codes.dtype is torch.float8_e4m3fn and wide == -(-n // 128) * 128, "codes: rows x n in whole blocks of 128, e4m3"
+        assert scales.is_cuda and scales.dtype is torch.float8_e8m0fnu and scales.shape == (rows, wide // 32), "scales: one e8m0 per 32 codes"
+        ld, lds = _matrix(codes, (rows, wide), codes, "codes"), _matrix(scales, (rows, wide // 32), scales, "scales")
+        self.rows, self.n, self.codes, self.scales = rows, n, codes, scales
+        self._struct = PackedQ8(rows, n, codes.data_ptr(), ld, scales.data_ptr(), lds)
+        self._ref = ctypes.byref(self._struct)
+
+
+def _new_q8(like, rows, n, stream):
+    torch = _torch
+    wide = (n + 127) // 128 * 128
+    return Q8(n, _new_empty(like, (rows, wide), torch.float8_e4m3fn, stream), _new_empty(like, (rows, wide // 32), torch.float8_e8m0fnu, stream))
+
+
+def _result_q8(q, rows, n, like, what, stream):
+    if q is None:
+        return _new_q8(like, rows, n, stream)
+    assert q.rows == rows and q.n == n, what
+    return q
+
+
+def q8_pack(A, columns=False, packed=None, stream=None):
+    """Packs a device matrix (fp32, bf16, fp16) into a Q8: its rows, or with columns=True its columns, as a weight
+    matrix n x m is held (m rows of n)."""
+    assert A.dim() == 2
+    rows, n = (A.shape[1], A.shape[0]) if columns else A.shape
+    lda = _matrix(A, tuple(A.shape), A, "A")
+    packed = _result_q8(packed, rows, n, A, "packed: the matrix's size", stream)
+    st = lib().q8_pack(_storage(A.dtype), int(columns), A.data_ptr(), lda, packed._ref, _stream(stream))
+    if st != 0:
+        _check(st, "q8_pack")
+    return packed
+
+
+def block_norm8(x, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e-6, r=None, y=None, stream=None):
+    """block_norm with y in 8 bits (a Q8), rounded from the y that is not yet rounded to x's type; w_pre is needed."""
+    assert x.dim() == 2 and w_pre is not None
+    storage = _storage(x.dtype)
+    block, shape, _ = _norm_block(x, b, w_post, gate, w_pre, scale, eps)
+    ldx, ldr, at_r = _matrix(x, shape, x, "x"), 0, None
+    if b is None:
+        r = x
+    else:
+        r, ldr = _result(r, shape, x, "r", stream)
+        at_r = r.data_ptr()
+    y = _result_q8(y, shape[0], shape[1], x, "y: a Q8 of x's size", stream)
+    st = lib().block_norm8_forward(storage, ctypes.byref(block), x.data_ptr(), ldx, at_r, ldr, y._ref, _stream(stream))
+    if st != 0:
+        _check(st, "block_norm8_forward")
+    return r, y
+
+
+def q8_workspace_bytes(tokens, n, m, gated=False):
+    out = ctypes.c_size_t(0)
+    _check(lib().mlproj_q8_workspace_bytes(tokens, n, m, int(gated), ctypes.byref(out)), "mlproj_q8_workspace_bytes")
+    return out.value
+
+
+def _q8_result(out, like, shape, dtype, what, stream):
+    if out is None:
+        return _new_empty(like, shape, dtype, stream), shape[1]
+    return out, _matrix(out, shape, out, what)
+
+
+def q8_linear(x, W, bias=None, residual=None, act=None, dtype=None, y=None, workspace=None, stream=None):
+    """y = residual + act(x W + bias) with x (tokens of n) and W (packed by its columns) Q8s; bias, residual and y of one type:
+    `dtype`, or that of the first of them there is, else bf16.  act: None, "silu", "gelu" or "relu".  y may be the residual."""
+    torch = _import_torch()
+    shape, given = (x.rows, W.rows), y if y is not None else residual if residual is not None else bias
+    assert W.n == x.n, "x and W: rows of one length"
+    if dtype is None:
+        dtype = given.dtype if given is not None else torch.bfloat16
+    storage = _storage(dtype)
+    y, ldy = _q8_result(y, x.codes, shape, dtype, "y", stream)
+    assert y.dtype is dtype, "y: of that type"
+    at_bias = None if bias is None else _vector(bias, (W.rows,), y, "bias: one entry per column")
+    ldr = 0 if residual is None else _matrix(residual, shape, y, "residual")
+    if workspace is None:
+        workspace = Workspace(q8_workspace_bytes(x.rows, x.n, W.rows), device=x.codes.device, stream=stream)
+    st = lib().q8_linear(storage, _ACTS[act], x._ref, W._ref, at_bias, _ptr(residual), ldr, y.data_ptr(), ldy,
+                         workspace.buf.data_ptr(), workspace.nbytes, _stream(stream))
+    if st != 0:
+        _check(st, "q8_linear")
+    return y
+
+
+def q8_gated(x, Wg, Wu, act="silu", dtype=None, h=None, workspace=None, stream=None):
+    """h = act(x Wg) * (x Wu) with x, Wg and Wu Q8s (the weights packed by their columns, of one size); h of `dtype` (bf16)."""
+    torch = _import_torch()
+    shape = (x.rows, Wg.rows)
+    assert Wg.n == x.n and Wu.n == x.n and Wu.rows == Wg.rows, "x, Wg and Wu: rows of one length"
+    if dtype is None:
+        dtype = h.dtype if h is not None else torch.bfloat16
+    storage = _storage(dtype)
+    h, ldh = _q8_result(h, x.codes, shape, dtype, "h", stream)
+    assert h.dtype is dtype, "h: of that type"
+    if workspace is None:
+        workspace = Workspace(q8_workspace_bytes(x.rows, x.n, Wg.rows, True), device=x.codes.device, stream=stream)
+    st = lib().q8_gated(storage, _ACTS[act], x._ref, Wg._ref, Wu._ref, h.data_ptr(), ldh, workspace.buf.data_ptr(), workspace.nbytes,
+                        _stream(stream))
+    if st != 0:
+        _check(st, "q8_gated")
+    return h
 
 
 def w4_bytes(n, m, group):

@@ -1,6 +1,7 @@
 // mlproj: the norms before and after a block, fused with its gate and the residual scale; kernels, plan and C ABI.
 #include "ffcommon.h"
 #include "host.h"
+#include "q8.h"
 
 namespace mlproj {
 namespace {
@@ -23,6 +24,8 @@ struct BnArgs {
   float* partial;                               // [3][workgroups][n] sums over a workgroup's rows
   long long ldx, ldb, gate_stride, ldr, ldy, lddr, lddy, lddx, lddb, dgate_stride;
   long long tokens, n;
+  unsigned char *codes, *scales;                // forward, y in 8 bits: instead of y
+  long long ldq, lds;
   float scale, eps;
   int want_post, want_gate, want_pre;           // backward: which sums over tokens are wanted
 };
@@ -53,6 +56,19 @@ __device__ __forceinline__ void bn_store(T* p, long long valid, const float (&x)
   }
 }
 
+// Entries at .. at + VEC - 1 of y in 8 bits.  All lanes of a wavefront are here, those past the row's end too: it is filled up with
+// zeros to whole blocks.
+template <int VEC>
+__device__ __forceinline__ void bn_eight(const BnArgs& a, long long row, long long at, float (&v)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; i++) v[i] = at + i < a.n ? v[i] : 0.0f;
+  unsigned codes[VEC / 4];
+  const unsigned scale = q8_round<VEC>(v, codes);
+  if (at >= q8_wide(a.n)) return;
+  __builtin_memcpy(a.codes + row * a.ldq + at, codes, VEC);
+  if (at % Q8_GROUP == 0) a.scales[row * a.lds + at / Q8_GROUP] = (unsigned char)scale;
+}
+
 // Sums N values over the row's threads, everyone gets them.  `slot`: LDS of [2][N][16], the halves used in turn so
 // that one barrier per sum is enough.
 template <int THREADS, int N>
@@ -80,7 +96,7 @@ __device__ __forceinline__ void bn_sum(float (&v)[N], float (*slot)[16], int lan
 constexpr int BN_LONG = 512;
 // Rows too long for registers: CH pieces per thread at a time, and every phase reads them again (from L2, where a row
 // still is).
-template <typename T>
+template <typename T, bool EIGHT>
 __global__ __launch_bounds__(BN_LONG) void bn_forward_long_kernel(BnArgs a) {
   constexpr int THREADS = BN_LONG, CH = 2;
   constexpr int VEC = BN_VEC<T>;
@@ -153,6 +169,15 @@ __global__ __launch_bounds__(BN_LONG) void bn_forward_long_kernel(BnArgs a) {
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       const long long at = pass * per + ((long long)c * THREADS + t) * VEC;
+      if (EIGHT) {
+        float w[VEC];
+        bn_load<T, VEC>(w_pre + at, n - at, w);
+        if (b && at < n) bn_store<T, VEC>(r + at, n - at, vx[c]);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) w[i] *= vx[c][i] * rr;
+        bn_eight<VEC>(a, row, at, w);
+        continue;
+      }
       if (at >= n) break;
       if (b) bn_store<T, VEC>(r + at, n - at, vx[c]);
       if (w_pre) {
@@ -350,7 +375,7 @@ struct BnPieces {
 template <int THREADS> constexpr int BN_GROUP = THREADS < 256 ? 256 : THREADS;   // threads of a workgroup
 template <int THREADS> constexpr int BN_ROWS = BN_GROUP<THREADS> / THREADS;      // rows it has in hand
 
-template <typename T, int THREADS, int CH, bool AHEAD>
+template <typename T, int THREADS, int CH, bool AHEAD, bool EIGHT>
 __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a) {
   constexpr int ROWS = BN_ROWS<THREADS>;
   using Pieces = BnPieces<T, THREADS, CH>;
@@ -426,6 +451,15 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
 #pragma unroll
     for (int c = 0; c < CH; c++) {
       const long long at = ((long long)c * THREADS + t) * VEC;
+      if (EIGHT) {
+        float w[VEC];
+        piece(w_pre, p_pre, c, w);
+        if (block && at < n) bn_store<T, VEC>(static_cast<T*>(a.r) + row * a.ldr + at, n - at, v[c]);
+#pragma unroll
+        for (int i = 0; i < VEC; i++) w[i] *= v[c][i] * rr;
+        bn_eight<VEC>(a, row, at, w);
+        continue;
+      }
       if (at >= n) break;
       if (block) bn_store<T, VEC>(static_cast<T*>(a.r) + row * a.ldr + at, n - at, v[c]);
       if (pre) {
@@ -435,6 +469,11 @@ __global__ __launch_bounds__(BN_GROUP<THREADS>) void bn_forward_kernel(BnArgs a)
         for (int i = 0; i < VEC; i++) w[i] *= v[c][i] * rr;
         bn_store<T, VEC>(static_cast<T*>(a.y) + row * a.ldy + at, n - at, w);
       }
+    }
+    if constexpr (EIGHT && THREADS * CH * VEC < Q8_BLOCK) {
+      // fp32 rows of up to 64 entries: the other half of their block
+      float zero[VEC] = {};
+      bn_eight<VEC>(a, row, (long long)(THREADS * CH + t) * VEC, zero);
     }
     if (!AHEAD && row + workers < a.tokens) fetch(row + workers);
   }
@@ -680,14 +719,14 @@ long long bn_groups(int threads, long long tokens) {
   return groups < most ? groups : most;
 }
 
-template <typename T>
+template <typename T, bool EIGHT>
 int run_forward(const BnArgs& a, hipStream_t stream) {
   bn_shape<T>(a.n, [&](auto th, auto ch, auto ahead) {
     mark(stream);
     if constexpr (ch.value == 0)
-      launch(bn_forward_long_kernel<T>, dim3((unsigned)a.tokens), dim3(BN_LONG), stream, a);
+      launch(bn_forward_long_kernel<T, EIGHT>, dim3((unsigned)a.tokens), dim3(BN_LONG), stream, a);
     else
-      launch(bn_forward_kernel<T, th.value, ch.value, ahead.value>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
+      launch(bn_forward_kernel<T, th.value, ch.value, ahead.value, EIGHT>, dim3((unsigned)bn_groups(th.value, a.tokens)), dim3(BN_GROUP<th.value>), stream, a);
   });
   mark(stream);
   return launch_status();
@@ -792,9 +831,30 @@ int block_norm_forward(int storage, const mlproj_norm_block* k, const void* x, l
   BnArgs a = bn_start(k);
   a.x = x; a.ldx = ldx; a.r = r; a.ldr = ldr; a.y = y; a.ldy = ldy;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (storage == MLPROJ_STORE_F32) return run_forward<float>(a, s);
-  if (storage == MLPROJ_STORE_BF16) return run_forward<bf16_t>(a, s);
-  return run_forward<f16_t>(a, s);
+  if (storage == MLPROJ_STORE_F32) return run_forward<float, false>(a, s);
+  if (storage == MLPROJ_STORE_BF16) return run_forward<bf16_t, false>(a, s);
+  return run_forward<f16_t, false>(a, s);
+}
+
+int block_norm8_forward(int storage, const mlproj_norm_block* k, const void* x, long long ldx, void* r, long long ldr,
+                        const mlproj_q8* y, void* stream) {
+  BN_TRY(bn_check(storage, k));
+  const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
+  const bool some = k->tokens > 0;
+  if (!k->w_pre) return MLPROJ_ERR_NULL_POINTER;
+  BN_TRY(bn_inputs(k, es));
+  BN_TRY(bn_array(x, some, k->n, ldx, es));
+  BN_TRY(bn_array(r, some && k->w_post, k->n, ldr, es));
+  BN_TRY(q8_check(y, k->tokens, k->n, some));
+  if (!some) return MLPROJ_OK;
+  BnArgs a = bn_start(k);
+  a.x = x; a.ldx = ldx; a.r = r; a.ldr = ldr;
+  a.codes = static_cast<unsigned char*>(y->codes); a.ldq = y->ld;
+  a.scales = static_cast<unsigned char*>(y->scales); a.lds = y->lds;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (storage == MLPROJ_STORE_F32) return run_forward<float, true>(a, s);
+  if (storage == MLPROJ_STORE_BF16) return run_forward<bf16_t, true>(a, s);
+  return run_forward<f16_t, true>(a, s);
 }
 
 int mlproj_block_norm_workspace_bytes(long long tokens, long long n, size_t* bytes_out) {
