@@ -102,7 +102,7 @@ void q8_tiles(const Q8Product& q, int kind, hipStream_t stream) {
   const long long M = q.p.M, N = q.p.N, splits = q.p.splits;
   if constexpr (!EXACT) {
     if (kind == 0) {
-      launch(q8_tile_kernel<T, DUAL, EPI, 256, 256, 2, 2, EXACT>, dim3((unsigned)(ff_cdiv(M, 256) * ff_cdiv(N, 256 / HALF) * splits)), dim3(256), stream, q);
+      launch(q8_tile_kernel<T, DUAL, EPI, 256, 256, 2, 4, EXACT>, dim3((unsigned)(ff_cdiv(M, 256) * ff_cdiv(N, 256 / HALF) * splits)), dim3(512), stream, q);
       return;
     }
   }

@@ -35,29 +35,36 @@ __device__ __forceinline__ bf16x8 q8_widen(int lo, int hi, unsigned scale) {
 }
 
 // ------------------------------------------------------------------ tiles
-// The ring of ffdirect.h with rows of 64 codes: a step is one 32 x 32 x 64 matrix instruction per operand pair, whose lane holds 16 codes
-// of each of two groups of a row and the scale of one of them.  The scales of two steps (a block of 128) are one dword per
-// row, which comes with the even step's tile into one of two places.
+// Blocks of 128 along K lie in LDS in two places, each row's 128 codes together: a cache line, which a load's eight lanes bring
+// in whole.  A block is two steps of 32 x 32 x 64 matrix instructions, whose lane holds 16 codes of each of two groups of a row and
+// the scale of one of them.  While the matrix cores work on a step's operands, which are in registers, the next step's are read
+// from LDS; once the second step's are, everybody meets, and the loads of the block after the next one take the block's
+// place.  Scales come four blocks at a time: a row's scales of one block are four bytes of a cache line of their own.
+//
+// Bound by L2, which hands a compute unit about 22 bytes per cycle, beside the matrix cores: 4096 x 16384 -> 4096, 256 tiles of 256 x
+// 256, 2.1 GB: loads alone take 170 us, products alone 174.  Rows of 64 codes in a ring of four places, as ffdirect.h has
+// it, ask for half lines: 200 us for the loads alone, and scales block by block for as many lines as the codes: 211.
 constexpr int Q8_STEP = 64;
 
-// Loads of `W` rows.
+// Loads of `W` rows of a block, THREADS / 8 at a time: a thread's place in each of them is the same, and rows past the last
+// one lie past the end of the buffer resource, which brings zeros.
 template <int W, int THREADS>
 struct Q8Part {
-  static constexpr int LOADS = W * Q8_STEP / 16 / THREADS;
-  unsigned offset[LOADS];
-  __device__ __forceinline__ void plan(int tid, long long ld, long long there) {
-#pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-      const int q = tid + i * THREADS, row = q >> 2, piece = (q & 3) ^ fd_row_turn(row);
-      offset[i] = row < there ? (unsigned)(row * ld + piece * 16) : FD_OUT;
-    }
+  static constexpr int ROWS = THREADS / 8, LOADS = W / ROWS;
+  static_assert(ROWS % 8 == 0 && LOADS * ROWS == W, "whole turns of the permutation");
+  long long ld;
+  int there;
+  __device__ __forceinline__ void plan(long long stride, long long rows) {
+    ld = stride;
+    there = rows < 0 ? 0 : rows < W ? (int)rows : W;
   }
-  __device__ __forceinline__ void load(const unsigned char* base, bool there, unsigned char* lds, int wave) const {
-    __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, there ? 0x7ffffff0u : 0u, 0x00020000);
+  __device__ __forceinline__ void load(const unsigned char* base, bool some, unsigned offset, unsigned char* lds, int wave) const {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
-      const unsigned at = offset[i];
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(lds + (wave * 64 + i * THREADS) * 16), 16, at, 0, 0, 0);
+      const int rows = some ? there - i * ROWS : 0;
+      const unsigned bytes = rows <= 0 ? 0u : (unsigned)((rows < ROWS ? rows : ROWS) * (int)ld);
+      __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base + i * ROWS * ld), 0, bytes, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(lds + (wave * 64 + i * THREADS) * 16), 16, offset, 0, 0, 0);
     }
   }
 };
@@ -93,10 +100,10 @@ template <typename T, bool DUAL, int EPI, int BM, int BN, int WM, int WN, bool E
 __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   constexpr int WAVES = WM * WN, THREADS = WAVES * 64, BW = BN / 2;
   constexpr int RT = BM / WM / 32, CJ = BN / WN / 64;          // 32 x 32 tiles of a wavefront: down, across in each half
-  constexpr int STAGE = (BM + BN) * Q8_STEP;
-  constexpr int CHUNKS = (BM + BN) / 64, SLOADS = (CHUNKS + WAVES - 1) / WAVES;
-  __shared__ __align__(16) unsigned char lds0[STAGE], lds1[STAGE], lds2[STAGE], lds3[STAGE];
-  __shared__ __align__(16) unsigned char scales0[SLOADS * WAVES * 256], scales1[SLOADS * WAVES * 256];
+  constexpr int SLOT = (BM + BN) * Q8_BLOCK;
+  constexpr int CHUNKS = (BM + BN) / 64, SLOADS = (CHUNKS + WAVES - 1) / WAVES, SROWS = SLOADS * WAVES * 64;
+  __shared__ __align__(16) unsigned char lds0[SLOT], lds1[SLOT];
+  __shared__ __align__(16) unsigned char scales[2 * 4 * SROWS * 4];
   FfProduct& p = q.p;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -105,37 +112,45 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   long long row0, col0;
   if (!ff_tile<BM, COLS>(p, N, &row0, &col0)) return;
   const int blocks = (int)(p.K / Q8_BLOCK);
-  const int first = (int)((long long)blocks * p.share / p.splits) * 2, last = (int)((long long)blocks * (p.share + 1) / p.splits) * 2;
+  const int first = (int)((long long)blocks * p.share / p.splits), last = (int)((long long)blocks * (p.share + 1) / p.splits);
 
   Q8Part<BM, THREADS> pa;
   Q8Part<BW, THREADS> pb[2];
-  pa.plan(tid, p.lda, p.M - row0);
+  pa.plan(p.lda, p.M - row0);
 #pragma unroll
-  for (int i = 0; i < 2; i++) pb[i].plan(tid, p.ldb, N - (col0 + (DUAL ? 0 : i * BW)));
+  for (int i = 0; i < 2; i++) pb[i].plan(p.ldb, N - (col0 + (DUAL ? 0 : i * BW)));
+  // rows' 16-byte pieces are permuted by the row's number, so that eight rows' spread over all banks
+  const unsigned piece = ((tid & 7) ^ ((tid >> 3) & 7)) * 16, offset_a = (tid >> 3) * (unsigned)p.lda + piece, offset_b = (tid >> 3) * (unsigned)p.ldb + piece;
   const unsigned char *A = static_cast<const unsigned char*>(p.A0) + row0 * p.lda;
   const unsigned char* B[2] = {static_cast<const unsigned char*>(p.B0) + col0 * p.ldb,
                                DUAL ? static_cast<const unsigned char*>(p.B1) + col0 * p.ldb : static_cast<const unsigned char*>(p.B0) + (col0 + BW) * p.ldb};
-  auto load = [&](int step, unsigned char* lds) {
-    const long long k0 = (long long)step * Q8_STEP;
-    const bool there = step < last;
-    pa.load(A + k0, there, lds, wave);
+  auto load = [&](int block, unsigned char* lds) {
+    const long long k0 = (long long)block * Q8_BLOCK;
+    const bool there = block < last;
+    pa.load(A + k0, there, offset_a, lds, wave);
 #pragma unroll
-    for (int i = 0; i < 2; i++) pb[i].load(B[i] + k0, there, lds + (BM + i * BW) * Q8_STEP, wave);
+    for (int i = 0; i < 2; i++) pb[i].load(B[i] + k0, there, offset_b, lds + (BM + i * BW) * Q8_BLOCK, wave);
   };
-  const unsigned char *const sA = q.sA, *const sB0 = q.sB0, *const sB1 = q.sB1;
+  // (both products' scales from one pointer: two that a lambda chooses from would be kept in scratch memory, with all arguments)
+  const unsigned char *const sA = q.sA, *const sB = q.sB0;
+  const long long to_second = DUAL ? q.sB1 - q.sB0 : 0;
   const long long ldsa = q.ldsa, ldsb = q.ldsb;
   // 64 rows' scales per wavefront and load: A's, then those of both halves of B
-  auto load_scales = [&](int block, unsigned char* to) {
+  auto load_scales = [&](int block, unsigned char* to, bool some) {
 #pragma unroll
     for (int i = 0; i < SLOADS; i++) {
       const int chunk = wave + i * WAVES, of_b = chunk - BM / 64, half = of_b >= BW / 64;
       const long long at = of_b < 0 ? row0 + chunk * 64 : col0 + (DUAL || !half ? 0 : BW) + (of_b - half * (BW / 64)) * 64;
       const long long there = chunk >= CHUNKS ? 0 : (of_b < 0 ? p.M : N) - at, ld = of_b < 0 ? +ldsa : +ldsb;
       const unsigned char* base = sA;
-      if (of_b >= 0) base = DUAL && half ? +sB1 : +sB0;
-      base += at * ld + (long long)block * 4;
-      __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, block * 2 < last ? 0x7ffffff0u : 0u, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(to + chunk * 256), 4, lane < there ? (unsigned)(lane * ld) : FD_OUT, 0, 0, 0);
+      if (of_b >= 0) base = sB + (DUAL && half ? to_second : 0);
+      base += at * ld;
+      const unsigned from = lane < there ? (unsigned)(lane * ld) : FD_OUT;
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base + (long long)(block + k) * 4), 0, some && block + k < last ? 0x7ffffff0u : 0u, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(to + (k * SROWS + chunk * 64) * 4), 4, from, 0, 0, 0);
+      }
     }
   };
 
@@ -143,19 +158,21 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   const int r = lane & 31, h = lane >> 5;
   using Operands = Q8Operands<RT, 2 * CJ>;
   using Scales = Q8Scales<RT, 2 * CJ>;
-  const int turn = fd_row_turn(r), low = r * Q8_STEP + ((h ^ turn) << 4), high = r * Q8_STEP + (((2 + h) ^ turn) << 4);
-  auto fragment = [&](const unsigned char* lds, int row) {
-    u32x4 v[2] = {*reinterpret_cast<const u32x4*>(lds + (low + row * Q8_STEP)), *reinterpret_cast<const u32x4*>(lds + (high + row * Q8_STEP))};
+  // where a lane's two pieces of each half of a row lie
+  const int at[2][2] = {{r * Q8_BLOCK + ((h ^ (r & 7)) << 4), r * Q8_BLOCK + (((2 + h) ^ (r & 7)) << 4)},
+                        {r * Q8_BLOCK + (((4 + h) ^ (r & 7)) << 4), r * Q8_BLOCK + (((6 + h) ^ (r & 7)) << 4)}};
+  auto fragment = [&](const unsigned char* lds, int row, int half) {
+    u32x4 v[2] = {*reinterpret_cast<const u32x4*>(lds + (at[half][0] + row * Q8_BLOCK)), *reinterpret_cast<const u32x4*>(lds + (at[half][1] + row * Q8_BLOCK))};
     i32x8 f;
     __builtin_memcpy(&f, v, 32);
     return f;
   };
-  auto read = [&](const unsigned char* lds) {
+  auto read = [&](const unsigned char* lds, int half) {
     Operands o;
 #pragma unroll
-    for (int j = 0; j < 2 * CJ; j++) o.b[j] = fragment(lds, BM + (j / CJ) * BW + wn * CJ * 32 + j % CJ * 32);
+    for (int j = 0; j < 2 * CJ; j++) o.b[j] = fragment(lds, BM + (j / CJ) * BW + wn * CJ * 32 + j % CJ * 32, half);
 #pragma unroll
-    for (int i = 0; i < RT; i++) o.a[i] = fragment(lds, wm * RT * 32 + i * 32);
+    for (int i = 0; i < RT; i++) o.a[i] = fragment(lds, wm * RT * 32 + i * 32, half);
     return o;
   };
   // the scales a lane gives are those of group h of a step
@@ -173,57 +190,51 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
     }
     return s;
   };
-  // Behind this all loads but those of the last two steps are in LDS (an even step's come with scales), and nobody reads what was read before.
-  constexpr int LOADS = (BM + BN) * Q8_STEP / 16 / THREADS;
-  auto meet = [&]() {
+  constexpr int MFMAS = RT * 2 * CJ, READS = (RT + 2 * CJ) * 2, LOADS = (BM + BN) * Q8_BLOCK / 16 / THREADS;
+  Operands even, odd;
+  Scales here, next;
+  // A block's scales are in place (number / 4) % 2, four blocks' together, [number % 4][row]; number: of the workgroup's blocks.
+  // (They are read before any load goes out: the compiler waits for loads into the array that it reads, whichever part it is.  Three
+  // times of four their loads ask for nothing: a branch round them would cut the block's instructions into parts that are ordered
+  // each for itself.)
+  auto scales_of = [&](int number) { return scales + (number & 7) * SROWS * 4; };
+  auto block_of = [&](int block, unsigned char* mine, unsigned char* other) {
+    odd = read(mine, 1);
+    q8_multiply<EXACT, 0>(even, here, acc);
+    if constexpr (!EXACT) fd_schedule<0, MFMAS, READS>();
     asm volatile("" ::: "memory");
-    constexpr int v = 2 * LOADS + SLOADS;
+    __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0) lgkmcnt(0): the next block is there, and what was read of this one
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int number = block - first;
+    next = read_scales(scales_of(number + 1));
+    load_scales(block + 5, scales_of(number + 5), (number & 3) == 3);
+    load(block + 2, mine);
+    even = read(other, 0);
+    q8_multiply<EXACT, 1>(odd, here, acc);
+    if constexpr (!EXACT) fd_schedule<0, MFMAS, READS>();
+    here = next;
+  };
+  load_scales(first, scales_of(0), true);
+  load(first, lds0);
+  load(first + 1, lds1);
+  load_scales(first + 4, scales_of(4), true);
+  {
+    // all but the last two are there
+    asm volatile("" ::: "memory");
+    constexpr int v = LOADS + 4 * SLOADS;
     __builtin_amdgcn_s_waitcnt(0x0070 | (v & 15) | ((v >> 4) << 14));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-  };
-  constexpr int MFMAS = RT * 2 * CJ, READS = (RT + 2 * CJ) * 2;
-  Operands even, odd;
-  Scales here, next;
-  // An even step makes room in its block's place for the scales of the block after the next one; an odd step reads the next block's.
-  auto even_step = [&](int step, unsigned char* at, unsigned char* ahead, unsigned char* scales) {
-    meet();
-    load_scales(step / 2 + 2, scales);
-    load(step + 4, at);
-    odd = read(ahead);
-    q8_multiply<EXACT, 0>(even, here, acc);
-    if constexpr (!EXACT) fd_schedule<0, MFMAS, READS>();
-  };
-  auto odd_step = [&](int step, unsigned char* at, unsigned char* ahead, const unsigned char* scales) {
-    meet();
-    load(step + 4, at);
-    even = read(ahead);
-    next = read_scales(scales);
-    q8_multiply<EXACT, 1>(odd, here, acc);
-    if constexpr (!EXACT) fd_schedule<0, MFMAS, READS + RT + 2 * CJ>();
-    here = next;
-  };
-
-  load_scales(first / 2, scales0);
-  load(first, lds0);
-  load(first + 1, lds1);
-  load_scales(first / 2 + 1, scales1);
-  load(first + 2, lds2);
-  meet();
-  even = read(lds0);
-  here = read_scales(scales0);
-  load(first + 3, lds3);
-  int step = first;
-  for (; step + 2 < last; step += 4) {
-    even_step(step, lds0, lds1, scales0);
-    odd_step(step + 1, lds1, lds2, scales1);
-    even_step(step + 2, lds2, lds3, scales1);
-    odd_step(step + 3, lds3, lds0, scales0);
   }
-  if (step < last) {
-    even_step(step, lds0, lds1, scales0);
-    odd_step(step + 1, lds1, lds2, scales1);
+  here = read_scales(scales_of(0));
+  even = read(lds0, 0);
+  int block = first;
+  for (; block + 1 < last; block += 2) {
+    block_of(block, lds0, lds1);
+    block_of(block + 1, lds1, lds0);
   }
+  if (block < last) block_of(block, lds0, lds1);
   // no load may be under way where results go, or when the workgroup's LDS is given to another
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0)
@@ -232,12 +243,12 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   // Results through LDS, each wavefront's in a share of its own, in whole rows (as in ffdirect.h).
   constexpr int QUADS = 2 * CJ * 8, PITCH = QUADS * 16, TILES = RT < 2 ? RT : 2, CHUNK = 4;
   constexpr int ACROSS = DUAL ? QUADS / 2 : QUADS, DOWN = 64 / ACROSS;      // of a wavefront's lanes
-  constexpr int SHARE = TILES * 32 * PITCH, PER = STAGE / SHARE;
-  static_assert(PER >= 1 && PER * 4 >= WAVES, "a wavefront's share of the stages");
+  constexpr int SHARE = TILES * 32 * PITCH, PER = SLOT / SHARE;
+  static_assert(PER >= 1 && PER * 2 >= WAVES, "a wavefront's share of the stages");
   typedef __attribute__((address_space(3))) unsigned char byte_t;
   typedef __attribute__((address_space(3))) f32x4 quad_t;
   const int stage = wave / PER;
-  byte_t* mine = (stage == 0 ? (byte_t*)lds0 : stage == 1 ? (byte_t*)lds1 : stage == 2 ? (byte_t*)lds2 : (byte_t*)lds3) + wave % PER * SHARE;
+  byte_t* mine = (stage == 0 ? (byte_t*)lds0 : (byte_t*)lds1) + wave % PER * SHARE;
   dropout_at_step(p.drop);
   const int quad = lane % ACROSS, down = lane / ACROSS, j = quad >> 3;
   const long long col = col0 + wn * CJ * 32 + (j < CJ ? j * 32 : BW + (j - CJ) * 32) + (quad & 7) * 4;
