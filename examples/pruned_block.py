@@ -1,9 +1,10 @@
 """A feed-forward block whose hidden channels the projection prunes: trained, projected after every step, packed to
-4 bits and asked token by token.
+4 bits and asked token by token, and packed to 8 bits and asked.
 
     python examples/pruned_block.py
 
-The block is  r = x + scale * gate * norm(h Wd),  y = norm(r)  with  h = silu(z Wg) * (z Wu)  and  z = norm(x).  It learns a
+The block is  r = x + scale * gate * norm(D(h Wd)),  y = norm(r)  with  h = silu(z Wg) * (z Wu),  z = norm(x)  and D a dropout
+(none by default).  It learns a
 teacher of the same form with few hidden channels; the l1,inf projection of Wg after every step leaves the channels that
 matter and the mask that the block's products skip the others by.
 """
@@ -35,22 +36,23 @@ class PrunedBlock:
     def cast(self):
         self.w = {k: v.to(torch.bfloat16) for k, v in self.master.items()}
 
-    def forward(self, x):
+    def forward(self, x, dropout=None):
         w = self.w
         _, z = mp.block_norm(x, w_pre=w["w_in"])
         h = mp.gated_ff(z, w["Wg"], w["Wu"], mask=self.mask)
-        b = h @ w["Wd"]
+        b = mp.linear(h, w["Wd"], dropout=dropout)
         r, y = mp.block_norm(x, b, w["w_post"], w["gate"], w["w_out"], scale=self.scale)
-        return y, (x, z, h, b, r)
+        return y, (x, z, h, b, r, dropout)
 
     def backward(self, dy, saved):
         """Gradients of the weights for the gradient dy of the result."""
         w = self.w
-        x, z, h, b, r = saved
+        x, z, h, b, r, dropout = saved
         _, db, dw_post, dgate, dw_out = mp.block_norm_backward(None, dy, r, b, w["w_post"], w["gate"], w["w_out"], scale=self.scale)
-        dz, dWg, dWu = mp.gated_ff_backward(db @ w["Wd"].t(), z, w["Wg"], w["Wu"], mask=self.mask)
+        dh, dWd, _ = mp.linear_backward(db, h, w["Wd"], dropout=dropout)
+        dz, dWg, dWu = mp.gated_ff_backward(dh, z, w["Wg"], w["Wu"], mask=self.mask)
         _, _, _, _, dw_in = mp.block_norm_backward(None, dz, x, w_pre=w["w_in"])
-        return {"Wg": dWg, "Wu": dWu, "Wd": h.t() @ db, "w_in": dw_in, "w_post": dw_post, "gate": dgate, "w_out": dw_out}
+        return {"Wg": dWg, "Wu": dWu, "Wd": dWd, "w_in": dw_in, "w_post": dw_post, "gate": dgate, "w_out": dw_out}
 
     def step(self, gradients, rate):
         for k, g in gradients.items():
@@ -75,8 +77,19 @@ class PrunedBlock:
         b = mp.w4_matvec(h, packed["Wd"])
         return mp.block_norm(x, b, w["w_post"], w["gate"], w["w_out"], scale=self.scale)[1]
 
+    def packed8(self):
+        return {k: mp.q8_pack(self.w[k], columns=True) for k in ("Wg", "Wu", "Wd")}
 
-def main(n=256, m=512, relevant=48, tokens=512, steps=60, rate=16.0, radius=0.03, seed=0):
+    def answer8(self, x, packed):
+        """The block on any number of tokens with tokens and weights in 8 bits."""
+        w = self.w
+        _, z = mp.block_norm8(x, w_pre=w["w_in"])
+        h = mp.q8_gated(z, packed["Wg"], packed["Wu"])
+        b = mp.q8_linear(mp.q8_pack(h), packed["Wd"])
+        return mp.block_norm(x, b, w["w_post"], w["gate"], w["w_out"], scale=self.scale)[1]
+
+
+def main(n=256, m=512, relevant=48, tokens=512, steps=60, rate=16.0, radius=0.03, seed=0, dropout=0.0):
     """Trains; returns what `python examples/pruned_block.py` prints."""
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
@@ -84,10 +97,10 @@ def main(n=256, m=512, relevant=48, tokens=512, steps=60, rate=16.0, radius=0.03
     block = PrunedBlock(n, m, gen)
     eta = radius * float(block.master["Wg"].abs().amax(0).sum())
     losses = []
-    for _ in range(steps):
+    for step in range(steps):
         x = torch.randn(tokens, n, generator=gen, device="cuda").to(torch.bfloat16)
         target, _ = teacher.forward(x)
-        y, saved = block.forward(x)
+        y, saved = block.forward(x, mp.Dropout(dropout, seed, step) if dropout else None)
         off = y.float() - target.float()
         losses.append(float((off * off).mean()))
         block.step(block.backward((2 * off / tokens).to(torch.bfloat16), saved), rate / n)
@@ -95,8 +108,11 @@ def main(n=256, m=512, relevant=48, tokens=512, steps=60, rate=16.0, radius=0.03
     packed = block.packed()
     x = torch.randn(1, n, generator=gen, device="cuda").to(torch.bfloat16)
     exact, short = block.forward(x)[0].float(), block.answer(x, packed).float()
+    few = torch.randn(40, n, generator=gen, device="cuda").to(torch.bfloat16)
+    all_of, eight = block.forward(few)[0].float(), block.answer8(few, block.packed8()).float()
     return {"first_loss": losses[0], "last_loss": losses[-1], "kept": int(block.mask.sum()), "channels": m,
-            "four_bit_error": float((short - exact).norm() / exact.norm())}
+            "four_bit_error": float((short - exact).norm() / exact.norm()),
+            "eight_bit_error": float((eight - all_of).norm() / all_of.norm())}
 
 
 if __name__ == "__main__":

@@ -577,7 +577,7 @@ int block_norm_backward(int storage, const mlproj_norm_block* block /* host */, 
 
 /* A matrix in 8 bits: rows of codes in e4m3 (sign, four exponent bits, three fraction bits, no infinities: at most 448),
  * each times the power of two 2^(byte - 127) of its group, 32 neighbouring entries of its row.  Rows are in whole blocks of 128
- * entries: past n, codes are zeros (their scales are any but 255).  This is what the matrix cores multiply; a weight matrix n x m that x is
+ * entries: past n, codes are zeros (NaN in a group that is NaN) and their scales any but 255.  This is what the matrix cores multiply; a weight matrix n x m that x is
  * multiplied by (x W) is held by its columns, as m rows of n.
  *   codes   row i at codes + i * ld bytes; 16-byte aligned, ld a multiple of 16 and at least n in whole blocks
  *   scales  row i at scales + i * lds bytes; 4-byte aligned, lds a multiple of 4 and at least a byte per group of those    */

@@ -968,7 +968,7 @@ class Q8:
 
 
 def _new_q8(like, rows, n, stream):
-    torch = _torch
+    torch = _import_torch()
     wide = (n + 127) // 128 * 128
     return Q8(n, _new_empty(like, (rows, wide), torch.float8_e4m3fn, stream), _new_empty(like, (rows, wide // 32), torch.float8_e8m0fnu, stream))
 

@@ -66,21 +66,26 @@ __global__ __launch_bounds__(LN_THREADS) void ln_slopes_kernel(LnSlopes a) {
     a.partial[blockIdx.y * a.m + c] = s;
   }
 }
-// The workgroups' sums: 32 columns x 8 runs of workgroups here.
+// The workgroups' sums: 32 columns x 8 runs of workgroups here; of more columns than a launch has threads for, the next ones a
+// grid further on.
+constexpr long long LN_MOST_COLUMN_GROUPS = 1 << 21;
 __global__ __launch_bounds__(256) void ln_columns_kernel(const float* partial, int groups, long long m, float* out) {
   __shared__ float part[8][32];
   const int cx = threadIdx.x & 31, gy = threadIdx.x >> 5;
-  const long long col = (long long)blockIdx.x * 32 + cx;
-  float s = 0.0f;
-  if (col < m)
+  for (long long first = (long long)blockIdx.x * 32; first < m; first += (long long)gridDim.x * 32) {
+    const long long col = first + cx;
+    float s = 0.0f;
+    if (col < m)
 #pragma unroll 8
-    for (int g = gy; g < groups; g += 8) s += partial[g * m + col];
-  part[gy][cx] = s;
-  __syncthreads();
-  if (gy == 0 && col < m) {
+      for (int g = gy; g < groups; g += 8) s += partial[g * m + col];
+    part[gy][cx] = s;
+    __syncthreads();
+    if (gy == 0 && col < m) {
 #pragma unroll
-    for (int i = 1; i < 8; i++) s += part[i][cx];
-    out[col] = s;
+      for (int i = 1; i < 8; i++) s += part[i][cx];
+      out[col] = s;
+    }
+    __syncthreads();
   }
 }
 // What an empty batch leaves.
@@ -290,7 +295,8 @@ int run_backward(int act, const mlproj_linear* b, const void* dY, long long lddy
     if (write) dZ = {ws + L.dZ, L.ldm, true};
     if (dbias) {
       mark(stream);
-      launch(ln_columns_kernel, dim3((unsigned)ff_cdiv(b->m, 32)), dim3(256), stream, a.partial, s.down, b->m, dbias);
+      const long long columns = ff_cdiv(b->m, 32);
+      launch(ln_columns_kernel, dim3((unsigned)(columns < LN_MOST_COLUMN_GROUPS ? columns : LN_MOST_COLUMN_GROUPS)), dim3(256), stream, a.partial, s.down, b->m, dbias);
     }
   }
   const LnOperands o = ln_operands<T>(b, L, ws, dW != nullptr, dX != nullptr, stream);

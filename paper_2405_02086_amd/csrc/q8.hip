@@ -83,10 +83,21 @@ Q8Plan q8_plan(long long M, long long N, long long blocks, bool dual, bool exact
   }
   return best;
 }
-size_t q8_workspace(long long M, long long N, long long n, bool dual) {
+// Workgroups (along x) of a product's launch.
+long long q8_groups(int kind, long long M, long long N, bool dual, int splits) {
+  const int half = dual ? 2 : 1;
+  switch (kind) {
+    case 0: return ff_cdiv(M, 256) * ff_cdiv(N, 256 / half) * splits;
+    case 1: return ff_cdiv(M, 128) * ff_cdiv(N, 128 / half) * splits;
+    case 3: return ff_cdiv(N, Q8F_COLS);
+    default: return ff_cdiv(M, 64) * ff_cdiv(N, 128 / half) * splits;
+  }
+}
+size_t q8_workspace(long long M, long long N, long long n, bool dual, bool* fits) {
   size_t most = 0;
   for (bool exact : {false, true}) {
     const Q8Plan plan = q8_plan(M, N, q8_wide(n) / Q8_BLOCK, dual, exact);
+    if (q8_groups(plan.kind, M, N, dual, plan.splits) > FF_MOST_THREADS / 512) *fits = false;
     const size_t bytes = plan.splits > 1 ? (size_t)plan.splits * (dual ? 2 : 1) * M * (ff_cdiv(N, 4) * 4) * 4 : 0;
     most = bytes > most ? bytes : most;
   }
@@ -97,17 +108,16 @@ size_t q8_workspace(long long M, long long N, long long n, bool dual) {
 template <typename T, bool DUAL, int EPI>
 void q8_tiles(const Q8Product& q, int kind, hipStream_t stream) {
   constexpr bool EXACT = sizeof(T) == 4;
-  constexpr int HALF = DUAL ? 2 : 1;
   mark(stream);
-  const long long M = q.p.M, N = q.p.N, splits = q.p.splits;
+  const dim3 grid((unsigned)q8_groups(kind, q.p.M, q.p.N, DUAL, q.p.splits));
   if constexpr (!EXACT) {
     if (kind == 0) {
-      launch(q8_tile_kernel<T, DUAL, EPI, 256, 256, 2, 4, EXACT>, dim3((unsigned)(ff_cdiv(M, 256) * ff_cdiv(N, 256 / HALF) * splits)), dim3(512), stream, q);
+      launch(q8_tile_kernel<T, DUAL, EPI, 256, 256, 2, 4, EXACT>, grid, dim3(512), stream, q);
       return;
     }
   }
-  if (kind == 1) launch(q8_tile_kernel<T, DUAL, EPI, 128, 128, 2, 2, EXACT>, dim3((unsigned)(ff_cdiv(M, 128) * ff_cdiv(N, 128 / HALF) * splits)), dim3(256), stream, q);
-  else launch(q8_tile_kernel<T, DUAL, EPI, 64, 128, 2, 2, EXACT>, dim3((unsigned)(ff_cdiv(M, 64) * ff_cdiv(N, 128 / HALF) * splits)), dim3(256), stream, q);
+  if (kind == 1) launch(q8_tile_kernel<T, DUAL, EPI, 128, 128, 2, 2, EXACT>, grid, dim3(256), stream, q);
+  else launch(q8_tile_kernel<T, DUAL, EPI, 64, 128, 2, 2, EXACT>, grid, dim3(256), stream, q);
 }
 template <typename T, bool DUAL, int EPI>
 int q8_product(Q8Product q, void* workspace, hipStream_t stream) {
@@ -118,7 +128,7 @@ int q8_product(Q8Product q, void* workspace, hipStream_t stream) {
   p.partial = static_cast<float*>(workspace);
   if (plan.kind == 3) {
     mark(stream);
-    launch(q8_few_kernel<T, DUAL, EPI, 1, 2, 8, EXACT>, dim3((unsigned)ff_cdiv(p.N, Q8F_COLS), (unsigned)ff_cdiv(p.M, 16)), dim3(512), stream, q);
+    launch(q8_few_kernel<T, DUAL, EPI, 1, 2, 8, EXACT>, dim3((unsigned)q8_groups(3, p.M, p.N, DUAL, 1)), dim3(512), stream, q);
   } else if (p.splits == 1) {
     q8_tiles<T, DUAL, EPI>(q, plan.kind, stream);
   } else {
@@ -151,10 +161,12 @@ Q8Product q8_start(const mlproj_q8* x, const mlproj_q8* w0, const mlproj_q8* w1)
   p.M = x->rows; p.N = w0->rows; p.K = q8_wide(x->n);
   return q;
 }
-int q8_sizes(long long tokens, long long n, long long m) {
+int q8_sizes(long long tokens, long long n, long long m, bool dual, size_t* workspace) {
   if (tokens < 0 || n <= 0 || m <= 0) return MLPROJ_ERR_BAD_DIMENSION;
   if (tokens > Q8_MAX_DIM || n > Q8_MAX_DIM || m > Q8_MAX_DIM || tokens * m > (1LL << 38) || tokens * n > (1LL << 38) || n * m > (1LL << 38)) return MLPROJ_ERR_TOO_LARGE;
-  return MLPROJ_OK;
+  bool fits = true;
+  *workspace = q8_workspace(tokens, m, n, dual, &fits);
+  return fits || tokens == 0 ? MLPROJ_OK : MLPROJ_ERR_TOO_LARGE;
 }
 
 }  // namespace
@@ -190,10 +202,8 @@ int q8_pack(int storage, int by_columns, const void* A, long long lda, const mlp
 
 int mlproj_q8_workspace_bytes(long long tokens, long long n, long long m, int gated, size_t* bytes_out) {
   if (!bytes_out) return MLPROJ_ERR_NULL_POINTER;
-  FF_TRY(q8_sizes(tokens, n, m));
   if ((gated | 1) != 1) return MLPROJ_ERR_BAD_DIMENSION;
-  *bytes_out = q8_workspace(tokens, m, n, gated != 0);
-  return MLPROJ_OK;
+  return q8_sizes(tokens, n, m, gated != 0, bytes_out);
 }
 
 int q8_linear(int storage, int activation, const mlproj_q8* x, const mlproj_q8* W, const void* bias, const void* residual, long long ldr,
@@ -202,13 +212,14 @@ int q8_linear(int storage, int activation, const mlproj_q8* x, const mlproj_q8* 
   if (storage < MLPROJ_STORE_F32 || storage > MLPROJ_STORE_F16 || activation < MLPROJ_ACT_SILU || activation > MLPROJ_ACT_NONE) return MLPROJ_ERR_BAD_VARIANT;
   const int es = storage == MLPROJ_STORE_F32 ? 4 : 2;
   const bool some = x->rows > 0;
-  FF_TRY(q8_sizes(x->rows, x->n, W->rows));
+  size_t need;
+  FF_TRY(q8_sizes(x->rows, x->n, W->rows, false, &need));
   FF_TRY(q8_operand(x, x->n, some));
   FF_TRY(q8_operand(W, x->n, some));
   FF_TRY(ff_check_array(bias, false, W->rows, W->rows, es));
   FF_TRY(ff_check_array(residual, false, W->rows, ldr, es));
   FF_TRY(ff_check_array(y, some, W->rows, ldy, es));
-  FF_TRY(ff_check_workspace(workspace, workspace_bytes, q8_workspace(x->rows, W->rows, x->n, false)));
+  FF_TRY(ff_check_workspace(workspace, workspace_bytes, need));
   if (!some) return MLPROJ_OK;
   Q8Product q = q8_start(x, W, nullptr);
   q.p.act = activation;
@@ -226,13 +237,14 @@ int q8_gated(int storage, int activation, const mlproj_q8* x, const mlproj_q8* W
   if (!x || !Wg || !Wu) return MLPROJ_ERR_NULL_POINTER;
   if (storage < MLPROJ_STORE_F32 || storage > MLPROJ_STORE_F16 || activation < MLPROJ_ACT_SILU || activation > MLPROJ_ACT_RELU) return MLPROJ_ERR_BAD_VARIANT;
   const bool some = x->rows > 0;
-  FF_TRY(q8_sizes(x->rows, x->n, Wg->rows));
+  size_t need;
+  FF_TRY(q8_sizes(x->rows, x->n, Wg->rows, true, &need));
   FF_TRY(q8_operand(x, x->n, some));
   FF_TRY(q8_operand(Wg, x->n, some));
   FF_TRY(q8_operand(Wu, x->n, some));
   if (Wu->rows != Wg->rows || Wu->ld != Wg->ld || Wu->lds != Wg->lds) return MLPROJ_ERR_BAD_DIMENSION;
   FF_TRY(ff_check_array(h, some, Wg->rows, ldh, storage == MLPROJ_STORE_F32 ? 4 : 2));
-  FF_TRY(ff_check_workspace(workspace, workspace_bytes, q8_workspace(x->rows, Wg->rows, x->n, true)));
+  FF_TRY(ff_check_workspace(workspace, workspace_bytes, need));
   if (!some) return MLPROJ_OK;
   Q8Product q = q8_start(x, Wg, Wu);
   q.p.act = activation;

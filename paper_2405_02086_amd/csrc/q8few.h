@@ -20,7 +20,7 @@ __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
   __shared__ f32x4 sums[WAVES][VALUES][64];
   FfProduct& p = q.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const long long col0 = (long long)blockIdx.x * Q8F_COLS, row0 = (long long)blockIdx.y * 16 * MT;
+  const long long col0 = (long long)blockIdx.x * Q8F_COLS;
   const int blocks = (int)(p.K / Q8_BLOCK);
   const long long col = col0 + r < p.N ? col0 + r : p.N - 1;
   const unsigned char *w[MATS], *sw[MATS], *x[MT], *sx[MT];
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
   }
 #pragma unroll
   for (int t = 0; t < MT; t++) {
-    const long long row = row0 + t * 16 + r < p.M ? row0 + t * 16 + r : p.M - 1;
+    const long long row = t * 16 + r < p.M ? t * 16 + r : p.M - 1;
     x[t] = static_cast<const unsigned char*>(p.A0) + row * p.lda + 16 * g;
     sx[t] = q.sA + row * q.ldsa;
   }
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
   dropout_at_step(p.drop);
   for (int at = threadIdx.x; at < MT * 64; at += WAVES * 64) {
     const int t = at >> 6, l = at & 63;
-    const long long row = row0 + t * 16 + (l & 15), c = col0 + (l >> 4) * 4;
+    const long long row = t * 16 + (l & 15), c = col0 + (l >> 4) * 4;
     if (row >= p.M || c >= p.N) continue;
     f32x4 v[2] = {};
 #pragma unroll

@@ -53,17 +53,20 @@ struct Q8Part {
   static constexpr int ROWS = THREADS / 8, LOADS = W / ROWS;
   static_assert(ROWS % 8 == 0 && LOADS * ROWS == W, "whole turns of the permutation");
   long long ld;
-  int there;
+  unsigned bytes[LOADS];       // of the rows that are there, from a load's first one
   __device__ __forceinline__ void plan(long long stride, long long rows) {
     ld = stride;
-    there = rows < 0 ? 0 : rows < W ? (int)rows : W;
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      const long long left = rows - i * ROWS;
+      bytes[i] = (unsigned)((left < 0 ? 0 : left < ROWS ? left : ROWS) * stride);
+    }
   }
   __device__ __forceinline__ void load(const unsigned char* base, bool some, unsigned offset, unsigned char* lds, int wave) const {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
-      const int rows = some ? there - i * ROWS : 0;
-      const unsigned bytes = rows <= 0 ? 0u : (unsigned)((rows < ROWS ? rows : ROWS) * (int)ld);
-      __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base + i * ROWS * ld), 0, bytes, 0x00020000);
+      const unsigned size = some ? bytes[i] : 0u;
+      __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base + i * ROWS * ld), 0, size, 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(lds + (wave * 64 + i * THREADS) * 16), 16, offset, 0, 0, 0);
     }
   }
@@ -131,27 +134,29 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
 #pragma unroll
     for (int i = 0; i < 2; i++) pb[i].load(B[i] + k0, there, offset_b, lds + (BM + i * BW) * Q8_BLOCK, wave);
   };
-  // (both products' scales from one pointer: two that a lambda chooses from would be kept in scratch memory, with all arguments)
-  const unsigned char *const sA = q.sA, *const sB = q.sB0;
-  const long long to_second = DUAL ? q.sB1 - q.sB0 : 0;
-  const long long ldsa = q.ldsa, ldsb = q.ldsb;
-  // 64 rows' scales per wavefront and load: A's, then those of both halves of B
-  auto load_scales = [&](int block, unsigned char* to, bool some) {
+  // 64 rows' scales per wavefront and load: A's, then those of both halves of B.  (Where they come from is found here: choosing
+  // between pointers in the loop would be branches, or all arguments in scratch memory.)
+  unsigned long long scale_rows[SLOADS];
+  unsigned scale_offset[SLOADS];
 #pragma unroll
-    for (int i = 0; i < SLOADS; i++) {
-      const int chunk = wave + i * WAVES, of_b = chunk - BM / 64, half = of_b >= BW / 64;
-      const long long at = of_b < 0 ? row0 + chunk * 64 : col0 + (DUAL || !half ? 0 : BW) + (of_b - half * (BW / 64)) * 64;
-      const long long there = chunk >= CHUNKS ? 0 : (of_b < 0 ? p.M : N) - at, ld = of_b < 0 ? +ldsa : +ldsb;
-      const unsigned char* base = sA;
-      if (of_b >= 0) base = sB + (DUAL && half ? to_second : 0);
-      base += at * ld;
-      const unsigned from = lane < there ? (unsigned)(lane * ld) : FD_OUT;
+  for (int i = 0; i < SLOADS; i++) {
+    const int chunk = wave + i * WAVES, of_b = chunk - BM / 64, half = of_b >= BW / 64;
+    const long long at = of_b < 0 ? row0 + chunk * 64 : col0 + (DUAL || !half ? 0 : BW) + (of_b - half * (BW / 64)) * 64;
+    const long long there = chunk >= CHUNKS ? 0 : (of_b < 0 ? p.M : N) - at, ld = of_b < 0 ? q.ldsa : q.ldsb;
+    const unsigned long long from = of_b < 0 ? (unsigned long long)q.sA : (unsigned long long)q.sB0 + (DUAL && half ? (unsigned long long)q.sB1 - (unsigned long long)q.sB0 : 0);
+    scale_rows[i] = from + at * ld;
+    scale_offset[i] = lane < there ? (unsigned)(lane * ld) : FD_OUT;
+  }
+  // four blocks' at a time
+  auto load_scales = [&](int block, unsigned char* to) {
+#pragma unroll
+    for (int i = 0; i < SLOADS; i++)
 #pragma unroll
       for (int k = 0; k < 4; k++) {
-        __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base + (long long)(block + k) * 4), 0, some && block + k < last ? 0x7ffffff0u : 0u, 0x00020000);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(to + (k * SROWS + chunk * 64) * 4), 4, from, 0, 0, 0);
+        __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(scale_rows[i] + (long long)(block + k) * 4), 0, block + k < last ? 0x7ffffff0u : 0u, 0x00020000);
+        const unsigned offset = scale_offset[i];
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (fd_lds_t*)(to + (k * SROWS + (wave + i * WAVES) * 64) * 4), 4, offset, 0, 0, 0);
       }
-    }
   };
 
   f32x16 acc[RT][2 * CJ] = {};
@@ -193,12 +198,11 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   constexpr int MFMAS = RT * 2 * CJ, READS = (RT + 2 * CJ) * 2, LOADS = (BM + BN) * Q8_BLOCK / 16 / THREADS;
   Operands even, odd;
   Scales here, next;
-  // A block's scales are in place (number / 4) % 2, four blocks' together, [number % 4][row]; number: of the workgroup's blocks.
-  // (They are read before any load goes out: the compiler waits for loads into the array that it reads, whichever part it is.  Three
-  // times of four their loads ask for nothing: a branch round them would cut the block's instructions into parts that are ordered
-  // each for itself.)
+  // Scales are in two places, four blocks' together, [block][row].  (They are read before any load goes out: the compiler waits for
+  // loads into the array that it reads, whichever part it is.)
   auto scales_of = [&](int number) { return scales + (number & 7) * SROWS * 4; };
-  auto block_of = [&](int block, unsigned char* mine, unsigned char* other) {
+  // K: the block's number within its four, `group` the first one's among the workgroup's
+  auto block_of = [&](int k, int group, unsigned char* mine, unsigned char* other) {
     odd = read(mine, 1);
     q8_multiply<EXACT, 0>(even, here, acc);
     if constexpr (!EXACT) fd_schedule<0, MFMAS, READS>();
@@ -206,19 +210,18 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
     __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0) lgkmcnt(0): the next block is there, and what was read of this one
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const int number = block - first;
-    next = read_scales(scales_of(number + 1));
-    load_scales(block + 5, scales_of(number + 5), (number & 3) == 3);
-    load(block + 2, mine);
+    next = read_scales(scales_of(group + k + 1));
+    if (k == 3) load_scales(first + group + 8, scales_of(group + 8));
+    load(first + group + k + 2, mine);
     even = read(other, 0);
     q8_multiply<EXACT, 1>(odd, here, acc);
     if constexpr (!EXACT) fd_schedule<0, MFMAS, READS>();
     here = next;
   };
-  load_scales(first, scales_of(0), true);
+  load_scales(first, scales_of(0));
   load(first, lds0);
   load(first + 1, lds1);
-  load_scales(first + 4, scales_of(4), true);
+  load_scales(first + 4, scales_of(4));
   {
     // all but the last two are there
     asm volatile("" ::: "memory");
@@ -229,12 +232,16 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   }
   here = read_scales(scales_of(0));
   even = read(lds0, 0);
-  int block = first;
-  for (; block + 1 < last; block += 2) {
-    block_of(block, lds0, lds1);
-    block_of(block + 1, lds1, lds0);
+  int group = 0;
+  for (; group + 3 < last - first; group += 4) {
+    block_of(0, group, lds0, lds1);
+    block_of(1, group, lds1, lds0);
+    block_of(2, group, lds0, lds1);
+    block_of(3, group, lds1, lds0);
   }
-  if (block < last) block_of(block, lds0, lds1);
+  if (group < last - first) block_of(0, group, lds0, lds1);
+  if (group + 1 < last - first) block_of(1, group, lds1, lds0);
+  if (group + 2 < last - first) block_of(2, group, lds0, lds1);
   // no load may be under way where results go, or when the workgroup's LDS is given to another
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0)
