@@ -968,9 +968,16 @@ class Q8:
 
 
 def _new_q8(like, rows, n, stream):
+    """A Q8 on memory of its own, without the checks of one that is given."""
     torch = _import_torch()
     wide = (n + 127) // 128 * 128
-    return Q8(n, _new_empty(like, (rows, wide), torch.float8_e4m3fn, stream), _new_empty(like, (rows, wide // 32), torch.float8_e8m0fnu, stream))
+    q = Q8.__new__(Q8)
+    q.rows, q.n = rows, n
+    q.codes = codes = _new_empty(like, (rows, wide), torch.float8_e4m3fn, stream)
+    q.scales = scales = _new_empty(like, (rows, wide // 32), torch.float8_e8m0fnu, stream)
+    q._struct = PackedQ8(rows, n, codes.data_ptr(), wide, scales.data_ptr(), wide // 32)
+    q._ref = ctypes.byref(q._struct)
+    return q
 
 
 def _result_q8(q, rows, n, like, what, stream):

@@ -54,31 +54,38 @@ __global__ __launch_bounds__(256) void q8_pack_columns_kernel(Q8Pack a) {
 }
 
 // ------------------------------------------------------------------ plan
-// The cheapest tiles and number of shares of the sum by what was measured, as ff_plan.
+// The cheapest tiles and number of shares of the sum by what was measured: a block of 128 of a tile by how many workgroups the
+// compute unit holds, a tile beside its blocks (more where others on the unit want the same), and joining shares.  Fitted to
+// both products of 40 shapes with 16-bit results and 18 with fp32 ones, 17 x 92 -> 593 to 4096 x 16384 -> 4096, each in every tile
+// and with every number of shares: the plan's choice takes 1.2 % more than the best one on average, 14 % at most.  256 x 256 tiles
+// (one workgroup per compute unit) have the fastest blocks, 64 x 128 (two) fill the chip where there are few: 4096 x 4096 -> 4096 takes
+// 70 us in them, in 128 x 128 (two) 86, in 64 x 128 126; 300 x 300 -> 5000 18, 11 and 8.  (256 x 256 with fp32 results would need
+// more registers than there are.)
 constexpr long long Q8_FEW = 16;       // most tokens that go without tiles
 struct Q8Kind {
-  int rows, cols, places;
-  double step[2], tile, each;          // us: a step of 64 with one workgroup on the unit and more for each further one; a tile beside its steps
+  int name, rows, cols, places;
+  double block[2], tile, crowd;        // us; one workgroup on the unit, two
 };
 struct Q8Plan { int kind, splits; double us; };
 Q8Plan q8_plan(long long M, long long N, long long blocks, bool dual, bool exact) {
   if (M <= Q8_FEW) return {3, 1, 0.0};
-  static const Q8Kind kinds[3] = {{256, 256, 1, {0.60, 0.0}, 9.0, 0.0}, {128, 128, 2, {0.26, 0.20}, 3.0, 0.0}, {64, 128, 3, {0.18, 0.14}, 1.5, 0.0}};
-  static const int names[3] = {0, 1, 4};
-  constexpr double LAUNCH = 3.6;
+  static const Q8Kind kinds[2][3] = {
+      {{0, 256, 256, 1, {1.46, 0.0}, 5.0, 0.0}, {1, 128, 128, 2, {0.60, 1.01}, 2.4, 0.87}, {4, 64, 128, 2, {0.50, 0.74}, 1.1, 1.5}},
+      {{1, 128, 128, 2, {0.94, 1.51}, 2.2, 0.80}, {4, 64, 128, 2, {0.67, 0.97}, 0.55, 4.2}, {}}};
+  constexpr double LAUNCH = 4.0, JOIN = 2.5;
   Q8Plan best{1, 1, 1e30};
   const double planes = 4.0 * M * N * (dual ? 2 : 1);
-  for (int i = exact ? 1 : 0; i < 3; i++) {
-    const Q8Kind& k = kinds[i];
+  for (const Q8Kind& k : kinds[exact]) {
+    if (k.rows == 0) continue;
     const long long tiles = ff_cdiv(M, k.rows) * ff_cdiv(N, dual ? k.cols / 2 : k.cols);
     for (int splits = 1; splits <= 64; splits *= 2) {
-      if (splits > 1 && (blocks / splits < 2 || planes * splits > 512e6)) break;
-      const long long groups = tiles * splits, units = 256LL * k.places, rest = groups % units, steps = 2 * ff_cdiv(blocks, splits);
-      auto turn = [&](long long on) { return steps * (k.step[0] + k.step[1] * (on - 1)) * (exact ? 3.0 : 1.0) + k.tile; };
+      if (splits > 1 && (blocks < splits || planes * splits > 512e6)) break;
+      const long long groups = tiles * splits, units = 256LL * k.places, rest = groups % units, each = ff_cdiv(blocks, splits);
+      auto turn = [&](long long on) { return each * k.block[on - 1] + k.tile * (1.0 + k.crowd * (on - 1)); };
       double us = LAUNCH + (double)(groups / units) * turn(k.places);
       if (rest) us += turn(ff_cdiv(rest, 256));
-      if (splits > 1) us += 3.0 + planes * 2 * splits / 5.7e6;
-      if (us < best.us) best = {names[i], splits, us};
+      if (splits > 1) us += JOIN + planes * 2 * splits / 5.0e6;
+      if (us < best.us) best = {k.name, splits, us};
     }
   }
   return best;
@@ -128,7 +135,14 @@ int q8_product(Q8Product q, void* workspace, hipStream_t stream) {
   p.partial = static_cast<float*>(workspace);
   if (plan.kind == 3) {
     mark(stream);
-    launch(q8_few_kernel<T, DUAL, EPI, 1, 2, 8, EXACT>, dim3((unsigned)q8_groups(3, p.M, p.N, DUAL, 1)), dim3(512), stream, q);
+    auto go = [&](auto* kernel, int columns) { launch(kernel, dim3((unsigned)ff_cdiv(p.N, columns)), dim3(512), stream, q); };
+    if constexpr (DUAL) {
+      if (p.M > 4 && p.N >= 4096) go(q8_few_kernel<T, true, EPI, 2, 4, 8, EXACT>, 32);
+      else go(q8_few_kernel<T, true, EPI, 1, 4, 8, EXACT>, 16);
+    } else {
+      if (p.K >= 64 * Q8_BLOCK) go(q8_few_kernel<T, false, EPI, 1, 8, 8, EXACT>, 16);
+      else go(q8_few_kernel<T, false, EPI, 1, 4, 8, EXACT>, 16);
+    }
   } else if (p.splits == 1) {
     q8_tiles<T, DUAL, EPI>(q, plan.kind, stream);
   } else {

@@ -8,33 +8,34 @@ namespace mlproj {
 namespace {
 
 // ------------------------------------------------------------------ few tokens
-// A workgroup has 16 columns (DUAL: of both products) and up to 16 MT tokens; its wavefronts share out K, U blocks of 128 at a
+// A workgroup has 16 CB columns (DUAL: of both products) and up to 16 tokens; its wavefronts share out K, U blocks of 128 at a
 // time, and add their sums in LDS in their order.  Loads bring operands as the matrix cores take them: a lane 16 codes of
 // each of two groups and the scale of one, so that four neighbouring lanes read 64 neighbouring bytes of a row.  Rows past
-// the end are the last one again, and not stored.  Bound by HBM: every weight is read once.
+// the end are the last one again, and not stored.  Bound by HBM and by how many loads are under way: every weight is read once, and a
+// wavefront waits once a round.  us, U = 2 / 4 / 8 with eight wavefronts, weights that were not read just before: one token 4096 -> 2 x
+// 16384 31 / 26 / 40 (32 blocks of 128 are half a round), 16384 -> 4096 17 / 19 / 14, 8 tokens 8192 -> 8192 17 / 16 / 16, one token 4096
+// -> 4096 6.2 / 5.6 / 5.4; four or sixteen wavefronts are no faster.  Sixteen tokens through both products of a pair: 32 columns
+// halve what is read of the tokens (4096 -> 2 x 16384 31.9 -> 30.1, 2048 -> 2 x 8192 8.5 -> 7.7); one product loses (16384 -> 4096
+// 19 -> 26).
 constexpr int Q8F_COLS = 16;
 
-template <typename T, bool DUAL, int EPI, int MT, int U, int WAVES, bool EXACT>
+template <typename T, bool DUAL, int EPI, int CB, int U, int WAVES, bool EXACT>
 __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
-  constexpr int MATS = DUAL ? 2 : 1, VALUES = MATS * MT;
+  constexpr int MATS = DUAL ? 2 : 1, VALUES = MATS * CB;
   __shared__ f32x4 sums[WAVES][VALUES][64];
   FfProduct& p = q.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const long long col0 = (long long)blockIdx.x * Q8F_COLS;
+  const long long col0 = (long long)blockIdx.x * (Q8F_COLS * CB);
   const int blocks = (int)(p.K / Q8_BLOCK);
-  const long long col = col0 + r < p.N ? col0 + r : p.N - 1;
-  const unsigned char *w[MATS], *sw[MATS], *x[MT], *sx[MT];
+  const unsigned char *w[VALUES], *sw[VALUES];
 #pragma unroll
-  for (int i = 0; i < MATS; i++) {
-    w[i] = static_cast<const unsigned char*>(i ? p.B1 : p.B0) + col * p.ldb + 16 * g;
-    sw[i] = (i ? q.sB1 : q.sB0) + col * q.ldsb;
+  for (int i = 0; i < VALUES; i++) {
+    const long long at = col0 + i % CB * 16 + r, col = at < p.N ? at : p.N - 1;
+    w[i] = static_cast<const unsigned char*>(i >= CB ? p.B1 : p.B0) + col * p.ldb + 16 * g;
+    sw[i] = (i >= CB ? q.sB1 : q.sB0) + col * q.ldsb;
   }
-#pragma unroll
-  for (int t = 0; t < MT; t++) {
-    const long long row = t * 16 + r < p.M ? t * 16 + r : p.M - 1;
-    x[t] = static_cast<const unsigned char*>(p.A0) + row * p.lda + 16 * g;
-    sx[t] = q.sA + row * q.ldsa;
-  }
+  const long long row = r < p.M ? r : p.M - 1;
+  const unsigned char *x = static_cast<const unsigned char*>(p.A0) + row * p.lda + 16 * g, *sx = q.sA + row * q.ldsa;
   struct Operand { i32x8 codes; unsigned scale; };
   auto fetch = [&](const unsigned char* codes, const unsigned char* scales, int block) {
     Operand o;
@@ -59,52 +60,56 @@ __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
       return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.codes, b.codes, c, 0, 0, 0, (int)(a.scale >> (8 * g)), 0, (int)(b.scale >> (8 * g)));
     }
   };
-  // whole rounds of U blocks, the next round's weights on their way while the present one's are multiplied; then what is left
   int block = wave * U;
   for (; block + U <= blocks; block += WAVES * U) {
-    Operand ow[U][MATS], ox[U][MT];
+    Operand ow[U][VALUES], ox[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
 #pragma unroll
-      for (int i = 0; i < MATS; i++) ow[u][i] = fetch(w[i], sw[i], block + u);
-#pragma unroll
-      for (int t = 0; t < MT; t++) ox[u][t] = fetch(x[t], sx[t], block + u);
+      for (int i = 0; i < VALUES; i++) ow[u][i] = fetch(w[i], sw[i], block + u);
+      ox[u] = fetch(x, sx, block + u);
     }
 #pragma unroll
     for (int u = 0; u < U; u++)
 #pragma unroll
-      for (int i = 0; i < MATS; i++)
-#pragma unroll
-        for (int t = 0; t < MT; t++) acc[i * MT + t] = multiply(ow[u][i], ox[u][t], acc[i * MT + t]);
+      for (int i = 0; i < VALUES; i++) acc[i] = multiply(ow[u][i], ox[u], acc[i]);
   }
-  for (; block < blocks; block++) {
+  if (block < blocks) {
+    // a round that is not whole: its last block again in the place of those that are not there, and not multiplied
+    Operand ow[U][VALUES], ox[U];
 #pragma unroll
-    for (int i = 0; i < MATS; i++) {
-      const Operand ow = fetch(w[i], sw[i], block);
+    for (int u = 0; u < U - 1; u++) {
+      const int at = block + u < blocks ? block + u : blocks - 1;
 #pragma unroll
-      for (int t = 0; t < MT; t++) acc[i * MT + t] = multiply(ow, fetch(x[t], sx[t], block), acc[i * MT + t]);
+      for (int i = 0; i < VALUES; i++) ow[u][i] = fetch(w[i], sw[i], at);
+      ox[u] = fetch(x, sx, at);
     }
+#pragma unroll
+    for (int u = 0; u < U - 1; u++)
+      if (block + u < blocks)
+#pragma unroll
+        for (int i = 0; i < VALUES; i++) acc[i] = multiply(ow[u][i], ox[u], acc[i]);
   }
 #pragma unroll
   for (int v = 0; v < VALUES; v++) sums[wave][v][lane] = acc[v];
   __syncthreads();
   // a lane's four sums are neighbouring columns of one token
   dropout_at_step(p.drop);
-  for (int at = threadIdx.x; at < MT * 64; at += WAVES * 64) {
-    const int t = at >> 6, l = at & 63;
-    const long long row = t * 16 + (l & 15), c = col0 + (l >> 4) * 4;
-    if (row >= p.M || c >= p.N) continue;
+  for (int at = threadIdx.x; at < CB * 64; at += WAVES * 64) {
+    const int b = at >> 6, l = at & 63;
+    const long long t = l & 15, c = col0 + b * 16 + (l >> 4) * 4;
+    if (t >= p.M || c >= p.N) continue;
     f32x4 v[2] = {};
 #pragma unroll
     for (int i = 0; i < MATS; i++)
-      for (int s = 0; s < WAVES; s++) v[i] += sums[s][i * MT + t][l];
+      for (int s = 0; s < WAVES; s++) v[i] += sums[s][i * CB + b][l];
     FfVec4<T> d = {};
     f32x4 bias = {};
     if constexpr (EPI == FF_LINEAR) {
-      d = ff_upstream<T>(p, row, c, p.N);
+      d = ff_upstream<T>(p, t, c, p.N);
       bias = ff_bias<T>(p, c, p.N);
     }
-    ff_finish<EPI, DUAL, T>(p, row, c, p.N, v[0], v[1], d, bias);
+    ff_finish<EPI, DUAL, T>(p, t, c, p.N, v[0], v[1], d, bias);
   }
 }
 
