@@ -728,3 +728,33 @@ def test_the_example_trains_with_dropout_and_answers_in_eight_bits(mp):  # noqa:
     close(dWd, want[1], np.abs(values(h)).T @ e + sum_bound(40, "bf16") * (np.abs(values(h)).T @ (np.abs(want[3]) + e)) + stored(want[1], "bf16"), "dWd")
     B = lo.linear(values(h), values(block.w["Wd"]), drop=(0.25, 17, 4))[0]
     close(b, B, sum_bound(96, "bf16") * (np.abs(values(h)) @ np.abs(values(block.w["Wd"]))) / 0.75 + 4 * U32 * np.abs(B) + stored(B, "bf16"), "b")
+
+
+def test_linear_whole_turns_of_large_tiles_and_the_rest(mp):  # noqa: F811
+    """306 tiles of 256 x 256: one turn of the compute units, and 50 that go out in smaller ones; against fp64 on the device."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    tokens, n, m = 4400, 1024, 4160
+    X, W = (torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16) for s in ((tokens, n), (n, m)))
+    W = (W.float() * n ** -0.5).to(torch.bfloat16)
+    R, b = (torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16) for s in ((tokens, m), (m,)))
+    drop = mp.Dropout(0.2, 77, 3)
+    x, w, r = X.double(), W.double(), R.double()
+    z = x @ w + b.double()
+    v = z * torch.sigmoid(z)
+    eZ = (2 * n + 66) * U32 * (x.abs() @ w.abs() + b.double().abs())
+    keep = mp.dropout(torch.ones(tokens, m, device="cuda"), drop) != 0      # (itself against the oracle elsewhere)
+    v, e = torch.where(keep, v / 0.8, 0.0), torch.where(keep, (SLOPE * eZ + 16 * U32 * (v.abs() + z.abs())) / 0.8, 0.0)
+    want = r + v
+    for out in (None, R.clone()):
+        Z = torch.empty_like(R)
+        y = mp.linear(X, W, bias=b, residual=R if out is None else out, act="silu", dropout=drop, Y=out, z_out=Z)
+        assert ((y.double() - want).abs() <= e + 4 * U32 * (v.abs() + r.abs()) + 2.0 ** -8 * 1.001 * want.abs()).all()
+        assert ((Z.double() - z).abs() <= eZ + 2.0 ** -8 * 1.001 * z.abs()).all()
+    dY = torch.randn(tokens, m, generator=gen, device="cuda").to(torch.bfloat16)
+    dX, dW, dbias = mp.linear_backward(dY, X, W, need_dbias=True)
+    d = dY.double()
+    for got, a, c in ((dX, d, w.t()), (dW, x.t(), d)):
+        exact, size = a @ c, a.abs() @ c.abs()
+        assert ((got.double() - exact).abs() <= (2 * a.shape[1] + 64) * U32 * size + 2.0 ** -8 * 1.001 * exact.abs()).all()
+    assert ((dbias.double() - d.sum(0)).abs() <= (2 * tokens + 64) * U32 * d.abs().sum(0)).all()
