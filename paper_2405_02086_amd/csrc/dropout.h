@@ -45,13 +45,15 @@ __device__ __forceinline__ void dropout_at_step(Dropout& d) {
 }
 
 typedef unsigned philox_t __attribute__((ext_vector_type(4)));
+// a ^ b ^ c in one instruction (0x96 is the truth table)
+__device__ __forceinline__ unsigned philox_xor(unsigned a, unsigned b, unsigned c) { return (unsigned)__builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 __device__ __forceinline__ philox_t dropout_words(const Dropout& d, unsigned row, unsigned quad) {
   philox_t c = {quad, row, (unsigned)d.offset, (unsigned)(d.offset >> 32)};
   unsigned k0 = (unsigned)d.seed, k1 = (unsigned)(d.seed >> 32);
 #pragma unroll
   for (int i = 0; i < 10; i++) {
     const unsigned long long a = (unsigned long long)c[0] * 0xD2511F53u, b = (unsigned long long)c[2] * 0xCD9E8D57u;
-    c = philox_t{(unsigned)(b >> 32) ^ c[1] ^ k0, (unsigned)b, (unsigned)(a >> 32) ^ c[3] ^ k1, (unsigned)a};
+    c = philox_t{philox_xor((unsigned)(b >> 32), c[1], k0), (unsigned)b, philox_xor((unsigned)(a >> 32), c[3], k1), (unsigned)a};
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }

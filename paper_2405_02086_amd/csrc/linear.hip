@@ -122,10 +122,20 @@ __global__ __launch_bounds__(256) void ln_dropout_kernel(LnDrop a) {
   constexpr int VEC = 16 / sizeof(T);
   struct alignas(sizeof(T)) Piece { T v[VEC]; };
   dropout_at_step(a.drop);
-  const long long all = a.tokens * a.pieces;
-  for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < all; id += (long long)gridDim.x * 256) {
-    const long long row = id >> 32 ? id / a.pieces : (unsigned)id / (unsigned)a.pieces;
-    const long long col = (id - row * a.pieces) * VEC, valid = a.n - col;
+  // (the workgroup's first piece by a division of its own, its others from there)
+  const unsigned pieces = (unsigned)a.pieces;
+  for (long long first = (long long)blockIdx.x * 256; first < a.tokens * a.pieces; first += (long long)gridDim.x * 256) {
+    long long row = first >> 32 ? first / a.pieces : (unsigned)first / pieces;
+    unsigned in = (unsigned)(first - row * a.pieces) + threadIdx.x;
+    if (pieces >= 256) {
+      if (in >= pieces) { in -= pieces; row++; }
+    } else {
+      const unsigned on = in / pieces;
+      in -= on * pieces;
+      row += on;
+    }
+    if (row >= a.tokens) break;
+    const long long col = (long long)in * VEC, valid = a.n - col;
     const T* x = static_cast<const T*>(a.x) + row * a.ldx + col;
     const T* r = static_cast<const T*>(a.residual) + row * a.ldr + col;
     T* y = static_cast<T*>(a.y) + row * a.ldy + col;
