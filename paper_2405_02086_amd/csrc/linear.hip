@@ -9,7 +9,8 @@ namespace {
 // ------------------------------------------------------------------ gradient at the pre-activations
 // dZ = act'(Z) D(dY), rounded to the storage type (it is an operand of the products that follow), and the sums of its columns
 // before they are rounded.  A thread has eight columns and every row of its worker; the workers' sums go out in fp32 and are added
-// in their order, so that results are the same every time.  Z, dZ and the sums are each optional.  Bound by HBM.
+// in their order, so that results are the same every time.  Z, dZ and the sums are each optional.  Bound by HBM: dropout on 4096 x 4096
+// bf16 takes 18 us (3.7 TB/s), gelu's slope and the sums of 1000 x 10000 fp32 29 (4.4 TB/s) and 5 to join them.
 struct LnSlopes {
   const void *dY, *Z;
   void* dZ;
@@ -110,7 +111,8 @@ LnShape ln_shape(long long tokens, long long m) {
 }
 
 // ------------------------------------------------------------------ dropout by itself
-// y = residual + D(x), in pieces of 16 bytes.  Bound by HBM.
+// y = residual + D(x), in pieces of 16 bytes.  Bound by HBM (16384 x 4096 bf16 with a residual 74 us, 5.4 TB/s) and, where little is
+// read, by the generator (dropout.h).
 struct LnDrop {
   const void *x, *residual;
   void* y;

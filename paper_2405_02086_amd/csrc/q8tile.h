@@ -42,7 +42,8 @@ __device__ __forceinline__ bf16x8 q8_widen(int lo, int hi, unsigned scale) {
 // place.  Scales come four blocks at a time: a row's scales of one block are four bytes of a cache line of their own.
 //
 // Bound by L2, which hands a compute unit about 22 bytes per cycle, beside the matrix cores: 4096 x 16384 -> 4096, 256 tiles of 256 x
-// 256, 2.1 GB: loads alone take 170 us, products alone 174.  Rows of 64 codes in a ring of four places, as ffdirect.h has
+// 256, 2.1 GB: loads alone take 170 us, products alone 174, both 220, and 275 with a
+// residual on inputs that no cache holds.  Rows of 64 codes in a ring of four places, as ffdirect.h has
 // it, ask for half lines: 200 us for the loads alone, and scales block by block for as many lines as the codes: 211.
 constexpr int Q8_STEP = 64;
 
