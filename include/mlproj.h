@@ -499,7 +499,7 @@ typedef struct mlproj_dropout {
 } mlproj_dropout;
 
 /* y = residual + D(x), rows of n entries.  The gradient is the same call: dx = D(dy).  residual may be NULL; y may be x or
- * the residual (in place).                                                                   */
+ * the residual (in place, same stride).                                                                   */
 int dropout_forward(int storage, const mlproj_dropout* dropout /* host */, long long tokens, long long n,
                     const void* x /* device */, long long ldx, const void* residual /* device; may be NULL */, long long ldr,
                     void* y /* device */, long long ldy, void* stream);

@@ -759,11 +759,20 @@ def _vector(t, shape, like, what):
     return t.data_ptr()
 
 
+def _fixed(self, name, value):
+    """What a structure of the library was made of stays as it is, or the two would differ."""
+    if "_ref" in self.__dict__:
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed: make another one")
+    object.__setattr__(self, name, value)
+
+
 class Dropout:
     """Dropout whose mask is a function of the place of an entry (mlproj_dropout of include/mlproj.h): D(v) keeps an entry
     with probability 1 - p and divides it by 1 - p.  The same object in a call and in the call of its gradient is the
     same mask; calls with another `offset` (a number of the layer and the step, say) have independent ones.  step: a device tensor
-    of one int64 that is added to offset when the kernels run, so that a captured graph's replays differ."""
+    of one int64 that is added to offset when the kernels run, so that a captured graph's replays differ.  The object does not
+    change: the next step has one of its own, or advances `step`."""
+    __setattr__ = _fixed
 
     def __init__(self, p, seed, offset=0, step=None):
         if step is not None:
@@ -954,7 +963,9 @@ def block_norm_backward(dr, dy, r, b=None, w_post=None, gate=None, w_pre=None, s
 class Q8:
     """A matrix in 8 bits (mlproj_q8 of include/mlproj.h): rows of n entries, each a code times the power of two of its 32
     neighbours.  codes: a float8_e4m3fn tensor of rows x n filled up with zeros to whole blocks of 128, scales: a float8_e8m0fnu
-    tensor of rows x one per 32 of those; the rows of either may be further apart (codes by multiples of 16, scales of 4)."""
+    tensor of rows x one per 32 of those; the rows of either may be further apart (codes by multiples of 16, scales of 4).  The tensors' entries may
+    change, the object does not."""
+    __setattr__ = _fixed
 
     def __init__(self, n, codes, scales):
         torch = _import_torch()
@@ -972,11 +983,10 @@ def _new_q8(like, rows, n, stream):
     torch = _import_torch()
     wide = (n + 127) // 128 * 128
     q = Q8.__new__(Q8)
-    q.rows, q.n = rows, n
-    q.codes = codes = _new_empty(like, (rows, wide), torch.float8_e4m3fn, stream)
-    q.scales = scales = _new_empty(like, (rows, wide // 32), torch.float8_e8m0fnu, stream)
-    q._struct = PackedQ8(rows, n, codes.data_ptr(), wide, scales.data_ptr(), wide // 32)
-    q._ref = ctypes.byref(q._struct)
+    codes = _new_empty(like, (rows, wide), torch.float8_e4m3fn, stream)
+    scales = _new_empty(like, (rows, wide // 32), torch.float8_e8m0fnu, stream)
+    struct = PackedQ8(rows, n, codes.data_ptr(), wide, scales.data_ptr(), wide // 32)
+    q.__dict__.update(rows=rows, n=n, codes=codes, scales=scales, _struct=struct, _ref=ctypes.byref(struct))
     return q
 
 

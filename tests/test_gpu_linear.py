@@ -758,3 +758,14 @@ def test_linear_whole_turns_of_large_tiles_and_the_rest(mp):  # noqa: F811
         exact, size = a @ c, a.abs() @ c.abs()
         assert ((got.double() - exact).abs() <= (2 * a.shape[1] + 64) * U32 * size + 2.0 ** -8 * 1.001 * exact.abs()).all()
     assert ((dbias.double() - d.sum(0)).abs() <= (2 * tokens + 64) * U32 * d.abs().sum(0)).all()
+
+
+def test_q8_object_is_fixed(mp):  # noqa: F811
+    """The library reads the memory that it was made of."""
+    A = torch.ones(3, 200, device="cuda")
+    packed = mp.q8_pack(A)
+    for q in (packed, mp.Q8(200, packed.codes.clone(), packed.scales.clone())):
+        for name in ("rows", "n", "codes", "scales"):
+            with pytest.raises(AttributeError):
+                setattr(q, name, getattr(packed, name))
+        assert torch.equal(mp.q8_linear(q, packed, dtype=torch.float32), torch.full((3, 3), 200.0, device="cuda"))

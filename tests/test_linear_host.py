@@ -220,3 +220,13 @@ def test_q8_workspace(lib):
         for gated in (0, 1):
             assert ask(*sizes, gated, ctypes.byref(out)) == OK
             assert 0 < out.value < 16 << 30
+
+
+def test_dropout_object_is_fixed():
+    """Its mask is its own: a program that advances an attribute would get the old mask again."""
+    d = binding.Dropout(0.1, 3, 7)
+    for name, value in (("p", 0.2), ("seed", 4), ("offset", 8), ("step", None)):
+        with pytest.raises(AttributeError):
+            setattr(d, name, value)
+    assert (d.p, d.seed, d.offset, d.step) == (0.1, 3, 7, None)
+    assert (d._struct.p, d._struct.seed, d._struct.offset) == (0.1, 3, 7)
