@@ -16,7 +16,8 @@ static double ff_products_us(int es, long long tokens, long long n, long long m,
   return us;
 }
 // Whether 16-bit operands whose rows are not in whole 16-byte pieces are copied into rows that are (ff_pad_kernel), for
-// the direct tiles: where that is cheaper than the staged tiles by the plan.  Copies go at 4 TB/s, read and written.
+// the direct tiles: where that is cheaper than the staged tiles by the plan.  Copies are reckoned at 4 TB/s, read and written (large
+// ones reach 5), and 5 us.
 static bool ff_pads(int es, long long tokens, long long n, long long m, bool backward, bool masked) {
   if (es != 2 || (n % 8 == 0 && (m % 8 == 0 || masked))) return false;
   const double elements = (double)tokens * n + (masked ? 0.0 : 2.0 * n * m);

@@ -177,7 +177,8 @@ double ln_products_us(int es, long long tokens, long long n, long long m, bool b
   return ff_plan(tokens, n, ff_steps(m, 1), false, FF_STORE, direct, es).us + ff_plan(n, m, ff_steps(tokens, 1), false, FF_STORE, direct, es).us;
 }
 // Whether 16-bit operands whose rows are not in whole 16-byte pieces are copied into rows that are: where that is
-// cheaper than the staged tiles by the plan.  Copies go at 4 TB/s, read and written.
+// cheaper than the staged tiles by the plan.  Copies are reckoned at 4 TB/s, read and written (large
+// ones reach 5), and 5 us.
 bool ln_pads(int es, long long tokens, long long n, long long m, bool backward) {
   if (es != 2 || (n % 8 == 0 && m % 8 == 0)) return false;
   const double elements = (n % 8 ? (double)tokens * n : 0.0) + (m % 8 ? (double)n * m : 0.0);
