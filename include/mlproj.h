@@ -525,7 +525,8 @@ int linear_forward(int storage, int activation, const mlproj_linear* block /* ho
                    void* workspace /* device */, size_t workspace_bytes, void* stream);
 
 /* Its gradients for a given dY (the residual's is dY itself):
- *   dZ = act'(Z) D(dY)      (rounded to the storage type as an operand of the products that follow)
+ *   dZ = act'(Z) D(dY)      (with an activation rounded to the storage type as an operand of the products that follow;
+ *                            without one their operand is dY, dropped entries as zeros, and 1/(1 - p) is applied to their sums)
  *   dX = dZ W^T,  dW = X^T dZ,  dbias = sum over tokens of dZ before it is rounded (fp32, m entries)
  * Z is the forward call's (not read with MLPROJ_ACT_NONE); dropout has to be the forward call's.  dX, dW and dbias may each
  * be NULL; X is read for dW and W for dX alone, bias is not read.                                */

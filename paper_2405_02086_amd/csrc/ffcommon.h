@@ -29,9 +29,10 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 //            dX, dWg and dWu grow by the root of two (bf16 1.7e-3 -> 2.4e-3 of a result's norm, fp16 2.1e-4 -> 2.9e-4); without it
 //            these products would be in fp32, six times their operations
 //   LINEAR   Z = v + bias, C0 = residual + D(act(Z)) with D the dropout; Z too where the caller wants it
+//   SCALED   C0 = scale * v: the gradients of LINEAR, whose operand dY is exact in 16 bits and dY / (1 - p) is not
 //   PARTIAL  the sums over this workgroup's share of K, in fp32, for the join kernel
 enum : int { FF_WHOLE = 0, FF_TURNS = 1, FF_REST = 2 };
-enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3, FF_LINEAR = 4 };
+enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3, FF_LINEAR = 4, FF_SCALED = 5 };
 
 // One product C = A B (M x N, summed over K), or two that share A: C0 = A B0, C1 = A B1.
 // A: `a_kc` its rows run along K (row-major M x K); otherwise its rows are the K index (K x M).
@@ -50,6 +51,7 @@ struct FfProduct {
   const void* dH;              // GRAD; LINEAR: the residual, or null
   const void* bias;            // LINEAR, or null
   Dropout drop;                // LINEAR
+  float scale;                 // SCALED
   long long ldg, ldh;
   const unsigned char* keep;   // one byte per column of the result, or null
   const int* kept;             // packed channels, on the device: how many there are, instead of N (dX: of K); or null
@@ -249,6 +251,7 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
     return;
   }
   f32x4 o0 = v0, o1 = v1;
+  if constexpr (EPI == FF_SCALED) o0 *= p.scale;
   if constexpr (EPI == FF_LINEAR) {
     v0 += bias;
     o0 = ff_value4<sizeof(T) == 4>(p.act, v0);

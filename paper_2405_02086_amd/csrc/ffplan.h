@@ -153,7 +153,7 @@ void ff_launch(const FfProduct& p, int kind, hipStream_t stream) {
 template <typename T, bool A_KC, bool B_KC, bool DUAL, int EPI>
 void ff_product(FfProduct p, void* partial, hipStream_t stream) {
   if (p.M == 0) return;
-  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, EPI, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
+  const FfPlan plan = ff_plan(p.M, p.N, ff_steps(p.K, p.segs), DUAL, EPI == FF_SCALED ? FF_STORE : EPI, ff_direct<A_KC, B_KC, T>(p), sizeof(T));
   p.splits = plan.splits;
   p.partial = static_cast<float*>(partial);
   // (packed channels: how many tiles there will be is not known here, so both launches go out wherever they are many)

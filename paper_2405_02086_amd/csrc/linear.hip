@@ -8,9 +8,11 @@ namespace {
 
 // ------------------------------------------------------------------ gradient at the pre-activations
 // dZ = act'(Z) D(dY), rounded to the storage type (it is an operand of the products that follow), and the sums of its columns
-// before they are rounded.  A thread has eight columns and every row of its worker; the workers' sums go out in fp32 and are added
-// in their order, so that results are the same every time.  Z, dZ and the sums are each optional.  Bound by HBM: dropout on 4096 x 4096
-// bf16 takes 18 us (3.7 TB/s), gelu's slope and the sums of 1000 x 10000 fp32 29 (4.4 TB/s) and 5 to join them.
+// before they are rounded.  Without an activation dZ is left without dropout's factor, which the products apply to their sums in
+// fp32: dY's entries and zeros need no rounding, dY / (1 - p) does (bf16 errors of dX and dW are 1.7e-3 of a result's norm, and were
+// 2.4e-3 with the factor here).  A thread has eight columns and every row of its worker; the workers' sums go out in fp32 and are
+// added in their order, so that results are the same every time.  Z, dZ and the sums are each optional.  Bound by HBM: dropout on
+// 4096 x 4096 bf16 takes 18 us (3.7 TB/s), gelu's slope and the sums of 1000 x 10000 fp32 29 (4.4 TB/s) and 5 to join them.
 struct LnSlopes {
   const void *dY, *Z;
   void* dZ;
@@ -18,6 +20,7 @@ struct LnSlopes {
   long long lddy, ldz, lddz, tokens, m;
   int act, lanes;              // lanes: threads side by side along a row, a power of two up to 64
   Dropout drop;
+  float factor;                // of the sums: dropout's where dZ is left without it (drop.scale is 1 then), else 1
 };
 constexpr int LN_THREADS = 256;
 template <typename T>
@@ -47,7 +50,7 @@ __global__ __launch_bounds__(LN_THREADS) void ln_slopes_kernel(LnSlopes a) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
           v[i] = col + 4 * h + i < a.m ? v[i] * slope[i] : 0.0f;
-          sum[4 * h + i] += v[i];
+          sum[4 * h + i] += v[i] * a.factor;
           out.v[4 * h + i] = ff_round<T>(v[i]);
         }
       }
@@ -292,6 +295,7 @@ int run_backward(int act, const mlproj_linear* b, const void* dY, long long lddy
   char* ws = static_cast<char*>(workspace);
   const Dropout drop = dropout_start(b->dropout);
   const bool slopes = act != MLPROJ_ACT_NONE, products = dX || dW;
+  const float factor = !slopes && drop.threshold ? drop.scale : 1.0f;
   LnOperand dZ{dY, lddy, false};
   // dY itself is dZ where there is neither activation nor dropout, and its rows may stay as they are
   const bool write = products && (slopes || drop.threshold || (L.pads && b->m % 8));
@@ -303,6 +307,8 @@ int run_backward(int act, const mlproj_linear* b, const void* dY, long long lddy
     a.partial = dbias ? reinterpret_cast<float*>(ws + L.columns) : nullptr;
     a.tokens = b->tokens; a.m = b->m; a.act = act; a.lanes = s.lanes;
     a.drop = drop;
+    a.factor = factor;
+    if (!slopes) a.drop.scale = 1.0f;
     mark(stream);
     launch(ln_slopes_kernel<T>, dim3((unsigned)s.across, (unsigned)s.down), dim3(LN_THREADS), stream, a);
     if (write) dZ = {ws + L.dZ, L.ldm, true};
@@ -320,7 +326,8 @@ int run_backward(int act, const mlproj_linear* b, const void* dY, long long lddy
     p.B0 = o.W.at; p.ldb = o.W.ld; p.b_filled = o.W.filled;
     p.M = b->tokens; p.N = b->n; p.K = b->m;
     p.C0 = dX; p.ldc = lddx;
-    ff_product<T, true, true, false, FF_STORE>(p, ws + L.partial, stream);
+    p.scale = factor;
+    ff_product<T, true, true, false, FF_SCALED>(p, ws + L.partial, stream);
   }
   if (dW) {
     FfProduct p{};
@@ -329,7 +336,8 @@ int run_backward(int act, const mlproj_linear* b, const void* dY, long long lddy
     p.B0 = dZ.at; p.ldb = dZ.ld; p.b_filled = dZ.filled;
     p.M = b->n; p.N = b->m; p.K = b->tokens;
     p.C0 = dW; p.ldc = lddw;
-    ff_product<T, false, false, false, FF_STORE>(p, ws + L.partial, stream);
+    p.scale = factor;
+    ff_product<T, false, false, false, FF_SCALED>(p, ws + L.partial, stream);
   }
   mark(stream);
   return launch_status();

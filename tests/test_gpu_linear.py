@@ -769,3 +769,18 @@ def test_q8_object_is_fixed(mp):  # noqa: F811
             with pytest.raises(AttributeError):
                 setattr(q, name, getattr(packed, name))
         assert torch.equal(mp.q8_linear(q, packed, dtype=torch.float32), torch.full((3, 3), 200.0, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens,n,m", [(300, 40, 1), (1, 300, 40), (1, 1, 1), (7, 33, 5), (65, 127, 129), (300, 264, 1032), (40, 2048, 1024), (520, 512, 640)])
+def test_gradients_through_dropout_alone_are_rounded_once(mp, tokens, n, m, dtype):  # noqa: F811
+    """dY's entries and zeros are exact in every type, dY / (1 - p) is not: dX and dW are sums in fp32, their factor and one rounding."""
+    rng = np.random.default_rng(310)
+    for p, gap in ((0.3, 0), (0.1, 1), (0.9, 8)):
+        (X, x), (W, w), (dY, dy) = matrix(rng, tokens, n, dtype, gap=gap), matrix(rng, n, m, dtype, n ** -0.5, gap), matrix(rng, tokens, m, dtype, gap=gap)
+        drop, plain = dropped(mp, rng, p)
+        dX, dW, dbias, dZ = lo.linear_backward(dy, x, w, drop=plain)
+        got = mp.linear_backward(dY, X, W, dropout=drop, need_dbias=True)
+        for g, want, a, b, K, what in ((got[0], dX, dZ, w.T, m, "dX"), (got[1], dW, x.T, dZ, tokens, "dW")):
+            close(g, want, sum_bound(K, dtype) * (np.abs(a) @ np.abs(b)) + 4 * U32 * np.abs(want) + stored(want, dtype), what)
+        close(got[2], dbias, (2 * tokens + 64) * U32 * np.abs(dZ).sum(0) + 1e-37, "dbias")
