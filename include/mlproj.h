@@ -528,8 +528,8 @@ int linear_forward(int storage, int activation, const mlproj_linear* block /* ho
  *   dZ = act'(Z) D(dY)      (with an activation rounded to the storage type as an operand of the products that follow;
  *                            without one their operand is dY, dropped entries as zeros, and 1/(1 - p) is applied to their sums)
  *   dX = dZ W^T,  dW = X^T dZ,  dbias = sum over tokens of dZ before it is rounded (fp32, m entries)
- * Z is the forward call's (not read with MLPROJ_ACT_NONE); dropout has to be the forward call's.  dX, dW and dbias may each
- * be NULL; X is read for dW and W for dX alone, bias is not read.                                */
+ * Z is the forward call's (not read with MLPROJ_ACT_NONE); dropout has to be the forward call's, and dZ of an entry that it dropped
+ * is zero whatever Z is.  dX, dW and dbias may each be NULL; X is read for dW and W for dX alone, bias is not read.        */
 int linear_backward(int storage, int activation, const mlproj_linear* block /* host */,
                     const void* dY /* device, tokens x m */, long long lddy,
                     const void* Z /* device, tokens x m; may be NULL */, long long ldz,

@@ -67,6 +67,18 @@ __device__ __forceinline__ V dropout4(const Dropout& d, long long row, long long
   for (int i = 0; i < 4; i++) v[i] = w[i] >= d.threshold ? v[i] * d.scale : 0.0f;
   return v;
 }
+// Of a gradient, and what it is to be multiplied by: a slope at a NaN that was dropped is none.
+template <typename V>
+__device__ __forceinline__ V dropout4(const Dropout& d, long long row, long long quad, V v, V& slope) {
+  const philox_t w = dropout_words(d, (unsigned)row, (unsigned)quad);
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const bool kept = w[i] >= d.threshold;
+    v[i] = kept ? v[i] * d.scale : 0.0f;
+    slope[i] = kept ? slope[i] : 0.0f;
+  }
+  return v;
+}
 
 }  // namespace mlproj
 #endif

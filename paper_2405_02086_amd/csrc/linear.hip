@@ -40,13 +40,13 @@ __global__ __launch_bounds__(LN_THREADS) void ln_slopes_kernel(LnSlopes a) {
         f32x4 v, value, slope = {1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
         for (int i = 0; i < 4; i++) v[i] = (float)y.v[4 * h + i];
-        if (a.drop.threshold) v = dropout4(a.drop, row, (col >> 2) + h, v);
         if (a.Z) {
           f32x4 at;
 #pragma unroll
           for (int i = 0; i < 4; i++) at[i] = (float)z.v[4 * h + i];
           ff_gate4<sizeof(T) == 4>(a.act, at, value, slope);
         }
+        if (a.drop.threshold) v = dropout4(a.drop, row, (col >> 2) + h, v, slope);
 #pragma unroll
         for (int i = 0; i < 4; i++) {
           v[i] = col + 4 * h + i < a.m ? v[i] * slope[i] : 0.0f;

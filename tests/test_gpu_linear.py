@@ -784,3 +784,26 @@ def test_gradients_through_dropout_alone_are_rounded_once(mp, tokens, n, m, dtyp
         for g, want, a, b, K, what in ((got[0], dX, dZ, w.T, m, "dX"), (got[1], dW, x.T, dZ, tokens, "dW")):
             close(g, want, sum_bound(K, dtype) * (np.abs(a) @ np.abs(b)) + 4 * U32 * np.abs(want) + stored(want, dtype), what)
         close(got[2], dbias, (2 * tokens + 64) * U32 * np.abs(dZ).sum(0) + 1e-37, "dbias")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_gradients_at_dropped_entries_are_zeros_whatever_z_is(mp, act, dtype):  # noqa: F811
+    """A result that was dropped is zero whatever its pre-activation was, so nothing of that reaches a gradient; of one that was kept it does."""
+    rng = np.random.default_rng(311)
+    tokens, n, m = 33, 40, 52
+    (X, _), (W, _), (dY, _), (Z, _) = (matrix(rng, *s, dtype) for s in ((tokens, n), (n, m), (tokens, m), (tokens, m)))
+    drop, plain = dropped(mp, rng, 0.5)
+    keep = torch.from_numpy(lo.kept(tokens, m, *plain)).cuda()
+    want = mp.linear_backward(dY, X, W, Z=Z, act=act, dropout=drop, need_dbias=True)
+    for bad in ("nan", "inf", "-inf"):
+        z = Z.clone()
+        z[~keep] = float(bad)
+        for p, q in zip(mp.linear_backward(dY, X, W, Z=z, act=act, dropout=drop, need_dbias=True), want):
+            assert torch.equal(p, q), bad
+    row, col = (int(i) for i in torch.nonzero(keep)[100])
+    z = Z.clone()
+    z[row, col] = float("nan")
+    dX, dW, dbias = mp.linear_backward(dY, X, W, Z=z, act=act, dropout=drop, need_dbias=True)
+    assert torch.isnan(dX[row]).all() and torch.isnan(dW[:, col]).all() and torch.isnan(dbias[col])
+    assert torch.isnan(dX).sum() == n and torch.isnan(dW).sum() == n and torch.isnan(dbias).sum() == 1
