@@ -155,6 +155,8 @@ __device__ __forceinline__ bool ff_tile(FfProduct& p, long long N, long long* ro
 // library's forms cost a tenth of the whole tile's time.  Phi is taken from the side on which it is small, Phi(-|g|) = erfc(|g| /
 // sqrt 2) / 2: 1 + erf would cancel there.  Largest relative error of the 16-bit form: 5e-5 above -3, 0.1 % above -4.5, 0.4 % above -6
 // (1 + erf: 5 % above -5, nothing right below).
+// Slopes are 0 and 1 from |g| = 128 on, and are taken there past it, as a gradient's act(g) is below -128: a g that is infinite, which
+// finite sums are once they are stored in fp16, would give infinity times zero.
 template <bool EXACT> __device__ __forceinline__ float ff_exp(float x) {
   return EXACT ? expf(x) : __builtin_amdgcn_exp2f(x * 1.44269504f);
 }
@@ -173,13 +175,14 @@ template <bool EXACT> __device__ __forceinline__ float ff_normal(float g, float 
   }
   return g < 0.0f ? below : 1.0f - below;
 }
+__device__ __forceinline__ float ff_near(float g) { return __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f); }   // (a NaN is in s or e as well)
 template <bool EXACT> __device__ __forceinline__ void ff_gate4(int act, f32x4 g, f32x4& value, f32x4& slope) {
   if (act == MLPROJ_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       const float s = ff_reciprocal<EXACT>(1.0f + ff_exp<EXACT>(-g[i]));
       value[i] = g[i] * s;
-      slope[i] = s * (1.0f + g[i] * (1.0f - s));
+      slope[i] = s * (1.0f + ff_near(g[i]) * (1.0f - s));
     }
   } else if (act == MLPROJ_ACT_GELU) {
 #pragma unroll
@@ -187,7 +190,7 @@ template <bool EXACT> __device__ __forceinline__ void ff_gate4(int act, f32x4 g,
       const float e = ff_exp<EXACT>(-0.5f * g[i] * g[i]);
       const float phi = ff_normal<EXACT>(g[i], e);
       value[i] = g[i] * phi;
-      slope[i] = phi + g[i] * 0.39894228f * e;
+      slope[i] = phi + ff_near(g[i]) * 0.39894228f * e;
     }
   } else {
 #pragma unroll
@@ -260,8 +263,13 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
     for (int i = 0; i < 4; i++) o0[i] += (float)d.v[i];
   }
   if constexpr (EPI == FF_FWD || EPI == FF_GRAD) {
-    f32x4 value, slope;
-    ff_gate4<sizeof(T) == 4>(p.act, v0, value, slope);
+    f32x4 value, slope, g = v0;
+    if constexpr (EPI == FF_GRAD) {
+      // (0 from -128 down, an infinity included)
+#pragma unroll
+      for (int i = 0; i < 4; i++) g[i] = g[i] < -128.0f ? -128.0f : g[i];
+    }
+    ff_gate4<sizeof(T) == 4>(p.act, g, value, slope);
     if constexpr (EPI == FF_FWD) {
       o0 = value * v1;
     } else {

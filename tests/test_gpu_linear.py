@@ -807,3 +807,42 @@ def test_gradients_at_dropped_entries_are_zeros_whatever_z_is(mp, act, dtype):  
     dX, dW, dbias = mp.linear_backward(dY, X, W, Z=z, act=act, dropout=drop, need_dbias=True)
     assert torch.isnan(dX[row]).all() and torch.isnan(dW[:, col]).all() and torch.isnan(dbias[col])
     assert torch.isnan(dX).sum() == n and torch.isnan(dW).sum() == n and torch.isnan(dbias).sum() == 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_slopes_at_infinite_pre_activations_are_their_limits(mp, act, dtype):  # noqa: F811
+    """0 and 1, as they are in fp32 from 200 on: the same gradients to the bit."""
+    rng = np.random.default_rng(312)
+    tokens, n, m = 40, 72, 56
+    (X, _), (W, _), (dY, _), (Z, _) = (matrix(rng, *s, dtype) for s in ((tokens, n), (n, m), (tokens, m), (tokens, m)))
+    far = {"+": torch.from_numpy(rng.random((tokens, m)) < 0.1).cuda(), "-": torch.from_numpy(rng.random((tokens, m)) < 0.1).cuda()}
+    grads = []
+    for size in (200.0, float("inf")):
+        z = Z.clone()
+        for sign, at in far.items():
+            z[at] = float(sign + str(size))
+        grads.append(mp.linear_backward(dY, X, W, Z=z, act=act, need_dbias=True))
+    for p, q in zip(*grads):
+        assert torch.isfinite(p).all() and torch.equal(p, q)
+
+
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_pre_activations_past_fp16_have_their_gradients(mp, act):  # noqa: F811
+    """A pre-activation of -2^17 is an infinity in fp16, its result zero (relu's and the others' limit) and so is its gradient."""
+    X = torch.zeros(3, 8, dtype=torch.float16, device="cuda")
+    X[0, 0], X[1, 0], X[2, 1] = -2.0 ** 10, 2.0 ** -10, 1.0
+    W = torch.full((8, 16), 2.0 ** 7, dtype=torch.float16, device="cuda")
+    Z = torch.empty(3, 16, dtype=torch.float16, device="cuda")
+    y = mp.linear(X, W, act=act, z_out=Z)
+    assert torch.isinf(Z[0]).all() and torch.isfinite(Z[1:]).all() and not y[0].any()
+    dX, dW, dbias = mp.linear_backward(torch.ones_like(y), X, W, Z=Z, act=act, need_dbias=True)
+    assert not dX[0].any() and torch.isfinite(dX).all() and torch.isfinite(dW).all() and torch.isfinite(dbias).all()
+    # a gated block's saved gate
+    U = torch.ones_like(Z)
+    dH = torch.ones_like(y)
+    got = mp.gated_ff_backward(dH, X, W, W, act=act, G=Z, U=U)
+    want = mp.gated_ff_backward(dH, X, W, W, act=act, G=Z.clamp_min(-200), U=U)
+    for p, q in zip(got, want):
+        # (dX of the last row is 16 (1 + 2^7) 2^7 = 264192, an infinity in fp16)
+        assert torch.isfinite(p[:2]).all() and not torch.isnan(p).any() and torch.equal(p, q)
