@@ -176,12 +176,13 @@ template <bool EXACT> __device__ __forceinline__ float ff_normal(float g, float 
   return g < 0.0f ? below : 1.0f - below;
 }
 __device__ __forceinline__ float ff_near(float g) { return __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f); }   // (a NaN is in s or e as well)
-template <bool EXACT> __device__ __forceinline__ void ff_gate4(int act, f32x4 g, f32x4& value, f32x4& slope) {
+template <bool LIMITS> __device__ __forceinline__ float ff_above(float g) { return LIMITS ? __builtin_amdgcn_fmed3f(g, -128.0f, __builtin_inff()) : g; }
+template <bool EXACT, bool LIMITS = false> __device__ __forceinline__ void ff_gate4(int act, f32x4 g, f32x4& value, f32x4& slope) {
   if (act == MLPROJ_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       const float s = ff_reciprocal<EXACT>(1.0f + ff_exp<EXACT>(-g[i]));
-      value[i] = g[i] * s;
+      value[i] = ff_above<LIMITS>(g[i]) * s;
       slope[i] = s * (1.0f + ff_near(g[i]) * (1.0f - s));
     }
   } else if (act == MLPROJ_ACT_GELU) {
@@ -189,7 +190,7 @@ template <bool EXACT> __device__ __forceinline__ void ff_gate4(int act, f32x4 g,
     for (int i = 0; i < 4; i++) {
       const float e = ff_exp<EXACT>(-0.5f * g[i] * g[i]);
       const float phi = ff_normal<EXACT>(g[i], e);
-      value[i] = g[i] * phi;
+      value[i] = ff_above<LIMITS>(g[i]) * phi;
       slope[i] = phi + ff_near(g[i]) * 0.39894228f * e;
     }
   } else {
@@ -263,13 +264,8 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
     for (int i = 0; i < 4; i++) o0[i] += (float)d.v[i];
   }
   if constexpr (EPI == FF_FWD || EPI == FF_GRAD) {
-    f32x4 value, slope, g = v0;
-    if constexpr (EPI == FF_GRAD) {
-      // (0 from -128 down, an infinity included)
-#pragma unroll
-      for (int i = 0; i < 4; i++) g[i] = g[i] < -128.0f ? -128.0f : g[i];
-    }
-    ff_gate4<sizeof(T) == 4>(p.act, g, value, slope);
+    f32x4 value, slope;
+    ff_gate4<sizeof(T) == 4, EPI == FF_GRAD>(p.act, v0, value, slope);
     if constexpr (EPI == FF_FWD) {
       o0 = value * v1;
     } else {
