@@ -29,10 +29,11 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 //            dX, dWg and dWu grow by the root of two (bf16 1.7e-3 -> 2.4e-3 of a result's norm, fp16 2.1e-4 -> 2.9e-4); without it
 //            these products would be in fp32, six times their operations
 //   LINEAR   Z = v + bias, C0 = residual + D(act(Z)) with D the dropout; Z too where the caller wants it
+//   PLAIN    C0 = residual + act(v + bias): LINEAR where there is neither dropout nor Z (8 bits)
 //   SCALED   C0 = scale * v: the gradients of LINEAR, whose operand dY is exact in 16 bits and dY / (1 - p) is not
 //   PARTIAL  the sums over this workgroup's share of K, in fp32, for the join kernel
 enum : int { FF_WHOLE = 0, FF_TURNS = 1, FF_REST = 2 };
-enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3, FF_LINEAR = 4, FF_SCALED = 5 };
+enum : int { FF_STORE = 0, FF_FWD = 1, FF_GRAD = 2, FF_PARTIAL = 3, FF_LINEAR = 4, FF_SCALED = 5, FF_PLAIN = 6 };
 
 // One product C = A B (M x N, summed over K), or two that share A: C0 = A B0, C1 = A B1.
 // A: `a_kc` its rows run along K (row-major M x K); otherwise its rows are the K index (K x M).
@@ -48,8 +49,8 @@ struct FfProduct {
   void *C0, *C1;
   long long ldc;
   void *G, *U;                 // FWD: optional outputs; LINEAR: Z in G
-  const void* dH;              // GRAD; LINEAR: the residual, or null
-  const void* bias;            // LINEAR, or null
+  const void* dH;              // GRAD; LINEAR, PLAIN: the residual, or null
+  const void* bias;            // LINEAR, PLAIN, or null
   Dropout drop;                // LINEAR
   float scale;                 // SCALED
   long long ldg, ldh;
@@ -213,8 +214,8 @@ template <bool EXACT> __device__ __forceinline__ f32x4 ff_value4(int act, f32x4 
 // ------------------------------------------------------------------ epilogue
 // Columns col .. col+3 of row `row`, of which those below N exist; v0, v1: their sums in the two products.
 // A pruned channel's outputs are zeros whatever its sums are, NaN included.
-// ff_upstream: GRAD's four entries of dH, LINEAR's of the residual; all of a thread's are fetched before its first store, which the
-// compiler could not move them across.  ff_bias: LINEAR's of the bias.
+// ff_upstream: GRAD's four entries of dH, LINEAR's and PLAIN's of the residual; all of a thread's are fetched before its first store,
+// which the compiler could not move them across.  ff_bias: LINEAR's and PLAIN's of the bias.
 template <typename T>
 __device__ __forceinline__ FfVec4<T> ff_upstream(const FfProduct& p, long long row, long long col, long long N) {
   FfVec4<T> d;
@@ -230,7 +231,8 @@ __device__ __forceinline__ FfVec4<T> ff_upstream(const FfProduct& p, long long r
   }
   return d;
 }
-template <int EPI> constexpr bool FF_UPSTREAM = EPI == FF_GRAD || EPI == FF_LINEAR;
+template <int EPI> constexpr bool FF_BIAS = EPI == FF_LINEAR || EPI == FF_PLAIN;
+template <int EPI> constexpr bool FF_UPSTREAM = EPI == FF_GRAD || FF_BIAS<EPI>;
 template <typename T>
 __device__ __forceinline__ f32x4 ff_bias(const FfProduct& p, long long col, long long N) {
   f32x4 b = {};
@@ -256,10 +258,11 @@ __device__ __forceinline__ void ff_finish(const FfProduct& p, long long row, lon
   }
   f32x4 o0 = v0, o1 = v1;
   if constexpr (EPI == FF_SCALED) o0 *= p.scale;
-  if constexpr (EPI == FF_LINEAR) {
+  if constexpr (FF_BIAS<EPI>) {
     v0 += bias;
     o0 = ff_value4<sizeof(T) == 4>(p.act, v0);
-    if (p.drop.threshold) o0 = dropout4(p.drop, row, col >> 2, o0);
+    if constexpr (EPI == FF_LINEAR)
+      if (p.drop.threshold) o0 = dropout4(p.drop, row, col >> 2, o0);
 #pragma unroll
     for (int i = 0; i < 4; i++) o0[i] += (float)d.v[i];
   }

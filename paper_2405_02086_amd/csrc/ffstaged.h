@@ -313,10 +313,8 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p) {
   FfVec4<T> d = {};
   f32x4 bias = {};
   if constexpr (FF_UPSTREAM<EPI>) d = ff_upstream<T>(p, row, col, N);
-  if constexpr (EPI == FF_LINEAR) {
-    dropout_at_step(p.drop);
-    bias = ff_bias<T>(p, col, N);
-  }
+  if constexpr (EPI == FF_LINEAR) dropout_at_step(p.drop);
+  if constexpr (FF_BIAS<EPI>) bias = ff_bias<T>(p, col, N);
   ff_finish<EPI, DUAL, T>(p, row, col, N, v[0], v[1], d, bias);
 }
 

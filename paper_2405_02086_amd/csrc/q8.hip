@@ -241,9 +241,9 @@ int q8_linear(int storage, int activation, const mlproj_q8* x, const mlproj_q8* 
   q.p.dH = residual; q.p.ldh = ldr;
   q.p.C0 = y; q.p.ldc = ldy;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (storage == MLPROJ_STORE_F32) return q8_product<float, false, FF_LINEAR>(q, workspace, s);
-  if (storage == MLPROJ_STORE_BF16) return q8_product<bf16_t, false, FF_LINEAR>(q, workspace, s);
-  return q8_product<f16_t, false, FF_LINEAR>(q, workspace, s);
+  if (storage == MLPROJ_STORE_F32) return q8_product<float, false, FF_PLAIN>(q, workspace, s);
+  if (storage == MLPROJ_STORE_BF16) return q8_product<bf16_t, false, FF_PLAIN>(q, workspace, s);
+  return q8_product<f16_t, false, FF_PLAIN>(q, workspace, s);
 }
 
 int q8_gated(int storage, int activation, const mlproj_q8* x, const mlproj_q8* Wg, const mlproj_q8* Wu, void* h, long long ldh,

@@ -94,7 +94,6 @@ __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
   for (int v = 0; v < VALUES; v++) sums[wave][v][lane] = acc[v];
   __syncthreads();
   // a lane's four sums are neighbouring columns of one token
-  dropout_at_step(p.drop);
   for (int at = threadIdx.x; at < CB * 64; at += WAVES * 64) {
     const int b = at >> 6, l = at & 63;
     const long long t = l & 15, c = col0 + b * 16 + (l >> 4) * 4;
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(WAVES * 64) void q8_few_kernel(Q8Product q) {
       for (int s = 0; s < WAVES; s++) v[i] += sums[s][i * CB + b][l];
     FfVec4<T> d = {};
     f32x4 bias = {};
-    if constexpr (EPI == FF_LINEAR) {
+    if constexpr (EPI == FF_PLAIN) {
       d = ff_upstream<T>(p, t, c, p.N);
       bias = ff_bias<T>(p, c, p.N);
     }

@@ -257,10 +257,9 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
   typedef __attribute__((address_space(3))) f32x4 quad_t;
   const int stage = wave / PER;
   byte_t* mine = (stage == 0 ? (byte_t*)lds0 : (byte_t*)lds1) + wave % PER * SHARE;
-  dropout_at_step(p.drop);
   const int quad = lane % ACROSS, down = lane / ACROSS, j = quad >> 3;
   const long long col = col0 + wn * CJ * 32 + (j < CJ ? j * 32 : BW + (j - CJ) * 32) + (quad & 7) * 4;
-  const f32x4 bias = EPI == FF_LINEAR && col < N ? ff_bias<T>(p, col, N) : f32x4{};
+  const f32x4 bias = EPI == FF_PLAIN && col < N ? ff_bias<T>(p, col, N) : f32x4{};
 #pragma unroll
   for (int pass = 0; pass < RT / TILES; pass++) {
 #pragma unroll
@@ -279,7 +278,7 @@ __global__ __launch_bounds__(WM * WN * 64) void q8_tile_kernel(Q8Product q) {
       for (int u = 0; u < CHUNK; u++) {
         const long long row = first_row + (chunk * CHUNK + u) * DOWN;
         to[u] = {};
-        if (EPI == FF_LINEAR && p.dH && row < p.M && col < N) to[u] = ff_upstream<T>(p, row, col, N);
+        if (EPI == FF_PLAIN && p.dH && row < p.M && col < N) to[u] = ff_upstream<T>(p, row, col, N);
       }
     };
     constexpr int ROUNDS = TILES * 32 / DOWN / CHUNK;
