@@ -846,3 +846,58 @@ def test_pre_activations_past_fp16_have_their_gradients(mp, act):  # noqa: F811
     for p, q in zip(got, want):
         # (dX of the last row is 16 (1 + 2^7) 2^7 = 264192, an infinity in fp16)
         assert torch.isfinite(p[:2]).all() and not torch.isnan(p).any() and torch.equal(p, q)
+
+
+# 32 columns per workgroup for pairs of more than 4 tokens from m = 4096 on, with a remainder of columns; 64 blocks a round from n = 8065 on,
+# with rounds that are not whole, and a second one
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens,n,m", [(5, 300, 4099), (16, 1000, 4128), (4, 520, 4100), (1, 8200, 40), (9, 12345, 33), (16, 16500, 24), (3, 8064, 20)])
+def test_q8_products_of_few_tokens_take_every_form(mp, tokens, n, m, dtype):  # noqa: F811
+    rng = np.random.default_rng(703)
+    X, x, W, w = q8_case(mp, rng, tokens, n, m)
+    U, u = q8_case(mp, rng, 1, n, m)[2:]
+    (B, b), (R, r) = (matrix(rng, k, m, dtype) for k in (1, tokens))
+    Z, e = x @ w + b, q8_bound(x, w, dtype)
+    eZ = e + 2 * U32 * np.abs(Z)
+    V = bo.activation("gelu", Z)
+    eV = SLOPE * eZ + 16 * U32 * (np.abs(V) + np.abs(Z)) + gelu_short("gelu", dtype, Z) * np.abs(V)
+    out, intact = guarded(tokens, m, dtype)
+    mp.q8_linear(X, W, bias=B[0], residual=R, act="gelu", y=out, workspace=workspace(mp, mp.q8_workspace_bytes(tokens, n, m)))
+    torch.cuda.synchronize()
+    close(out, r + V, eV + 4 * U32 * (np.abs(V) + np.abs(r)) + stored(r + V, dtype), "y")
+    intact()
+    g, up, eu = x @ w, x @ u, q8_bound(x, u, dtype)
+    a = bo.activation("silu", g)
+    ea = SLOPE * e + 16 * U32 * (np.abs(a) + np.abs(g))
+    out, intact = guarded(tokens, m, dtype)
+    mp.q8_gated(X, W, U, act="silu", h=out, workspace=workspace(mp, mp.q8_workspace_bytes(tokens, n, m, True)))
+    torch.cuda.synchronize()
+    close(out, a * up, ea * (np.abs(up) + eu) + np.abs(a) * eu + 2 * U32 * np.abs(a * up) + stored(a * up, dtype), "h")
+    intact()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens,n,m", [(1, 640, 40), (16, 1200, 64), (7, 9000, 24), (40, 256, 136), (130, 300, 257), (300, 1024, 520), (600, 384, 2056), (1500, 160, 4100)])
+def test_q8_products_find_every_group_s_scale(mp, tokens, n, m, dtype):  # noqa: F811
+    """Whole numbers whose groups of 32 along n are multiplied by 2^s in x and by 2^-s in w, with another s in every group, and whose rows by powers of
+    two of their own: products are exact however the matrix cores add, and another group's or row's scale would show."""
+    rng = np.random.default_rng(704)
+    size = {"bf16": 2 ** 8, "f16": 2 ** 11, "f32": 2 ** 24}[dtype]
+    density = min(1.0, size / 4 / (4 * 16) / n * 8)
+    groups = -(-n // 32)
+    s = rng.permutation(groups) % 61 - 30
+    assert len(set(s)) == min(groups, 61)
+
+    def whole(rows, sign):
+        v = rng.integers(-4, 5, (rows, groups, 32)) * (rng.random((rows, groups, 32)) < density ** 0.5)
+        v = v.reshape(rows, -1)[:, :n].astype(np.float64)
+        of_row = -rng.integers(0, 4, (rows, 1))
+        q = mp.q8_pack(torch.from_numpy(v * 2.0 ** of_row * 2.0 ** (sign * np.repeat(s, 32)[:n])).float().cuda())
+        return v, of_row, q
+    (x, tx, X), (w, tw, W) = whole(tokens, 1), whole(m, -1)
+    sums = x @ w.T
+    assert np.abs(sums).max() <= size
+    want = sums * 2.0 ** (tx + tw.T)
+    np.testing.assert_array_equal(values(mp.q8_linear(X, W, dtype=TYPES[dtype])), want)
+    h = (np.maximum(want, 0) * want).astype(np.float32)
+    np.testing.assert_array_equal(mp.q8_gated(X, W, W, act="relu", dtype=torch.float32).cpu().numpy(), h)
