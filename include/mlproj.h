@@ -577,9 +577,9 @@ int block_norm_backward(int storage, const mlproj_norm_block* block /* host */, 
                         void* workspace /* device */, size_t workspace_bytes, void* stream);
 
 /* A matrix in 8 bits: rows of codes in e4m3 (sign, four exponent bits, three fraction bits, no infinities: at most 448),
- * each times the power of two 2^(byte - 127) of its group, 32 neighbouring entries of its row.  Rows are in whole blocks of 128
- * entries: past n, codes are zeros (NaN in a group that is NaN) and their scales any but 255.  This is what the matrix cores multiply; a weight matrix n x m that x is
- * multiplied by (x W) is held by its columns, as m rows of n.
+ * each times the power of two 2^(byte - 127) of its group, 32 neighbouring entries of its row (255: all of them are NaN).  Rows
+ * are in whole blocks of 128 entries: past n, codes are zeros (NaN in a group that is NaN) and their scales any but 255.  This is
+ * what the matrix cores multiply; a weight matrix n x m that x is multiplied by (x W) is held by its columns, as m rows of n.
  *   codes   row i at codes + i * ld bytes; 16-byte aligned, ld a multiple of 16 and at least n in whole blocks
  *   scales  row i at scales + i * lds bytes; 4-byte aligned, lds a multiple of 4 and at least a byte per group of those    */
 typedef struct mlproj_q8 {
@@ -601,8 +601,9 @@ int block_norm8_forward(int storage, const mlproj_norm_block* block /* host */, 
                         void* r /* device */, long long ldr, const mlproj_q8* y /* host */, void* stream);
 
 /* Products with both operands in 8 bits: x is tokens x n, W holds an n x m matrix by its columns (m rows of n); every other
- * array is of the storage type.  With fp32 storage products and sums are fp32 (entries below 2^-126 count as zeros); with 16 bits they are
- * the matrix cores' own, whose sums of eight products keep 16 bits beside the largest of them.
+ * array is of the storage type.  With fp32 storage products and sums are fp32, of entries as bf16 holds them: exactly, but below
+ * 2^-126 as multiples of 2^-133 and from 2^128 on as infinities; with 16 bits they are the matrix cores' own, whose sums of eight
+ * products keep 16 bits beside the largest of them.
  * q8_linear: y = residual + act(x W + bias); bias and residual may be NULL, y may be the residual (in place, same stride).
  * q8_gated:  h = act(x Wg) * (x Wu); Wg and Wu of the same size and strides.  A pruned column is a row of zeros.
  * Strides of packed rows are at most 2^22 here (MLPROJ_ERR_TOO_LARGE).                              */

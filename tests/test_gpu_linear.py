@@ -901,3 +901,26 @@ def test_q8_products_find_every_group_s_scale(mp, tokens, n, m, dtype):  # noqa:
     np.testing.assert_array_equal(values(mp.q8_linear(X, W, dtype=TYPES[dtype])), want)
     h = (np.maximum(want, 0) * want).astype(np.float32)
     np.testing.assert_array_equal(mp.q8_gated(X, W, W, act="relu", dtype=torch.float32).cpu().numpy(), h)
+
+
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_q8_products_at_the_ends_of_the_scales(mp, tokens):  # noqa: F811
+    """With fp32 results entries are those of bf16: multiples of 2^-133 below 2^-126 (half a step off at most), infinities from 2^128 on.
+    A scale of 255 is NaN in every type."""
+    def q8(codes, scale):
+        c = torch.zeros(len(codes), 128, dtype=torch.uint8, device="cuda")
+        c[:, 0] = torch.as_tensor(codes, device="cuda")
+        return mp.Q8(128, c.view(torch.float8_e4m3fn), torch.full((len(codes), 4), scale, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu))
+    positive = np.arange(127, dtype=np.uint8)                  # every code but NaN, in their order
+    one = np.full(tokens, 0x38, np.uint8)
+    value = torch.from_numpy(positive).view(torch.float8_e4m3fn).float().double().numpy()
+    for scale in (0, 1, 2, 5, 6, 10, 200, 246, 247, 248, 254):
+        other = 227 if scale < 100 else 27                     # 2^100, 2^-100
+        got = values(mp.q8_linear(q8(one, other), q8(positive, scale), dtype=torch.float32)) * 2.0 ** (127.0 - other)
+        entry = value * 2.0 ** (scale - 127.0)
+        inside = entry < 2.0 ** 128
+        off = np.where(entry < 2.0 ** -126, 2.0 ** -134, 0.0)
+        assert (np.abs(got - entry)[:, inside] <= off[inside]).all() and np.isinf(got[:, ~inside]).all(), scale
+    for dtype in TYPES.values():
+        assert torch.isnan(mp.q8_linear(q8(one, 255), q8(positive, 127), dtype=dtype)).all()
+        assert torch.isnan(mp.q8_linear(q8(one, 127), q8(positive, 255), dtype=dtype)).all()
