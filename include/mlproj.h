@@ -427,6 +427,8 @@ int mlproj_multilevel_one_pass(int storage, int fibre_norm, long long d0, long l
  * be 0: then nothing is read, and sums over tokens are zeros.  Sizes past what one launch takes (2^32
  * threads) are MLPROJ_ERR_TOO_LARGE.
  * Calls enqueue on `stream`, keep no state and need no cleared workspace, as everywhere above.
+ * Workspace sizes do not grow with `tokens` alone: few tokens are summed in shares that are kept there, more are not.  A size is
+ * that of the call with these arguments; one workspace for calls of several sizes and directions has the largest of theirs.
  * Outputs must not overlap inputs or one another except where said.
  * --------------------------------------------------------------------------------------------- */
 

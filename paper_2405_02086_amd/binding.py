@@ -676,7 +676,8 @@ def _result(t, shape, like, what, stream):
 
 
 def gated_ff_workspace_bytes(tokens, n, m, dtype, backward=False, masked=True):
-    """Bytes a call needs; masked=False: for calls without a mask only, which need far less."""
+    """Bytes a call of these sizes needs (one of fewer tokens may need more); masked=False: for calls without a mask only, which
+    need far less."""
     out = ctypes.c_size_t(0)
     _check(lib().mlproj_gated_ff_workspace_bytes(_storage(dtype), tokens, n, m, int(backward), int(masked), ctypes.byref(out)),
            "mlproj_gated_ff_workspace_bytes")
@@ -803,6 +804,7 @@ def dropout_backward(dy, drop, dx=None, stream=None):
 
 
 def linear_workspace_bytes(tokens, n, m, dtype, backward=False):
+    """Bytes a call of these sizes needs (one of fewer tokens may need more)."""
     out = ctypes.c_size_t(0)
     _check(lib().mlproj_linear_workspace_bytes(_storage(dtype), tokens, n, m, int(backward), ctypes.byref(out)),
            "mlproj_linear_workspace_bytes")
@@ -1029,6 +1031,7 @@ def block_norm8(x, b=None, w_post=None, gate=None, w_pre=None, scale=1.0, eps=1e
 
 
 def q8_workspace_bytes(tokens, n, m, gated=False):
+    """Bytes a call of these sizes needs (one of fewer tokens may need more)."""
     out = ctypes.c_size_t(0)
     _check(lib().mlproj_q8_workspace_bytes(tokens, n, m, int(gated), ctypes.byref(out)), "mlproj_q8_workspace_bytes")
     return out.value

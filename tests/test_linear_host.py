@@ -230,3 +230,25 @@ def test_dropout_object_is_fixed():
             setattr(d, name, value)
     assert (d.p, d.seed, d.offset, d.step) == (0.1, 3, 7, None)
     assert (d._struct.p, d._struct.seed, d._struct.offset) == (0.1, 3, 7)
+
+
+def test_a_workspace_is_that_of_a_call_s_own_sizes(lib):
+    """Fewer tokens may need more: their sums are cut into shares.  Less than the size of the call is refused."""
+    out = ctypes.c_size_t(0)
+
+    def linear(storage, tokens, back):
+        assert lib.mlproj_linear_workspace_bytes(storage, tokens, 16384, 4096, back, ctypes.byref(out)) == OK
+        return out.value
+
+    def eight(tokens):
+        assert lib.mlproj_q8_workspace_bytes(tokens, 16384, 4096, 0, ctypes.byref(out)) == OK
+        return out.value
+    assert linear(0, 300, 0) > linear(0, 4096, 0) and linear(1, 512, 1) > linear(1, 1024, 1) and eight(300) > eight(4096)
+    for tokens in (300, 4096):
+        b = block(tokens, 16384, 4096, ldx=16384, ldw=4096)
+        assert forward(lib, b, storage=0, ldy=4096, nbytes=linear(0, tokens, 0) - 1) == WS
+        assert backward(lib, b, lddy=4096, ldz=4096, lddx=16384, lddw=4096, nbytes=linear(1, tokens, 1) - 1) == WS
+        x, W = q8(tokens, 16384, ld=16384, lds=512), q8(4096, 16384, ld=16384, lds=512)
+        assert lib.q8_linear(1, 3, ctypes.byref(x), ctypes.byref(W), None, None, 0, P, 4096, P, eight(tokens) - 1, None) == WS
+    # (a call without tokens enqueues nothing)
+    assert forward(lib, block(0, 16384, 4096, X=None, ldx=16384, W=None, ldw=4096), storage=0, Y=None, nbytes=linear(0, 0, 0)) == OK
