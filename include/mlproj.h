@@ -489,10 +489,12 @@ int gated_ff_backward(int storage, int activation, const mlproj_gated_block* blo
 
 /* Dropout whose mask is never stored: it is a function of the place of an entry, computed where it is needed.  Entry (t, c) of
  * a matrix is kept if word c % 4 of Philox4x32-10 at counter (c / 4, t, low half of o, high half of o) and key (low, high half
- * of seed) is at least p * 2^32 (rounded to a whole number); kept entries are divided by 1 - p, the others are zeros whatever
- * they were.  o is `offset`, plus the number in device memory at `step` if there is one: a call that is captured in a graph
- * reads it at every replay, so that the program advances the mask by advancing that number (and leaves it alone until
- * the gradient that belongs to it is done).  Calls with different o have independent masks.  0 <= p < 1 (MLPROJ_ERR_BAD_VALUE).
+ * of seed) is at least p * 2^32 (rounded to a whole number, 2^32 - 1 at most); kept entries are divided by 1 - p, the others are
+ * zeros whatever they were.  o is `offset`, plus the number in device memory at `step` if there is one: a call that is captured in
+ * a graph reads it at every replay, so that the program advances the mask by advancing that number (and leaves it alone until
+ * the gradient that belongs to it is done).  Calls with different o or seeds have independent masks, and calls with the same o and
+ * seed the same one: offset 1 at step 0 is offset 0 at step 1, so layers that share a seed and a step have offsets further apart than
+ * the step will ever go (layer << 40, say), or seeds of their own.  0 <= p < 1 (MLPROJ_ERR_BAD_VALUE).
  * Below, D(v) is v after dropout, and v itself where there is none.                              */
 typedef struct mlproj_dropout {
   double p;

@@ -771,8 +771,9 @@ class Dropout:
     """Dropout whose mask is a function of the place of an entry (mlproj_dropout of include/mlproj.h): D(v) keeps an entry
     with probability 1 - p and divides it by 1 - p.  The same object in a call and in the call of its gradient is the
     same mask; calls with another `offset` (a number of the layer and the step, say) have independent ones.  step: a device tensor
-    of one int64 that is added to offset when the kernels run, so that a captured graph's replays differ.  The object does not
-    change: the next step has one of its own, or advances `step`."""
+    of one int64 that is added to offset when the kernels run, so that a captured graph's replays differ.  What counts is the sum:
+    layers that share a seed and a step take offsets further apart than the step will ever go (layer << 40), or seeds of their
+    own.  The object does not change: the next step has one of its own, or advances `step`."""
     __setattr__ = _fixed
 
     def __init__(self, p, seed, offset=0, step=None):

@@ -924,3 +924,31 @@ def test_q8_products_at_the_ends_of_the_scales(mp, tokens):  # noqa: F811
     for dtype in TYPES.values():
         assert torch.isnan(mp.q8_linear(q8(one, 255), q8(positive, 127), dtype=dtype)).all()
         assert torch.isnan(mp.q8_linear(q8(one, 127), q8(positive, 255), dtype=dtype)).all()
+
+
+def test_layers_that_share_a_step_have_masks_of_their_own(mp):  # noqa: F811
+    """Offsets further apart than the step goes, or seeds; the mask is that of the sum of offset and step."""
+    x = torch.ones(20, 64, device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    masks = []
+    layers = [mp.Dropout(0.5, 9, layer << 40, step=step) for layer in range(4)] + [mp.Dropout(0.5, seed, 0, step=step) for seed in (10, 11)]
+    for now in range(4):
+        step.fill_(now)
+        for k, drop in enumerate(layers):
+            y = mp.dropout(x, drop)
+            masks.append(y != 0)
+            seed, offset = (9, k << 40) if k < 4 else (6 + k, 0)
+            np.testing.assert_array_equal(values(masks[-1]) != 0, lo.kept(20, 64, 0.5, seed, offset + now))
+    for i in range(len(masks)):
+        for j in range(i):
+            assert not torch.equal(masks[i], masks[j])
+    step.fill_(3)
+    assert torch.equal(mp.dropout(x, mp.Dropout(0.5, 9, 1, step=step)), mp.dropout(x, mp.Dropout(0.5, 9, 4)))
+
+
+def test_dropout_of_nearly_everything(mp):  # noqa: F811
+    """p next to 1: the threshold is the largest word, and what is kept is divided by 1 - p."""
+    x = torch.ones(64, 512, device="cuda")
+    for p in (1 - 2.0 ** -12, 1 - 2.0 ** -32, 1 - 2.0 ** -40, 1 - 2.0 ** -53):
+        y, keep = values(mp.dropout(x, mp.Dropout(p, 5, 6))), lo.kept(64, 512, p, 5, 6)
+        np.testing.assert_array_equal(y, np.where(keep, 1 / (1 - p), 0.0))
