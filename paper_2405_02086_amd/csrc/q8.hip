@@ -90,6 +90,12 @@ Q8Plan q8_plan(long long M, long long N, long long blocks, bool dual, bool exact
   }
   return best;
 }
+// Whether a pair of products of few tokens with 16-bit results takes 32 columns per workgroup and not 16 (q8few.h).
+bool q8_few_wide(long long tokens, long long m, long long n) {
+  if (ff_cdiv(m, 4096) % 2) return false;                       // half of the last 32-column workgroups' places would be empty
+  if (m > 8192) return tokens >= 8 || n <= 2048;
+  return tokens >= 8 && n >= 4096 && (m < 8192 || n < 8192);
+}
 // Workgroups (along x) of a product's launch.
 long long q8_groups(int kind, long long M, long long N, bool dual, int splits) {
   const int half = dual ? 2 : 1;
@@ -137,8 +143,14 @@ int q8_product(Q8Product q, void* workspace, hipStream_t stream) {
     mark(stream);
     auto go = [&](auto* kernel, int columns) { launch(kernel, dim3((unsigned)ff_cdiv(p.N, columns)), dim3(512), stream, q); };
     if constexpr (DUAL) {
-      if (p.M > 4 && p.N >= 4096) go(q8_few_kernel<T, true, EPI, 2, 4, 8, EXACT>, 32);
-      else go(q8_few_kernel<T, true, EPI, 1, 4, 8, EXACT>, 16);
+      if constexpr (!EXACT) {
+        if (q8_few_wide(p.M, p.N, p.K)) {
+          go(q8_few_kernel<T, true, EPI, 2, 4, 8, false>, 32);
+          mark(stream);
+          return launch_status();
+        }
+      }
+      go(q8_few_kernel<T, true, EPI, 1, 4, 8, EXACT>, 16);
     } else {
       if (p.K >= 64 * Q8_BLOCK) go(q8_few_kernel<T, false, EPI, 1, 8, 8, EXACT>, 16);
       else go(q8_few_kernel<T, false, EPI, 1, 4, 8, EXACT>, 16);

@@ -14,9 +14,19 @@ namespace {
 // the end are the last one again, and not stored.  Bound by HBM and by how many loads are under way: every weight is read once, and a
 // wavefront waits once a round.  us, U = 2 / 4 / 8 with eight wavefronts, weights that were not read just before: one token 4096 -> 2 x
 // 16384 31 / 26 / 40 (32 blocks of 128 are half a round), 16384 -> 4096 17 / 19 / 14, 8 tokens 8192 -> 8192 17 / 16 / 16, one token 4096
-// -> 4096 6.2 / 5.6 / 5.4; four or sixteen wavefronts are no faster.  Sixteen tokens through both products of a pair: 32 columns
-// halve what is read of the tokens (4096 -> 2 x 16384 31.9 -> 30.1, 2048 -> 2 x 8192 8.5 -> 7.7); one product loses (16384 -> 4096
-// 19 -> 26).
+// -> 4096 6.2 / 5.6 / 5.4; four or sixteen wavefronts are no faster.
+//
+// Pairs of products with 16-bit results in 32 columns (CB = 2) read the tokens half as often and have half as many workgroups, two on
+// a compute unit where three of 16 columns are.  16 against 32 columns, us, m columns in each product, weights as above:
+//   m <= 4096: half the compute units would be idle (16 tokens 4096 -> 2 x 4096 9.7 / 14.2), and as at m = 10240 (24.0 / 27.0) and 12288
+//     (25.9 / 27.7) whenever the last 4096 columns are the first half of 8192;
+//   m > 12288: a second turn of 16 columns.  5 tokens 1024 -> 2 x 12288 8.0 / 8.9, 2 x 12544 10.9 / 8.9, 2 x 16384 12.0 / 9.2; where n is
+//     longer HBM covers it for few tokens (2048 -> 2 x 16384 3 tokens 16.9 / 14.6; 4096 -> 2 x 16384 3, 8 and 16 tokens 27.2 / 29.1, 29.0 /
+//     29.3, 33.2 / 30.9);
+//   4096 < m <= 8192: the tokens' share of the reads decides.  16 tokens 1024, 2048, 4096 -> 2 x 6144 7.2 / 7.6, 9.1 / 9.3, 17.1 / 15.0,
+//     5 tokens 4096 -> 2 x 5120 14.0 / 13.5; 16 tokens 4096 and 8192 -> 2 x 8192 18.2 / 16.2 and 32.7 / 39.1.
+// Over 320 shapes the rule (q8_few_wide) takes 0.4 % more than the better of both, 15 % at most.  With fp32 results 32 columns lose
+// throughout (16 tokens 4096 -> 2 x 8192 18.7 / 20.4, 1024 -> 2 x 16384 12.2 / 21.7), and so does one product (16384 -> 4096 19 / 26).
 constexpr int Q8F_COLS = 16;
 
 template <typename T, bool DUAL, int EPI, int CB, int U, int WAVES, bool EXACT>

@@ -848,10 +848,11 @@ def test_pre_activations_past_fp16_have_their_gradients(mp, act):  # noqa: F811
         assert torch.isfinite(p[:2]).all() and not torch.isnan(p).any() and torch.equal(p, q)
 
 
-# 32 columns per workgroup for pairs of more than 4 tokens from m = 4096 on, with a remainder of columns; 64 blocks a round from n = 8065 on,
-# with rounds that are not whole, and a second one
+# Pairs in 32 columns per workgroup on both sides of that rule, with a remainder of columns; 64 blocks a round from n = 8065 on, with rounds
+# that are not whole, and a second one
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("tokens,n,m", [(5, 300, 4099), (16, 1000, 4128), (4, 520, 4100), (1, 8200, 40), (9, 12345, 33), (16, 16500, 24), (3, 8064, 20)])
+@pytest.mark.parametrize("tokens,n,m", [(5, 300, 4099), (16, 1000, 4128), (4, 520, 4100), (1, 300, 12290), (5, 300, 12301), (16, 1000, 12320),
+                                        (8, 4200, 4111), (7, 4200, 4111), (1, 8200, 40), (9, 12345, 33), (16, 16500, 24), (3, 8064, 20)])
 def test_q8_products_of_few_tokens_take_every_form(mp, tokens, n, m, dtype):  # noqa: F811
     rng = np.random.default_rng(703)
     X, x, W, w = q8_case(mp, rng, tokens, n, m)
