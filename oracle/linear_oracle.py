@@ -49,6 +49,8 @@ def linear_backward(dY, X, W, Z=None, act=None, drop=None):
     dZ = np.asarray(dY, np.float64) if drop is None else dropout(np.asarray(dY, np.float64), *drop)
     if act is not None:
         dZ = dZ * activation_slope(act, np.asarray(Z, np.float64))
+    if drop is not None:      # (a dropped entry's is zero at a NaN, too)
+        dZ = np.where(kept(*dZ.shape, *drop), dZ, 0.0)
     return dZ @ np.asarray(W, np.float64).T, np.asarray(X, np.float64).T @ dZ, dZ.sum(0), dZ
 
 

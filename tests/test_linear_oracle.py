@@ -85,3 +85,12 @@ def test_packing():
     group = np.repeat(s, 32, 1)[:, :200]
     # half a step: 2^-4 of the value, or of the smallest normal code's binade
     assert (np.abs(back - A)[fine] <= np.maximum(np.abs(A) * 2.0 ** -4, group * 2.0 ** -10)[fine]).all()
+
+
+def test_a_dropped_entry_s_gradient_is_zero_whatever_its_pre_activation_was():
+    X, W, dY, Z = RNG.standard_normal((6, 4)), RNG.standard_normal((4, 8)), RNG.standard_normal((6, 8)), RNG.standard_normal((6, 8))
+    drop = (0.5, 21, 2)
+    want = lo.linear_backward(dY, X, W, Z, "silu", drop)
+    Z[~lo.kept(6, 8, *drop)] = np.nan
+    for p, q in zip(lo.linear_backward(dY, X, W, Z, "silu", drop), want):
+        np.testing.assert_array_equal(p, q)
